@@ -354,6 +354,107 @@ int gva_decode_tokens_ragged(gva_handle *h, const gva_cache *cache, const float 
                              const int32_t *seq_lens, float *out, float *lse, void *workspace, size_t workspace_bytes, int B,
                              int max_q_len, int max_seq_len, int num_splits, int32_t *dev_status, void *stream);
 
+/* ---- A cache that is kept small: 4-bit values, gathered attention weights, eviction --------------------------------
+ * (Not in the paper, which stores 16-bit values and keeps every token: this library's extension of its byte accounting,
+ * Section 3.4.)  All calls below want the handle's device to be the current one (GVA_ERR_INVALID_ARG otherwise), use no
+ * state of the handle on the device, and may be captured into CUDA graphs and replayed; calls on different streams may
+ * overlap as long as they share no workspace, no output and no page that one of them writes.  Any of the head shapes of
+ * gva_create is served, with every page size.
+ *
+ * The 4-bit cache.  A value row x[0 .. d_v) of one token and group is held as d_v codes of 4 bits and two f16 numbers:
+ *     lowest z = the largest f16 <= min x,   step s = the smallest f16 with z + 15 s >= max x,
+ *     code c = the number of k in 0 .. 14 with x >= z + (k + 1/2) s,   value = z + s c,   hence |value - x| <= s / 2.
+ * Elements beyond +-65504 are clamped first; a row with a NaN anywhere reads as NaN; a row of one value has s = 0.
+ * Positional keys are bf16.  A token takes G (d_v / 2 + 4) + 2 d_r bytes: 176 against the bf16 cache's 544 with H = 16,
+ * G = 4, d_v = 64, d_r = 16.  The calls take a handle with cache_dtype = GVA_BF16 (GVA_ERR_UNSUPPORTED otherwise), which
+ * serves bf16 caches beside it: gva_q4_widen brings tokens into bf16 pages for the calls that have no 4-bit form
+ * (gva_prefill, gva_decode_tokens, gva_decode_multi). */
+typedef struct {
+    void *v_pool;               /* [num_pages][G][page_size][d_v / 2] bytes: dim 2 i low, dim 2 i + 1 high nibble; 16-byte aligned */
+    void *sz_pool;              /* [num_pages][G][page_size] pairs of f16 (step, lowest)                   16-byte aligned */
+    void *kr_pool;              /* [num_pages][page_size][d_r] bf16; unused with d_r = 0                   16-byte aligned */
+    const int32_t *block_table; /* [B][max_pages_per_seq] or NULL (contiguous)                             */
+    int32_t num_pages;
+    int32_t max_pages_per_seq;
+} gva_q4_cache;
+
+/* gva_append_cache where the slot is not the position (a cache that has lost tokens to gva_evict, any cache type):
+ *   slots [B] i32   slot of the new token, normally the number of tokens the sequence holds
+ *   pos   [B] i32   position its key is rotated to; < 0 -> GVA_ERR_SEQ_LEN in *dev_status, the sequence is skipped
+ * With slots == pos it writes what gva_append_cache writes. */
+int gva_append_cache_at(gva_handle *h, const gva_cache *cache, const float *v_new, const float *kr_new, const int32_t *slots,
+                        const int32_t *pos, int B, int32_t *dev_status, void *stream);
+
+/* Append of one new token per sequence to the 4-bit cache: arguments and device-side errors as gva_append_cache_at. */
+int gva_q4_append(gva_handle *h, const gva_q4_cache *cache, const float *v_new, const float *kr_new, const int32_t *slots,
+                  const int32_t *pos, int B, int32_t *dev_status, void *stream);
+
+/* Append of a chunk of new tokens per sequence to the 4-bit cache: rows and errors as gva_append_chunk (row cu_q[b] + i goes
+ * to slot ctx_lens[b] + i); the key of that row is rotated to position first_pos[b] + i (first_pos NULL: to its slot).
+ * Rows at or beyond cu_q[B] are not read. */
+int gva_q4_append_chunk(gva_handle *h, const gva_q4_cache *cache, const float *v_new, const float *kr_new, const int32_t *cu_q,
+                        const int32_t *ctx_lens, const int32_t *first_pos, int B, int n_q, int32_t *dev_status, void *stream);
+
+/* Slots starts[b] .. seq_lens[b] - 1 (starts NULL: from 0) of every sequence as rows of a bf16 cache with the same page size,
+ * same slots: value rows z + s c rounded once, positional rows as they are.  Nothing else of the bf16 cache changes.
+ * max_seq_len sizes the launch (longer sequences are widened whole).  The two caches must not share memory. */
+int gva_q4_widen(gva_handle *h, const gva_q4_cache *cache, const gva_cache *wide, const int32_t *starts, const int32_t *seq_lens,
+                 int B, int max_seq_len, int32_t *dev_status, void *stream);
+
+/* Decode attention over the 4-bit cache: arguments, splitting, outputs and errors as gva_decode (a tile whose page is bad
+ * counts as empty).  Queries and softmax weights enter the products as two f16 numbers each, accumulation is f32: the
+ * result is that of f32 arithmetic on the cached values.  Bitwise reproducible for fixed arguments.
+ * Workspace: at least gva_q4_decode_workspace_bytes(h, B, max_seq_len, num_splits) bytes, 256-byte aligned. */
+size_t gva_q4_decode_workspace_bytes(const gva_handle *h, int B, int max_seq_len, int num_splits);
+int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, const int32_t *seq_lens, float *out, float *lse,
+                  void *workspace, size_t workspace_bytes, int B, int max_seq_len, int num_splits, int32_t *dev_status, void *stream);
+
+/* The attention every cached token has received, added up:
+ *   weights_out[b][t] = decay * weights_in[b][t] + sum over the new rows r of sequence b that see slot t, and over all
+ *                       heads, of exp(scale * score(r, head, t) - lse[r][head]),        t < seq_lens[b]
+ * i.e. the softmax weights of the attention whose lse is given (a row whose lse is -inf adds nothing).
+ *   q_abs [rows][H][d_v+d_r], lse [rows][H] f32   as the attention call had and returned them
+ *   cu_q  [B + 1] i32 or NULL    rows cu_q[b] .. cu_q[b+1] - 1 belong to sequence b, at most max_q_len are counted; row i of
+ *                                q_len_b sees seq_lens[b] - (q_len_b - 1 - i) slots.  NULL: one row per sequence
+ *   decay                        >= 0, finite; 0: weights_in is not read
+ *   weights_in / weights_out     [B][stride] f32, stride >= max_seq_len; weights_in may be NULL (zeros) or weights_out itself
+ * Slots at or beyond seq_lens[b] keep what weights_out held.  seq_lens[b] < 0, beyond the block table or beyond stride ->
+ * GVA_ERR_SEQ_LEN, the sequence is skipped; a slot whose page is bad gets decay * weights_in.  Any cache type. */
+int gva_attention_weights(gva_handle *h, const gva_cache *cache, const float *q_abs, const float *lse, const int32_t *cu_q,
+                          const int32_t *seq_lens, float decay, const float *weights_in, float *weights_out, int stride, int B,
+                          int max_q_len, int max_seq_len, int32_t *dev_status, void *stream);
+int gva_q4_attention_weights(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, const float *lse, const int32_t *cu_q,
+                             const int32_t *seq_lens, float decay, const float *weights_in, float *weights_out, int stride, int B,
+                             int max_q_len, int max_seq_len, int32_t *dev_status, void *stream);
+
+/* Eviction: of sequence b's seq_lens[b] tokens the n = min(keep[b], seq_lens[b]) first in this order stay -- tokens at
+ * positions < sinks or >= next_pos[b] - recent before all others (as if their weight were +inf), then by weight from large
+ * to small (NaN counts as -inf), then by slot from low to high.  Survivors in slots below n stay where they are; the i-th
+ * survivor behind them moves to the i-th slot below n that has become free, rows bit for bit.  The order of tokens in the
+ * cache carries no meaning (keys are rotated already), so no more than that is moved; afterwards the sequence has n tokens
+ * in slots 0 .. n - 1 and goes on growing with gva_append_cache_at / gva_q4_append (slot n, its own position).
+ *   weights_in / weights_out       [B][stride] f32, as from gva_attention_weights; stride >= max_seq_len
+ *   positions_in / positions_out   [B][stride] i32: position of the token in each slot; positions_in NULL: its slot.  Each
+ *                                  pair may be one buffer or two that do not overlap
+ *                                  for slots t < seq_lens[b] the outputs get what now is in the slot, 0 and -1 for t >= n;
+ *                                  slots at or beyond seq_lens[b] are left as they were
+ *   keep [B] i32, next_pos [B] i32 (position of the sequence's next token; NULL if recent = 0)
+ *   new_lens [B] i32               n; may be seq_lens itself
+ *   max_seq_len                    upper bound on seq_lens[] (here a longer sequence is an error)
+ *   workspace                      gva_evict_workspace_bytes(h, B, max_seq_len) bytes, 256-byte aligned
+ * Pages must belong to one sequence only.  keep[b] < 0 or a bad length -> GVA_ERR_SEQ_LEN, a bad page in the live range of a
+ * sequence that would lose tokens -> GVA_ERR_BAD_PAGE: that sequence stays as it is (a bad length: its outputs too), with
+ * new_lens[b] = seq_lens[b].  Any cache type. */
+size_t gva_evict_workspace_bytes(const gva_handle *h, int B, int max_seq_len);
+int gva_evict(gva_handle *h, const gva_cache *cache, const float *weights_in, const int32_t *positions_in, const int32_t *seq_lens,
+              const int32_t *keep, const int32_t *next_pos, int sinks, int recent, float *weights_out, int32_t *positions_out,
+              int32_t *new_lens, int stride, void *workspace, size_t workspace_bytes, int B, int max_seq_len, int32_t *dev_status,
+              void *stream);
+int gva_q4_evict(gva_handle *h, const gva_q4_cache *cache, const float *weights_in, const int32_t *positions_in, const int32_t *seq_lens,
+                 const int32_t *keep, const int32_t *next_pos, int sinks, int recent, float *weights_out, int32_t *positions_out,
+                 int32_t *new_lens, int stride, void *workspace, size_t workspace_bytes, int B, int max_seq_len, int32_t *dev_status,
+                 void *stream);
+
 /* Geometry of the most recent gva_decode / gqa_decode launch on this handle (reporting only):
  * number of split-KV partitions launched (thread blocks of the decode kernel). */
 int gva_last_num_splits(const gva_handle *h);

@@ -24,7 +24,9 @@ GVA_KERNEL_AUTO, GVA_KERNEL_FMA, GVA_KERNEL_MMA = 0, 1, 2
 EXPORTS = ["gva_create", "gva_destroy", "gva_decode_workspace_bytes", "gva_absorb_query", "gva_append_cache",
            "gva_decode", "gva_decode_static", "gqa_decode", "gva_decode_step", "gva_step_scratch_bytes", "gva_decode_step_host", "gva_input_width", "gva_pack_input_weights", "gva_pack_bf16",
            "gva_project_in", "gva_project_out", "gva_layer_step", "gva_last_num_splits", "gva_last_kernel", "gva_last_tile_tokens",
-           "gva_status_string", "gva_append_chunk", "gva_prefill", "gva_decode_multi_workspace_bytes", "gva_decode_multi", "gva_decode_tokens_workspace_bytes", "gva_decode_tokens", "gva_decode_tokens_ragged"]
+           "gva_status_string", "gva_append_chunk", "gva_prefill", "gva_decode_multi_workspace_bytes", "gva_decode_multi", "gva_decode_tokens_workspace_bytes", "gva_decode_tokens", "gva_decode_tokens_ragged",
+           "gva_append_cache_at", "gva_q4_append", "gva_q4_append_chunk", "gva_q4_widen", "gva_q4_decode_workspace_bytes", "gva_q4_decode",
+           "gva_attention_weights", "gva_q4_attention_weights", "gva_evict_workspace_bytes", "gva_evict", "gva_q4_evict"]
 
 
 class GvaConfig(ctypes.Structure):
@@ -42,6 +44,11 @@ class GvaCache(ctypes.Structure):
 class GqaCache(ctypes.Structure):
     _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
                 ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32)]
+
+
+class GvaQ4Cache(ctypes.Structure):
+    _fields_ = [("v_pool", ctypes.c_void_p), ("sz_pool", ctypes.c_void_p), ("kr_pool", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32)]
 
 
 class GvaError(RuntimeError):
@@ -93,12 +100,27 @@ def load() -> ctypes.CDLL:
     lib.gva_project_out.argtypes = [vp, vp, vp, ip, vp, ip, vp]
     lib.gva_layer_step.argtypes = [vp, ctypes.POINTER(GvaCache), vp, vp, vp, ip, vp, vp, vp, vp, vp, vp, sz, ip, ip, ip,
                                    vp, vp]
+    q4, pool, fl = ctypes.POINTER(GvaQ4Cache), ctypes.POINTER(GvaCache), ctypes.c_float
+    lib.gva_append_cache_at.argtypes = [vp, pool, vp, vp, vp, vp, ip, vp, vp]
+    lib.gva_q4_append.argtypes = [vp, q4, vp, vp, vp, vp, ip, vp, vp]
+    lib.gva_q4_append_chunk.argtypes = [vp, q4, vp, vp, vp, vp, vp, ip, ip, vp, vp]
+    lib.gva_q4_widen.argtypes = [vp, q4, pool, vp, vp, ip, ip, vp, vp]
+    lib.gva_q4_decode_workspace_bytes.argtypes = [vp, ip, ip, ip]
+    lib.gva_q4_decode_workspace_bytes.restype = sz
+    lib.gva_q4_decode.argtypes = [vp, q4, vp, vp, vp, vp, vp, sz, ip, ip, ip, vp, vp]
+    lib.gva_attention_weights.argtypes = [vp, pool, vp, vp, vp, vp, fl, vp, vp, ip, ip, ip, ip, vp, vp]
+    lib.gva_q4_attention_weights.argtypes = [vp, q4, vp, vp, vp, vp, fl, vp, vp, ip, ip, ip, ip, vp, vp]
+    lib.gva_evict_workspace_bytes.argtypes = [vp, ip, ip]
+    lib.gva_evict_workspace_bytes.restype = sz
+    lib.gva_evict.argtypes = [vp, pool, vp, vp, vp, vp, vp, ip, ip, vp, vp, vp, ip, vp, sz, ip, ip, vp, vp]
+    lib.gva_q4_evict.argtypes = [vp, q4, vp, vp, vp, vp, vp, ip, ip, vp, vp, vp, ip, vp, sz, ip, ip, vp, vp]
     for name in ("gva_last_num_splits", "gva_last_kernel", "gva_last_tile_tokens"):
         getattr(lib, name).argtypes = [vp]
     lib.gva_status_string.argtypes = [ip]
     lib.gva_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
-        if name not in ("gva_decode_workspace_bytes", "gva_step_scratch_bytes", "gva_status_string", "gva_pack_bf16"):
+        if name not in ("gva_decode_workspace_bytes", "gva_step_scratch_bytes", "gva_status_string", "gva_pack_bf16",
+                        "gva_q4_decode_workspace_bytes", "gva_evict_workspace_bytes"):
             getattr(lib, name).restype = ip
     _lib = lib
     return lib
@@ -300,6 +322,8 @@ def prepare_call(name: str, *args):
             conv.append(ctypes.byref(a))
         elif t is ctypes.c_void_p:
             conv.append(ctypes.c_void_p(a if isinstance(a, int) else _ptr(a)))
+        elif t is ctypes.c_float:
+            conv.append(t(float(a)))
         else:
             conv.append(t(int(a)))
     conv = tuple(conv)
@@ -388,6 +412,115 @@ def gva_layer_step(handle: int, cache: GvaCache, x, W_in, W_o, d_model: int, pos
     if check:
         _check(rc, "gva_layer_step")
     return rc
+
+
+# ---- the 4-bit cache, gathered attention weights, eviction ----
+
+def make_q4_cache(v_pool, sz_pool, kr_pool, block_table, num_pages: int, max_pages_per_seq: int) -> GvaQ4Cache:
+    return GvaQ4Cache(_ptr(v_pool), _ptr(sz_pool), _ptr(kr_pool), _ptr(block_table), int(num_pages), int(max_pages_per_seq))
+
+
+def _nbytes(t) -> int:
+    return 0 if t is None else int(t.numel() * t.element_size())
+
+
+def gva_append_cache_at(handle: int, cache: GvaCache, v_new, kr_new, slots, pos, B: int, dev_status=None, check: bool = True) -> int:
+    rc = load().gva_append_cache_at(handle, ctypes.byref(cache), _ptr(v_new), _ptr(kr_new), _ptr(slots), _ptr(pos), int(B),
+                                    _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gva_append_cache_at")
+    return rc
+
+
+def gva_q4_append(handle: int, cache: GvaQ4Cache, v_new, kr_new, slots, pos, B: int, dev_status=None, check: bool = True) -> int:
+    rc = load().gva_q4_append(handle, ctypes.byref(cache), _ptr(v_new), _ptr(kr_new), _ptr(slots), _ptr(pos), int(B),
+                              _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gva_q4_append")
+    return rc
+
+
+def gva_q4_append_chunk(handle: int, cache: GvaQ4Cache, v_new, kr_new, cu_q, ctx_lens, first_pos, B: int, n_q: int,
+                        dev_status=None, check: bool = True) -> int:
+    rc = load().gva_q4_append_chunk(handle, ctypes.byref(cache), _ptr(v_new), _ptr(kr_new), _ptr(cu_q), _ptr(ctx_lens),
+                                    _ptr(first_pos), int(B), int(n_q), _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gva_q4_append_chunk")
+    return rc
+
+
+def gva_q4_widen(handle: int, cache: GvaQ4Cache, wide: GvaCache, starts, seq_lens, B: int, max_seq_len: int, dev_status=None,
+                 check: bool = True) -> int:
+    rc = load().gva_q4_widen(handle, ctypes.byref(cache), ctypes.byref(wide), _ptr(starts), _ptr(seq_lens), int(B),
+                             int(max_seq_len), _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gva_q4_widen")
+    return rc
+
+
+def gva_q4_decode_workspace_bytes(handle: int, B: int, max_seq_len: int, num_splits: int = 0) -> int:
+    return int(load().gva_q4_decode_workspace_bytes(handle, int(B), int(max_seq_len), int(num_splits)))
+
+
+def gva_q4_decode(handle: int, cache: GvaQ4Cache, q_abs, seq_lens, out, lse, workspace, B: int, max_seq_len: int,
+                  num_splits: int = 0, dev_status=None, workspace_bytes: Optional[int] = None, check: bool = True) -> int:
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    rc = load().gva_q4_decode(handle, ctypes.byref(cache), _ptr(q_abs), _ptr(seq_lens), _ptr(out), _ptr(lse), _ptr(workspace), wb,
+                              int(B), int(max_seq_len), int(num_splits), _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gva_q4_decode")
+    return rc
+
+
+def _attention_weights(name: str, handle, cache, q_abs, lse, cu_q, seq_lens, decay, weights_in, weights_out, stride, B, max_q_len,
+                       max_seq_len, dev_status, check) -> int:
+    rc = getattr(load(), name)(handle, ctypes.byref(cache), _ptr(q_abs), _ptr(lse), _ptr(cu_q), _ptr(seq_lens), float(decay),
+                               _ptr(weights_in), _ptr(weights_out), int(stride), int(B), int(max_q_len), int(max_seq_len),
+                               _ptr(dev_status), _stream())
+    if check:
+        _check(rc, name)
+    return rc
+
+
+def gva_attention_weights(handle: int, cache: GvaCache, q_abs, lse, cu_q, seq_lens, decay: float, weights_in, weights_out, stride: int,
+                          B: int, max_q_len: int, max_seq_len: int, dev_status=None, check: bool = True) -> int:
+    return _attention_weights("gva_attention_weights", handle, cache, q_abs, lse, cu_q, seq_lens, decay, weights_in, weights_out,
+                              stride, B, max_q_len, max_seq_len, dev_status, check)
+
+
+def gva_q4_attention_weights(handle: int, cache: GvaQ4Cache, q_abs, lse, cu_q, seq_lens, decay: float, weights_in, weights_out,
+                             stride: int, B: int, max_q_len: int, max_seq_len: int, dev_status=None, check: bool = True) -> int:
+    return _attention_weights("gva_q4_attention_weights", handle, cache, q_abs, lse, cu_q, seq_lens, decay, weights_in, weights_out,
+                              stride, B, max_q_len, max_seq_len, dev_status, check)
+
+
+def gva_evict_workspace_bytes(handle: int, B: int, max_seq_len: int) -> int:
+    return int(load().gva_evict_workspace_bytes(handle, int(B), int(max_seq_len)))
+
+
+def _evict(name: str, handle, cache, weights_in, positions_in, seq_lens, keep, next_pos, sinks, recent, weights_out, positions_out,
+           new_lens, stride, workspace, B, max_seq_len, dev_status, workspace_bytes, check) -> int:
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    rc = getattr(load(), name)(handle, ctypes.byref(cache), _ptr(weights_in), _ptr(positions_in), _ptr(seq_lens), _ptr(keep),
+                               _ptr(next_pos), int(sinks), int(recent), _ptr(weights_out), _ptr(positions_out), _ptr(new_lens),
+                               int(stride), _ptr(workspace), wb, int(B), int(max_seq_len), _ptr(dev_status), _stream())
+    if check:
+        _check(rc, name)
+    return rc
+
+
+def gva_evict(handle: int, cache: GvaCache, weights_in, positions_in, seq_lens, keep, next_pos, sinks: int, recent: int, weights_out,
+              positions_out, new_lens, stride: int, workspace, B: int, max_seq_len: int, dev_status=None,
+              workspace_bytes: Optional[int] = None, check: bool = True) -> int:
+    return _evict("gva_evict", handle, cache, weights_in, positions_in, seq_lens, keep, next_pos, sinks, recent, weights_out,
+                  positions_out, new_lens, stride, workspace, B, max_seq_len, dev_status, workspace_bytes, check)
+
+
+def gva_q4_evict(handle: int, cache: GvaQ4Cache, weights_in, positions_in, seq_lens, keep, next_pos, sinks: int, recent: int,
+                 weights_out, positions_out, new_lens, stride: int, workspace, B: int, max_seq_len: int, dev_status=None,
+                 workspace_bytes: Optional[int] = None, check: bool = True) -> int:
+    return _evict("gva_q4_evict", handle, cache, weights_in, positions_in, seq_lens, keep, next_pos, sinks, recent, weights_out,
+                  positions_out, new_lens, stride, workspace, B, max_seq_len, dev_status, workspace_bytes, check)
 
 
 def gva_last_num_splits(handle: int) -> int:

@@ -9,41 +9,56 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgva.so")
 PROBE_LIB = os.path.join(HERE, "libgva_probe.so")      # the benchmark's read-only streaming probe (not part of the C ABI)
-SOURCES = ["gva_api.cu"]
-HEADERS = ["gva_common.cuh", "gva_small_kernels.cuh", "gva_decode_fma.cuh", "gva_decode_mma.cuh", "gva_decode_fp8.cuh", "gva_prefill.cuh", "gva_project.cuh",
-           os.path.join("..", "..", "include", "gva.h")]
+_SHARED = ["gva_common.cuh", "gva_rope.cuh", "gva_decode_mma.cuh", "gva_handle.cuh", os.path.join("..", "..", "include", "gva.h")]
+SOURCES = {   # source -> the headers it is compiled from
+    "gva_api.cu": _SHARED + ["gva_small_kernels.cuh", "gva_decode_fma.cuh", "gva_decode_fp8.cuh", "gva_prefill.cuh", "gva_project.cuh"],
+    "gva_compact.cu": _SHARED + ["gva_q4.cuh", "gva_evict.cuh"],
+}
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    for f in SOURCES + HEADERS:
-        p = os.path.join(CSRC, f)
-        if os.path.exists(p) and os.path.getmtime(p) > t:
-            return True
-    return False
+def _newer(target: str, files) -> bool:
+    """Whether target is there and no file is newer than it."""
+    return os.path.exists(target) and all(os.path.getmtime(target) >= os.path.getmtime(f) for f in files if os.path.exists(f))
+
+
+def _files(source: str):
+    return [os.path.join(CSRC, f) for f in [source] + SOURCES[source]]
+
+
+def _object(source: str) -> str:
+    return os.path.join(CSRC, source[:-3] + ".o")
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     if os.environ.get("GVA_LIBRARY"):      # a prebuilt library was named explicitly: nothing to do
         return os.environ["GVA_LIBRARY"]
-    if not force and not _stale():
+    if not force and all(_newer(LIB, _files(f)) for f in SOURCES):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
-             "-Xcompiler", "-fPIC"]
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    flags = arch + ["-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
     if os.path.exists(os.path.join(CSRC, "gva_decode_mma.cuh")):
         flags.append("-DGVA_WITH_MMA")
     flags += os.environ.get("GVA_EXTRA_NVCC_FLAGS", "").split()   # e.g. tuning macros such as -DGVA_MMA_WPG64=1
     if verbose:
         flags += ["-Xptxas", "-v"]
-    cmd = [nvcc] + flags + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-    if res.returncode != 0:
+    jobs = []                                                     # the sources are compiled side by side
+    for f in SOURCES:
+        if force or not _newer(_object(f), _files(f)):
+            cmd = [nvcc, "-c"] + flags + [os.path.join(CSRC, f), "-o", _object(f)]
+            jobs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+    failed = False
+    for job in jobs:
+        said = job.communicate()[0]
+        failed |= job.returncode != 0
+        if verbose or job.returncode != 0:
+            sys.stderr.write(said)
+    if failed:
         raise RuntimeError("nvcc failed building libgva.so")
+    link = subprocess.run([nvcc] + arch + ["-shared"] + [_object(f) for f in SOURCES] + ["-o", LIB], capture_output=True, text=True)
+    if link.returncode != 0:
+        sys.stderr.write(link.stdout + link.stderr)
+        raise RuntimeError("nvcc failed linking libgva.so")
     return LIB
 
 

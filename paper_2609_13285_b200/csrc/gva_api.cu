@@ -17,30 +17,9 @@
 #include "gva_decode_fp8.cuh"
 #include "gva_prefill.cuh"
 #endif
+#include "gva_handle.cuh"
 
 using namespace gva;
-
-struct gva_handle {
-    gva_config cfg;
-    int device;
-    int sm_count;
-    int smem_optin;          // max dynamic shared memory per block
-    int smem_per_sm;         // shared memory of one SM
-    float scale;             // softmax scale of gva_decode
-    RopeTable rope;
-    int last_num_splits;
-    int last_kernel;
-    int last_tile;
-    int epoch;               // number of the last decode call on this handle (see kSync* in gva_common.cuh)
-    int serial;              // number of this handle among all created in this process (see kHdrEpoch)
-    int32_t *sync_base;      // device address of the sync arena on this handle's device
-    int sync_off, sync_cap;  // the region of the arena in use (words)
-    int n_regions;           // regions reserved so far (the earlier, smaller ones are kept until gva_destroy)
-    int region_off[24], region_cap[24];
-#ifdef GVA_WITH_MMA
-    MmaHostState mma;
-#endif
-};
 
 // ---- device-side scheduling state ------------------------------------------------------------------
 // The decode and combine kernels coordinate through a few int32 words per handle (gva_common.cuh, kSync*): the tickets
@@ -118,8 +97,6 @@ int ensure_sync(gva_handle *h, int need, cudaStream_t stream) {
 
 namespace {
 
-inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // ---- FMA kernel dispatch ---------------------------------------------------------------------
 using KernelFn = void (*)(DecodeParams);
@@ -227,15 +204,6 @@ WorkspaceLayout workspace_layout(const gva_handle *h, int B, int num_splits, int
     w.total = w.hdr_bytes + w.rec_o_bytes + w.rec_ml_bytes;
     w.sync_ints = kSyncWords;
     return w;
-}
-
-int check_common(const gva_handle *h, int B, int max_seq_len, int num_splits) {
-    if (!h) return GVA_ERR_INVALID_ARG;
-    if (B < 0 || max_seq_len < 0 || num_splits < 0) return GVA_ERR_INVALID_ARG;
-    if (B > 8192 || num_splits > 4096) return GVA_ERR_UNSUPPORTED;
-    // total tiles must fit an int with headroom
-    if ((long long)B * ((max_seq_len + 31) / 32 + 1) >= (1ll << 30)) return GVA_ERR_UNSUPPORTED;
-    return GVA_OK;
 }
 
 // Validates and launches one decode kernel (which also merges its partial results).  dry = true runs every host-side
@@ -522,6 +490,26 @@ int gva_append_cache(gva_handle *h, const gva_cache *cache, const float *v_new, 
         return GVA_ERR_CUDA;
     }
     return GVA_OK;
+}
+
+int gva_append_cache_at(gva_handle *h, const gva_cache *cache, const float *v_new, const float *kr_new, const int32_t *slots,
+                        const int32_t *pos, int B, int32_t *dev_status, void *stream) {
+    int rc = check_plain(h, cache);
+    if (rc != GVA_OK) return rc;
+    if (B < 0) return GVA_ERR_INVALID_ARG;
+    if (B == 0) return GVA_OK;
+    if (!v_new || (h->cfg.d_r > 0 && !kr_new) || !slots || !pos) return GVA_ERR_INVALID_ARG;
+    if (!aligned(v_new, 4) || !aligned(kr_new, 4) || !aligned(slots, 4) || !aligned(pos, 4)) return GVA_ERR_INVALID_ARG;
+    const gva_config &c = h->cfg;
+    if (c.G * c.d_v > kAppendMaxPerThread * 128) return GVA_ERR_UNSUPPORTED;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+#define GVA_APPEND_AT(CT_) launched(launch_pdl(append_at_kernel<CT_>, dim3(B), dim3(128), 0, s, static_cast<CT_ *>(cache->v_pool), \
+        static_cast<CT_ *>(cache->kr_pool), cache->block_table, v_new, kr_new, slots, pos, c.G, c.d_v, c.d_r, c.page_size,          \
+        cache->num_pages, cache->max_pages_per_seq, dev_status, h->rope))
+    if (c.cache_dtype == GVA_E4M3) return GVA_APPEND_AT(uint8_t);
+    if (c.cache_dtype == GVA_BF16) return GVA_APPEND_AT(__nv_bfloat16);
+    return GVA_APPEND_AT(float);
+#undef GVA_APPEND_AT
 }
 
 int gva_append_chunk(gva_handle *h, const gva_cache *cache, const float *v_new, const float *kr_new, const int32_t *cu_q,

@@ -1,0 +1,292 @@
+// Host side of the calls that keep a cache small (include/gva.h): the 4-bit cache, gathered attention weights, eviction.
+// As in gva_api.cu, nothing here allocates device memory or synchronises.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "gva_evict.cuh"
+#include "gva_handle.cuh"
+
+using namespace gva;
+
+namespace {
+int check_q4(const gva_handle *h, const gva_q4_cache *cache) {
+    if (!h || !cache) return GVA_ERR_INVALID_ARG;
+    if (h->cfg.cache_dtype != GVA_BF16) return GVA_ERR_UNSUPPORTED;
+    if (!cache->v_pool || !cache->sz_pool || (h->cfg.d_r > 0 && !cache->kr_pool)) return GVA_ERR_INVALID_ARG;
+    if (cache->num_pages <= 0 || cache->max_pages_per_seq <= 0) return GVA_ERR_INVALID_ARG;
+    if (!aligned(cache->v_pool, 16) || !aligned(cache->sz_pool, 16) || !aligned(cache->kr_pool, 16) || !aligned(cache->block_table, 4))
+        return GVA_ERR_INVALID_ARG;
+    return check_device(h);
+}
+Q4Pools q4_pools(const gva_q4_cache *c) {
+    return Q4Pools{static_cast<uint8_t *>(c->v_pool), static_cast<__half2 *>(c->sz_pool), static_cast<uint16_t *>(c->kr_pool),
+                   c->block_table, c->num_pages, c->max_pages_per_seq};
+}
+int append_q4(gva_handle *h, const gva_q4_cache *cache, const float *v_new, const float *kr_new, const int32_t *cu_q,
+              const int32_t *slot0, const int32_t *pos0, int B, int n_q, int rows, int32_t *dev_status, void *stream) {
+    if (!v_new || (h->cfg.d_r > 0 && !kr_new) || !aligned(v_new, 4) || !aligned(kr_new, 4) || !aligned(slot0, 4) || !aligned(pos0, 4))
+        return GVA_ERR_INVALID_ARG;
+    const gva_config &c = h->cfg;
+    AppendQ4Params p;
+    std::memset(&p, 0, sizeof(p));
+    p.c = q4_pools(cache);
+    p.v_new = v_new; p.kr_new = kr_new; p.cu_q = cu_q; p.slot0 = slot0; p.pos0 = pos0;
+    p.B = B; p.n_q = n_q; p.G = c.G; p.d_v = c.d_v; p.d_r = c.d_r; p.P = c.page_size; p.rows = rows;
+    p.vec = aligned(v_new, 16) ? 1 : 0;
+    p.dev_status = dev_status;
+    return launched(launch_pdl(append_q4_kernel, dim3((n_q + rows - 1) / rows), dim3(kAppendQ4Threads), 0,
+                               static_cast<cudaStream_t>(stream), p, h->rope));
+}
+
+int q4_splits(const gva_handle *h, int B, int max_seq_len, int num_splits) {
+    if (num_splits > 0) return num_splits;
+    const int tiles = std::max(1, (max_seq_len + 63) / 64);
+    return std::max(1, std::min(tiles, 8 * h->sm_count / std::max(1, B * h->cfg.G)));
+}
+struct Q4Workspace {
+    size_t rec_o, rec_ml, total;
+    int n_rec;
+};
+Q4Workspace q4_workspace(const gva_handle *h, int B, int max_seq_len, int num_splits) {
+    Q4Workspace w;
+    w.n_rec = std::max(1, B * q4_splits(h, B, max_seq_len, num_splits));
+    w.rec_o = 0;
+    w.rec_ml = align_up((size_t)w.n_rec * h->cfg.H * h->cfg.d_v * 4, 256);
+    w.total = w.rec_ml + align_up((size_t)w.n_rec * h->cfg.H * 2 * 4, 256);
+    return w;
+}
+
+int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_abs, const float *lse, const int32_t *cu_q,
+                      const int32_t *seq_lens, float decay, const float *weights_in, float *weights_out, int stride, int B,
+                      int max_q_len, int max_seq_len, int32_t *dev_status, void *stream) {
+    if (B < 0 || max_q_len < 0 || max_seq_len < 0 || stride < 0) return GVA_ERR_INVALID_ARG;
+    if (B == 0 || max_seq_len == 0) return GVA_OK;
+    if (!q_abs || !lse || !seq_lens || !weights_out || stride < max_seq_len || !(decay >= 0.f) || std::isinf(decay)) return GVA_ERR_INVALID_ARG;
+    if (!aligned(q_abs, 16) || !aligned(lse, 4) || !aligned(cu_q, 4) || !aligned(seq_lens, 4) || !aligned(weights_in, 4) || !aligned(weights_out, 4))
+        return GVA_ERR_INVALID_ARG;
+    if (B > 65535) return GVA_ERR_UNSUPPORTED;
+    const gva_config &c = h->cfg;
+    p.q = q_abs; p.lse = lse; p.cu_q = cu_q; p.seq_lens = seq_lens; p.decay = decay; p.w_in = decay > 0.f ? weights_in : nullptr; p.w_out = weights_out;
+    p.stride = stride; p.B = B; p.max_q_len = max_q_len; p.H = c.H; p.G = c.G; p.P = c.page_size;
+    p.scale = h->scale;
+    p.dev_status = dev_status;
+    const dim3 grid((max_seq_len + kWeightTile - 1) / kWeightTile, B);
+    void (*fn)(WeightParams, int) = nullptr;
+#define GVA_WEIGHTS(KIND_) (c.d_v == 64 ? weights_simple_kernel<KIND_, 64> : weights_simple_kernel<KIND_, 128>)
+    fn = kind == kCacheQ4 ? GVA_WEIGHTS(kCacheQ4) : kind == kCacheE4m3 ? GVA_WEIGHTS(kCacheE4m3) : kind == kCacheBf16 ? GVA_WEIGHTS(kCacheBf16) : GVA_WEIGHTS(kCacheF32);
+#undef GVA_WEIGHTS
+    return launched(launch_pdl(fn, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), p, c.d_r));
+}
+
+// Blocks per sequence of the eviction's selection: as many as leave the device with about one block per SM, eight (the
+// portable cluster size) at most, and no more than the longest sequence has work for.
+int evict_cluster(const gva_handle *h, int B, int max_seq_len) {
+    int c = 1;
+    while (c < 8 && 2 * c * B <= h->sm_count && c * 2 * kEvictThreads <= max_seq_len) c *= 2;
+    return c;
+}
+size_t evict_workspace(int B, int max_seq_len) {
+    const size_t stride = ((size_t)max_seq_len / 2 + 64) / 64 * 64;
+    return align_up((size_t)B * 4, 256) + 2 * align_up((size_t)B * stride * 4, 256);
+}
+int evict(gva_handle *h, const int32_t *block_table, int num_pages, int max_pages, MovePools pools, const float *weights_in,
+          const int32_t *positions_in, const int32_t *seq_lens, const int32_t *keep, const int32_t *next_pos, int sinks, int recent,
+          float *weights_out, int32_t *positions_out, int32_t *new_lens, int stride, void *workspace, size_t workspace_bytes, int B,
+          int max_seq_len, int32_t *dev_status, void *stream) {
+    if (B < 0 || max_seq_len < 0 || stride < 0 || sinks < 0 || recent < 0) return GVA_ERR_INVALID_ARG;
+    if (B == 0) return GVA_OK;
+    if (!weights_in || !seq_lens || !keep || (recent > 0 && !next_pos) || !weights_out || !positions_out || !new_lens || stride < max_seq_len)
+        return GVA_ERR_INVALID_ARG;
+    if (!aligned(weights_in, 4) || !aligned(positions_in, 4) || !aligned(seq_lens, 4) || !aligned(keep, 4) || !aligned(next_pos, 4) ||
+        !aligned(weights_out, 4) || !aligned(positions_out, 4) || !aligned(new_lens, 4))
+        return GVA_ERR_INVALID_ARG;
+    if (B > 8192) return GVA_ERR_UNSUPPORTED;
+    if (!workspace || workspace_bytes < evict_workspace(B, max_seq_len)) return GVA_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return GVA_ERR_INVALID_ARG;
+    EvictParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.w_in = weights_in; p.pos_in = positions_in; p.seq_lens = seq_lens; p.keep = keep; p.next_pos = recent > 0 ? next_pos : nullptr;
+    p.sinks = sinks; p.recent = recent; p.w_out = weights_out; p.pos_out = positions_out; p.new_lens = new_lens;
+    p.stride = stride; p.B = B; p.max_seq_len = max_seq_len; p.P = h->cfg.page_size; p.num_pages = num_pages; p.max_pages = max_pages;
+    p.block_table = block_table;
+    p.move_stride = (int)(((size_t)max_seq_len / 2 + 64) / 64 * 64);
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    p.n_moves = reinterpret_cast<int32_t *>(ws);
+    p.holes = reinterpret_cast<int32_t *>(ws + align_up((size_t)B * 4, 256));
+    p.sources = reinterpret_cast<int32_t *>(ws + align_up((size_t)B * 4, 256) + align_up((size_t)B * p.move_stride * 4, 256));
+    p.dev_status = dev_status;
+    const int C = evict_cluster(h, B, max_seq_len);
+    const int per_block = ((max_seq_len + C - 1) / C + 1023) / 1024 * 1024;
+    const int held = std::min(per_block, kEvictKeysMax);
+    const size_t smem = (size_t)held * 4;
+    if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GVA_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(B * C);
+    cfg.blockDim = dim3(kEvictThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    int rc = launched(cudaLaunchKernelEx(&cfg, evict_select_kernel, p, held));
+    if (rc != GVA_OK) return rc;
+    const int blocks = std::max(1, std::min((max_seq_len / 2 + 31) / 32, (8 * h->sm_count + B - 1) / B));
+    return launched(launch_pdl(evict_move_kernel, dim3(blocks, B), dim3(kMoveThreads), 0, static_cast<cudaStream_t>(stream), p, pools, h->cfg.G));
+}
+}  // namespace
+
+extern "C" {
+
+int gva_q4_append(gva_handle *h, const gva_q4_cache *cache, const float *v_new, const float *kr_new, const int32_t *slots,
+                  const int32_t *pos, int B, int32_t *dev_status, void *stream) {
+    int rc = check_q4(h, cache);
+    if (rc != GVA_OK) return rc;
+    if (B < 0) return GVA_ERR_INVALID_ARG;
+    if (B == 0) return GVA_OK;
+    if (!slots || !pos) return GVA_ERR_INVALID_ARG;
+    return append_q4(h, cache, v_new, kr_new, nullptr, slots, pos, B, B, 1, dev_status, stream);
+}
+
+int gva_q4_append_chunk(gva_handle *h, const gva_q4_cache *cache, const float *v_new, const float *kr_new, const int32_t *cu_q,
+                        const int32_t *ctx_lens, const int32_t *first_pos, int B, int n_q, int32_t *dev_status, void *stream) {
+    int rc = check_q4(h, cache);
+    if (rc != GVA_OK) return rc;
+    if (B < 0 || n_q < 0) return GVA_ERR_INVALID_ARG;
+    if (B == 0 || n_q == 0) return GVA_OK;
+    if (!cu_q || !aligned(cu_q, 4) || !ctx_lens) return GVA_ERR_INVALID_ARG;
+    return append_q4(h, cache, v_new, kr_new, cu_q, ctx_lens, first_pos ? first_pos : ctx_lens, B, n_q, kAppendQ4Rows, dev_status, stream);
+}
+
+int gva_q4_widen(gva_handle *h, const gva_q4_cache *cache, const gva_cache *wide, const int32_t *starts, const int32_t *seq_lens,
+                 int B, int max_seq_len, int32_t *dev_status, void *stream) {
+    int rc = check_q4(h, cache);
+    if (rc == GVA_OK) rc = check_plain(h, wide);
+    if (rc != GVA_OK) return rc;
+    if (B < 0 || max_seq_len < 0) return GVA_ERR_INVALID_ARG;
+    if (B == 0 || max_seq_len == 0) return GVA_OK;
+    if (!seq_lens || !aligned(starts, 4) || !aligned(seq_lens, 4)) return GVA_ERR_INVALID_ARG;
+    if (B > 65535) return GVA_ERR_UNSUPPORTED;
+    const gva_config &c = h->cfg;
+    WidenParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.c = q4_pools(cache);
+    p.v = static_cast<uint16_t *>(wide->v_pool);
+    p.kr = static_cast<uint16_t *>(wide->kr_pool);
+    p.block_table = wide->block_table;
+    p.num_pages = wide->num_pages;
+    p.max_pages = wide->max_pages_per_seq;
+    p.starts = starts;
+    p.seq_lens = seq_lens;
+    p.G = c.G; p.d_v = c.d_v; p.d_r = c.d_r; p.P = c.page_size;
+    p.dev_status = dev_status;
+    return launched(launch_pdl(widen_q4_kernel, dim3((max_seq_len + kWidenTokens - 1) / kWidenTokens, B), dim3(256), 0,
+                               static_cast<cudaStream_t>(stream), p));
+}
+
+size_t gva_q4_decode_workspace_bytes(const gva_handle *h, int B, int max_seq_len, int num_splits) {
+    if (check_common(h, B, max_seq_len, num_splits) != GVA_OK) return 0;
+    return q4_workspace(h, B, max_seq_len, num_splits).total;
+}
+
+int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, const int32_t *seq_lens, float *out, float *lse,
+                  void *workspace, size_t workspace_bytes, int B, int max_seq_len, int num_splits, int32_t *dev_status, void *stream) {
+    int rc = check_common(h, B, max_seq_len, num_splits);
+    if (rc == GVA_OK) rc = check_q4(h, cache);
+    if (rc != GVA_OK) return rc;
+    if (B == 0) return GVA_OK;
+    if (!q_abs || !seq_lens || !out || !aligned(q_abs, 16) || !aligned(out, 16) || !aligned(seq_lens, 4) || !aligned(lse, 4)) return GVA_ERR_INVALID_ARG;
+    const Q4Workspace w = q4_workspace(h, B, max_seq_len, num_splits);
+    if (!workspace || workspace_bytes < w.total) return GVA_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return GVA_ERR_INVALID_ARG;
+    const gva_config &c = h->cfg;
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    DecodeParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.seq_lens = seq_lens;
+    p.q = q_abs;
+    p.rec_o = reinterpret_cast<float *>(ws + w.rec_o);
+    p.rec_ml = reinterpret_cast<float *>(ws + w.rec_ml);
+    p.dev_status = dev_status;
+    p.B = B; p.H = c.H; p.G = c.G; p.P = c.page_size;
+    p.num_pages = cache->num_pages;
+    p.max_pages = cache->max_pages_per_seq;
+    p.num_splits = q4_splits(h, B, max_seq_len, num_splits);
+    p.scale_log2 = h->scale * kLog2e;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const dim3 grid(B * p.num_splits, c.G);
+    rc = launched(c.d_v == 64 ? launch_pdl(decode_q4_simple_kernel<64>, grid, dim3(128), 0, s, p, q4_pools(cache), 64, c.d_r)
+                              : launch_pdl(decode_q4_simple_kernel<128>, grid, dim3(128), 0, s, p, q4_pools(cache), 64, c.d_r));
+    if (rc != GVA_OK) return rc;
+    MergeParams m;
+    m.rec_o = p.rec_o; m.rec_ml = p.rec_ml; m.seq_lens = seq_lens; m.out = out; m.lse = lse;
+    m.B = B; m.H = c.H; m.P = c.page_size; m.max_pages = cache->max_pages_per_seq; m.num_splits = p.num_splits;
+    m.n_blocks = B * p.num_splits; m.tile = 64;
+    const int threads = 256, parts = threads / (c.d_v / 4);
+    const size_t smem = (size_t)parts * (c.d_v + 1) * 4;
+    return launched(c.d_v == 64 ? launch_pdl(merge_records_kernel<64>, dim3(B, c.H), dim3(threads), smem, s, m)
+                                : launch_pdl(merge_records_kernel<128>, dim3(B, c.H), dim3(threads), smem, s, m));
+}
+
+int gva_attention_weights(gva_handle *h, const gva_cache *cache, const float *q_abs, const float *lse, const int32_t *cu_q,
+                          const int32_t *seq_lens, float decay, const float *weights_in, float *weights_out, int stride, int B,
+                          int max_q_len, int max_seq_len, int32_t *dev_status, void *stream) {
+    const int rc = check_plain(h, cache);
+    if (rc != GVA_OK) return rc;
+    WeightParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.v = cache->v_pool; p.kr = cache->kr_pool;
+    p.block_table = cache->block_table; p.num_pages = cache->num_pages; p.max_pages = cache->max_pages_per_seq;
+    const int kind = h->cfg.cache_dtype == GVA_E4M3 ? kCacheE4m3 : h->cfg.cache_dtype == GVA_BF16 ? kCacheBf16 : kCacheF32;
+    return attention_weights(h, p, kind, q_abs, lse, cu_q, seq_lens, decay, weights_in, weights_out, stride, B, max_q_len, max_seq_len, dev_status, stream);
+}
+
+int gva_q4_attention_weights(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, const float *lse, const int32_t *cu_q,
+                             const int32_t *seq_lens, float decay, const float *weights_in, float *weights_out, int stride, int B,
+                             int max_q_len, int max_seq_len, int32_t *dev_status, void *stream) {
+    const int rc = check_q4(h, cache);
+    if (rc != GVA_OK) return rc;
+    WeightParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.v = cache->v_pool; p.sz = static_cast<const __half2 *>(cache->sz_pool); p.kr = cache->kr_pool;
+    p.block_table = cache->block_table; p.num_pages = cache->num_pages; p.max_pages = cache->max_pages_per_seq;
+    return attention_weights(h, p, kCacheQ4, q_abs, lse, cu_q, seq_lens, decay, weights_in, weights_out, stride, B, max_q_len, max_seq_len, dev_status, stream);
+}
+
+size_t gva_evict_workspace_bytes(const gva_handle *h, int B, int max_seq_len) {
+    if (!h || B < 0 || max_seq_len < 0 || B > 8192) return 0;
+    return evict_workspace(B, max_seq_len);
+}
+
+int gva_evict(gva_handle *h, const gva_cache *cache, const float *weights_in, const int32_t *positions_in, const int32_t *seq_lens,
+              const int32_t *keep, const int32_t *next_pos, int sinks, int recent, float *weights_out, int32_t *positions_out,
+              int32_t *new_lens, int stride, void *workspace, size_t workspace_bytes, int B, int max_seq_len, int32_t *dev_status,
+              void *stream) {
+    const int rc = check_plain(h, cache);
+    if (rc != GVA_OK) return rc;
+    const int elem = h->cfg.cache_dtype == GVA_E4M3 ? 1 : h->cfg.cache_dtype == GVA_BF16 ? 2 : 4;
+    const MovePools pools{static_cast<uint8_t *>(cache->v_pool), h->cfg.d_r > 0 ? static_cast<uint8_t *>(cache->kr_pool) : nullptr, nullptr,
+                          h->cfg.d_v * elem, h->cfg.d_r * elem};
+    return evict(h, cache->block_table, cache->num_pages, cache->max_pages_per_seq, pools, weights_in, positions_in, seq_lens, keep, next_pos,
+                 sinks, recent, weights_out, positions_out, new_lens, stride, workspace, workspace_bytes, B, max_seq_len, dev_status, stream);
+}
+
+int gva_q4_evict(gva_handle *h, const gva_q4_cache *cache, const float *weights_in, const int32_t *positions_in, const int32_t *seq_lens,
+                 const int32_t *keep, const int32_t *next_pos, int sinks, int recent, float *weights_out, int32_t *positions_out,
+                 int32_t *new_lens, int stride, void *workspace, size_t workspace_bytes, int B, int max_seq_len, int32_t *dev_status,
+                 void *stream) {
+    const int rc = check_q4(h, cache);
+    if (rc != GVA_OK) return rc;
+    const MovePools pools{static_cast<uint8_t *>(cache->v_pool), h->cfg.d_r > 0 ? static_cast<uint8_t *>(cache->kr_pool) : nullptr,
+                          static_cast<uint32_t *>(cache->sz_pool), h->cfg.d_v / 2, h->cfg.d_r * 2};
+    return evict(h, cache->block_table, cache->num_pages, cache->max_pages_per_seq, pools, weights_in, positions_in, seq_lens, keep, next_pos,
+                 sinks, recent, weights_out, positions_out, new_lens, stride, workspace, workspace_bytes, B, max_seq_len, dev_status, stream);
+}
+
+}  // extern "C"

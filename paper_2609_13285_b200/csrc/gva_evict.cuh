@@ -1,0 +1,393 @@
+// What every cached token has gathered of the attention, and the eviction of those that gathered least.
+#pragma once
+
+#include <cooperative_groups.h>
+
+#include "gva_q4.cuh"
+
+namespace gva {
+
+// ---- gathered weights -----------------------------------------------------------------------------------------------
+// w_out[b][t] = decay w_in[b][t] + sum over the new rows r of b that see t, and all heads, of exp(score(r, h, t) - lse[r][h]).
+struct WeightParams {
+    const void *v;               // value pool of the cache's type (4-bit: codes)
+    const __half2 *sz;           // 4-bit only
+    const void *kr;
+    const int32_t *block_table;
+    int num_pages, max_pages;
+    const float *q, *lse;        // [rows][H][d_v + d_r], [rows][H]
+    const int32_t *cu_q;         // nullable: one row per sequence
+    const int32_t *seq_lens;
+    float decay;
+    const float *w_in;           // nullable
+    float *w_out;
+    int stride, B, max_q_len, H, G, P;
+    float scale;
+    int32_t *dev_status;
+};
+
+enum WeightCache { kCacheF32 = 0, kCacheBf16 = 1, kCacheE4m3 = 2, kCacheQ4 = 3 };
+
+template <int KIND>
+__device__ __forceinline__ float cache_element(const void *pool, size_t i) {
+    if constexpr (KIND == kCacheF32) return static_cast<const float *>(pool)[i];
+    else if constexpr (KIND == kCacheBf16) return __uint_as_float((uint32_t) static_cast<const uint16_t *>(pool)[i] << 16);
+    else return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<const uint8_t *>(pool)[i], __NV_E4M3)));
+}
+
+// One warp per token, d_v / 32 dims per lane, on the CUDA cores.
+constexpr int kWeightTile = 64;
+template <int KIND, int DV>
+__global__ void __launch_bounds__(256)
+weights_simple_kernel(WeightParams p, int DR) {
+    grid_dependency_launch();
+    grid_dependency_wait();
+    const int b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5;
+    const int len = p.seq_lens[b];
+    if (len < 0 || (long long)len > (long long)p.max_pages * p.P || len > p.stride) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
+        return;
+    }
+    const int row0 = p.cu_q ? p.cu_q[b] : b;
+    const int rows = p.cu_q ? min(max(p.cu_q[b + 1] - row0, 0), p.max_q_len) : 1;
+    const int DQ = DV + DR;
+    constexpr int E = DV / 32;
+    for (long long t0 = (long long)blockIdx.x * kWeightTile; t0 < len; t0 += (long long)gridDim.x * kWeightTile) {
+        for (int t = (int)t0 + warp; t < min((long long)len, t0 + kWeightTile); t += n_warps) {
+            const int page = locate_page(p.block_table, p.num_pages, p.max_pages, p.P, b, t, p.dev_status);
+            float total = 0.f;
+            if (page >= 0) {
+                const int slot = t % p.P;
+                float k = 0.f;
+                if (lane < DR) k = cache_element<KIND == kCacheQ4 ? kCacheBf16 : KIND>(p.kr, ((size_t)page * p.P + slot) * DR + lane);
+                for (int g = 0; g < p.G; ++g) {
+                    const size_t row = ((size_t)page * p.G + g) * p.P + slot;
+                    float v[E];
+                    if constexpr (KIND == kCacheQ4) {
+                        const float2 sz = __half22float2(p.sz[row]);
+                        for (int e = 0; e < E; e += 2) {
+                            const uint8_t x = static_cast<const uint8_t *>(p.v)[row * (DV / 2) + lane * (E / 2) + e / 2];
+                            v[e] = fmaf((float)(x & 15), sz.x, sz.y);
+                            v[e + 1] = fmaf((float)(x >> 4), sz.x, sz.y);
+                        }
+                    } else {
+                        for (int e = 0; e < E; ++e) v[e] = cache_element<KIND>(p.v, row * DV + lane * E + e);
+                    }
+                    for (int r = 0; r < rows; ++r) {
+                        if (t >= len - (rows - 1 - r)) continue;
+                        for (int j = 0; j < kHeadsPerGroup; ++j) {
+                            const int h = g * kHeadsPerGroup + j;
+                            const float *q = p.q + ((size_t)(row0 + r) * p.H + h) * DQ;
+                            float x = lane < DR ? q[DV + lane] * k : 0.f;
+                            for (int e = 0; e < E; ++e) x = fmaf(q[lane * E + e], v[e], x);
+                            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+                            const float lse = p.lse[(size_t)(row0 + r) * p.H + h];
+                            if (lse != -INFINITY) total += exp2f(fmaf(x, p.scale, -lse) * kLog2e);
+                        }
+                    }
+                }
+            }
+            if (lane == 0) {
+                const size_t i = (size_t)b * p.stride + t;
+                p.w_out[i] = p.w_in ? fmaf(p.decay, p.w_in[i], total) : total;
+            }
+        }
+    }
+}
+
+// ---- eviction -------------------------------------------------------------------------------------------------------
+// A token counts by its weight; those at positions below `sinks` or within the last `recent` positions count as +inf, a
+// NaN as -inf.  The keep[b] first in the order (weight descending, slot ascending) stay.  Attention does not care in which
+// order the cache holds its tokens (their positional keys are rotated already), so nothing is shifted: with n = min(keep,
+// len), survivors in slots below n stay where they are, and the i-th survivor behind n goes to the i-th free slot before n.
+// Sources and targets are disjoint, so the moves need no order among themselves.
+//
+// select: one cluster of blocks per sequence finds the n-th key by a radix select (digits of 11, 11 and 10 bits from the
+// top, histograms in shared memory summed over the cluster), counts the ties that still fit, and writes weights and
+// positions of the slots that stay, zero and -1 for those that leave, and the lists of free slots and of survivors to move.
+// move: warps copy the rows of the moves, 16 bytes per lane and piece, weights and positions with them.
+constexpr int kEvictThreads = 1024;
+constexpr int kEvictBins = 2048;
+constexpr int kEvictKeysMax = 32768;     // keys of one block that are kept in shared memory; beyond, they are made again
+
+struct EvictParams {
+    const float *w_in;
+    const int32_t *pos_in;       // nullable: position = slot
+    const int32_t *seq_lens, *keep, *next_pos;
+    int sinks, recent;
+    float *w_out;
+    int32_t *pos_out, *new_lens;
+    int stride, B, max_seq_len, P, num_pages, max_pages;
+    const int32_t *block_table;
+    int32_t *n_moves;            // [B]
+    int32_t *holes, *sources;    // [B][move_stride]
+    int move_stride;
+    int32_t *dev_status;
+};
+
+// Order-preserving image of the weight: larger key = more worth keeping.
+__device__ __forceinline__ uint32_t evict_key(float w) {
+    if (w != w) w = -INFINITY;
+    const uint32_t u = __float_as_uint(w + 0.f);             // -0 counts as 0
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+constexpr uint32_t kEvictKeyInf = 0xff800000u;               // evict_key(+inf)
+
+// Sum over the block of one int per thread and the exclusive prefix of whole warps: every lane passes its warp's value.
+__device__ __forceinline__ int warp_prefix_of_block(int mine, int *s_warp, int &total) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = blockDim.x >> 5;
+    __syncthreads();
+    if (lane == 0) s_warp[warp] = mine;
+    __syncthreads();
+    const int x = lane < n ? s_warp[lane] : 0;
+    int incl = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    total = __shfl_sync(0xffffffffu, incl, 31);
+    return __shfl_sync(0xffffffffu, incl - x, warp);
+}
+
+__global__ void __launch_bounds__(kEvictThreads)
+evict_select_kernel(EvictParams p, int keys_in_smem) {
+    namespace cg = cooperative_groups;
+    grid_dependency_launch();
+    extern __shared__ uint32_t s_keys[];                     // [keys_in_smem]
+    __shared__ int s_hist[kEvictBins];
+    __shared__ int s_warp[32];
+    __shared__ int s_share[4];                               // read by the other blocks of the cluster
+    __shared__ int s_digit, s_rest;
+    __shared__ int s_bad;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int b = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int kWarps = kEvictThreads / 32;
+    if (tid == 0) s_bad = 0;
+    grid_dependency_wait();
+    __syncthreads();
+    const int len_in = p.seq_lens[b], keep_in = p.keep[b], next = p.next_pos ? p.next_pos[b] : 0;
+    bool bad = len_in < 0 || len_in > p.max_seq_len || (long long)len_in > (long long)p.max_pages * p.P || keep_in < 0;
+    const int len = bad ? 0 : len_in;
+    if (bad && rank == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
+    // every page of the live range has to be there before a row is moved
+    if (!bad && p.block_table && keep_in < len) {
+        for (int j = tid; j < (len + p.P - 1) / p.P; j += kEvictThreads) {
+            const int page = p.block_table[(size_t)b * p.max_pages + j];
+            if (page < 0 || page >= p.num_pages) s_bad = 1;
+        }
+    } else if (!bad && keep_in < len && ((long long)b * p.max_pages + (len + p.P - 1) / p.P > p.num_pages)) {
+        s_bad = 1;
+    }
+    __syncthreads();
+    if (s_bad) {
+        if (rank == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_BAD_PAGE, b);
+        bad = true;
+    }
+    const int keep = bad || keep_in >= len ? len : keep_in;
+    cluster.sync();                                          // everyone has read the lengths: new_lens may be seq_lens
+    if (rank == 0 && tid == 0) {
+        p.new_lens[b] = bad ? len_in : keep;
+        if (keep == len) p.n_moves[b] = 0;
+    }
+    const float *w = p.w_in + (size_t)b * p.stride;
+    const int32_t *pos = p.pos_in ? p.pos_in + (size_t)b * p.stride : nullptr;
+    float *w_out = p.w_out + (size_t)b * p.stride;
+    int32_t *pos_out = p.pos_out + (size_t)b * p.stride;
+    // this block's slots: a multiple of 32 per warp, warps one after the other
+    const int per_block = ((len + C - 1) / C + 1023) / 1024 * 1024;
+    const int lo = min(len, rank * per_block), hi = min(len, lo + per_block);
+    if (keep == len) {                                       // nothing leaves (uniform over the cluster)
+        for (int t = lo + tid; t < hi; t += kEvictThreads) {
+            if (w_out != w) w_out[t] = w[t];
+            if (pos_out != pos) pos_out[t] = pos ? pos[t] : t;
+        }
+        return;
+    }
+    auto make_key = [&](int t) -> uint32_t {
+        const int at = pos ? pos[t] : t;
+        const bool safe = at < p.sinks || (p.recent > 0 && (long long)at >= (long long)next - p.recent);
+        return safe ? kEvictKeyInf : evict_key(w[t]);
+    };
+    const bool held = per_block <= keys_in_smem;
+    if (held)
+        for (int t = lo + tid; t < hi; t += kEvictThreads) s_keys[t - lo] = make_key(t);
+    __syncthreads();
+    auto key_of = [&](int t) -> uint32_t { return held ? s_keys[t - lo] : make_key(t); };
+
+    // ---- the key of rank `keep`, from the top digit down ----
+    uint32_t prefix = 0, mask = 0;
+    int want = keep;                                         // this many are still to be found among the keys with this prefix
+    if (want > 0)
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, bins = 1 << bits;
+        for (int i = tid; i < kEvictBins; i += kEvictThreads) s_hist[i] = 0;
+        __syncthreads();
+        for (int t0 = lo; t0 < hi; t0 += kEvictThreads) {
+            const int t = t0 + tid;
+            uint32_t key = 0;
+            bool on = t < hi;
+            if (on) key = key_of(t);
+            on = on && (key & mask) == prefix;
+            const int digit = (key >> shift) & (bins - 1);
+            // equal digits across the warp (runs of equal weights) are counted once
+            const uint32_t live = __ballot_sync(0xffffffffu, on);
+            if (live == 0) continue;
+            const int lead = __ffs(live) - 1;
+            const int first = __shfl_sync(0xffffffffu, digit, lead);
+            if (__all_sync(0xffffffffu, !on || digit == first)) {
+                if (lane == lead) atomicAdd(&s_hist[digit], __popc(live));
+            } else if (on) {
+                atomicAdd(&s_hist[digit], 1);
+            }
+        }
+        cluster.sync();
+        // bins from the top: thread i takes bins 2 i and 2 i + 1 counted from the top
+        int n0 = 0, n1 = 0;
+        const int i0 = bins - 1 - 2 * tid, i1 = i0 - 1;
+        if (i1 >= 0) {
+            for (int c = 0; c < C; ++c) {
+                const int *hist = cluster.map_shared_rank(s_hist, c);
+                n0 += hist[i0];
+                n1 += hist[i1];
+            }
+        }
+        int incl = n0 + n1;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        int total;
+        const int before_warp = warp_prefix_of_block(__shfl_sync(0xffffffffu, incl, 31), s_warp, total);
+        const int above = before_warp + incl - (n0 + n1);     // keys in bins above i0
+        if (above < want && above + n0 + n1 >= want) {
+            const bool second = above + n0 < want;
+            s_digit = second ? i1 : i0;
+            s_rest = want - above - (second ? n0 : 0);
+        }
+        __syncthreads();
+        prefix |= (uint32_t)s_digit << shift;
+        mask |= (uint32_t)(bins - 1) << shift;
+        want = s_rest;
+        cluster.sync();                                      // the histograms may be cleared again
+    }
+    const bool none = keep == 0;
+
+    // ---- in slot order: ties that still fit, free slots before `keep`, survivors behind it ----
+    const int rows = per_block / kWarps;                     // slots of a warp
+    const int w_lo = min(hi, lo + warp * rows), w_hi = min(hi, w_lo + rows);
+    int ties = 0;
+    for (int t0 = w_lo; t0 < w_hi; t0 += 32) {
+        const int t = t0 + lane;
+        ties += __popc(__ballot_sync(0xffffffffu, !none && t < w_hi && key_of(t) == prefix));
+    }
+    int block_ties;
+    int tie_base = warp_prefix_of_block(ties, s_warp, block_ties);
+    if (tid == 0) s_share[0] = block_ties;
+    cluster.sync();
+    for (int c = 0; c < rank; ++c) tie_base += cluster.map_shared_rank(s_share, c)[0];
+    int holes = 0, sources = 0;
+    {
+        int seen = tie_base;
+        for (int t0 = w_lo; t0 < w_hi; t0 += 32) {
+            const int t = t0 + lane;
+            const uint32_t key = t < w_hi ? key_of(t) : 0;
+            const uint32_t tie = __ballot_sync(0xffffffffu, !none && t < w_hi && key == prefix);
+            const bool kept = !none && t < w_hi && (key > prefix || (key == prefix && seen + __popc(tie & ((1u << lane) - 1)) < want));
+            holes += __popc(__ballot_sync(0xffffffffu, t < w_hi && t < keep && !kept));
+            sources += __popc(__ballot_sync(0xffffffffu, kept && t >= keep));
+            seen += __popc(tie);
+        }
+    }
+    int block_holes, block_sources;
+    int hole_base = warp_prefix_of_block(holes, s_warp, block_holes);
+    int source_base = warp_prefix_of_block(sources, s_warp, block_sources);
+    if (tid == 0) {
+        s_share[1] = block_holes;
+        s_share[2] = block_sources;
+    }
+    cluster.sync();
+    int all_holes = 0;
+    for (int c = 0; c < C; ++c) {
+        const int *other = cluster.map_shared_rank(s_share, c);
+        if (c < rank) {
+            hole_base += other[1];
+            source_base += other[2];
+        }
+        all_holes += other[1];
+    }
+    if (rank == 0 && tid == 0) p.n_moves[b] = all_holes;
+    cluster.sync();                                          // no block leaves while another still reads its shared memory
+    {
+        int seen = tie_base;
+        for (int t0 = w_lo; t0 < w_hi; t0 += 32) {
+            const int t = t0 + lane;
+            const uint32_t key = t < w_hi ? key_of(t) : 0;
+            const uint32_t tie = __ballot_sync(0xffffffffu, !none && t < w_hi && key == prefix), below = (1u << lane) - 1;
+            const bool kept = !none && t < w_hi && (key > prefix || (key == prefix && seen + __popc(tie & below) < want));
+            const bool hole = t < w_hi && t < keep && !kept, source = kept && t >= keep;
+            const uint32_t hm = __ballot_sync(0xffffffffu, hole), sm = __ballot_sync(0xffffffffu, source);
+            if (hole) p.holes[(size_t)b * p.move_stride + hole_base + __popc(hm & below)] = t;
+            if (source) p.sources[(size_t)b * p.move_stride + source_base + __popc(sm & below)] = t;
+            if (kept && t < keep) {
+                if (w_out != w) w_out[t] = w[t];
+                if (pos_out != pos) pos_out[t] = pos ? pos[t] : t;
+            } else if (t < w_hi && t >= keep && !kept) {     // leaves; the slot is behind the new end
+                w_out[t] = 0.f;
+                pos_out[t] = -1;
+            }
+            hole_base += __popc(hm);
+            source_base += __popc(sm);
+            seen += __popc(tie);
+        }
+    }
+}
+
+// One cached row of a pool: `groups` segments of `bytes` each, `bytes` apart by a page's slots.
+struct MovePools {
+    uint8_t *v, *kr;             // kr: nullable
+    uint32_t *sz;                // 4-bit only, else NULL
+    int v_bytes, kr_bytes;       // bytes of a value row of one group, of a positional row (multiples of 16)
+};
+constexpr int kMoveThreads = 256;
+__global__ void __launch_bounds__(kMoveThreads)
+evict_move_kernel(EvictParams p, MovePools c, int G) {
+    grid_dependency_launch();
+    grid_dependency_wait();
+    const int b = blockIdx.y, n = p.n_moves[b];
+    const int warp = blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31, warps = gridDim.x * (kMoveThreads / 32);
+    const int pv = c.v_bytes / 16, pk = c.kr ? c.kr_bytes / 16 : 0, pieces = G * pv + pk;
+    for (int i = warp; i < n; i += warps) {
+        const int to = p.holes[(size_t)b * p.move_stride + i], from = p.sources[(size_t)b * p.move_stride + i];
+        const size_t table = (size_t)b * p.max_pages;
+        const size_t page_to = p.block_table ? (size_t)p.block_table[table + to / p.P] : table + to / p.P;
+        const size_t page_from = p.block_table ? (size_t)p.block_table[table + from / p.P] : table + from / p.P;
+        const int slot_to = to % p.P, slot_from = from % p.P;
+        for (int e = lane; e < pieces; e += 32) {
+            if (e < G * pv) {
+                const int g = e / pv, k = e % pv;
+                *reinterpret_cast<uint4 *>(c.v + ((page_to * G + g) * p.P + slot_to) * c.v_bytes + 16 * k) =
+                    *reinterpret_cast<const uint4 *>(c.v + ((page_from * G + g) * p.P + slot_from) * c.v_bytes + 16 * k);
+            } else {
+                const int k = e - G * pv;
+                *reinterpret_cast<uint4 *>(c.kr + (page_to * p.P + slot_to) * c.kr_bytes + 16 * k) =
+                    *reinterpret_cast<const uint4 *>(c.kr + (page_from * p.P + slot_from) * c.kr_bytes + 16 * k);
+            }
+        }
+        if (c.sz && lane < G) c.sz[(page_to * G + lane) * p.P + slot_to] = c.sz[(page_from * G + lane) * p.P + slot_from];
+        if (lane == 31) {
+            const size_t row = (size_t)b * p.stride;
+            p.w_out[row + to] = p.w_in[row + from];
+            p.w_out[row + from] = 0.f;
+        }
+        if (lane == 30) {
+            const size_t row = (size_t)b * p.stride;
+            p.pos_out[row + to] = p.pos_in ? p.pos_in[row + from] : from;
+            p.pos_out[row + from] = -1;
+        }
+    }
+}
+
+}  // namespace gva

@@ -1,0 +1,413 @@
+// The 4-bit cache: how rows enter it, how they leave it as bf16, and the pieces its readers share.
+//
+// A value row x[0 .. d_v) of one token and group is held as d_v codes of 4 bits and two f16 numbers,
+//     lowest z = the largest f16 <= min x,      step s = the smallest f16 with z + 15 s >= max x,
+//     code c = the number of k in 0 .. 14 with x >= z + (k + 1/2) s,      value = z + s c,
+// so that |value - x| <= s / 2 for every x: z is rounded down and s up, hence the codes always cover the row.  Elements
+// beyond +-65504 are clamped first; a row with a NaN anywhere reads as NaN.  A row of one value has s = 0.
+// Byte i of a row holds dims 2 i (low nibble) and 2 i + 1 (high nibble).  Positional keys are bf16, as in the bf16 cache.
+#pragma once
+
+#include "gva_rope.cuh"
+
+namespace gva {
+
+struct Q4Pools {
+    uint8_t *v;                  // [num_pages][G][P][d_v / 2]
+    __half2 *sz;                 // [num_pages][G][P] (step, lowest)
+    uint16_t *kr;                // [num_pages][P][d_r] bf16
+    const int32_t *block_table;  // nullable
+    int num_pages, max_pages;
+};
+
+// Page of slot t of sequence b, or -1 after reporting why there is none.
+__device__ __forceinline__ int locate_page(const int32_t *block_table, int num_pages, int max_pages, int P, int b, int t, int32_t *dev_status) {
+    if (t < 0 || t / P >= max_pages) {
+        report_error(dev_status, GVA_ERR_SEQ_LEN, b);
+        return -1;
+    }
+    const long long page = block_table ? (long long)block_table[(size_t)b * max_pages + t / P] : (long long)b * max_pages + t / P;
+    if (page < 0 || page >= num_pages) {
+        report_error(dev_status, GVA_ERR_BAD_PAGE, b);
+        return -1;
+    }
+    return (int)page;
+}
+
+// ---- append -----------------------------------------------------------------------------------------------------
+// A block takes `rows` input rows.  Its first warps quantise: d_v / 8 neighbouring lanes hold one value row, eight
+// elements each (two 16-byte loads), reduce minimum and maximum with shuffles, and each writes its eight codes as one
+// 32-bit word.  Its last threads rotate the positional pairs in fp64 meanwhile.
+// All comparisons against the borders z + (k + 1/2) s are exact in f32: 15 s and (k + 1/2) s have at most 16 significant
+// bits, and "x - z >= T" for an f32 number T holds exactly if it holds for x - z rounded down (max - z <= 15 s: up).
+struct AppendQ4Params {
+    Q4Pools c;
+    const float *v_new, *kr_new;
+    const int32_t *cu_q;        // nullable: one row per sequence
+    const int32_t *slot0;       // per sequence: slot of its first row
+    const int32_t *pos0;        // per sequence: position of its first row
+    int B, n_q, G, d_v, d_r, P, rows;
+    int vec;                    // v_new is 16-byte aligned
+    int32_t *dev_status;
+};
+constexpr int kAppendQ4Threads = 256;
+constexpr int kAppendQ4Rows = 8;          // rows of a block at most
+
+__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], float z, float s, float inv_s) {
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float d = __fsub_rd(x[i], z);                  // >= 0
+        float c = rintf(fminf(d * inv_s, 15.f));             // off by at most one
+        if (d < (c - 0.5f) * s) c -= 1.f;                    // (a product of <= 5 by 11 bits: exact)
+        else if (d >= (c + 0.5f) * s) c += 1.f;
+        c = fminf(fmaxf(c, 0.f), 15.f);
+        word |= (uint32_t)(int)c << (4 * i);
+    }
+    return word;
+}
+
+__global__ void __launch_bounds__(kAppendQ4Threads)
+append_q4_kernel(AppendQ4Params p, RopeTable rope) {
+    grid_dependency_launch();
+    __shared__ int s_page[kAppendQ4Rows], s_slot[kAppendQ4Rows], s_pos[kAppendQ4Rows];   // page -1: the row is not written
+    grid_dependency_wait();
+    const int tid = threadIdx.x, n0 = blockIdx.x * p.rows;
+    if (tid < p.rows) {
+        const int n = n0 + tid;
+        int page = -1, slot = 0, pos = 0;
+        const int total = p.cu_q ? min(p.n_q, p.cu_q[p.B]) : p.n_q;
+        if (n < total) {
+            int b = n, i = 0;
+            if (p.cu_q) {
+                int lo = 0, hi = p.B - 1;                    // largest b with cu_q[b] <= n (empty sequences repeat an offset)
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (p.cu_q[mid] <= n) lo = mid;
+                    else hi = mid - 1;
+                }
+                b = lo;
+                i = n - p.cu_q[b];
+            }
+            const long long t = (long long)p.slot0[b] + i, at = (long long)p.pos0[b] + i;
+            if (p.slot0[b] < 0 || p.pos0[b] < 0 || t > 0x7fffffff || at > 0x7fffffff) {
+                report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
+            } else {
+                page = locate_page(p.c.block_table, p.c.num_pages, p.c.max_pages, p.P, b, (int)t, p.dev_status);
+                slot = (int)t % p.P;
+                pos = (int)at;
+            }
+        }
+        s_page[tid] = page;
+        s_slot[tid] = slot;
+        s_pos[tid] = pos;
+    }
+    __syncthreads();
+    const int L = p.d_v / 8;                                 // lanes per value row: 8 or 16
+    const int per_row = p.G * L;
+    const int n_quant = p.rows * per_row;
+    // a multiple of the warp size: the shuffles of the quantising lanes stay among whole warps
+    for (int base = 0; base < (n_quant + 31) / 32 * 32; base += kAppendQ4Threads) {
+        const int e = base + tid;
+        if (e >= (n_quant + 31) / 32 * 32) break;            // whole warps leave together
+        const int r = min(e / per_row, p.rows - 1), g = e % per_row / L, l = e % L;
+        const bool on = e < n_quant && s_page[r] >= 0;
+        float x[8];
+        if (on) {
+            const float *src = p.v_new + ((size_t)(n0 + r) * p.G + g) * p.d_v + 8 * l;
+            if (p.vec) {
+                const float4 a = *reinterpret_cast<const float4 *>(src), b = *reinterpret_cast<const float4 *>(src + 4);
+                x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+                x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = src[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        }
+        bool nan = false;
+        float mn = 65504.f, mx = -65504.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            nan |= x[i] != x[i];
+            x[i] = fminf(fmaxf(x[i], -65504.f), 65504.f);    // (a NaN becomes a number here; its row is marked below)
+            mn = fminf(mn, x[i]);
+            mx = fmaxf(mx, x[i]);
+        }
+        for (int o = 1; o < L; o <<= 1) {
+            mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            nan |= __shfl_xor_sync(0xffffffffu, (int)nan, o) != 0;
+        }
+        const __half zh = __float2half_rd(mn);
+        const float z = __half2float(zh);
+        const __half sh = __float2half_ru(__fdiv_ru(__fsub_ru(mx, z), 15.f));   // smallest f16 with 15 s >= max - z
+        const float s = __half2float(sh);
+        if (on) {
+            const size_t row = ((size_t)s_page[r] * p.G + g) * p.P + s_slot[r];
+            const uint32_t word = s > 0.f ? quantise8(x, z, s, __frcp_rn(s)) : 0u;
+            *reinterpret_cast<uint32_t *>(p.c.v + row * (p.d_v / 2) + 4 * l) = nan ? 0u : word;
+            if (l == 0) p.c.sz[row] = nan ? __halves2half2(__float2half(0.f), __ushort_as_half(0x7fff)) : __halves2half2(sh, zh);
+        }
+    }
+    // positional pairs, from the last thread down
+    const int pairs = p.d_r / 2;
+    for (int e = kAppendQ4Threads - 1 - tid; e < p.rows * pairs; e += kAppendQ4Threads) {
+        const int r = e / pairs, k = e % pairs;
+        if (s_page[r] < 0) continue;
+        const float *src = p.kr_new + (size_t)(n0 + r) * p.d_r + 2 * k;
+        double y0, y1;
+        rope_pair((double)src[0], (double)src[1], s_pos[r], rope.inv_freq[k], y0, y1);
+        uint16_t *dst = p.c.kr + ((size_t)s_page[r] * p.P + s_slot[r]) * p.d_r + 2 * k;
+        *reinterpret_cast<uint32_t *>(dst) = (uint32_t)double_to_bf16_bits(y0) | ((uint32_t)double_to_bf16_bits(y1) << 16);
+    }
+}
+
+// ---- widen ------------------------------------------------------------------------------------------------------
+// Slots [starts[b], seq_lens[b]) of every sequence as bf16 rows of another cache: z + s c in f32, rounded once.  A block
+// takes 64 slots of one sequence; d_v / 8 lanes widen one row, 4 bytes in and 16 bytes out per lane, neighbouring slots of
+// a group one after the other, so that reads and writes run through a page's rows in order.
+constexpr int kWidenTokens = 64;
+struct WidenParams {
+    Q4Pools c;
+    uint16_t *v, *kr;            // bf16 pools
+    const int32_t *block_table;  // of the bf16 cache; nullable
+    int num_pages, max_pages;
+    const int32_t *starts, *seq_lens;
+    int G, d_v, d_r, P;
+    int32_t *dev_status;
+};
+__global__ void __launch_bounds__(256)
+widen_q4_kernel(WidenParams p) {
+    grid_dependency_launch();
+    __shared__ int s_src[kWidenTokens], s_dst[kWidenTokens];
+    grid_dependency_wait();
+    const int b = blockIdx.y, tid = threadIdx.x;
+    const int start = p.starts ? p.starts[b] : 0, len = p.seq_lens[b];
+    if (start < 0 || len < 0) {
+        if (blockIdx.x == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
+        return;
+    }
+    const int L = p.d_v / 8;
+    for (long long t0 = start + (long long)blockIdx.x * kWidenTokens; t0 < len; t0 += (long long)gridDim.x * kWidenTokens) {
+        const int n = (int)min((long long)kWidenTokens, len - t0);
+        if (tid < n) {
+            const int t = (int)t0 + tid;
+            int a = locate_page(p.c.block_table, p.c.num_pages, p.c.max_pages, p.P, b, t, p.dev_status);
+            const int d = locate_page(p.block_table, p.num_pages, p.max_pages, p.P, b, t, p.dev_status);
+            s_src[tid] = d < 0 ? -1 : a;
+            s_dst[tid] = d;
+        }
+        __syncthreads();
+        for (int e = tid; e < p.G * n * L; e += blockDim.x) {
+            const int l = e % L, k = e / L % n, g = e / L / n;
+            if (s_src[k] < 0) continue;
+            const int slot = ((int)t0 + k) % p.P;
+            const size_t row = ((size_t)s_src[k] * p.G + g) * p.P + slot;
+            const uint32_t word = *reinterpret_cast<const uint32_t *>(p.c.v + row * (p.d_v / 2) + 4 * l);
+            const float2 sz = __half22float2(p.c.sz[row]);
+            uint32_t out[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float a = fmaf((float)((word >> (8 * i)) & 15u), sz.x, sz.y), c = fmaf((float)((word >> (8 * i + 4)) & 15u), sz.x, sz.y);
+                out[i] = (uint32_t)float_to_bf16_bits(a) | ((uint32_t)float_to_bf16_bits(c) << 16);
+            }
+            const size_t to = (((size_t)s_dst[k] * p.G + g) * p.P + slot) * p.d_v + 8 * l;
+            *reinterpret_cast<uint4 *>(p.v + to) = make_uint4(out[0], out[1], out[2], out[3]);
+        }
+        const int pieces = p.d_r / 8;                        // 16-byte pieces of a positional row
+        for (int e = tid; e < n * pieces; e += blockDim.x) {
+            const int k = e / pieces, i = e % pieces;
+            if (s_src[k] < 0) continue;
+            const int slot = ((int)t0 + k) % p.P;
+            reinterpret_cast<uint4 *>(p.kr)[((size_t)s_dst[k] * p.P + slot) * pieces + i] =
+                reinterpret_cast<const uint4 *>(p.c.kr)[((size_t)s_src[k] * p.P + slot) * pieces + i];
+        }
+        __syncthreads();
+    }
+}
+
+// ---- merge of split-KV partials -----------------------------------------------------------------------------------
+// Records of sequence b, known from the lengths alone: in the balanced partition block c of the decode kernel holds flat
+// tiles [range_begin(c), range_begin(c + 1)) and its part of sequence b is record c + b; with num_splits ranges per
+// sequence they are b * num_splits onwards.  One block per (sequence, head); d_v / 4 lanes read one record's output in
+// 16-byte pieces, the other threads other records; the order of the sum is fixed by the number of threads.
+struct MergeParams {
+    const float *rec_o, *rec_ml;   // [n_rec][H][d_v], [n_rec][H][2]
+    const int32_t *seq_lens;
+    float *out, *lse;
+    int B, H, P, max_pages, num_splits, n_blocks, tile;
+};
+template <int DV>
+__global__ void __launch_bounds__(1024)
+merge_records_kernel(MergeParams p) {
+    grid_dependency_launch();
+    __shared__ int s_before[32], s_all[32];
+    __shared__ float s_red[32];
+    extern __shared__ float s_o[];                           // [parts][DV] outputs, [parts] sums
+    const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
+    grid_dependency_wait();
+    int first, count;
+    const long long cap = (long long)p.max_pages * p.P;
+    if (p.num_splits > 0) {
+        const int len = p.seq_lens[b];
+        first = b * p.num_splits;
+        count = len > 0 && len <= cap ? p.num_splits : 0;
+    } else {
+        int before = 0, all = 0, mine = 0;
+        for (int i = tid; i < p.B; i += nt) {
+            int len = p.seq_lens[i];
+            if (len < 0 || len > cap) len = 0;
+            const int tiles = (len + p.tile - 1) / p.tile;
+            all += tiles;
+            if (i < b) before += tiles;
+        }
+        {
+            int len = p.seq_lens[b];
+            if (len < 0 || len > cap) len = 0;
+            mine = (len + p.tile - 1) / p.tile;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            before += __shfl_xor_sync(0xffffffffu, before, o);
+            all += __shfl_xor_sync(0xffffffffu, all, o);
+        }
+        if (lane == 0) {
+            s_before[warp] = before;
+            s_all[warp] = all;
+        }
+        __syncthreads();
+        before = all = 0;
+        for (int w = 0; w < nt / 32; ++w) {
+            before += s_before[w];
+            all += s_all[w];
+        }
+        first = count = 0;
+        if (mine > 0) {
+            const int n_eff = partitions_in_use(all, p.n_blocks);
+            const int c0 = range_owner(before, all, n_eff), c1 = range_owner(before + mine - 1, all, n_eff);
+            first = c0 + b;
+            count = c1 - c0 + 1;
+        }
+    }
+    // running maximum over the records, then weights
+    float m = -INFINITY;
+    for (int r = tid; r < count; r += nt) m = fmaxf(m, p.rec_ml[((size_t)(first + r) * p.H + h) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) s_red[warp] = m;
+    __syncthreads();
+    m = -INFINITY;
+    for (int w = 0; w < nt / 32; ++w) m = fmaxf(m, s_red[w]);
+    const float base = m == -INFINITY ? 0.f : m;
+    constexpr int L = DV / 4;
+    const int parts = nt / L, part = tid / L, l = tid % L;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int r = part; r < count; r += parts) {
+        const size_t rh = (size_t)(first + r) * p.H + h;
+        const float2 ml = *reinterpret_cast<const float2 *>(p.rec_ml + rh * 2);
+        const float w = exp2f(ml.x - base);
+        const float4 o = *reinterpret_cast<const float4 *>(p.rec_o + rh * DV + 4 * l);
+        if (ml.x != -INFINITY) {                             // (an empty range leaves its output unwritten)
+            acc.x = fmaf(w, o.x, acc.x);
+            acc.y = fmaf(w, o.y, acc.y);
+            acc.z = fmaf(w, o.z, acc.z);
+            acc.w = fmaf(w, o.w, acc.w);
+            sum = fmaf(w, ml.y, sum);
+        }
+    }
+    *reinterpret_cast<float4 *>(s_o + part * DV + 4 * l) = acc;
+    if (l == 0) s_o[parts * DV + part] = sum;
+    __syncthreads();
+    if (tid < DV) {
+        float o = 0.f, t = 0.f;
+        for (int k = 0; k < parts; ++k) {
+            o += s_o[k * DV + tid];
+            t += s_o[parts * DV + k];
+        }
+        p.out[((size_t)b * p.H + h) * DV + tid] = count > 0 && t != 0.f ? o / t : 0.f;
+        if (tid == 0 && p.lse) p.lse[(size_t)b * p.H + h] = count > 0 ? (m + log2f(t)) * kLn2 : -INFINITY;
+    }
+}
+
+// ---- decode, plain form -------------------------------------------------------------------------------------------
+// One block per (range of tiles, group); a warp per token, d_v / 32 dims per lane.
+template <int DV>
+__global__ void __launch_bounds__(128)
+decode_q4_simple_kernel(DecodeParams p, Q4Pools c, int tile, int DR) {
+    grid_dependency_launch();
+    grid_dependency_wait();
+    const int b = blockIdx.x / p.num_splits, s = blockIdx.x % p.num_splits, g = blockIdx.y;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int len = p.seq_lens[b];
+    if (len < 0 || (long long)len > (long long)p.max_pages * p.P) {
+        if (threadIdx.x == 0 && s == 0 && g == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
+        len = 0;
+    }
+    const int tiles = (len + tile - 1) / tile, DQ = DV + DR;
+    const int lo = (int)((long long)s * tiles / p.num_splits) * tile, hi = min(len, (int)((long long)(s + 1) * tiles / p.num_splits) * tile);
+    constexpr int E = DV / 32;
+    float q[4][E], qr[4], m[4], l[4], o[4][E];
+    for (int j = 0; j < 4; ++j) {
+        const float *src = p.q + ((size_t)b * p.H + g * 4 + j) * DQ;
+        for (int e = 0; e < E; ++e) {
+            q[j][e] = src[lane * E + e];
+            o[j][e] = 0.f;
+        }
+        qr[j] = lane < DR ? src[DV + lane] : 0.f;
+        m[j] = -INFINITY;
+        l[j] = 0.f;
+    }
+    for (int t = lo + warp; t < hi; t += 4) {
+        const int page = locate_page(c.block_table, c.num_pages, c.max_pages, p.P, b, t, p.dev_status);
+        if (page < 0) continue;
+        const size_t row = ((size_t)page * p.G + g) * p.P + t % p.P;
+        const float2 sz = __half22float2(c.sz[row]);
+        float v[E];
+        for (int e = 0; e < E; e += 2) {
+            const uint8_t x = c.v[row * (DV / 2) + lane * (E / 2) + e / 2];
+            v[e] = fmaf((float)(x & 15), sz.x, sz.y);
+            v[e + 1] = fmaf((float)(x >> 4), sz.x, sz.y);
+        }
+        const float k = lane < DR ? __uint_as_float((uint32_t)c.kr[((size_t)page * p.P + t % p.P) * DR + lane] << 16) : 0.f;
+        for (int j = 0; j < 4; ++j) {
+            float x = qr[j] * k;
+            for (int e = 0; e < E; ++e) x = fmaf(q[j][e], v[e], x);
+            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+            x *= p.scale_log2;
+            const float mn = fmaxf(m[j], x), f = exp2f(m[j] - mn), w = exp2f(x - mn);
+            m[j] = mn;
+            l[j] = fmaf(l[j], f, w);
+            for (int e = 0; e < E; ++e) o[j][e] = fmaf(o[j][e], f, w * v[e]);
+        }
+    }
+    __shared__ float s_o[4][4][DV], s_ml[4][4][2];
+    for (int j = 0; j < 4; ++j) {
+        for (int e = 0; e < E; ++e) s_o[warp][j][lane * E + e] = o[j][e];
+        s_ml[warp][j][0] = m[j];
+        s_ml[warp][j][1] = l[j];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4 * DV; i += 128) {
+        const int j = i / DV, d = i % DV;
+        float mm = -INFINITY, a = 0.f, ll = 0.f;
+        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w][j][0]);
+        for (int w = 0; w < 4; ++w) {
+            const float f = s_ml[w][j][0] == -INFINITY ? 0.f : exp2f(s_ml[w][j][0] - mm);
+            a = fmaf(f, s_o[w][j][d], a);
+            ll = fmaf(f, s_ml[w][j][1], ll);
+        }
+        const size_t rh = (size_t)blockIdx.x * p.H + g * 4 + j;
+        p.rec_o[rh * DV + d] = a;
+        if (d == 0) {
+            p.rec_ml[rh * 2] = mm;
+            p.rec_ml[rh * 2 + 1] = ll;
+        }
+    }
+}
+
+}  // namespace gva

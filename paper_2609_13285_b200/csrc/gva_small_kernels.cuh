@@ -4,42 +4,9 @@
 
 #include <type_traits>
 
-#include "gva_common.cuh"
+#include "gva_rope.cuh"
 
 namespace gva {
-
-constexpr int kMaxRopePairs = 16;   // d_r <= 32
-
-struct RopeTable {
-    double inv_freq[kMaxRopePairs];   // base^(-2i/d_r), computed once on the host in fp64
-};
-
-// fp64 -> bf16, round to nearest even without double rounding: truncate to f32 toward zero, fold
-// everything that was cut off into the f32's last mantissa bit (round to odd), then round that
-// f32 to 8 significant bits.  f32 keeps 16 more bits than bf16, so the two-step result equals the
-// direct rounding of the fp64 value.
-__device__ __forceinline__ uint16_t double_to_bf16_bits(double x) {
-    float f = __double2float_rz(x);
-    uint32_t u = __float_as_uint(f);
-    if ((double)f != x && (u & 0x7f800000u) != 0x7f800000u) u |= 1u;
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40);   // NaN stays NaN
-    u += 0x7fffu + ((u >> 16) & 1u);
-    return (uint16_t)(u >> 16);
-}
-__device__ __forceinline__ uint16_t float_to_bf16_bits(float f) {
-    return __bfloat16_as_ushort(__float2bfloat16_rn(f));
-}
-// 8-bit e4m3 codes: round to nearest even, finite overflow and infinity saturate to +-448, NaN stays NaN
-__device__ __forceinline__ uint8_t float_to_e4m3_bits(float f) { return (uint8_t)__nv_cvt_float_to_fp8(f, __NV_SATFINITE, __NV_E4M3); }
-__device__ __forceinline__ uint8_t double_to_e4m3_bits(double x) { return (uint8_t)__nv_cvt_double_to_fp8(x, __NV_SATFINITE, __NV_E4M3); }
-
-// One pair of y = x R_pos^T in fp64.
-__device__ __forceinline__ void rope_pair(double x0, double x1, int pos, double inv_freq, double &y0, double &y1) {
-    double s, c;
-    sincos((double)pos * inv_freq, &s, &c);
-    y0 = x0 * c - x1 * s;
-    y1 = x0 * s + x1 * c;
-}
 
 // ---- absorb --------------------------------------------------------------------------------------
 // grid (H, ceil(B / kAbsorbBatch)), block 256.  M_h is staged once per block in shared memory
@@ -466,6 +433,30 @@ append_kernel(CT *__restrict__ v_pool, CT *__restrict__ kr_pool, const int32_t *
     grid_dependency_wait();
     append_block<CT>(v_pool, kr_pool, block_table, v_new, kr_new, pos, G, d_v, d_r, P, num_pages, max_pages, dev_status,
                      rope, blockIdx.x);
+}
+
+// The same where the slot is not the position: after an eviction the cache of a sequence holds fewer tokens than the
+// sequence has had, so the next free slot is behind the position the new key is rotated to.
+template <typename CT>
+__global__ void __launch_bounds__(128)
+append_at_kernel(CT *__restrict__ v_pool, CT *__restrict__ kr_pool, const int32_t *__restrict__ block_table,
+                 const float *__restrict__ v_new, const float *__restrict__ kr_new, const int32_t *__restrict__ slots,
+                 const int32_t *__restrict__ pos, int G, int d_v, int d_r, int P, int num_pages, int max_pages,
+                 int32_t *dev_status, RopeTable rope) {
+    grid_dependency_launch();
+    grid_dependency_wait();
+    const int b = blockIdx.x, slot = slots[b], at = pos[b];
+    if (at < 0) {
+        if (threadIdx.x == 0) report_error(dev_status, GVA_ERR_SEQ_LEN, b);
+        return;
+    }
+    AppendRegs r = append_load(v_new, kr_new, G, d_v, d_r, b);
+    append_locate(r, block_table, P, max_pages, dev_status, b, slot);
+    if (r.t < 0) return;
+    r.t = at;                       // the rotation goes by the position,
+    append_rotate(r, d_r, rope);
+    r.t = slot;                     // the store by the slot
+    append_store<CT>(r, v_pool, kr_pool, G, d_v, d_r, P, num_pages, dev_status, b);
 }
 
 // Append of a chunk of new tokens per sequence: input row n becomes token ctx_lens[b] + (n - cu_q[b]) of the sequence b

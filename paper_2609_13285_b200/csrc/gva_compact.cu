@@ -5,9 +5,18 @@
 #include <cstring>
 
 #include "gva_evict.cuh"
+#include "gva_q4_decode.cuh"
 #include "gva_handle.cuh"
 
 using namespace gva;
+
+// build-time knobs of the 4-bit decode: ring depth, resident blocks per SM (d_v = 64, G <= 4)
+#ifndef GVA_Q4_NSTAGE
+#define GVA_Q4_NSTAGE 4
+#endif
+#ifndef GVA_Q4_BLOCKS
+#define GVA_Q4_BLOCKS 4
+#endif
 
 namespace {
 int check_q4(const gva_handle *h, const gva_q4_cache *cache) {
@@ -39,19 +48,49 @@ int append_q4(gva_handle *h, const gva_q4_cache *cache, const float *v_new, cons
                                static_cast<cudaStream_t>(stream), p, h->rope));
 }
 
-int q4_splits(const gva_handle *h, int B, int max_seq_len, int num_splits) {
+// ---- 4-bit decode: which kernel, which grid ----
+using Q4DecodeFn = void (*)(DecodeParams, Q4Pools);
+struct Q4Plan {
+    Q4DecodeFn fn;
+    size_t smem;
+    int tile, threads, blocks_per_sm;
+};
+template <int DV, int DR, int TILE>
+Q4Plan q4_plan_t(const gva_handle *h, int B) {
+    using T = Q4Traits<DV, DR, TILE>;
+    constexpr int NSTAGE = GVA_Q4_NSTAGE, B4 = DV == 64 ? GVA_Q4_BLOCKS : 2, B8 = DV == 64 ? 2 : 1;
+    Q4Plan p;
+    const bool narrow = h->cfg.G <= 4;
+    p.fn = narrow ? decode_q4_kernel<DV, DR, TILE, NSTAGE, 4, B4> : decode_q4_kernel<DV, DR, TILE, NSTAGE, 8, B8>;
+    p.blocks_per_sm = narrow ? B4 : B8;
+    p.smem = (size_t)NSTAGE * T::stage_bytes(h->cfg.G) + T::tail_bytes(B, NSTAGE);
+    p.tile = TILE;
+    p.threads = 32 * (h->cfg.G + 1);
+    return p;
+}
+Q4Plan q4_plan(const gva_handle *h, int B) {
+    const gva_config &c = h->cfg;
+    const bool t64 = c.page_size % 64 == 0;              // a tile lies in one page
+#define GVA_Q4(DV_, DR_) (t64 ? q4_plan_t<DV_, DR_, 64>(h, B) : q4_plan_t<DV_, DR_, 32>(h, B))
+    if (c.d_v == 64) return c.d_r == 16 ? GVA_Q4(64, 16) : c.d_r == 24 ? GVA_Q4(64, 24) : GVA_Q4(64, 0);
+    return c.d_r == 32 ? GVA_Q4(128, 32) : GVA_Q4(128, 0);
+#undef GVA_Q4
+}
+// Ranges per sequence.  Automatic: one where every sequence is a few tiles at most -- a block then writes the result itself
+// and there is nothing to merge -- else 0, the balanced partition over all resident blocks.
+int q4_splits(const gva_handle *h, int max_seq_len, int num_splits) {
     if (num_splits > 0) return num_splits;
-    const int tiles = std::max(1, (max_seq_len + 63) / 64);
-    return std::max(1, std::min(tiles, 8 * h->sm_count / std::max(1, B * h->cfg.G)));
+    const int tile = h->cfg.page_size % 64 == 0 ? 64 : 32;
+    return max_seq_len <= 2 * tile ? 1 : 0;
 }
 struct Q4Workspace {
-    size_t rec_o, rec_ml, total;
+    size_t rec_ml, total;
     int n_rec;
 };
 Q4Workspace q4_workspace(const gva_handle *h, int B, int max_seq_len, int num_splits) {
     Q4Workspace w;
-    w.n_rec = std::max(1, B * q4_splits(h, B, max_seq_len, num_splits));
-    w.rec_o = 0;
+    const int splits = q4_splits(h, max_seq_len, num_splits);
+    w.n_rec = std::max(1, splits > 0 ? B * splits : q4_plan(h, B).blocks_per_sm * h->sm_count + B);
     w.rec_ml = align_up((size_t)w.n_rec * h->cfg.H * h->cfg.d_v * 4, 256);
     w.total = w.rec_ml + align_up((size_t)w.n_rec * h->cfg.H * 2 * 4, 256);
     return w;
@@ -206,30 +245,38 @@ int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, 
     if (!workspace || workspace_bytes < w.total) return GVA_ERR_WORKSPACE;
     if (!aligned(workspace, 256)) return GVA_ERR_INVALID_ARG;
     const gva_config &c = h->cfg;
+    const Q4Plan plan = q4_plan(h, B);
+    if (plan.smem > (size_t)h->smem_optin) return GVA_ERR_UNSUPPORTED;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     DecodeParams p;
     std::memset(&p, 0, sizeof(p));
     p.seq_lens = seq_lens;
+    p.block_table = cache->block_table;
     p.q = q_abs;
-    p.rec_o = reinterpret_cast<float *>(ws + w.rec_o);
+    p.out = out;
+    p.lse = lse;
+    p.rec_o = reinterpret_cast<float *>(ws);
     p.rec_ml = reinterpret_cast<float *>(ws + w.rec_ml);
     p.dev_status = dev_status;
     p.B = B; p.H = c.H; p.G = c.G; p.P = c.page_size;
     p.num_pages = cache->num_pages;
     p.max_pages = cache->max_pages_per_seq;
-    p.num_splits = q4_splits(h, B, max_seq_len, num_splits);
+    p.num_splits = q4_splits(h, max_seq_len, num_splits);
     p.scale_log2 = h->scale * kLog2e;
+    const long long tiles = std::max<long long>(1, (long long)B * ((max_seq_len + plan.tile - 1) / plan.tile));
+    const int grid = p.num_splits > 0 ? B * p.num_splits : (int)std::min<long long>(tiles, (long long)plan.blocks_per_sm * h->sm_count);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const dim3 grid(B * p.num_splits, c.G);
-    rc = launched(c.d_v == 64 ? launch_pdl(decode_q4_simple_kernel<64>, grid, dim3(128), 0, s, p, q4_pools(cache), 64, c.d_r)
-                              : launch_pdl(decode_q4_simple_kernel<128>, grid, dim3(128), 0, s, p, q4_pools(cache), 64, c.d_r));
-    if (rc != GVA_OK) return rc;
+    if (cudaFuncSetAttribute(plan.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem) != cudaSuccess) return GVA_ERR_CUDA;
+    rc = launched(launch_pdl(plan.fn, dim3(grid), dim3(plan.threads), plan.smem, s, p, q4_pools(cache)));
+    if (rc != GVA_OK || p.num_splits == 1) return rc;
     MergeParams m;
     m.rec_o = p.rec_o; m.rec_ml = p.rec_ml; m.seq_lens = seq_lens; m.out = out; m.lse = lse;
     m.B = B; m.H = c.H; m.P = c.page_size; m.max_pages = cache->max_pages_per_seq; m.num_splits = p.num_splits;
-    m.n_blocks = B * p.num_splits; m.tile = 64;
-    const int threads = 256, parts = threads / (c.d_v / 4);
-    const size_t smem = (size_t)parts * (c.d_v + 1) * 4;
+    m.n_blocks = grid; m.tile = plan.tile;
+    const int records = p.num_splits > 0 ? p.num_splits : grid / B + 2;      // of a sequence, about
+    int threads = 64;
+    while (threads < 1024 && threads / (c.d_v / 4) * 4 < records) threads *= 2;
+    const size_t smem = (size_t)(threads / (c.d_v / 4)) * (c.d_v + 1) * 4;
     return launched(c.d_v == 64 ? launch_pdl(merge_records_kernel<64>, dim3(B, c.H), dim3(threads), smem, s, m)
                                 : launch_pdl(merge_records_kernel<128>, dim3(B, c.H), dim3(threads), smem, s, m));
 }

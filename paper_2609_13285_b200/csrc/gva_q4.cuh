@@ -290,6 +290,7 @@ merge_records_kernel(MergeParams p) {
             const int c0 = range_owner(before, all, n_eff), c1 = range_owner(before + mine - 1, all, n_eff);
             first = c0 + b;
             count = c1 - c0 + 1;
+            if (count == 1) return;                          // one block had the whole sequence and wrote the result
         }
     }
     // running maximum over the records, then weights
@@ -323,90 +324,14 @@ merge_records_kernel(MergeParams p) {
     *reinterpret_cast<float4 *>(s_o + part * DV + 4 * l) = acc;
     if (l == 0) s_o[parts * DV + part] = sum;
     __syncthreads();
-    if (tid < DV) {
+    for (int d = tid; d < DV; d += nt) {
         float o = 0.f, t = 0.f;
         for (int k = 0; k < parts; ++k) {
-            o += s_o[k * DV + tid];
+            o += s_o[k * DV + d];
             t += s_o[parts * DV + k];
         }
-        p.out[((size_t)b * p.H + h) * DV + tid] = count > 0 && t != 0.f ? o / t : 0.f;
-        if (tid == 0 && p.lse) p.lse[(size_t)b * p.H + h] = count > 0 ? (m + log2f(t)) * kLn2 : -INFINITY;
-    }
-}
-
-// ---- decode, plain form -------------------------------------------------------------------------------------------
-// One block per (range of tiles, group); a warp per token, d_v / 32 dims per lane.
-template <int DV>
-__global__ void __launch_bounds__(128)
-decode_q4_simple_kernel(DecodeParams p, Q4Pools c, int tile, int DR) {
-    grid_dependency_launch();
-    grid_dependency_wait();
-    const int b = blockIdx.x / p.num_splits, s = blockIdx.x % p.num_splits, g = blockIdx.y;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int len = p.seq_lens[b];
-    if (len < 0 || (long long)len > (long long)p.max_pages * p.P) {
-        if (threadIdx.x == 0 && s == 0 && g == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
-        len = 0;
-    }
-    const int tiles = (len + tile - 1) / tile, DQ = DV + DR;
-    const int lo = (int)((long long)s * tiles / p.num_splits) * tile, hi = min(len, (int)((long long)(s + 1) * tiles / p.num_splits) * tile);
-    constexpr int E = DV / 32;
-    float q[4][E], qr[4], m[4], l[4], o[4][E];
-    for (int j = 0; j < 4; ++j) {
-        const float *src = p.q + ((size_t)b * p.H + g * 4 + j) * DQ;
-        for (int e = 0; e < E; ++e) {
-            q[j][e] = src[lane * E + e];
-            o[j][e] = 0.f;
-        }
-        qr[j] = lane < DR ? src[DV + lane] : 0.f;
-        m[j] = -INFINITY;
-        l[j] = 0.f;
-    }
-    for (int t = lo + warp; t < hi; t += 4) {
-        const int page = locate_page(c.block_table, c.num_pages, c.max_pages, p.P, b, t, p.dev_status);
-        if (page < 0) continue;
-        const size_t row = ((size_t)page * p.G + g) * p.P + t % p.P;
-        const float2 sz = __half22float2(c.sz[row]);
-        float v[E];
-        for (int e = 0; e < E; e += 2) {
-            const uint8_t x = c.v[row * (DV / 2) + lane * (E / 2) + e / 2];
-            v[e] = fmaf((float)(x & 15), sz.x, sz.y);
-            v[e + 1] = fmaf((float)(x >> 4), sz.x, sz.y);
-        }
-        const float k = lane < DR ? __uint_as_float((uint32_t)c.kr[((size_t)page * p.P + t % p.P) * DR + lane] << 16) : 0.f;
-        for (int j = 0; j < 4; ++j) {
-            float x = qr[j] * k;
-            for (int e = 0; e < E; ++e) x = fmaf(q[j][e], v[e], x);
-            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-            x *= p.scale_log2;
-            const float mn = fmaxf(m[j], x), f = exp2f(m[j] - mn), w = exp2f(x - mn);
-            m[j] = mn;
-            l[j] = fmaf(l[j], f, w);
-            for (int e = 0; e < E; ++e) o[j][e] = fmaf(o[j][e], f, w * v[e]);
-        }
-    }
-    __shared__ float s_o[4][4][DV], s_ml[4][4][2];
-    for (int j = 0; j < 4; ++j) {
-        for (int e = 0; e < E; ++e) s_o[warp][j][lane * E + e] = o[j][e];
-        s_ml[warp][j][0] = m[j];
-        s_ml[warp][j][1] = l[j];
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 4 * DV; i += 128) {
-        const int j = i / DV, d = i % DV;
-        float mm = -INFINITY, a = 0.f, ll = 0.f;
-        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w][j][0]);
-        for (int w = 0; w < 4; ++w) {
-            const float f = s_ml[w][j][0] == -INFINITY ? 0.f : exp2f(s_ml[w][j][0] - mm);
-            a = fmaf(f, s_o[w][j][d], a);
-            ll = fmaf(f, s_ml[w][j][1], ll);
-        }
-        const size_t rh = (size_t)blockIdx.x * p.H + g * 4 + j;
-        p.rec_o[rh * DV + d] = a;
-        if (d == 0) {
-            p.rec_ml[rh * 2] = mm;
-            p.rec_ml[rh * 2 + 1] = ll;
-        }
+        p.out[((size_t)b * p.H + h) * DV + d] = count > 0 && t != 0.f ? o / t : 0.f;
+        if (d == 0 && p.lse) p.lse[(size_t)b * p.H + h] = count > 0 ? (m + log2f(t)) * kLn2 : -INFINITY;
     }
 }
 

@@ -1,0 +1,497 @@
+// Split-KV decode over the 4-bit cache on the tensor cores (mma.sync m16n8k16, f16 in, f32 accumulate).
+//
+// With value = z + s c (gva_q4.cuh) the score of token t and its share of the output are
+//     q . v_t = s_t (q . c_t) + z_t sum(q),          sum_t p_t v_t = sum_t (p_t s_t) c_t + sum_t p_t z_t,
+// so the products run over the codes and step and lowest come in afterwards, per token, in f32.
+//
+// Codes as MMA operands.  Score: a nibble in the low bits of a 16-bit half word, the rest zero, is an f16 subnormal: c 2^-24, or
+// c 2^-20 one nibble further up.  Masking is all it takes to widen two codes (four masks and one shift for a word of
+// eight), and the powers of two are undone in the query.  Tensor cores multiply subnormals exactly but align products by
+// their nominal exponent 2^-14, which costs the sum up to ten of its bits: 8e-7 (rms) of a score, which the softmax can
+// take.  The output cannot (3e-5 measured), nor the offset of codes that are all positive: over T tokens it cancels to
+// T^-1/2 of its size.  So there the codes are centred, c - 8, and made normal numbers: one subtraction per two codes more, and
+//     sum_t p_t v_t = sum_t (p_t s_t) (c_t - 8) + sum_t p_t (z_t + 8 s_t).
+//
+// Both products need the contraction index in pairs inside a register: dims for the score, tokens for the output.  A lane
+// therefore reads the tile twice, as whole words: for the score the d_v / 4 dims [c d_v / 4, ...) of its two token rows
+// (c = lane % 4), for the output eight dims of four tokens, whose words two byte permutes interleave into token pairs.  The
+// order of dims inside the score's contraction and of dims over the output's rows is free, so no transposing load is needed.
+// Tokens stand in the order rowmap() in both, which keeps the two access patterns free of bank conflicts for d_v = 64.
+//
+// Precision: query and softmax weight enter as two f16 numbers (hi + lo, the 4 heads x 2 are the 8 MMA columns), each scaled
+// by a power of two so that neither overflows nor loses bits to f16's range: per head for the query, and for the weights
+// p s by the largest step seen so far, which is followed like the running maximum.
+//
+// A block streams a contiguous range of tiles through an NSTAGE ring of bulk copies (one producer warp, G consumer warps,
+// one group each); see gva_common.cuh for the ranges.  All waits are bounded.
+#pragma once
+
+#include "gva_decode_mma.cuh"
+#include "gva_q4.cuh"
+
+namespace gva {
+
+template <int DV_, int DR_, int TILE_>
+struct Q4Traits {
+    static constexpr int DV = DV_, DR = DR_, TILE = TILE_;
+    static constexpr int ROW = DV / 2;                       // bytes of codes per token and group
+    static constexpr int V_BYTES = TILE * ROW, SZ_BYTES = TILE * 4, KR_ROW = DR * 2, KR_BYTES = TILE * KR_ROW;
+    static constexpr int WORDS = DV / 32;                    // words of a row a lane takes for the score: two k-steps each
+    static constexpr int KSTEPS = DV / 16;
+    static constexpr int MT = DV / 16;
+    static constexpr int CHUNKS = TILE / 16;
+    static constexpr int DQ = DV + DR;
+    __host__ __device__ static constexpr int stage_bytes(int G) { return G * (V_BYTES + SZ_BYTES) + KR_BYTES; }
+    __host__ __device__ static constexpr int tail_bytes(int B, int nstage) { return nstage * 32 + 16 + (B + 1) * 4; }
+};
+
+__device__ __forceinline__ int rowmap(int r) { return r ^ ((r >> 2) & 1); }
+
+// A copy of whole 16-byte pieces that nobody else reads: evict-first in L2.
+__device__ __forceinline__ void bulk_load_stream(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t pol) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;\n" ::"r"(dst),
+        "l"(src), "r"(bytes), "r"(bar), "l"(pol)
+        : "memory");
+}
+__device__ __forceinline__ void mma_f16_q4(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_half2(float x, float y) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// (x0, x1) -> {hi, lo} f16 pairs of each
+__device__ __forceinline__ void split_pair_f16(float x0, float x1, uint32_t &s0, uint32_t &s1) {
+    const __half2 h = __floats2half2_rn(x0, x1);
+    const float2 f = __half22float2(h);
+    const uint32_t hu = *reinterpret_cast<const uint32_t *>(&h), lu = pack_half2(x0 - f.x, x1 - f.y);
+    s0 = __byte_perm(hu, lu, 0x5410);
+    s1 = __byte_perm(hu, lu, 0x7632);
+}
+// hi (part 0) or lo (part 1) of x as f16 bits; hi, mid, lo (part 2) as bf16 bits
+__device__ __forceinline__ uint32_t part_f16(float x, int part) {
+    const __half hi = __float2half_rn(x);
+    return __half_as_ushort(part ? __float2half_rn(x - __half2float(hi)) : hi);
+}
+__device__ __forceinline__ uint32_t part_bf16(float x, int part) {
+    __nv_bfloat16 y = __float2bfloat16_rn(x);
+    for (int i = 0; i < part; ++i) {
+        x -= __bfloat162float(y);
+        y = __float2bfloat16_rn(x);
+    }
+    return __bfloat16_as_ushort(y);
+}
+
+// Two codes as signed f16 numbers c - 8: 1024 + c (or 64 + c, one nibble up) by masks, less 1032 (72), exactly.
+__device__ __forceinline__ uint32_t centred_low(uint32_t x) {
+    const uint32_t y = (x & 0x000f000fu) | 0x64006400u, off = 0x64086408u;
+    const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&y), *reinterpret_cast<const __half2 *>(&off));
+    return *reinterpret_cast<const uint32_t *>(&d);
+}
+__device__ __forceinline__ uint32_t centred_high(uint32_t x) {
+    const uint32_t y = (x & 0x00f000f0u) | 0x54005400u, off = 0x54805480u;
+    const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&y), *reinterpret_cast<const __half2 *>(&off));
+    return *reinterpret_cast<const uint32_t *>(&d);
+}
+
+// One group's four queries as the score product's B fragments, for the MMA column n = lane / 4 = 2 head + {hi, lo}, scaled
+// by `factor` (softmax scale and log2 e).  Content: q 2^-e 2^10 with |q 2^-e| <= 1, times 16 where the code stands in the low
+// nibble; unscale = 2^(e + 10) of the head whose scores this lane holds (lane % 4); sum = sum of that head's content query.
+// Position: the keys are bf16 and so are the query's parts, of which two carry 16 bits only (measured: a max-abs error of
+// 3e-5 over 600 short sequences); the third stands in r2, in the hi columns, against one more MMA per 16 tokens.
+template <class T>
+struct Q4Query {
+    uint32_t v[T::KSTEPS][2];
+    uint32_t r[T::DR > 0 ? (T::DR + 15) / 16 : 1][2], r2[T::DR > 0 ? (T::DR + 15) / 16 : 1][2];
+    float unscale, sum;
+};
+template <class T>
+__device__ __forceinline__ void load_q4_query(Q4Query<T> &out, const float *q /* first of the group's four heads */, float factor, int lane) {
+    const int n = lane >> 2, c = lane & 3, head = n >> 1, part = n & 1;
+    const float *src = q + (size_t)head * T::DQ;
+    float v[T::DV / 4];
+    float top = 0.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < T::DV / 16; ++i) {                   // dims c DV / 4 + 4 i ..
+        const float4 x = *reinterpret_cast<const float4 *>(src + c * (T::DV / 4) + 4 * i);
+        v[4 * i] = x.x * factor; v[4 * i + 1] = x.y * factor; v[4 * i + 2] = x.z * factor; v[4 * i + 3] = x.w * factor;
+    }
+#pragma unroll
+    for (int i = 0; i < T::DV / 4; ++i) {
+        top = fmaxf(top, fabsf(v[i]));
+        sum += v[i];
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));  // over the four lanes that share this column
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    // 2^e >= top, with e held inside what keeps 2^-e 2^14 and 2^(e + 10) finite
+    int e = (int)((__float_as_uint(top) >> 23) & 255u) - 126;
+    e = min(max(e, -100), 110);
+    const float down = __uint_as_float((uint32_t)(127 - e + 10) << 23), down16 = 16.f * down;
+#pragma unroll
+    for (int w = 0; w < T::WORDS; ++w) {
+        const float *x = v + 8 * w;
+        out.v[2 * w][0] = part_f16(x[0] * down16, part) | (part_f16(x[4] * down16, part) << 16);
+        out.v[2 * w][1] = part_f16(x[1] * down, part) | (part_f16(x[5] * down, part) << 16);
+        out.v[2 * w + 1][0] = part_f16(x[2] * down16, part) | (part_f16(x[6] * down16, part) << 16);
+        out.v[2 * w + 1][1] = part_f16(x[3] * down, part) | (part_f16(x[7] * down, part) << 16);
+    }
+    // from the column's lanes to the lanes that hold the head's scores: lane % 4 = head, columns 2 head and 2 head + 1 alike
+    const float up = __uint_as_float((uint32_t)(127 + e + 10) << 23);      // c 2^-24 x q 2^-e 2^14 = c q 2^-(e + 10)
+    out.unscale = __shfl_sync(0xffffffffu, up, 8 * c);
+    out.sum = __shfl_sync(0xffffffffu, sum, 8 * c);
+    if constexpr (T::DR > 0) {
+        const float *r = src + T::DV;
+        // whole 16-wide k-steps: a lane's positional dims lie side by side (DR / 16 pairs of pairs from c DR' / 4 on), see score_q4
+        constexpr int FULL = T::DR / 16;
+        auto pair = [&](const float *x, int pt) { return part_bf16(x[0] * factor, pt) | (part_bf16(x[1] * factor, pt) << 16); };
+#pragma unroll
+        for (int k = 0; k < FULL; ++k) {
+            const float *x = r + c * 4 * FULL + 4 * k;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                out.r[k][i] = pair(x + 2 * i, part);
+                out.r2[k][i] = part ? 0u : pair(x + 2 * i, 2);
+            }
+        }
+        if constexpr (T::DR % 16 == 8) {
+            const float *x = r + 16 * FULL + 2 * c;
+            out.r[FULL][0] = pair(x, part);
+            out.r2[FULL][0] = part ? 0u : pair(x, 2);
+        }
+    }
+}
+
+// Content and positional products of one 16-token chunk with one group's queries.  acc: codes (to be multiplied by unscale
+// and the token's step), rot: positional part, in f32; columns hi and lo of head lane % 4 in [0], [1] for token row
+// rowmap(lane / 4) and in [2], [3] for that row + 8.
+template <class T>
+__device__ __forceinline__ void score_q4(const unsigned char *v_lo, const unsigned char *kr_lo, const Q4Query<T> &q, float (&acc)[4], float (&rot)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = rot[i] = 0.f;
+    uint32_t lo[T::WORDS], hi[T::WORDS];
+    if constexpr (T::WORDS == 2) {
+        const uint2 a = *reinterpret_cast<const uint2 *>(v_lo), b = *reinterpret_cast<const uint2 *>(v_lo + 8 * T::ROW);
+        lo[0] = a.x; lo[1] = a.y; hi[0] = b.x; hi[1] = b.y;
+    } else {
+        const uint4 a = *reinterpret_cast<const uint4 *>(v_lo), b = *reinterpret_cast<const uint4 *>(v_lo + 8 * T::ROW);
+        lo[0] = a.x; lo[1] = a.y; lo[2] = a.z; lo[3] = a.w; hi[0] = b.x; hi[1] = b.y; hi[2] = b.z; hi[3] = b.w;
+    }
+#pragma unroll
+    for (int w = 0; w < T::WORDS; ++w) {
+        mma_f16_q4(acc, lo[w] & 0x000f000fu, hi[w] & 0x000f000fu, lo[w] & 0x00f000f0u, hi[w] & 0x00f000f0u, q.v[2 * w][0], q.v[2 * w][1]);
+        const uint32_t l8 = lo[w] >> 8, h8 = hi[w] >> 8;
+        mma_f16_q4(acc, l8 & 0x000f000fu, h8 & 0x000f000fu, l8 & 0x00f000f0u, h8 & 0x00f000f0u, q.v[2 * w + 1][0], q.v[2 * w + 1][1]);
+    }
+    if constexpr (T::DR == 16 || T::DR == 24) {
+        const uint2 a = *reinterpret_cast<const uint2 *>(kr_lo), b = *reinterpret_cast<const uint2 *>(kr_lo + 8 * T::KR_ROW);
+        const uint32_t f[4] = {a.x, b.x, a.y, b.y};
+        mma_bf16(rot, f, q.r2[0][0], q.r2[0][1]);
+        mma_bf16(rot, f, q.r[0][0], q.r[0][1]);
+    }
+    if constexpr (T::DR == 32) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(kr_lo), b = *reinterpret_cast<const uint4 *>(kr_lo + 8 * T::KR_ROW);
+        const uint32_t f0[4] = {a.x, b.x, a.y, b.y}, f1[4] = {a.z, b.z, a.w, b.w};
+        mma_bf16(rot, f0, q.r2[0][0], q.r2[0][1]);
+        mma_bf16(rot, f1, q.r2[1][0], q.r2[1][1]);
+        mma_bf16(rot, f0, q.r[0][0], q.r[0][1]);
+        mma_bf16(rot, f1, q.r[1][0], q.r[1][1]);
+    }
+}
+// ... and the last 8 of 24 positional dims, which lie apart: kr_tail = row base + 32 + 4 (lane % 4) bytes
+template <class T>
+__device__ __forceinline__ void score_q4_tail(const unsigned char *kr_tail, const Q4Query<T> &q, float (&rot)[4]) {
+    if constexpr (T::DR == 24) {
+        const uint32_t f[2] = {*reinterpret_cast<const uint32_t *>(kr_tail), *reinterpret_cast<const uint32_t *>(kr_tail + 8 * T::KR_ROW)};
+        mma_bf16_k8(rot, f, q.r2[1][0]);
+        mma_bf16_k8(rot, f, q.r[1][0]);
+    }
+}
+
+// What the producer tells the consumers about a stage.
+struct TileMeta {
+    int b, t0, n_valid, flags;   // sequence, first slot, live tokens, bit 0 / 1: first / last tile of the block's part of the sequence
+};
+
+// The producer warp: walks flat tiles [lo, hi), 32 look-ups at a time (a lane each), and fills the ring.  copy(stage base,
+// page, first slot, full barrier, lane) starts the copies, any lane any of them; bytes = what they add up to.
+template <int TILE, int NSTAGE, class Copy>
+__device__ __forceinline__ void produce_tiles(const int *s_off, const int32_t *seq_lens, const int32_t *block_table, int B, int P, int num_pages,
+                                              int max_pages, int32_t *dev_status, int lo, int hi, uint64_t *full_bar, uint64_t *empty_bar,
+                                              TileMeta *s_meta, volatile int *s_abort, uint32_t bytes, Copy copy) {
+    const int lane = threadIdx.x & 31;
+    int issued = 0;
+    bool ok = true;
+    for (int base = lo; base < hi && ok; base += 32) {
+        const int f = base + lane;
+        int b = 0, t0 = 0, n_valid = 0, flags = 0;
+        long long page = 0;
+        if (f < hi) {
+            b = seq_of_tile(s_off, B, f);
+            t0 = (f - s_off[b]) * TILE;
+            const int len = seq_lens[b];
+            page = block_table ? (long long)block_table[(size_t)b * max_pages + t0 / P] : (long long)b * max_pages + t0 / P;
+            n_valid = min(TILE, len - t0);
+            flags = ((f == lo || t0 == 0) ? 1 : 0) | ((f + 1 == hi || f + 1 == s_off[b + 1]) ? 2 : 0);
+            if (page < 0 || page >= num_pages) {
+                report_error(dev_status, GVA_ERR_BAD_PAGE, b);
+                page = 0;                                    // there is one; what is read of it counts for nothing
+                n_valid = 0;
+            }
+        }
+        const int n = min(32, hi - base);
+        for (int i = 0; i < n; ++i, ++issued) {
+            const int st = issued % NSTAGE;
+            const int pg = (int)__shfl_sync(0xffffffffu, (int)page, i);
+            const int t = __shfl_sync(0xffffffffu, t0, i), nv = __shfl_sync(0xffffffffu, n_valid, i);
+            const int bb = __shfl_sync(0xffffffffu, b, i), fl = __shfl_sync(0xffffffffu, flags, i);
+            const uint32_t bar = smem_u32(&full_bar[st]);
+            int good = 1;
+            if (lane == 0) {
+                if (mbar_wait_bounded(smem_u32(&empty_bar[st]), ((issued / NSTAGE) & 1) ^ 1, s_abort)) {
+                    s_meta[st] = TileMeta{bb, t, nv, fl};
+                    mbar_expect_tx(bar, bytes);
+                } else {
+                    if (!*s_abort) report_error(dev_status, GVA_ERR_TIMEOUT, bb);
+                    *s_abort = 1;
+                    good = 0;
+                }
+            }
+            good = __shfl_sync(0xffffffffu, good, 0);
+            if (!good) {
+                ok = false;
+                break;
+            }
+            copy(st, (size_t)pg, t % P, bar, lane);
+        }
+    }
+    if (!ok && lane == 0) {                                  // every copy in flight must land before the shared memory is released
+        for (int i = max(0, issued - NSTAGE); i < issued; ++i)
+            for (int it = 0; it < kDrainPolls; ++it)
+                if (mbar_try_wait(smem_u32(&full_bar[i % NSTAGE]), (i / NSTAGE) & 1)) break;
+    }
+}
+
+// The copies of one 4-bit tile into a stage: value rows of every group, their (step, lowest) pairs, positional rows.  A page
+// that is one tile has all groups side by side: one copy each.
+template <class T>
+__device__ __forceinline__ void copy_q4_tile(uint32_t base, const Q4Pools &c, int G, int P, size_t page, int slot, uint32_t bar, uint64_t pol, int lane) {
+    if (P == T::TILE) {
+        if (lane == 0) bulk_load_stream(base, c.v + page * G * T::V_BYTES, G * T::V_BYTES, bar, pol);
+        if (lane == 1) bulk_load_stream(base + G * T::V_BYTES, c.sz + page * G * T::TILE, G * T::SZ_BYTES, bar, pol);
+    } else if (lane < G) {
+        bulk_load_stream(base + lane * T::V_BYTES, c.v + ((page * G + lane) * P + slot) * T::ROW, T::V_BYTES, bar, pol);
+    } else if (lane < 2 * G) {
+        const int g = lane - G;
+        bulk_load_stream(base + G * T::V_BYTES + g * T::SZ_BYTES, c.sz + (page * G + g) * P + slot, T::SZ_BYTES, bar, pol);
+    }
+    if (T::DR > 0 && lane == 31)
+        bulk_load_stream(base + G * (T::V_BYTES + T::SZ_BYTES), c.kr + (page * P + slot) * T::DR, T::KR_BYTES, bar, pol);
+}
+
+template <int DV, int DR, int TILE, int NSTAGE, int GMAX, int BLOCKS>
+__global__ void __launch_bounds__(32 * (GMAX + 1), BLOCKS)
+decode_q4_kernel(DecodeParams p, Q4Pools pools) {
+    using T = Q4Traits<DV, DR, TILE>;
+    grid_dependency_launch();
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int G = p.G, H = p.H, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int stage_bytes = T::stage_bytes(G);
+    unsigned char *tail = smem + (size_t)NSTAGE * stage_bytes;
+    uint64_t *full_bar = reinterpret_cast<uint64_t *>(tail), *empty_bar = full_bar + NSTAGE;
+    TileMeta *s_meta = reinterpret_cast<TileMeta *>(empty_bar + NSTAGE);
+    volatile int *s_abort = reinterpret_cast<volatile int *>(s_meta + NSTAGE);
+    int *s_off = reinterpret_cast<int *>(s_meta + NSTAGE) + 4;
+    if (tid == 0) {
+        for (int s = 0; s < NSTAGE; ++s) {
+            mbar_init(smem_u32(&full_bar[s]), 1);
+            mbar_init(smem_u32(&empty_bar[s]), G);
+        }
+        *s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    grid_dependency_wait();
+    compute_tile_offsets<TILE>(p, s_off);                    // ends with a barrier
+    const BlockRange rg = block_range(p, s_off);
+    if (rg.lo >= rg.hi) {
+        if (p.num_splits > 0) {                              // an empty split: its record weighs nothing, an only split is the result
+            const int b = blockIdx.x / p.num_splits;
+            if (p.num_splits == 1) {
+                for (int i = tid; i < H * DV; i += blockDim.x) p.out[(size_t)b * H * DV + i] = 0.f;
+                if (p.lse)
+                    for (int i = tid; i < H; i += blockDim.x) p.lse[(size_t)b * H + i] = -INFINITY;
+            } else {
+                for (int i = tid; i < H; i += blockDim.x) {
+                    p.rec_ml[((size_t)rg.rec_fixed * H + i) * 2] = -INFINITY;
+                    p.rec_ml[((size_t)rg.rec_fixed * H + i) * 2 + 1] = 0.f;
+                }
+            }
+        }
+        return;
+    }
+    if (warp == G) {
+        const uint64_t pol = l2_policy_evict_first();
+        produce_tiles<TILE, NSTAGE>(s_off, p.seq_lens, p.block_table, p.B, p.P, p.num_pages, p.max_pages, p.dev_status, rg.lo, rg.hi,
+                                    full_bar, empty_bar, s_meta, s_abort, (uint32_t)stage_bytes,
+                                    [&](int st, size_t page, int slot, uint32_t bar, int ln) {
+                                        copy_q4_tile<T>(smem_u32(smem + (size_t)st * stage_bytes), pools, G, p.P, page, slot, bar, pol, ln);
+                                    });
+    } else {
+        const int g = warp, c = lane & 3, r8 = lane >> 2;
+        const int tok_lo = rowmap(r8), tok_hi = tok_lo + 8;
+        const int pa = rowmap(2 * c), pb = rowmap(2 * c + 1);            // tokens of the output product's k = 2 c, 2 c + 1 (+ 8)
+        Q4Query<T> q;
+        float oacc[T::MT][4];
+        float m_run = -INFINITY, l_run = 0.f, z_run = 0.f, step_ref = 0.f, kappa = 1.f;
+        int cur_b = rg.b_first;
+        load_q4_query<T>(q, p.q + ((size_t)cur_b * H + g * kHeadsPerGroup) * T::DQ, p.scale_log2, lane);
+        const int n_tiles = rg.hi - rg.lo;
+#pragma unroll 1
+        for (int i = 0; i < n_tiles; ++i) {
+            const int st = i % NSTAGE;
+            if (!mbar_wait_bounded(smem_u32(&full_bar[st]), (i / NSTAGE) & 1, s_abort)) {
+                if (!*s_abort && lane == 0) report_error(p.dev_status, GVA_ERR_TIMEOUT, cur_b);
+                *s_abort = 1;
+                break;
+            }
+            const TileMeta meta = s_meta[st];
+            if (meta.flags & 1) {
+                if (meta.b != cur_b) {
+                    cur_b = meta.b;
+                    load_q4_query<T>(q, p.q + ((size_t)cur_b * H + g * kHeadsPerGroup) * T::DQ, p.scale_log2, lane);
+                }
+                m_run = -INFINITY;
+                l_run = z_run = step_ref = 0.f;
+                kappa = 1.f;
+#pragma unroll
+                for (int mt = 0; mt < T::MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) oacc[mt][e] = 0.f;
+            }
+            const unsigned char *stage = smem + (size_t)st * stage_bytes;
+            const unsigned char *vt = stage + (size_t)g * T::V_BYTES;
+            const __half2 *szt = reinterpret_cast<const __half2 *>(stage + (size_t)G * T::V_BYTES + (size_t)g * T::SZ_BYTES);
+            const unsigned char *krt = stage + (size_t)G * (T::V_BYTES + T::SZ_BYTES);
+            const bool ragged = meta.n_valid < TILE;
+
+            // ---- scores (log2 units) of this lane's head and token rows ----
+            float x[T::CHUNKS][2], step[T::CHUNKS][2], mid[T::CHUNKS][2];
+            float top = -INFINITY, smax = 0.f;
+#pragma unroll
+            for (int k = 0; k < T::CHUNKS; ++k) {
+                float acc[4], rot[4];
+                const unsigned char *kr = krt + (k * 16 + tok_lo) * T::KR_ROW;
+                score_q4<T>(vt + (k * 16 + tok_lo) * T::ROW + c * (T::ROW / 4), kr + c * 8 * (DR / 16), q, acc, rot);
+                score_q4_tail<T>(kr + 32 + 4 * c, q, rot);
+                const float2 a = __half22float2(szt[k * 16 + tok_lo]), b = __half22float2(szt[k * 16 + tok_hi]);
+                step[k][0] = a.x; mid[k][0] = fmaf(8.f, a.x, a.y); step[k][1] = b.x; mid[k][1] = fmaf(8.f, b.x, b.y);
+                x[k][0] = fmaf((acc[0] + acc[1]) * q.unscale, a.x, fmaf(a.y, q.sum, rot[0] + rot[1]));
+                x[k][1] = fmaf((acc[2] + acc[3]) * q.unscale, b.x, fmaf(b.y, q.sum, rot[2] + rot[3]));
+                if (ragged) {                                // (what stands behind the sequence may be anything)
+                    if (k * 16 + tok_lo >= meta.n_valid) { x[k][0] = -INFINITY; step[k][0] = mid[k][0] = 0.f; }
+                    if (k * 16 + tok_hi >= meta.n_valid) { x[k][1] = -INFINITY; step[k][1] = mid[k][1] = 0.f; }
+                }
+                top = fmaxf(top, fmaxf(x[k][0], x[k][1]));
+                smax = fmaxf(smax, fmaxf(step[k][0], step[k][1]));
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+            const float m_new = fmaxf(m_run, top);
+            const float m_use = m_new != -INFINITY ? m_new : 0.f;
+            if (__any_sync(0xffffffffu, m_new != m_run || smax > step_ref)) {    // rare once maximum and largest step have settled
+                const float corr = fast_exp2(m_run - m_use);
+                l_run *= corr;
+                z_run *= corr;
+                float f = corr;
+                const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(smax));     // steps are not negative
+                if (__uint_as_float(most) > step_ref) {
+                    const int e = min(max((int)(most >> 23) - 126, -30), 60);                    // 2^e > the largest step
+                    const float k_new = __uint_as_float((uint32_t)(127 + 10 - e) << 23);
+                    f *= step_ref > 0.f ? k_new / kappa : 1.f;
+                    kappa = k_new;
+                    step_ref = __uint_as_float((uint32_t)(127 + e) << 23);
+                }
+#pragma unroll
+                for (int mt = 0; mt < T::MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) oacc[mt][e] *= f;
+            }
+            m_run = m_new;
+
+            // ---- O^T += C_tile^T . (P s)^T ----
+#pragma unroll
+            for (int k = 0; k < T::CHUNKS; ++k) {
+                const float p0 = fast_exp2(x[k][0] - m_use), p1 = fast_exp2(x[k][1] - m_use);
+                l_run += p0 + p1;
+                z_run = fmaf(p0, mid[k][0], fmaf(p1, mid[k][1], z_run));
+                uint32_t s0, s1;
+                split_pair_f16(p0 * (step[k][0] * kappa), p1 * (step[k][1] * kappa), s0, s1);
+                const uint32_t b0 = movmatrix_trans(s0), b1 = movmatrix_trans(s1);
+                const unsigned char *row = vt + k * 16 * T::ROW + r8 * 4;
+#pragma unroll
+                for (int h = 0; h < DV / 64; ++h) {          // words lane / 4 and, for d_v = 128, lane / 4 + 8
+                    uint32_t even[2], odd[2];                // [pair of tokens]: low and high half words interleaved by token
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t w0 = *reinterpret_cast<const uint32_t *>(row + (pa + 8 * u) * T::ROW + 32 * h);
+                        const uint32_t w1 = *reinterpret_cast<const uint32_t *>(row + (pb + 8 * u) * T::ROW + 32 * h);
+                        even[u] = __byte_perm(w0, w1, 0x5410);
+                        odd[u] = __byte_perm(w0, w1, 0x7632);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {            // dims 8 word + 2 u and + 1
+                        const uint32_t e0 = u < 2 ? even[0] : odd[0], e1 = u < 2 ? even[1] : odd[1];
+                        const uint32_t f0 = u % 2 ? e0 >> 8 : e0, f1 = u % 2 ? e1 >> 8 : e1;
+                        mma_f16_q4(oacc[4 * h + u], centred_low(f0), centred_high(f0), centred_low(f1), centred_high(f1), b0, b1);
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&empty_bar[st]));
+
+            if (meta.flags & 2) {                            // this block's part of the sequence ends: one partial record, or the result
+                float l = l_run, z = z_run;
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) {
+                    l += __shfl_xor_sync(0xffffffffu, l, o);
+                    z += __shfl_xor_sync(0xffffffffu, z, o);
+                }
+                const bool whole = s_off[meta.b + 1] - 1 == rg.lo + i && s_off[meta.b] >= rg.lo && p.num_splits <= 1;
+                const int head = g * kHeadsPerGroup + c;
+                const size_t rh = (size_t)(rg.rec_fixed >= 0 ? rg.rec_fixed : (int)blockIdx.x + meta.b) * H + head;
+                const size_t oh = (size_t)meta.b * H + head;
+                const float norm = whole ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
+                float *dst = (whole ? p.out + oh * DV : p.rec_o + rh * DV);
+                const float back = 1.f / kappa;
+#pragma unroll
+                for (int h = 0; h < DV / 64; ++h) {
+                    float o[8];
+#pragma unroll
+                    for (int mt = 0; mt < 4; ++mt) {         // rows r8 and r8 + 8 of m-tile mt: dims 8 word + 2 mt and + 1
+                        o[2 * mt] = fmaf(oacc[4 * h + mt][0] + oacc[4 * h + mt][1], back, z) * norm;
+                        o[2 * mt + 1] = fmaf(oacc[4 * h + mt][2] + oacc[4 * h + mt][3], back, z) * norm;
+                    }
+                    *reinterpret_cast<float4 *>(dst + 64 * h + 8 * r8) = make_float4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<float4 *>(dst + 64 * h + 8 * r8 + 4) = make_float4(o[4], o[5], o[6], o[7]);
+                }
+                if (r8 == 0) {
+                    if (whole) {
+                        if (p.lse) p.lse[oh] = (m_run + log2f(l)) * kLn2;
+                    } else {
+                        p.rec_ml[rh * 2] = m_run;
+                        p.rec_ml[rh * 2 + 1] = l;
+                    }
+                }
+            }
+        }
+    }
+    __syncthreads();                                         // shared memory stays until every warp is done with it
+}
+
+}  // namespace gva

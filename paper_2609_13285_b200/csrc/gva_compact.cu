@@ -14,6 +14,12 @@ using namespace gva;
 #ifndef GVA_Q4_NSTAGE
 #define GVA_Q4_NSTAGE 4
 #endif
+#ifndef GVA_Q4_TILE
+#define GVA_Q4_TILE 64
+#endif
+#ifndef GVA_Q4_BW
+#define GVA_Q4_BW 1
+#endif
 #ifndef GVA_Q4_BLOCKS
 #define GVA_Q4_BLOCKS 4
 #endif
@@ -58,7 +64,7 @@ struct Q4Plan {
 template <int DV, int DR, int TILE>
 Q4Plan q4_plan_t(const gva_handle *h, int B) {
     using T = Q4Traits<DV, DR, TILE>;
-    constexpr int NSTAGE = GVA_Q4_NSTAGE, B4 = DV == 64 ? GVA_Q4_BLOCKS : 2, B8 = DV == 64 ? 2 : 1;
+    constexpr int NSTAGE = GVA_Q4_NSTAGE, B4 = DV == 64 ? GVA_Q4_BLOCKS : 2, B8 = DV == 64 ? 2 : GVA_Q4_BW;
     Q4Plan p;
     const bool narrow = h->cfg.G <= 4;
     p.fn = narrow ? decode_q4_kernel<DV, DR, TILE, NSTAGE, 4, B4> : decode_q4_kernel<DV, DR, TILE, NSTAGE, 8, B8>;
@@ -70,7 +76,7 @@ Q4Plan q4_plan_t(const gva_handle *h, int B) {
 }
 Q4Plan q4_plan(const gva_handle *h, int B) {
     const gva_config &c = h->cfg;
-    const bool t64 = c.page_size % 64 == 0;              // a tile lies in one page
+    const bool t64 = c.page_size % 64 == 0 && GVA_Q4_TILE == 64;              // a tile lies in one page
 #define GVA_Q4(DV_, DR_) (t64 ? q4_plan_t<DV_, DR_, 64>(h, B) : q4_plan_t<DV_, DR_, 32>(h, B))
     if (c.d_v == 64) return c.d_r == 16 ? GVA_Q4(64, 16) : c.d_r == 24 ? GVA_Q4(64, 24) : GVA_Q4(64, 0);
     return c.d_r == 32 ? GVA_Q4(128, 32) : GVA_Q4(128, 0);
@@ -80,7 +86,7 @@ Q4Plan q4_plan(const gva_handle *h, int B) {
 // and there is nothing to merge -- else 0, the balanced partition over all resident blocks.
 int q4_splits(const gva_handle *h, int max_seq_len, int num_splits) {
     if (num_splits > 0) return num_splits;
-    const int tile = h->cfg.page_size % 64 == 0 ? 64 : 32;
+    const int tile = h->cfg.page_size % 64 == 0 && GVA_Q4_TILE == 64 ? 64 : 32;
     return max_seq_len <= 2 * tile ? 1 : 0;
 }
 struct Q4Workspace {

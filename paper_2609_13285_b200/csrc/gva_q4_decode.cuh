@@ -60,6 +60,19 @@ __device__ __forceinline__ void mma_f16_q4(float (&c)[4], uint32_t a0, uint32_t 
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// c = a b from nothing
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_bf16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t pack_half2(float x, float y) {
     const __half2 h = __floats2half2_rn(x, y);
     return *reinterpret_cast<const uint32_t *>(&h);
@@ -86,14 +99,19 @@ __device__ __forceinline__ uint32_t part_bf16(float x, int part) {
     return __bfloat16_as_ushort(y);
 }
 
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {      // one instruction, its constants in registers
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;\n" : "=r"(y) : "r"(x), "r"(mask), "r"(bits));
+    return y;
+}
 // Two codes as signed f16 numbers c - 8: 1024 + c (or 64 + c, one nibble up) by masks, less 1032 (72), exactly.
 __device__ __forceinline__ uint32_t centred_low(uint32_t x) {
-    const uint32_t y = (x & 0x000f000fu) | 0x64006400u, off = 0x64086408u;
+    const uint32_t y = and_or(x, 0x000f000fu, 0x64006400u), off = 0x64086408u;
     const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&y), *reinterpret_cast<const __half2 *>(&off));
     return *reinterpret_cast<const uint32_t *>(&d);
 }
 __device__ __forceinline__ uint32_t centred_high(uint32_t x) {
-    const uint32_t y = (x & 0x00f000f0u) | 0x54005400u, off = 0x54805480u;
+    const uint32_t y = and_or(x, 0x00f000f0u, 0x54005400u), off = 0x54805480u;
     const __half2 d = __hsub2(*reinterpret_cast<const __half2 *>(&y), *reinterpret_cast<const __half2 *>(&off));
     return *reinterpret_cast<const uint32_t *>(&d);
 }
@@ -167,49 +185,86 @@ __device__ __forceinline__ void load_q4_query(Q4Query<T> &out, const float *q /*
     }
 }
 
-// Content and positional products of one 16-token chunk with one group's queries.  acc: codes (to be multiplied by unscale
-// and the token's step), rot: positional part, in f32; columns hi and lo of head lane % 4 in [0], [1] for token row
-// rowmap(lane / 4) and in [2], [3] for that row + 8.
+// Content and positional products of two 16-token chunks with one group's queries, side by side so that neither waits for the
+// other's MMAs.  acc: codes (to be multiplied by unscale and the token's step), rot: positional part, in f32; columns hi and
+// lo of head lane % 4 in [0], [1] for token row rowmap(lane / 4) and in [2], [3] for that row + 8.  v, kr: this lane's share of the
+// first chunk's low token row (kr: of the row itself).
 template <class T>
-__device__ __forceinline__ void score_q4(const unsigned char *v_lo, const unsigned char *kr_lo, const Q4Query<T> &q, float (&acc)[4], float (&rot)[4]) {
+__device__ __forceinline__ void score_q4(const unsigned char *v, const unsigned char *kr, int c, const Q4Query<T> &q, float (&acc)[2][4], float (&rot)[2][4]) {
+    uint32_t lo[2][T::WORDS], hi[2][T::WORDS];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = rot[i] = 0.f;
-    uint32_t lo[T::WORDS], hi[T::WORDS];
-    if constexpr (T::WORDS == 2) {
-        const uint2 a = *reinterpret_cast<const uint2 *>(v_lo), b = *reinterpret_cast<const uint2 *>(v_lo + 8 * T::ROW);
-        lo[0] = a.x; lo[1] = a.y; hi[0] = b.x; hi[1] = b.y;
+    for (int k = 0; k < 2; ++k) {
+        const unsigned char *row = v + k * 16 * T::ROW;
+#pragma unroll
+        for (int w = 0; w < T::WORDS; w += 2) {
+            const uint2 a = *reinterpret_cast<const uint2 *>(row + 4 * w), b = *reinterpret_cast<const uint2 *>(row + 8 * T::ROW + 4 * w);
+            lo[k][w] = a.x; lo[k][w + 1] = a.y; hi[k][w] = b.x; hi[k][w + 1] = b.y;
+        }
+    }
+    if constexpr (T::DR == 0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) rot[k][0] = rot[k][1] = rot[k][2] = rot[k][3] = 0.f;
     } else {
-        const uint4 a = *reinterpret_cast<const uint4 *>(v_lo), b = *reinterpret_cast<const uint4 *>(v_lo + 8 * T::ROW);
-        lo[0] = a.x; lo[1] = a.y; lo[2] = a.z; lo[3] = a.w; hi[0] = b.x; hi[1] = b.y; hi[2] = b.z; hi[3] = b.w;
+        constexpr int FULL = T::DR / 16;
+        uint32_t f[2][FULL][4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int u = 0; u < FULL; ++u) {
+                const unsigned char *row = kr + k * 16 * T::KR_ROW + 8 * (c * FULL + u);
+                const uint2 a = *reinterpret_cast<const uint2 *>(row), b = *reinterpret_cast<const uint2 *>(row + 8 * T::KR_ROW);
+                f[k][u][0] = a.x; f[k][u][1] = b.x; f[k][u][2] = a.y; f[k][u][3] = b.y;
+            }
+#pragma unroll
+        for (int u = 0; u < FULL; ++u)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (u == 0) mma_bf16_first(rot[k], f[k][u], q.r2[u][0], q.r2[u][1]);
+                else mma_bf16(rot[k], f[k][u], q.r2[u][0], q.r2[u][1]);
+            }
+        if constexpr (T::DR % 16 == 8) {                     // the last 8 dims lie apart
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const unsigned char *row = kr + k * 16 * T::KR_ROW + 32 * FULL + 4 * c;
+                const uint32_t t[2] = {*reinterpret_cast<const uint32_t *>(row), *reinterpret_cast<const uint32_t *>(row + 8 * T::KR_ROW)};
+                mma_bf16_k8(rot[k], t, q.r2[FULL][0]);
+                mma_bf16_k8(rot[k], t, q.r[FULL][0]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < FULL; ++u)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) mma_bf16(rot[k], f[k][u], q.r[u][0], q.r[u][1]);
     }
 #pragma unroll
     for (int w = 0; w < T::WORDS; ++w) {
-        mma_f16_q4(acc, lo[w] & 0x000f000fu, hi[w] & 0x000f000fu, lo[w] & 0x00f000f0u, hi[w] & 0x00f000f0u, q.v[2 * w][0], q.v[2 * w][1]);
-        const uint32_t l8 = lo[w] >> 8, h8 = hi[w] >> 8;
-        mma_f16_q4(acc, l8 & 0x000f000fu, h8 & 0x000f000fu, l8 & 0x00f000f0u, h8 & 0x00f000f0u, q.v[2 * w + 1][0], q.v[2 * w + 1][1]);
-    }
-    if constexpr (T::DR == 16 || T::DR == 24) {
-        const uint2 a = *reinterpret_cast<const uint2 *>(kr_lo), b = *reinterpret_cast<const uint2 *>(kr_lo + 8 * T::KR_ROW);
-        const uint32_t f[4] = {a.x, b.x, a.y, b.y};
-        mma_bf16(rot, f, q.r2[0][0], q.r2[0][1]);
-        mma_bf16(rot, f, q.r[0][0], q.r[0][1]);
-    }
-    if constexpr (T::DR == 32) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(kr_lo), b = *reinterpret_cast<const uint4 *>(kr_lo + 8 * T::KR_ROW);
-        const uint32_t f0[4] = {a.x, b.x, a.y, b.y}, f1[4] = {a.z, b.z, a.w, b.w};
-        mma_bf16(rot, f0, q.r2[0][0], q.r2[0][1]);
-        mma_bf16(rot, f1, q.r2[1][0], q.r2[1][1]);
-        mma_bf16(rot, f0, q.r[0][0], q.r[0][1]);
-        mma_bf16(rot, f1, q.r[1][0], q.r[1][1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t a0 = lo[k][w] & 0x000f000fu, a1 = hi[k][w] & 0x000f000fu, a2 = lo[k][w] & 0x00f000f0u, a3 = hi[k][w] & 0x00f000f0u;
+            if (w == 0) mma_f16_first(acc[k], a0, a1, a2, a3, q.v[2 * w][0], q.v[2 * w][1]);
+            else mma_f16_q4(acc[k], a0, a1, a2, a3, q.v[2 * w][0], q.v[2 * w][1]);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t l = lo[k][w] >> 8, h = hi[k][w] >> 8;
+            mma_f16_q4(acc[k], l & 0x000f000fu, h & 0x000f000fu, l & 0x00f000f0u, h & 0x00f000f0u, q.v[2 * w + 1][0], q.v[2 * w + 1][1]);
+        }
     }
 }
-// ... and the last 8 of 24 positional dims, which lie apart: kr_tail = row base + 32 + 4 (lane % 4) bytes
-template <class T>
-__device__ __forceinline__ void score_q4_tail(const unsigned char *kr_tail, const Q4Query<T> &q, float (&rot)[4]) {
-    if constexpr (T::DR == 24) {
-        const uint32_t f[2] = {*reinterpret_cast<const uint32_t *>(kr_tail), *reinterpret_cast<const uint32_t *>(kr_tail + 8 * T::KR_ROW)};
-        mma_bf16_k8(rot, f, q.r2[1][0]);
-        mma_bf16_k8(rot, f, q.r[1][0]);
+
+// The producer's wait for a free slot of the ring: it is ahead by the whole ring and polls without hurry, so as to leave the
+// issue slots to the consumers (measured: a tenth of all instructions were its polls).  Bounded like mbar_wait_bounded.
+__device__ __forceinline__ bool mbar_wait_relaxed(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+    const unsigned long long t0 = global_timer_ns();
+    for (;;) {
+        uint32_t ok;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity), "r"(100000u)            // may sleep in hardware for 100 us
+            : "memory");
+        if (ok) return true;
+        if (*abort_flag || global_timer_ns() - t0 > kWaitLimitNs) return false;
     }
 }
 
@@ -253,7 +308,7 @@ __device__ __forceinline__ void produce_tiles(const int *s_off, const int32_t *s
             const uint32_t bar = smem_u32(&full_bar[st]);
             int good = 1;
             if (lane == 0) {
-                if (mbar_wait_bounded(smem_u32(&empty_bar[st]), ((issued / NSTAGE) & 1) ^ 1, s_abort)) {
+                if (mbar_wait_relaxed(smem_u32(&empty_bar[st]), ((issued / NSTAGE) & 1) ^ 1, s_abort)) {
                     s_meta[st] = TileMeta{bb, t, nv, fl};
                     mbar_expect_tx(bar, bytes);
                 } else {
@@ -344,10 +399,10 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
     } else {
         const int g = warp, c = lane & 3, r8 = lane >> 2;
         const int tok_lo = rowmap(r8), tok_hi = tok_lo + 8;
-        const int pa = rowmap(2 * c), pb = rowmap(2 * c + 1);            // tokens of the output product's k = 2 c, 2 c + 1 (+ 8)
+        const int ta = rowmap(2 * c), tb = rowmap(2 * c + 1);            // tokens of the output product's k = 2 c, 2 c + 1 (+ 8)
         Q4Query<T> q;
         float oacc[T::MT][4];
-        float m_run = -INFINITY, l_run = 0.f, z_run = 0.f, step_ref = 0.f, kappa = 1.f;
+        float m_run = -INFINITY, l_run = 0.f, z_run = 0.f, step_ref = 0.f, lift = 0.f;   // all sums carry the factor 2^lift
         int cur_b = rg.b_first;
         load_q4_query<T>(q, p.q + ((size_t)cur_b * H + g * kHeadsPerGroup) * T::DQ, p.scale_log2, lane);
         const int n_tiles = rg.hi - rg.lo;
@@ -367,7 +422,7 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
                 }
                 m_run = -INFINITY;
                 l_run = z_run = step_ref = 0.f;
-                kappa = 1.f;
+                lift = 0.f;
 #pragma unroll
                 for (int mt = 0; mt < T::MT; ++mt)
 #pragma unroll
@@ -377,25 +432,32 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
             const unsigned char *vt = stage + (size_t)g * T::V_BYTES;
             const __half2 *szt = reinterpret_cast<const __half2 *>(stage + (size_t)G * T::V_BYTES + (size_t)g * T::SZ_BYTES);
             const unsigned char *krt = stage + (size_t)G * (T::V_BYTES + T::SZ_BYTES);
-            const bool ragged = meta.n_valid < TILE;
 
             // ---- scores (log2 units) of this lane's head and token rows ----
             float x[T::CHUNKS][2], step[T::CHUNKS][2], mid[T::CHUNKS][2];
             float top = -INFINITY, smax = 0.f;
 #pragma unroll
-            for (int k = 0; k < T::CHUNKS; ++k) {
-                float acc[4], rot[4];
-                const unsigned char *kr = krt + (k * 16 + tok_lo) * T::KR_ROW;
-                score_q4<T>(vt + (k * 16 + tok_lo) * T::ROW + c * (T::ROW / 4), kr + c * 8 * (DR / 16), q, acc, rot);
-                score_q4_tail<T>(kr + 32 + 4 * c, q, rot);
-                const float2 a = __half22float2(szt[k * 16 + tok_lo]), b = __half22float2(szt[k * 16 + tok_hi]);
-                step[k][0] = a.x; mid[k][0] = fmaf(8.f, a.x, a.y); step[k][1] = b.x; mid[k][1] = fmaf(8.f, b.x, b.y);
-                x[k][0] = fmaf((acc[0] + acc[1]) * q.unscale, a.x, fmaf(a.y, q.sum, rot[0] + rot[1]));
-                x[k][1] = fmaf((acc[2] + acc[3]) * q.unscale, b.x, fmaf(b.y, q.sum, rot[2] + rot[3]));
-                if (ragged) {                                // (what stands behind the sequence may be anything)
+            for (int kk = 0; kk < T::CHUNKS; kk += 2) {
+                float acc[2][4], rot[2][4];
+                score_q4<T>(vt + (kk * 16 + tok_lo) * T::ROW + c * (T::ROW / 4), krt + (kk * 16 + tok_lo) * T::KR_ROW, c, q, acc, rot);
+#pragma unroll
+                for (int k = kk; k < kk + 2; ++k) {
+                    const float2 a = __half22float2(szt[k * 16 + tok_lo]), b = __half22float2(szt[k * 16 + tok_hi]);
+                    const float *s = acc[k - kk], *r = rot[k - kk];
+                    step[k][0] = a.x; mid[k][0] = fmaf(8.f, a.x, a.y); step[k][1] = b.x; mid[k][1] = fmaf(8.f, b.x, b.y);
+                    x[k][0] = fmaf((s[0] + s[1]) * q.unscale, a.x, fmaf(a.y, q.sum, r[0] + r[1]));
+                    x[k][1] = fmaf((s[2] + s[3]) * q.unscale, b.x, fmaf(b.y, q.sum, r[2] + r[3]));
+                }
+            }
+            if (meta.n_valid < TILE) {                       // (what stands behind the sequence may be anything)
+#pragma unroll
+                for (int k = 0; k < T::CHUNKS; ++k) {
                     if (k * 16 + tok_lo >= meta.n_valid) { x[k][0] = -INFINITY; step[k][0] = mid[k][0] = 0.f; }
                     if (k * 16 + tok_hi >= meta.n_valid) { x[k][1] = -INFINITY; step[k][1] = mid[k][1] = 0.f; }
                 }
+            }
+#pragma unroll
+            for (int k = 0; k < T::CHUNKS; ++k) {
                 top = fmaxf(top, fmaxf(x[k][0], x[k][1]));
                 smax = fmaxf(smax, fmaxf(step[k][0], step[k][1]));
             }
@@ -403,44 +465,49 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
             const float m_new = fmaxf(m_run, top);
-            const float m_use = m_new != -INFINITY ? m_new : 0.f;
             if (__any_sync(0xffffffffu, m_new != m_run || smax > step_ref)) {    // rare once maximum and largest step have settled
-                const float corr = fast_exp2(m_run - m_use);
-                l_run *= corr;
-                z_run *= corr;
-                float f = corr;
+                float f = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
                 const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(smax));     // steps are not negative
                 if (__uint_as_float(most) > step_ref) {
                     const int e = min(max((int)(most >> 23) - 126, -30), 60);                    // 2^e > the largest step
-                    const float k_new = __uint_as_float((uint32_t)(127 + 10 - e) << 23);
-                    f *= step_ref > 0.f ? k_new / kappa : 1.f;
-                    kappa = k_new;
+                    const float to = (float)(10 - e);
+                    f *= fast_exp2(to - lift);
+                    lift = to;
                     step_ref = __uint_as_float((uint32_t)(127 + e) << 23);
                 }
+                l_run *= f;
+                z_run *= f;
 #pragma unroll
                 for (int mt = 0; mt < T::MT; ++mt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) oacc[mt][e] *= f;
             }
             m_run = m_new;
+            const float base = m_new != -INFINITY ? m_new - lift : 0.f;          // keeps (-inf) - (-inf) out of the exponent
 
-            // ---- O^T += C_tile^T . (P s)^T ----
+            // ---- softmax weights times steps, as B fragments of the output product ----
+            uint32_t pb0[T::CHUNKS], pb1[T::CHUNKS];
 #pragma unroll
             for (int k = 0; k < T::CHUNKS; ++k) {
-                const float p0 = fast_exp2(x[k][0] - m_use), p1 = fast_exp2(x[k][1] - m_use);
+                const float p0 = fast_exp2(x[k][0] - base), p1 = fast_exp2(x[k][1] - base);
                 l_run += p0 + p1;
                 z_run = fmaf(p0, mid[k][0], fmaf(p1, mid[k][1], z_run));
                 uint32_t s0, s1;
-                split_pair_f16(p0 * (step[k][0] * kappa), p1 * (step[k][1] * kappa), s0, s1);
-                const uint32_t b0 = movmatrix_trans(s0), b1 = movmatrix_trans(s1);
+                split_pair_f16(p0 * step[k][0], p1 * step[k][1], s0, s1);
+                pb0[k] = movmatrix_trans(s0);
+                pb1[k] = movmatrix_trans(s1);
+            }
+            // ---- O^T += C_tile^T . (P s)^T ----
+#pragma unroll
+            for (int k = 0; k < T::CHUNKS; ++k) {
                 const unsigned char *row = vt + k * 16 * T::ROW + r8 * 4;
 #pragma unroll
                 for (int h = 0; h < DV / 64; ++h) {          // words lane / 4 and, for d_v = 128, lane / 4 + 8
                     uint32_t even[2], odd[2];                // [pair of tokens]: low and high half words interleaved by token
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const uint32_t w0 = *reinterpret_cast<const uint32_t *>(row + (pa + 8 * u) * T::ROW + 32 * h);
-                        const uint32_t w1 = *reinterpret_cast<const uint32_t *>(row + (pb + 8 * u) * T::ROW + 32 * h);
+                        const uint32_t w0 = *reinterpret_cast<const uint32_t *>(row + (ta + 8 * u) * T::ROW + 32 * h);
+                        const uint32_t w1 = *reinterpret_cast<const uint32_t *>(row + (tb + 8 * u) * T::ROW + 32 * h);
                         even[u] = __byte_perm(w0, w1, 0x5410);
                         odd[u] = __byte_perm(w0, w1, 0x7632);
                     }
@@ -448,7 +515,7 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
                     for (int u = 0; u < 4; ++u) {            // dims 8 word + 2 u and + 1
                         const uint32_t e0 = u < 2 ? even[0] : odd[0], e1 = u < 2 ? even[1] : odd[1];
                         const uint32_t f0 = u % 2 ? e0 >> 8 : e0, f1 = u % 2 ? e1 >> 8 : e1;
-                        mma_f16_q4(oacc[4 * h + u], centred_low(f0), centred_high(f0), centred_low(f1), centred_high(f1), b0, b1);
+                        mma_f16_q4(oacc[4 * h + u], centred_low(f0), centred_high(f0), centred_low(f1), centred_high(f1), pb0[k], pb1[k]);
                     }
                 }
             }
@@ -466,26 +533,25 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
                 const int head = g * kHeadsPerGroup + c;
                 const size_t rh = (size_t)(rg.rec_fixed >= 0 ? rg.rec_fixed : (int)blockIdx.x + meta.b) * H + head;
                 const size_t oh = (size_t)meta.b * H + head;
-                const float norm = whole ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
+                const float norm = whole ? (l != 0.f ? 1.f / l : 0.f) : fast_exp2(-lift);       // (a power of two: exact)
                 float *dst = (whole ? p.out + oh * DV : p.rec_o + rh * DV);
-                const float back = 1.f / kappa;
 #pragma unroll
                 for (int h = 0; h < DV / 64; ++h) {
                     float o[8];
 #pragma unroll
                     for (int mt = 0; mt < 4; ++mt) {         // rows r8 and r8 + 8 of m-tile mt: dims 8 word + 2 mt and + 1
-                        o[2 * mt] = fmaf(oacc[4 * h + mt][0] + oacc[4 * h + mt][1], back, z) * norm;
-                        o[2 * mt + 1] = fmaf(oacc[4 * h + mt][2] + oacc[4 * h + mt][3], back, z) * norm;
+                        o[2 * mt] = (oacc[4 * h + mt][0] + oacc[4 * h + mt][1] + z) * norm;
+                        o[2 * mt + 1] = (oacc[4 * h + mt][2] + oacc[4 * h + mt][3] + z) * norm;
                     }
                     *reinterpret_cast<float4 *>(dst + 64 * h + 8 * r8) = make_float4(o[0], o[1], o[2], o[3]);
                     *reinterpret_cast<float4 *>(dst + 64 * h + 8 * r8 + 4) = make_float4(o[4], o[5], o[6], o[7]);
                 }
                 if (r8 == 0) {
                     if (whole) {
-                        if (p.lse) p.lse[oh] = (m_run + log2f(l)) * kLn2;
+                        if (p.lse) p.lse[oh] = (m_run + (log2f(l) - lift)) * kLn2;
                     } else {
                         p.rec_ml[rh * 2] = m_run;
-                        p.rec_ml[rh * 2 + 1] = l;
+                        p.rec_ml[rh * 2 + 1] = l * norm;
                     }
                 }
             }

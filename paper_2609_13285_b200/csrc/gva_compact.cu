@@ -10,20 +10,6 @@
 
 using namespace gva;
 
-// build-time knobs of the 4-bit decode: ring depth, resident blocks per SM (d_v = 64, G <= 4)
-#ifndef GVA_Q4_NSTAGE
-#define GVA_Q4_NSTAGE 4
-#endif
-#ifndef GVA_Q4_TILE
-#define GVA_Q4_TILE 64
-#endif
-#ifndef GVA_Q4_BW
-#define GVA_Q4_BW 1
-#endif
-#ifndef GVA_Q4_BLOCKS
-#define GVA_Q4_BLOCKS 4
-#endif
-
 namespace {
 int check_q4(const gva_handle *h, const gva_q4_cache *cache) {
     if (!h || !cache) return GVA_ERR_INVALID_ARG;
@@ -55,51 +41,54 @@ int append_q4(gva_handle *h, const gva_q4_cache *cache, const float *v_new, cons
 }
 
 // ---- 4-bit decode: which kernel, which grid ----
-using Q4DecodeFn = void (*)(DecodeParams, Q4Pools);
-struct Q4Plan {
+using Q4DecodeFn = void (*)(DecodeParams, Q4Launch);
+struct Q4Kernel {
     Q4DecodeFn fn;
-    size_t smem;
-    int tile, threads, blocks_per_sm;
+    int tile;
+    size_t stage;
 };
 template <int DV, int DR, int TILE>
-Q4Plan q4_plan_t(const gva_handle *h, int B) {
-    using T = Q4Traits<DV, DR, TILE>;
-    constexpr int NSTAGE = GVA_Q4_NSTAGE, B4 = DV == 64 ? GVA_Q4_BLOCKS : 2, B8 = DV == 64 ? 2 : GVA_Q4_BW;
-    Q4Plan p;
-    const bool narrow = h->cfg.G <= 4;
-    p.fn = narrow ? decode_q4_kernel<DV, DR, TILE, NSTAGE, 4, B4> : decode_q4_kernel<DV, DR, TILE, NSTAGE, 8, B8>;
-    p.blocks_per_sm = narrow ? B4 : B8;
-    p.smem = (size_t)NSTAGE * T::stage_bytes(h->cfg.G) + T::tail_bytes(B, NSTAGE);
-    p.tile = TILE;
-    p.threads = 32 * (h->cfg.G + 1);
-    return p;
-}
-Q4Plan q4_plan(const gva_handle *h, int B) {
-    const gva_config &c = h->cfg;
-    const bool t64 = c.page_size % 64 == 0 && GVA_Q4_TILE == 64;              // a tile lies in one page
-#define GVA_Q4(DV_, DR_) (t64 ? q4_plan_t<DV_, DR_, 64>(h, B) : q4_plan_t<DV_, DR_, 32>(h, B))
+Q4Kernel q4_kernel_t(int G) { return Q4Kernel{decode_q4_kernel<DV, DR, TILE>, TILE, (size_t)Q4Traits<DV, DR, TILE>::stage_bytes(G)}; }
+Q4Kernel q4_kernel(const gva_config &c) {
+    const bool t64 = c.page_size % 64 == 0;              // a tile lies in one page
+#define GVA_Q4(DV_, DR_) (t64 ? q4_kernel_t<DV_, DR_, 64>(c.G) : q4_kernel_t<DV_, DR_, 32>(c.G))
     if (c.d_v == 64) return c.d_r == 16 ? GVA_Q4(64, 16) : c.d_r == 24 ? GVA_Q4(64, 24) : GVA_Q4(64, 0);
     return c.d_r == 32 ? GVA_Q4(128, 32) : GVA_Q4(128, 0);
 #undef GVA_Q4
 }
-// Ranges per sequence.  Automatic: one where every sequence is a few tiles at most -- a block then writes the result itself
-// and there is nothing to merge -- else 0, the balanced partition over all resident blocks.
-int q4_splits(const gva_handle *h, int max_seq_len, int num_splits) {
-    if (num_splits > 0) return num_splits;
-    const int tile = h->cfg.page_size % 64 == 0 && GVA_Q4_TILE == 64 ? 64 : 32;
-    return max_seq_len <= 2 * tile ? 1 : 0;
-}
-struct Q4Workspace {
-    size_t rec_ml, total;
-    int n_rec;
+// The launch for B sequences of at most max_seq_len tokens.  num_splits = 0: where every sequence is two tiles at most, one
+// block per sequence, which writes the result itself -- there is nothing to merge; else the balanced partition, one
+// block per SM with as many teams as there are tiles for.  num_splits >= 1: blocks of one team, num_splits per sequence.
+struct Q4Plan {
+    Q4Kernel k;
+    int num_splits, grid, teams, nstage, producers, n_rec;
+    size_t smem, rec_o, rec_ml, total;                   // shared memory of a block; workspace: segments, records, maxima and sums
 };
-Q4Workspace q4_workspace(const gva_handle *h, int B, int max_seq_len, int num_splits) {
-    Q4Workspace w;
-    const int splits = q4_splits(h, max_seq_len, num_splits);
-    w.n_rec = std::max(1, splits > 0 ? B * splits : q4_plan(h, B).blocks_per_sm * h->sm_count + B);
-    w.rec_ml = align_up((size_t)w.n_rec * h->cfg.H * h->cfg.d_v * 4, 256);
-    w.total = w.rec_ml + align_up((size_t)w.n_rec * h->cfg.H * 2 * 4, 256);
-    return w;
+Q4Plan q4_plan(const gva_handle *h, int B, int max_seq_len, int num_splits) {
+    Q4Plan p;
+    p.k = q4_kernel(h->cfg);
+    const long long tiles = (max_seq_len + p.k.tile - 1) / p.k.tile;
+    p.num_splits = num_splits > 0 ? num_splits : tiles <= 2 ? 1 : 0;
+    if (p.num_splits > 0) {
+        p.teams = 1;
+        p.grid = B * p.num_splits;
+        p.n_rec = p.grid;
+    } else {
+        p.grid = (int)std::min<long long>(tiles * B, h->sm_count);
+        p.teams = (int)std::min<long long>(std::max(1, q4_consumers(h->cfg.d_v) / h->cfg.G), std::max<long long>(1, (tiles * B + p.grid - 1) / p.grid));
+        p.n_rec = (p.grid + B) * p.teams;
+    }
+    // the ring: up to four slots per team, at most what the SM holds (one block per SM) or a third of it
+    const size_t room = (p.num_splits > 0 ? (size_t)h->smem_per_sm / 3 : (size_t)h->smem_optin) - (size_t)(B + 1) * 4 - 2048;
+    const int slots = (int)std::min<size_t>(4 * p.teams, room / p.k.stage);
+    p.nstage = std::max(p.teams == 1 ? 2 : p.teams, slots / p.teams * p.teams);
+    p.producers = kQ4Producers;
+    while (p.nstage % p.producers != 0) --p.producers;
+    p.smem = p.nstage * p.k.stage + Q4Traits<64, 0, 32>::tail_bytes(B, p.nstage);
+    p.rec_o = align_up((size_t)B * sizeof(int2), 256);
+    p.rec_ml = p.rec_o + align_up((size_t)p.n_rec * h->cfg.H * h->cfg.d_v * 4, 256);
+    p.total = p.rec_ml + align_up((size_t)p.n_rec * h->cfg.H * 2 * 4, 256);
+    return p;
 }
 
 int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_abs, const float *lse, const int32_t *cu_q,
@@ -237,7 +226,7 @@ int gva_q4_widen(gva_handle *h, const gva_q4_cache *cache, const gva_cache *wide
 
 size_t gva_q4_decode_workspace_bytes(const gva_handle *h, int B, int max_seq_len, int num_splits) {
     if (check_common(h, B, max_seq_len, num_splits) != GVA_OK) return 0;
-    return q4_workspace(h, B, max_seq_len, num_splits).total;
+    return q4_plan(h, std::max(B, 1), max_seq_len, num_splits).total;
 }
 
 int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, const int32_t *seq_lens, float *out, float *lse,
@@ -247,12 +236,11 @@ int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, 
     if (rc != GVA_OK) return rc;
     if (B == 0) return GVA_OK;
     if (!q_abs || !seq_lens || !out || !aligned(q_abs, 16) || !aligned(out, 16) || !aligned(seq_lens, 4) || !aligned(lse, 4)) return GVA_ERR_INVALID_ARG;
-    const Q4Workspace w = q4_workspace(h, B, max_seq_len, num_splits);
-    if (!workspace || workspace_bytes < w.total) return GVA_ERR_WORKSPACE;
+    const Q4Plan plan = q4_plan(h, B, max_seq_len, num_splits);
+    if (!workspace || workspace_bytes < plan.total) return GVA_ERR_WORKSPACE;
     if (!aligned(workspace, 256)) return GVA_ERR_INVALID_ARG;
-    const gva_config &c = h->cfg;
-    const Q4Plan plan = q4_plan(h, B);
     if (plan.smem > (size_t)h->smem_optin) return GVA_ERR_UNSUPPORTED;
+    const gva_config &c = h->cfg;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     DecodeParams p;
     std::memset(&p, 0, sizeof(p));
@@ -261,28 +249,29 @@ int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, 
     p.q = q_abs;
     p.out = out;
     p.lse = lse;
-    p.rec_o = reinterpret_cast<float *>(ws);
-    p.rec_ml = reinterpret_cast<float *>(ws + w.rec_ml);
+    p.rec_o = reinterpret_cast<float *>(ws + plan.rec_o);
+    p.rec_ml = reinterpret_cast<float *>(ws + plan.rec_ml);
     p.dev_status = dev_status;
     p.B = B; p.H = c.H; p.G = c.G; p.P = c.page_size;
     p.num_pages = cache->num_pages;
     p.max_pages = cache->max_pages_per_seq;
-    p.num_splits = q4_splits(h, max_seq_len, num_splits);
+    p.num_splits = plan.num_splits;
     p.scale_log2 = h->scale * kLog2e;
-    const long long tiles = std::max<long long>(1, (long long)B * ((max_seq_len + plan.tile - 1) / plan.tile));
-    const int grid = p.num_splits > 0 ? B * p.num_splits : (int)std::min<long long>(tiles, (long long)plan.blocks_per_sm * h->sm_count);
+    Q4Launch l;
+    l.pools = q4_pools(cache);
+    l.teams = plan.teams;
+    l.nstage = plan.nstage;
+    l.producers = plan.producers;
+    l.segments = plan.num_splits > 0 ? nullptr : reinterpret_cast<int2 *>(ws);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (cudaFuncSetAttribute(plan.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem) != cudaSuccess) return GVA_ERR_CUDA;
-    rc = launched(launch_pdl(plan.fn, dim3(grid), dim3(plan.threads), plan.smem, s, p, q4_pools(cache)));
-    if (rc != GVA_OK || p.num_splits == 1) return rc;
-    MergeParams m;
-    m.rec_o = p.rec_o; m.rec_ml = p.rec_ml; m.seq_lens = seq_lens; m.out = out; m.lse = lse;
-    m.B = B; m.H = c.H; m.P = c.page_size; m.max_pages = cache->max_pages_per_seq; m.num_splits = p.num_splits;
-    m.n_blocks = grid; m.tile = plan.tile;
-    const int records = p.num_splits > 0 ? p.num_splits : grid / B + 2;      // of a sequence, about
+    if (cudaFuncSetAttribute(plan.k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem) != cudaSuccess) return GVA_ERR_CUDA;
+    rc = launched(launch_pdl(plan.k.fn, dim3(plan.grid), dim3(32 * (plan.teams * c.G + plan.producers)), plan.smem, s, p, l));
+    if (rc != GVA_OK || plan.num_splits == 1) return rc;
+    const MergeParams m{p.rec_o, p.rec_ml, l.segments, out, lse, c.H, plan.num_splits, plan.teams};
+    const int records = plan.num_splits > 0 ? plan.num_splits : (plan.grid / B + 2) * plan.teams;      // of a sequence, about
     int threads = 64;
     while (threads < 1024 && threads / (c.d_v / 4) * 4 < records) threads *= 2;
-    const size_t smem = (size_t)(threads / (c.d_v / 4)) * (c.d_v + 1) * 4;
+    const size_t smem = (size_t)(threads / (c.d_v / 4)) * (c.d_v + 2) * 4;
     return launched(c.d_v == 64 ? launch_pdl(merge_records_kernel<64>, dim3(B, c.H), dim3(threads), smem, s, m)
                                 : launch_pdl(merge_records_kernel<128>, dim3(B, c.H), dim3(threads), smem, s, m));
 }

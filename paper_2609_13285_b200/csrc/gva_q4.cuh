@@ -230,108 +230,69 @@ widen_q4_kernel(WidenParams p) {
 }
 
 // ---- merge of split-KV partials -----------------------------------------------------------------------------------
-// Records of sequence b, known from the lengths alone: in the balanced partition block c of the decode kernel holds flat
-// tiles [range_begin(c), range_begin(c + 1)) and its part of sequence b is record c + b; with num_splits ranges per
-// sequence they are b * num_splits onwards.  One block per (sequence, head); d_v / 4 lanes read one record's output in
-// 16-byte pieces, the other threads other records; the order of the sum is fixed by the number of threads.
+// Records of sequence b: segments[b] = (first group of records, groups), as the decode kernel's block 0 has written it, or
+// num_splits groups from b num_splits on; a group is one record per team.  One block per (sequence, head).  d_v / 4
+// lanes read one record's output in 16-byte pieces, the other threads other records, each under its own running maximum, so
+// that a record costs one trip to memory; the parts are then joined in a fixed order.
 struct MergeParams {
     const float *rec_o, *rec_ml;   // [n_rec][H][d_v], [n_rec][H][2]
-    const int32_t *seq_lens;
+    const int2 *segments;
     float *out, *lse;
-    int B, H, P, max_pages, num_splits, n_blocks, tile;
+    int H, num_splits, teams;
 };
 template <int DV>
 __global__ void __launch_bounds__(1024)
 merge_records_kernel(MergeParams p) {
     grid_dependency_launch();
-    __shared__ int s_before[32], s_all[32];
-    __shared__ float s_red[32];
-    extern __shared__ float s_o[];                           // [parts][DV] outputs, [parts] sums
-    const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
-    grid_dependency_wait();
-    int first, count;
-    const long long cap = (long long)p.max_pages * p.P;
-    if (p.num_splits > 0) {
-        const int len = p.seq_lens[b];
-        first = b * p.num_splits;
-        count = len > 0 && len <= cap ? p.num_splits : 0;
-    } else {
-        int before = 0, all = 0, mine = 0;
-        for (int i = tid; i < p.B; i += nt) {
-            int len = p.seq_lens[i];
-            if (len < 0 || len > cap) len = 0;
-            const int tiles = (len + p.tile - 1) / p.tile;
-            all += tiles;
-            if (i < b) before += tiles;
-        }
-        {
-            int len = p.seq_lens[b];
-            if (len < 0 || len > cap) len = 0;
-            mine = (len + p.tile - 1) / p.tile;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            before += __shfl_xor_sync(0xffffffffu, before, o);
-            all += __shfl_xor_sync(0xffffffffu, all, o);
-        }
-        if (lane == 0) {
-            s_before[warp] = before;
-            s_all[warp] = all;
-        }
-        __syncthreads();
-        before = all = 0;
-        for (int w = 0; w < nt / 32; ++w) {
-            before += s_before[w];
-            all += s_all[w];
-        }
-        first = count = 0;
-        if (mine > 0) {
-            const int n_eff = partitions_in_use(all, p.n_blocks);
-            const int c0 = range_owner(before, all, n_eff), c1 = range_owner(before + mine - 1, all, n_eff);
-            first = c0 + b;
-            count = c1 - c0 + 1;
-            if (count == 1) return;                          // one block had the whole sequence and wrote the result
-        }
-    }
-    // running maximum over the records, then weights
-    float m = -INFINITY;
-    for (int r = tid; r < count; r += nt) m = fmaxf(m, p.rec_ml[((size_t)(first + r) * p.H + h) * 2]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane == 0) s_red[warp] = m;
-    __syncthreads();
-    m = -INFINITY;
-    for (int w = 0; w < nt / 32; ++w) m = fmaxf(m, s_red[w]);
-    const float base = m == -INFINITY ? 0.f : m;
     constexpr int L = DV / 4;
-    const int parts = nt / L, part = tid / L, l = tid % L;
+    extern __shared__ float s_part[];                        // [parts][DV] outputs, [parts] maxima, [parts] sums
+    const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, parts = blockDim.x / L, part = tid / L, l = tid % L;
+    float *s_m = s_part + parts * DV, *s_l = s_m + parts;
+    grid_dependency_wait();
+    const int2 seg = p.num_splits > 0 ? make_int2(b * p.num_splits, p.num_splits) : p.segments[b];
+    const int first = seg.x * p.teams, count = seg.y * p.teams;
+    float m = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-#pragma unroll 4
-    for (int r = part; r < count; r += parts) {
-        const size_t rh = (size_t)(first + r) * p.H + h;
-        const float2 ml = *reinterpret_cast<const float2 *>(p.rec_ml + rh * 2);
-        const float w = exp2f(ml.x - base);
-        const float4 o = *reinterpret_cast<const float4 *>(p.rec_o + rh * DV + 4 * l);
-        if (ml.x != -INFINITY) {                             // (an empty range leaves its output unwritten)
-            acc.x = fmaf(w, o.x, acc.x);
-            acc.y = fmaf(w, o.y, acc.y);
-            acc.z = fmaf(w, o.z, acc.z);
-            acc.w = fmaf(w, o.w, acc.w);
-            sum = fmaf(w, ml.y, sum);
+    constexpr int U = 4;                                     // records in flight per thread
+    for (int r0 = part; r0 < count; r0 += U * parts) {
+        float2 ml[U];
+        float4 o[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int r = r0 + u * parts;
+            const size_t rh = (size_t)(first + min(r, count - 1)) * p.H + h;
+            ml[u] = *reinterpret_cast<const float2 *>(p.rec_ml + rh * 2);
+            o[u] = *reinterpret_cast<const float4 *>(p.rec_o + rh * DV + 4 * l);
+            if (r >= count) ml[u].x = -INFINITY;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (ml[u].x == -INFINITY) continue;              // an empty range: its output is not written
+            const float top = fmaxf(m, ml[u].x), f = exp2f(m - top), w = exp2f(ml[u].x - top);
+            m = top;
+            acc.x = fmaf(w, o[u].x, acc.x * f);
+            acc.y = fmaf(w, o[u].y, acc.y * f);
+            acc.z = fmaf(w, o[u].z, acc.z * f);
+            acc.w = fmaf(w, o[u].w, acc.w * f);
+            sum = fmaf(w, ml[u].y, sum * f);
         }
     }
-    *reinterpret_cast<float4 *>(s_o + part * DV + 4 * l) = acc;
-    if (l == 0) s_o[parts * DV + part] = sum;
+    *reinterpret_cast<float4 *>(s_part + part * DV + 4 * l) = acc;
+    if (l == 0) {
+        s_m[part] = m;
+        s_l[part] = sum;
+    }
     __syncthreads();
-    for (int d = tid; d < DV; d += nt) {
-        float o = 0.f, t = 0.f;
+    for (int d = tid; d < DV; d += blockDim.x) {
+        float top = -INFINITY, o = 0.f, t = 0.f;
+        for (int k = 0; k < parts; ++k) top = fmaxf(top, s_m[k]);
         for (int k = 0; k < parts; ++k) {
-            o += s_o[k * DV + d];
-            t += s_o[parts * DV + k];
+            const float w = s_m[k] == -INFINITY ? 0.f : exp2f(s_m[k] - top);
+            o = fmaf(w, s_part[k * DV + d], o);
+            t = fmaf(w, s_l[k], t);
         }
-        p.out[((size_t)b * p.H + h) * DV + d] = count > 0 && t != 0.f ? o / t : 0.f;
-        if (d == 0 && p.lse) p.lse[(size_t)b * p.H + h] = count > 0 ? (m + log2f(t)) * kLn2 : -INFINITY;
+        p.out[((size_t)b * p.H + h) * DV + d] = t != 0.f ? o / t : 0.f;
+        if (d == 0 && p.lse) p.lse[(size_t)b * p.H + h] = (top + log2f(t)) * kLn2;
     }
 }
 

@@ -22,8 +22,11 @@
 // by a power of two so that neither overflows nor loses bits to f16's range: per head for the query, and for the weights
 // p s by the largest step seen so far, which is followed like the running maximum.
 //
-// A block streams a contiguous range of tiles through an NSTAGE ring of bulk copies (one producer warp, G consumer warps,
-// one group each); see gva_common.cuh for the ranges.  All waits are bounded.
+// Blocks.  One block per SM streams a contiguous range of tiles through a ring of bulk copies: up to four producer warps, and
+// teams of G consumer warps, one warp per group, up to 16 consumers in all.  Team k takes tiles k, k + teams, ..., keeps its own
+// running softmax and writes its own partial records, so results do not depend on who is faster; a team that the
+// scheduler favours meets the end of the ring and waits there for the others, which evens them out (four blocks per SM with
+// equal ranges each ended between 45 and 69 us on the 1 M token batch, median 57).  All waits are bounded.
 #pragma once
 
 #include "gva_decode_mma.cuh"
@@ -165,16 +168,15 @@ __device__ __forceinline__ void load_q4_query(Q4Query<T> &out, const float *q /*
     out.sum = __shfl_sync(0xffffffffu, sum, 8 * c);
     if constexpr (T::DR > 0) {
         const float *r = src + T::DV;
-        // whole 16-wide k-steps: a lane's positional dims lie side by side (DR / 16 pairs of pairs from c DR' / 4 on), see score_q4
         constexpr int FULL = T::DR / 16;
         auto pair = [&](const float *x, int pt) { return part_bf16(x[0] * factor, pt) | (part_bf16(x[1] * factor, pt) << 16); };
 #pragma unroll
         for (int k = 0; k < FULL; ++k) {
-            const float *x = r + c * 4 * FULL + 4 * k;
+            const float *x = r + 16 * k + 2 * c;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                out.r[k][i] = pair(x + 2 * i, part);
-                out.r2[k][i] = part ? 0u : pair(x + 2 * i, 2);
+                out.r[k][i] = pair(x + 8 * i, part);
+                out.r2[k][i] = part ? 0u : pair(x + 8 * i, 2);
             }
         }
         if constexpr (T::DR % 16 == 8) {
@@ -187,10 +189,14 @@ __device__ __forceinline__ void load_q4_query(Q4Query<T> &out, const float *q /*
 
 // Content and positional products of two 16-token chunks with one group's queries, side by side so that neither waits for the
 // other's MMAs.  acc: codes (to be multiplied by unscale and the token's step), rot: positional part, in f32; columns hi and
-// lo of head lane % 4 in [0], [1] for token row rowmap(lane / 4) and in [2], [3] for that row + 8.  v, kr: this lane's share of the
-// first chunk's low token row (kr: of the row itself).
+// lo of head lane % 4 in [0], [1] for token row rowmap(lane / 4) and in [2], [3] for that row + 8.  v: this lane's share of the
+// first chunk's low token row; kr: shared-memory address of the lane's row and piece of the first chunk (kr_lane()).
 template <class T>
-__device__ __forceinline__ void score_q4(const unsigned char *v, const unsigned char *kr, int c, const Q4Query<T> &q, float (&acc)[2][4], float (&rot)[2][4]) {
+__device__ __forceinline__ uint32_t kr_lane(int lane) {      // matrices: (low rows | high rows) x (first | second 16 bytes)
+    return (uint32_t)((rowmap(lane & 7) + 8 * ((lane >> 3) & 1)) * T::KR_ROW + 16 * (lane >> 4));
+}
+template <class T>
+__device__ __forceinline__ void score_q4(const unsigned char *v, uint32_t kr, const Q4Query<T> &q, float (&acc)[2][4], float (&rot)[2][4]) {
     uint32_t lo[2][T::WORDS], hi[2][T::WORDS];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -210,11 +216,7 @@ __device__ __forceinline__ void score_q4(const unsigned char *v, const unsigned 
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int u = 0; u < FULL; ++u) {
-                const unsigned char *row = kr + k * 16 * T::KR_ROW + 8 * (c * FULL + u);
-                const uint2 a = *reinterpret_cast<const uint2 *>(row), b = *reinterpret_cast<const uint2 *>(row + 8 * T::KR_ROW);
-                f[k][u][0] = a.x; f[k][u][1] = b.x; f[k][u][2] = a.y; f[k][u][3] = b.y;
-            }
+            for (int u = 0; u < FULL; ++u) ldsm_x4(kr + k * 16 * T::KR_ROW + 32 * u, f[k][u]);
 #pragma unroll
         for (int u = 0; u < FULL; ++u)
 #pragma unroll
@@ -225,8 +227,8 @@ __device__ __forceinline__ void score_q4(const unsigned char *v, const unsigned 
         if constexpr (T::DR % 16 == 8) {                     // the last 8 dims lie apart
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const unsigned char *row = kr + k * 16 * T::KR_ROW + 32 * FULL + 4 * c;
-                const uint32_t t[2] = {*reinterpret_cast<const uint32_t *>(row), *reinterpret_cast<const uint32_t *>(row + 8 * T::KR_ROW)};
+                uint32_t t[2];
+                ldsm_x2(kr + k * 16 * T::KR_ROW + 32 * FULL, t);             // lanes 0 .. 15 give the rows
                 mma_bf16_k8(rot[k], t, q.r2[FULL][0]);
                 mma_bf16_k8(rot[k], t, q.r[FULL][0]);
             }
@@ -270,21 +272,25 @@ __device__ __forceinline__ bool mbar_wait_relaxed(uint32_t bar, uint32_t parity,
 
 // What the producer tells the consumers about a stage.
 struct TileMeta {
-    int b, t0, n_valid, flags;   // sequence, first slot, live tokens, bit 0 / 1: first / last tile of the block's part of the sequence
+    int b, t0, n_valid, unused;  // sequence, first slot, live tokens
 };
 
-// The producer warp: walks flat tiles [lo, hi), 32 look-ups at a time (a lane each), and fills the ring.  copy(stage base,
-// page, first slot, full barrier, lane) starts the copies, any lane any of them; bytes = what they add up to.
-template <int TILE, int NSTAGE, class Copy>
-__device__ __forceinline__ void produce_tiles(const int *s_off, const int32_t *seq_lens, const int32_t *block_table, int B, int P, int num_pages,
-                                              int max_pages, int32_t *dev_status, int lo, int hi, uint64_t *full_bar, uint64_t *empty_bar,
-                                              TileMeta *s_meta, volatile int *s_abort, uint32_t bytes, Copy copy) {
-    const int lane = threadIdx.x & 31;
-    int issued = 0;
+// One of `n_producers` producer warps: takes every n_producers-th of the flat tiles [lo, hi), 32 look-ups at a time (a lane
+// each), and fills their slots of the ring.  nstage is a multiple of n_producers, so that a slot is always filled by the same warp:
+// the parity that a wait goes by tells a slot's turn from the one before, not from the one before that.  copy(stage, page, first slot, full barrier, lane) starts the copies, any lane any of
+// them; bytes = what they add up to.  (One warp needs about 1050 cycles a tile -- the issue of a bulk copy is slow, not
+// its flight -- against some 600 that sixteen consumer warps need: 89 us on the 1 M token batch.)
+template <int TILE, class Copy>
+__device__ __forceinline__ void produce_tiles(int producer, int n_producers, int nstage, const int *s_off, const int32_t *seq_lens,
+                                              const int32_t *block_table, int B, int P, int num_pages, int max_pages, int32_t *dev_status, int lo,
+                                              int hi, uint64_t *full_bar, uint64_t *empty_bar, TileMeta *s_meta, volatile int *s_abort,
+                                              uint32_t bytes, Copy copy) {
+    const int lane = threadIdx.x & 31, n_mine = (hi - lo - producer + n_producers - 1) / n_producers;
+    int issued = 0, st = producer, parity = 1;               // slot; parity of its empty barrier's phase to wait for
     bool ok = true;
-    for (int base = lo; base < hi && ok; base += 32) {
-        const int f = base + lane;
-        int b = 0, t0 = 0, n_valid = 0, flags = 0;
+    for (int base = 0; base < n_mine && ok; base += 32) {
+        const int f = lo + producer + (base + lane) * n_producers;
+        int b = 0, t0 = 0, n_valid = 0;
         long long page = 0;
         if (f < hi) {
             b = seq_of_tile(s_off, B, f);
@@ -292,24 +298,21 @@ __device__ __forceinline__ void produce_tiles(const int *s_off, const int32_t *s
             const int len = seq_lens[b];
             page = block_table ? (long long)block_table[(size_t)b * max_pages + t0 / P] : (long long)b * max_pages + t0 / P;
             n_valid = min(TILE, len - t0);
-            flags = ((f == lo || t0 == 0) ? 1 : 0) | ((f + 1 == hi || f + 1 == s_off[b + 1]) ? 2 : 0);
             if (page < 0 || page >= num_pages) {
                 report_error(dev_status, GVA_ERR_BAD_PAGE, b);
                 page = 0;                                    // there is one; what is read of it counts for nothing
                 n_valid = 0;
             }
         }
-        const int n = min(32, hi - base);
+        const int slot = t0 % P, n = min(32, n_mine - base);
         for (int i = 0; i < n; ++i, ++issued) {
-            const int st = issued % NSTAGE;
-            const int pg = (int)__shfl_sync(0xffffffffu, (int)page, i);
-            const int t = __shfl_sync(0xffffffffu, t0, i), nv = __shfl_sync(0xffffffffu, n_valid, i);
-            const int bb = __shfl_sync(0xffffffffu, b, i), fl = __shfl_sync(0xffffffffu, flags, i);
+            const int pg = (int)__shfl_sync(0xffffffffu, (int)page, i), sl = __shfl_sync(0xffffffffu, slot, i);
+            const int t = __shfl_sync(0xffffffffu, t0, i), nv = __shfl_sync(0xffffffffu, n_valid, i), bb = __shfl_sync(0xffffffffu, b, i);
             const uint32_t bar = smem_u32(&full_bar[st]);
             int good = 1;
             if (lane == 0) {
-                if (mbar_wait_relaxed(smem_u32(&empty_bar[st]), ((issued / NSTAGE) & 1) ^ 1, s_abort)) {
-                    s_meta[st] = TileMeta{bb, t, nv, fl};
+                if (mbar_wait_relaxed(smem_u32(&empty_bar[st]), parity, s_abort)) {
+                    s_meta[st] = TileMeta{bb, t, nv, 0};
                     mbar_expect_tx(bar, bytes);
                 } else {
                     if (!*s_abort) report_error(dev_status, GVA_ERR_TIMEOUT, bb);
@@ -322,13 +325,20 @@ __device__ __forceinline__ void produce_tiles(const int *s_off, const int32_t *s
                 ok = false;
                 break;
             }
-            copy(st, (size_t)pg, t % P, bar, lane);
+            copy(st, (size_t)pg, sl, bar, lane);
+            st += n_producers;
+            if (st >= nstage) {
+                st -= nstage;
+                parity ^= 1;
+            }
         }
     }
     if (!ok && lane == 0) {                                  // every copy in flight must land before the shared memory is released
-        for (int i = max(0, issued - NSTAGE); i < issued; ++i)
+        for (int i = max(0, issued - nstage / n_producers); i < issued; ++i) {
+            const int at = producer + i * n_producers;
             for (int it = 0; it < kDrainPolls; ++it)
-                if (mbar_try_wait(smem_u32(&full_bar[i % NSTAGE]), (i / NSTAGE) & 1)) break;
+                if (mbar_try_wait(smem_u32(&full_bar[at % nstage]), (at / nstage) & 1)) break;
+        }
     }
 }
 
@@ -349,21 +359,36 @@ __device__ __forceinline__ void copy_q4_tile(uint32_t base, const Q4Pools &c, in
         bulk_load_stream(base + G * (T::V_BYTES + T::SZ_BYTES), c.kr + (page * P + slot) * T::DR, T::KR_BYTES, bar, pol);
 }
 
-template <int DV, int DR, int TILE, int NSTAGE, int GMAX, int BLOCKS>
-__global__ void __launch_bounds__(32 * (GMAX + 1), BLOCKS)
-decode_q4_kernel(DecodeParams p, Q4Pools pools) {
+// What the launch adds to DecodeParams.
+struct Q4Launch {
+    Q4Pools pools;
+    int teams, producers, nstage;   // nstage: a multiple of both, see produce_tiles (a team likewise finds only its own tiles in a slot)
+    int2 *segments;              // per sequence: first record group and their number, for the merge (balanced partition only)
+};
+#ifndef GVA_Q4_CONS64
+#define GVA_Q4_CONS64 16
+#endif
+#ifndef GVA_Q4_CONS128
+#define GVA_Q4_CONS128 16
+#endif
+constexpr int kQ4Producers = 4;           // producer warps of a block at most
+__host__ __device__ constexpr int q4_consumers(int d_v) { return d_v == 64 ? GVA_Q4_CONS64 : GVA_Q4_CONS128; }   // consumer warps of a block at most
+
+template <int DV, int DR, int TILE>
+__global__ void __launch_bounds__(32 * (q4_consumers(DV) + kQ4Producers), 1)
+decode_q4_kernel(DecodeParams p, Q4Launch L) {
     using T = Q4Traits<DV, DR, TILE>;
     grid_dependency_launch();
     extern __shared__ __align__(128) unsigned char smem[];
-    const int G = p.G, H = p.H, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G = p.G, H = p.H, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nstage = L.nstage;
     const int stage_bytes = T::stage_bytes(G);
-    unsigned char *tail = smem + (size_t)NSTAGE * stage_bytes;
-    uint64_t *full_bar = reinterpret_cast<uint64_t *>(tail), *empty_bar = full_bar + NSTAGE;
-    TileMeta *s_meta = reinterpret_cast<TileMeta *>(empty_bar + NSTAGE);
-    volatile int *s_abort = reinterpret_cast<volatile int *>(s_meta + NSTAGE);
-    int *s_off = reinterpret_cast<int *>(s_meta + NSTAGE) + 4;
+    unsigned char *tail = smem + (size_t)nstage * stage_bytes;
+    uint64_t *full_bar = reinterpret_cast<uint64_t *>(tail), *empty_bar = full_bar + nstage;
+    TileMeta *s_meta = reinterpret_cast<TileMeta *>(empty_bar + nstage);
+    volatile int *s_abort = reinterpret_cast<volatile int *>(s_meta + nstage);
+    int *s_off = reinterpret_cast<int *>(s_meta + nstage) + 4;
     if (tid == 0) {
-        for (int s = 0; s < NSTAGE; ++s) {
+        for (int s = 0; s < nstage; ++s) {
             mbar_init(smem_u32(&full_bar[s]), 1);
             mbar_init(smem_u32(&empty_bar[s]), G);
         }
@@ -373,56 +398,98 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
     grid_dependency_wait();
     compute_tile_offsets<TILE>(p, s_off);                    // ends with a barrier
     const BlockRange rg = block_range(p, s_off);
+    if (L.segments && blockIdx.x == 0) {
+        const int total = s_off[p.B], n_eff = partitions_in_use(total, gridDim.x);
+        for (int b = tid; b < p.B; b += blockDim.x) {
+            int2 seg = make_int2(0, 0);
+            if (s_off[b + 1] > s_off[b]) {
+                const int c0 = range_owner(s_off[b], total, n_eff), c1 = range_owner(s_off[b + 1] - 1, total, n_eff);
+                seg = make_int2(c0 + b, c1 - c0 + 1);
+            }
+            L.segments[b] = seg;
+        }
+    }
+    // the result itself is written where a block has the whole sequence and one team
+    const bool direct = p.num_splits == 1;
     if (rg.lo >= rg.hi) {
-        if (p.num_splits > 0) {                              // an empty split: its record weighs nothing, an only split is the result
+        if (p.num_splits > 0) {                              // an empty split
             const int b = blockIdx.x / p.num_splits;
-            if (p.num_splits == 1) {
+            if (direct) {
                 for (int i = tid; i < H * DV; i += blockDim.x) p.out[(size_t)b * H * DV + i] = 0.f;
                 if (p.lse)
                     for (int i = tid; i < H; i += blockDim.x) p.lse[(size_t)b * H + i] = -INFINITY;
             } else {
-                for (int i = tid; i < H; i += blockDim.x) {
-                    p.rec_ml[((size_t)rg.rec_fixed * H + i) * 2] = -INFINITY;
-                    p.rec_ml[((size_t)rg.rec_fixed * H + i) * 2 + 1] = 0.f;
-                }
+                for (int i = tid; i < H; i += blockDim.x) *reinterpret_cast<float2 *>(p.rec_ml + ((size_t)rg.rec_fixed * H + i) * 2) = make_float2(-INFINITY, 0.f);
             }
         }
         return;
     }
-    if (warp == G) {
+    if (warp >= G * L.teams) {
         const uint64_t pol = l2_policy_evict_first();
-        produce_tiles<TILE, NSTAGE>(s_off, p.seq_lens, p.block_table, p.B, p.P, p.num_pages, p.max_pages, p.dev_status, rg.lo, rg.hi,
-                                    full_bar, empty_bar, s_meta, s_abort, (uint32_t)stage_bytes,
-                                    [&](int st, size_t page, int slot, uint32_t bar, int ln) {
-                                        copy_q4_tile<T>(smem_u32(smem + (size_t)st * stage_bytes), pools, G, p.P, page, slot, bar, pol, ln);
-                                    });
+        produce_tiles<TILE>(warp - G * L.teams, L.producers, nstage, s_off, p.seq_lens, p.block_table, p.B, p.P, p.num_pages, p.max_pages, p.dev_status, rg.lo, rg.hi,
+                            full_bar, empty_bar, s_meta, s_abort, (uint32_t)stage_bytes,
+                            [&](int st, size_t page, int slot, uint32_t bar, int ln) {
+                                copy_q4_tile<T>(smem_u32(smem + (size_t)st * stage_bytes), L.pools, G, p.P, page, slot, bar, pol, ln);
+                            });
     } else {
-        const int g = warp, c = lane & 3, r8 = lane >> 2;
+        const int team = warp / G, g = warp - team * G, c = lane & 3, r8 = lane >> 2;
         const int tok_lo = rowmap(r8), tok_hi = tok_lo + 8;
         const int ta = rowmap(2 * c), tb = rowmap(2 * c + 1);            // tokens of the output product's k = 2 c, 2 c + 1 (+ 8)
+        const int head = g * kHeadsPerGroup + c;
         Q4Query<T> q;
         float oacc[T::MT][4];
         float m_run = -INFINITY, l_run = 0.f, z_run = 0.f, step_ref = 0.f, lift = 0.f;   // all sums carry the factor 2^lift
-        int cur_b = rg.b_first;
-        load_q4_query<T>(q, p.q + ((size_t)cur_b * H + g * kHeadsPerGroup) * T::DQ, p.scale_log2, lane);
+        int cur_b = -1, next_b = rg.b_first;                 // sequence in hand; first one this team has not accounted for yet
+        auto record = [&](int b) { return (size_t)((rg.rec_fixed >= 0 ? rg.rec_fixed : (int)blockIdx.x + b) * L.teams + team) * H + head; };
+        // this team's part of the sequence in hand: one partial record, or the result
+        auto flush = [&]() {
+            float l = l_run, z = z_run;
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) {
+                l += __shfl_xor_sync(0xffffffffu, l, o);
+                z += __shfl_xor_sync(0xffffffffu, z, o);
+            }
+            const size_t at = direct ? (size_t)cur_b * H + head : record(cur_b);
+            const float norm = direct ? (l != 0.f ? 1.f / l : 0.f) : fast_exp2(-lift);               // (a power of two: exact)
+            float *dst = (direct ? p.out : p.rec_o) + at * DV;
+#pragma unroll
+            for (int h = 0; h < DV / 64; ++h) {
+                float o[8];
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt) {             // rows r8 and r8 + 8 of m-tile mt: dims 8 word + 2 mt and + 1
+                    o[2 * mt] = (oacc[4 * h + mt][0] + oacc[4 * h + mt][1] + z) * norm;
+                    o[2 * mt + 1] = (oacc[4 * h + mt][2] + oacc[4 * h + mt][3] + z) * norm;
+                }
+                *reinterpret_cast<float4 *>(dst + 64 * h + 8 * r8) = make_float4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<float4 *>(dst + 64 * h + 8 * r8 + 4) = make_float4(o[4], o[5], o[6], o[7]);
+            }
+            if (r8 == 0) {
+                if (!direct) *reinterpret_cast<float2 *>(p.rec_ml + at * 2) = make_float2(m_run, l * norm);
+                else if (p.lse) p.lse[at] = (m_run + (log2f(l) - lift)) * kLn2;
+            }
+        };
+        // sequences [next_b, to) of the block's range of which this team got no tile
+        auto mark_empty = [&](int to) {
+            for (; next_b < to; ++next_b)
+                if (r8 == 0) *reinterpret_cast<float2 *>(p.rec_ml + record(next_b) * 2) = make_float2(-INFINITY, 0.f);
+        };
         const int n_tiles = rg.hi - rg.lo;
 #pragma unroll 1
-        for (int i = 0; i < n_tiles; ++i) {
-            const int st = i % NSTAGE;
-            if (!mbar_wait_bounded(smem_u32(&full_bar[st]), (i / NSTAGE) & 1, s_abort)) {
-                if (!*s_abort && lane == 0) report_error(p.dev_status, GVA_ERR_TIMEOUT, cur_b);
+        for (int i = team, st = team, parity = 0; i < n_tiles; i += L.teams) {
+            if (!mbar_wait_bounded(smem_u32(&full_bar[st]), parity, s_abort)) {
+                if (!*s_abort && lane == 0) report_error(p.dev_status, GVA_ERR_TIMEOUT, cur_b < 0 ? 0 : cur_b);
                 *s_abort = 1;
                 break;
             }
             const TileMeta meta = s_meta[st];
-            if (meta.flags & 1) {
-                if (meta.b != cur_b) {
-                    cur_b = meta.b;
-                    load_q4_query<T>(q, p.q + ((size_t)cur_b * H + g * kHeadsPerGroup) * T::DQ, p.scale_log2, lane);
-                }
+            if (meta.b != cur_b) {
+                if (cur_b >= 0) flush();
+                if (!direct) mark_empty(meta.b);
+                cur_b = meta.b;
+                next_b = cur_b + 1;
+                load_q4_query<T>(q, p.q + ((size_t)cur_b * H + g * kHeadsPerGroup) * T::DQ, p.scale_log2, lane);
                 m_run = -INFINITY;
-                l_run = z_run = step_ref = 0.f;
-                lift = 0.f;
+                l_run = z_run = step_ref = lift = 0.f;
 #pragma unroll
                 for (int mt = 0; mt < T::MT; ++mt)
 #pragma unroll
@@ -431,7 +498,7 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
             const unsigned char *stage = smem + (size_t)st * stage_bytes;
             const unsigned char *vt = stage + (size_t)g * T::V_BYTES;
             const __half2 *szt = reinterpret_cast<const __half2 *>(stage + (size_t)G * T::V_BYTES + (size_t)g * T::SZ_BYTES);
-            const unsigned char *krt = stage + (size_t)G * (T::V_BYTES + T::SZ_BYTES);
+            const uint32_t krt = smem_u32(stage + (size_t)G * (T::V_BYTES + T::SZ_BYTES)) + kr_lane<T>(lane);
 
             // ---- scores (log2 units) of this lane's head and token rows ----
             float x[T::CHUNKS][2], step[T::CHUNKS][2], mid[T::CHUNKS][2];
@@ -439,7 +506,7 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
 #pragma unroll
             for (int kk = 0; kk < T::CHUNKS; kk += 2) {
                 float acc[2][4], rot[2][4];
-                score_q4<T>(vt + (kk * 16 + tok_lo) * T::ROW + c * (T::ROW / 4), krt + (kk * 16 + tok_lo) * T::KR_ROW, c, q, acc, rot);
+                score_q4<T>(vt + (kk * 16 + tok_lo) * T::ROW + c * (T::ROW / 4), krt + kk * 16 * T::KR_ROW, q, acc, rot);
 #pragma unroll
                 for (int k = kk; k < kk + 2; ++k) {
                     const float2 a = __half22float2(szt[k * 16 + tok_lo]), b = __half22float2(szt[k * 16 + tok_hi]);
@@ -521,41 +588,14 @@ decode_q4_kernel(DecodeParams p, Q4Pools pools) {
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&empty_bar[st]));
-
-            if (meta.flags & 2) {                            // this block's part of the sequence ends: one partial record, or the result
-                float l = l_run, z = z_run;
-#pragma unroll
-                for (int o = 4; o < 32; o <<= 1) {
-                    l += __shfl_xor_sync(0xffffffffu, l, o);
-                    z += __shfl_xor_sync(0xffffffffu, z, o);
-                }
-                const bool whole = s_off[meta.b + 1] - 1 == rg.lo + i && s_off[meta.b] >= rg.lo && p.num_splits <= 1;
-                const int head = g * kHeadsPerGroup + c;
-                const size_t rh = (size_t)(rg.rec_fixed >= 0 ? rg.rec_fixed : (int)blockIdx.x + meta.b) * H + head;
-                const size_t oh = (size_t)meta.b * H + head;
-                const float norm = whole ? (l != 0.f ? 1.f / l : 0.f) : fast_exp2(-lift);       // (a power of two: exact)
-                float *dst = (whole ? p.out + oh * DV : p.rec_o + rh * DV);
-#pragma unroll
-                for (int h = 0; h < DV / 64; ++h) {
-                    float o[8];
-#pragma unroll
-                    for (int mt = 0; mt < 4; ++mt) {         // rows r8 and r8 + 8 of m-tile mt: dims 8 word + 2 mt and + 1
-                        o[2 * mt] = (oacc[4 * h + mt][0] + oacc[4 * h + mt][1] + z) * norm;
-                        o[2 * mt + 1] = (oacc[4 * h + mt][2] + oacc[4 * h + mt][3] + z) * norm;
-                    }
-                    *reinterpret_cast<float4 *>(dst + 64 * h + 8 * r8) = make_float4(o[0], o[1], o[2], o[3]);
-                    *reinterpret_cast<float4 *>(dst + 64 * h + 8 * r8 + 4) = make_float4(o[4], o[5], o[6], o[7]);
-                }
-                if (r8 == 0) {
-                    if (whole) {
-                        if (p.lse) p.lse[oh] = (m_run + (log2f(l) - lift)) * kLn2;
-                    } else {
-                        p.rec_ml[rh * 2] = m_run;
-                        p.rec_ml[rh * 2 + 1] = l * norm;
-                    }
-                }
+            st += L.teams;
+            if (st >= nstage) {
+                st -= nstage;
+                parity ^= 1;
             }
         }
+        if (cur_b >= 0) flush();
+        if (!direct) mark_empty(rg.rec_fixed >= 0 ? (cur_b < 0 ? rg.b_first + 1 : next_b) : seq_of_tile(s_off, p.B, rg.hi - 1) + 1);
     }
     __syncthreads();                                         // shared memory stays until every warp is done with it
 }

@@ -12,7 +12,7 @@ PROBE_LIB = os.path.join(HERE, "libgva_probe.so")      # the benchmark's read-on
 _SHARED = ["gva_common.cuh", "gva_rope.cuh", "gva_decode_mma.cuh", "gva_handle.cuh", os.path.join("..", "..", "include", "gva.h")]
 SOURCES = {   # source -> the headers it is compiled from
     "gva_api.cu": _SHARED + ["gva_small_kernels.cuh", "gva_decode_fma.cuh", "gva_decode_fp8.cuh", "gva_prefill.cuh", "gva_project.cuh"],
-    "gva_compact.cu": _SHARED + ["gva_q4.cuh", "gva_q4_decode.cuh", "gva_evict.cuh"],
+    "gva_compact.cu": _SHARED + ["gva_q4.cuh", "gva_q4_decode.cuh", "gva_weights.cuh", "gva_evict.cuh"],
 }
 
 

@@ -76,9 +76,8 @@ __device__ __forceinline__ void report_error(int32_t *dev_status, int code, int 
 //   uniform mode (num_splits == S): block c handles split c % S of sequence c / S -> record c.
 // Must be called by every thread of the block; ends with a barrier.
 template <int TILE>
-__device__ __forceinline__ void compute_tile_offsets(const DecodeParams &p, int *s_off) {
+__device__ __forceinline__ void compute_tile_offsets(const DecodeParams &p, int *s_off, long long cap) {
     const int tid = threadIdx.x, nt = blockDim.x;
-    const long long cap = (long long)p.max_pages * p.P;
     for (int b = tid; b < p.B; b += nt) {
         int len = p.seq_lens[b];
         if (len < 0 || (long long)len > cap) {
@@ -108,6 +107,11 @@ __device__ __forceinline__ void compute_tile_offsets(const DecodeParams &p, int 
         }
     }
     __syncthreads();
+}
+
+template <int TILE>
+__device__ __forceinline__ void compute_tile_offsets(const DecodeParams &p, int *s_off) {
+    compute_tile_offsets<TILE>(p, s_off, (long long)p.max_pages * p.P);
 }
 
 __host__ __device__ __forceinline__ int partitions_in_use(int total_tiles, int n_blocks) {

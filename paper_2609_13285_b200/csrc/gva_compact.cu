@@ -6,6 +6,7 @@
 
 #include "gva_evict.cuh"
 #include "gva_q4_decode.cuh"
+#include "gva_weights.cuh"
 #include "gva_handle.cuh"
 
 using namespace gva;
@@ -56,6 +57,13 @@ Q4Kernel q4_kernel(const gva_config &c) {
     return c.d_r == 32 ? GVA_Q4(128, 32) : GVA_Q4(128, 0);
 #undef GVA_Q4
 }
+// Ring of up to four slots per team in `room` bytes: a multiple of the teams and of the producers (see produce_tiles).
+void ring(int teams, size_t stage, size_t room, int *nstage, int *producers) {
+    const int slots = (int)std::min<size_t>(4 * teams, room / stage);
+    *nstage = std::max(teams == 1 ? 2 : teams, slots / teams * teams);
+    *producers = kQ4Producers;
+    while (*nstage % *producers != 0) --*producers;
+}
 // The launch for B sequences of at most max_seq_len tokens.  num_splits = 0: where every sequence is two tiles at most, one
 // block per sequence, which writes the result itself -- there is nothing to merge; else the balanced partition, one
 // block per SM with as many teams as there are tiles for.  num_splits >= 1: blocks of one team, num_splits per sequence.
@@ -78,17 +86,45 @@ Q4Plan q4_plan(const gva_handle *h, int B, int max_seq_len, int num_splits) {
         p.teams = (int)std::min<long long>(std::max(1, q4_consumers(h->cfg.d_v) / h->cfg.G), std::max<long long>(1, (tiles * B + p.grid - 1) / p.grid));
         p.n_rec = (p.grid + B) * p.teams;
     }
-    // the ring: up to four slots per team, at most what the SM holds (one block per SM) or a third of it
+    // the ring takes what the SM holds (one block per SM) or a third of it
     const size_t room = (p.num_splits > 0 ? (size_t)h->smem_per_sm / 3 : (size_t)h->smem_optin) - (size_t)(B + 1) * 4 - 2048;
-    const int slots = (int)std::min<size_t>(4 * p.teams, room / p.k.stage);
-    p.nstage = std::max(p.teams == 1 ? 2 : p.teams, slots / p.teams * p.teams);
-    p.producers = kQ4Producers;
-    while (p.nstage % p.producers != 0) --p.producers;
+    ring(p.teams, p.k.stage, room, &p.nstage, &p.producers);
     p.smem = p.nstage * p.k.stage + Q4Traits<64, 0, 32>::tail_bytes(B, p.nstage);
     p.rec_o = align_up((size_t)B * sizeof(int2), 256);
     p.rec_ml = p.rec_o + align_up((size_t)p.n_rec * h->cfg.H * h->cfg.d_v * 4, 256);
     p.total = p.rec_ml + align_up((size_t)p.n_rec * h->cfg.H * 2 * 4, 256);
     return p;
+}
+
+// ---- gathered weights: which kernel ----
+struct WeightKernel {
+    void (*fn)(WeightParams, WeightLaunch);
+    int tile;
+    size_t stage;
+};
+template <int KIND, int DV, int DR, int TILE>
+WeightKernel weight_kernel_t(int G) { return WeightKernel{weights_mma_kernel<KIND, DV, DR, TILE>, TILE, (size_t)WeightTraits<KIND, DV, DR, TILE>::stage_bytes(G)}; }
+WeightKernel weight_kernel(int kind, const gva_config &c) {
+    // a tile lies in one page; the bf16 tile of wide heads is kept to 32 tokens, so that a ring of several fits
+    const bool t64 = c.page_size % 64 == 0;
+#define GVA_W(KIND_, DV_, DR_) (t64 ? weight_kernel_t<KIND_, DV_, DR_, 64>(c.G) : weight_kernel_t<KIND_, DV_, DR_, 32>(c.G))
+#define GVA_W_SHAPES(KIND_) \
+    if (c.d_v == 64 && c.d_r == 16) return GVA_W(KIND_, 64, 16); \
+    if (c.d_v == 64 && c.d_r == 0) return GVA_W(KIND_, 64, 0)
+    if (kind == kCacheQ4) {
+        GVA_W_SHAPES(kCacheQ4);
+        if (c.d_v == 64) return GVA_W(kCacheQ4, 64, 24);
+        return c.d_r == 32 ? GVA_W(kCacheQ4, 128, 32) : GVA_W(kCacheQ4, 128, 0);
+    }
+    if (kind == kCacheBf16) {
+        GVA_W_SHAPES(kCacheBf16);
+        if (c.d_v == 64) return GVA_W(kCacheBf16, 64, 24);
+        return c.d_r == 32 ? weight_kernel_t<kCacheBf16, 128, 32, 32>(c.G) : weight_kernel_t<kCacheBf16, 128, 0, 32>(c.G);
+    }
+    if (c.d_v == 64) return c.d_r == 16 ? weight_kernel_t<kCacheE4m3, 64, 16, 64>(c.G) : weight_kernel_t<kCacheE4m3, 64, 0, 64>(c.G);   // pages of 64 k tokens
+    return c.d_r == 32 ? weight_kernel_t<kCacheE4m3, 128, 32, 64>(c.G) : weight_kernel_t<kCacheE4m3, 128, 0, 64>(c.G);
+#undef GVA_W_SHAPES
+#undef GVA_W
 }
 
 int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_abs, const float *lse, const int32_t *cu_q,
@@ -99,18 +135,28 @@ int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_ab
     if (!q_abs || !lse || !seq_lens || !weights_out || stride < max_seq_len || !(decay >= 0.f) || std::isinf(decay)) return GVA_ERR_INVALID_ARG;
     if (!aligned(q_abs, 16) || !aligned(lse, 4) || !aligned(cu_q, 4) || !aligned(seq_lens, 4) || !aligned(weights_in, 4) || !aligned(weights_out, 4))
         return GVA_ERR_INVALID_ARG;
-    if (B > 65535) return GVA_ERR_UNSUPPORTED;
+    if (B > 8192) return GVA_ERR_UNSUPPORTED;
     const gva_config &c = h->cfg;
     p.q = q_abs; p.lse = lse; p.cu_q = cu_q; p.seq_lens = seq_lens; p.decay = decay; p.w_in = decay > 0.f ? weights_in : nullptr; p.w_out = weights_out;
     p.stride = stride; p.B = B; p.max_q_len = max_q_len; p.H = c.H; p.G = c.G; p.P = c.page_size;
     p.scale = h->scale;
     p.dev_status = dev_status;
-    const dim3 grid((max_seq_len + kWeightTile - 1) / kWeightTile, B);
-    void (*fn)(WeightParams, int) = nullptr;
-#define GVA_WEIGHTS(KIND_) (c.d_v == 64 ? weights_simple_kernel<KIND_, 64> : weights_simple_kernel<KIND_, 128>)
-    fn = kind == kCacheQ4 ? GVA_WEIGHTS(kCacheQ4) : kind == kCacheE4m3 ? GVA_WEIGHTS(kCacheE4m3) : kind == kCacheBf16 ? GVA_WEIGHTS(kCacheBf16) : GVA_WEIGHTS(kCacheF32);
-#undef GVA_WEIGHTS
-    return launched(launch_pdl(fn, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), p, c.d_r));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (kind == kCacheF32)
+        return launched(launch_pdl(c.d_v == 64 ? weights_f32_kernel<64> : weights_f32_kernel<128>, dim3((max_seq_len + kWeightTile - 1) / kWeightTile, B),
+                                   dim3(256), 0, s, p, c.d_r));
+    const WeightKernel k = weight_kernel(kind, c);
+    const long long tiles = (long long)B * ((max_seq_len + k.tile - 1) / k.tile);
+    const int grid = (int)std::min<long long>(tiles, h->sm_count);
+    WeightLaunch l;
+    l.teams = (int)std::min<long long>(std::max(1, kWeightConsumers / c.G), (tiles + grid - 1) / grid);
+    const size_t tail = (size_t)(B + 1) * 4 + 2048 + (size_t)l.teams * 2 * c.G * k.tile * 4;
+    ring(l.teams, k.stage, (size_t)h->smem_optin - tail, &l.nstage, &l.producers);
+    const size_t smem = l.nstage * k.stage + WeightTraits<kCacheQ4, 64, 0, 32>::tail_bytes(B, l.nstage, l.teams, c.G) +
+                        (size_t)l.teams * 2 * c.G * (k.tile - 32) * 4;
+    if (smem > (size_t)h->smem_optin) return GVA_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GVA_ERR_CUDA;
+    return launched(launch_pdl(k.fn, dim3(grid), dim3(32 * (l.teams * c.G + l.producers)), smem, s, p, l));
 }
 
 // Blocks per sequence of the eviction's selection: as many as leave the device with about one block per SM, eight (the

@@ -1,4 +1,4 @@
-// What every cached token has gathered of the attention, and the eviction of those that gathered least.
+// Eviction of the cached tokens that have gathered the least attention.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -6,94 +6,6 @@
 #include "gva_q4.cuh"
 
 namespace gva {
-
-// ---- gathered weights -----------------------------------------------------------------------------------------------
-// w_out[b][t] = decay w_in[b][t] + sum over the new rows r of b that see t, and all heads, of exp(score(r, h, t) - lse[r][h]).
-struct WeightParams {
-    const void *v;               // value pool of the cache's type (4-bit: codes)
-    const __half2 *sz;           // 4-bit only
-    const void *kr;
-    const int32_t *block_table;
-    int num_pages, max_pages;
-    const float *q, *lse;        // [rows][H][d_v + d_r], [rows][H]
-    const int32_t *cu_q;         // nullable: one row per sequence
-    const int32_t *seq_lens;
-    float decay;
-    const float *w_in;           // nullable
-    float *w_out;
-    int stride, B, max_q_len, H, G, P;
-    float scale;
-    int32_t *dev_status;
-};
-
-enum WeightCache { kCacheF32 = 0, kCacheBf16 = 1, kCacheE4m3 = 2, kCacheQ4 = 3 };
-
-template <int KIND>
-__device__ __forceinline__ float cache_element(const void *pool, size_t i) {
-    if constexpr (KIND == kCacheF32) return static_cast<const float *>(pool)[i];
-    else if constexpr (KIND == kCacheBf16) return __uint_as_float((uint32_t) static_cast<const uint16_t *>(pool)[i] << 16);
-    else return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<const uint8_t *>(pool)[i], __NV_E4M3)));
-}
-
-// One warp per token, d_v / 32 dims per lane, on the CUDA cores.
-constexpr int kWeightTile = 64;
-template <int KIND, int DV>
-__global__ void __launch_bounds__(256)
-weights_simple_kernel(WeightParams p, int DR) {
-    grid_dependency_launch();
-    grid_dependency_wait();
-    const int b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5;
-    const int len = p.seq_lens[b];
-    if (len < 0 || (long long)len > (long long)p.max_pages * p.P || len > p.stride) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
-        return;
-    }
-    const int row0 = p.cu_q ? p.cu_q[b] : b;
-    const int rows = p.cu_q ? min(max(p.cu_q[b + 1] - row0, 0), p.max_q_len) : 1;
-    const int DQ = DV + DR;
-    constexpr int E = DV / 32;
-    for (long long t0 = (long long)blockIdx.x * kWeightTile; t0 < len; t0 += (long long)gridDim.x * kWeightTile) {
-        for (int t = (int)t0 + warp; t < min((long long)len, t0 + kWeightTile); t += n_warps) {
-            const int page = locate_page(p.block_table, p.num_pages, p.max_pages, p.P, b, t, p.dev_status);
-            float total = 0.f;
-            if (page >= 0) {
-                const int slot = t % p.P;
-                float k = 0.f;
-                if (lane < DR) k = cache_element<KIND == kCacheQ4 ? kCacheBf16 : KIND>(p.kr, ((size_t)page * p.P + slot) * DR + lane);
-                for (int g = 0; g < p.G; ++g) {
-                    const size_t row = ((size_t)page * p.G + g) * p.P + slot;
-                    float v[E];
-                    if constexpr (KIND == kCacheQ4) {
-                        const float2 sz = __half22float2(p.sz[row]);
-                        for (int e = 0; e < E; e += 2) {
-                            const uint8_t x = static_cast<const uint8_t *>(p.v)[row * (DV / 2) + lane * (E / 2) + e / 2];
-                            v[e] = fmaf((float)(x & 15), sz.x, sz.y);
-                            v[e + 1] = fmaf((float)(x >> 4), sz.x, sz.y);
-                        }
-                    } else {
-                        for (int e = 0; e < E; ++e) v[e] = cache_element<KIND>(p.v, row * DV + lane * E + e);
-                    }
-                    for (int r = 0; r < rows; ++r) {
-                        if (t >= len - (rows - 1 - r)) continue;
-                        for (int j = 0; j < kHeadsPerGroup; ++j) {
-                            const int h = g * kHeadsPerGroup + j;
-                            const float *q = p.q + ((size_t)(row0 + r) * p.H + h) * DQ;
-                            float x = lane < DR ? q[DV + lane] * k : 0.f;
-                            for (int e = 0; e < E; ++e) x = fmaf(q[lane * E + e], v[e], x);
-                            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-                            const float lse = p.lse[(size_t)(row0 + r) * p.H + h];
-                            if (lse != -INFINITY) total += exp2f(fmaf(x, p.scale, -lse) * kLog2e);
-                        }
-                    }
-                }
-            }
-            if (lane == 0) {
-                const size_t i = (size_t)b * p.stride + t;
-                p.w_out[i] = p.w_in ? fmaf(p.decay, p.w_in[i], total) : total;
-            }
-        }
-    }
-}
 
 // ---- eviction -------------------------------------------------------------------------------------------------------
 // A token counts by its weight; those at positions below `sinks` or within the last `recent` positions count as +inf, a

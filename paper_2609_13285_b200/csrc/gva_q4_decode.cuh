@@ -272,7 +272,7 @@ __device__ __forceinline__ bool mbar_wait_relaxed(uint32_t bar, uint32_t parity,
 
 // What the producer tells the consumers about a stage.
 struct TileMeta {
-    int b, t0, n_valid, unused;  // sequence, first slot, live tokens
+    int b, t0, n_valid, len;     // sequence, first slot, live tokens (none if the page is bad), tokens of the sequence
 };
 
 // One of `n_producers` producer warps: takes every n_producers-th of the flat tiles [lo, hi), 32 look-ups at a time (a lane
@@ -290,12 +290,12 @@ __device__ __forceinline__ void produce_tiles(int producer, int n_producers, int
     bool ok = true;
     for (int base = 0; base < n_mine && ok; base += 32) {
         const int f = lo + producer + (base + lane) * n_producers;
-        int b = 0, t0 = 0, n_valid = 0;
+        int b = 0, t0 = 0, n_valid = 0, len = 0;
         long long page = 0;
         if (f < hi) {
             b = seq_of_tile(s_off, B, f);
             t0 = (f - s_off[b]) * TILE;
-            const int len = seq_lens[b];
+            len = seq_lens[b];
             page = block_table ? (long long)block_table[(size_t)b * max_pages + t0 / P] : (long long)b * max_pages + t0 / P;
             n_valid = min(TILE, len - t0);
             if (page < 0 || page >= num_pages) {
@@ -307,12 +307,12 @@ __device__ __forceinline__ void produce_tiles(int producer, int n_producers, int
         const int slot = t0 % P, n = min(32, n_mine - base);
         for (int i = 0; i < n; ++i, ++issued) {
             const int pg = (int)__shfl_sync(0xffffffffu, (int)page, i), sl = __shfl_sync(0xffffffffu, slot, i);
-            const int t = __shfl_sync(0xffffffffu, t0, i), nv = __shfl_sync(0xffffffffu, n_valid, i), bb = __shfl_sync(0xffffffffu, b, i);
+            const int t = __shfl_sync(0xffffffffu, t0, i), nv = __shfl_sync(0xffffffffu, n_valid, i), bb = __shfl_sync(0xffffffffu, b, i), ln = __shfl_sync(0xffffffffu, len, i);
             const uint32_t bar = smem_u32(&full_bar[st]);
             int good = 1;
             if (lane == 0) {
                 if (mbar_wait_relaxed(smem_u32(&empty_bar[st]), parity, s_abort)) {
-                    s_meta[st] = TileMeta{bb, t, nv, 0};
+                    s_meta[st] = TileMeta{bb, t, nv, ln};
                     mbar_expect_tx(bar, bytes);
                 } else {
                     if (!*s_abort) report_error(dev_status, GVA_ERR_TIMEOUT, bb);

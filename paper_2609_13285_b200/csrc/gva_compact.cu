@@ -103,11 +103,14 @@ struct WeightKernel {
     size_t stage;
 };
 template <int KIND, int DV, int DR, int TILE>
-WeightKernel weight_kernel_t(int G) { return WeightKernel{weights_mma_kernel<KIND, DV, DR, TILE>, TILE, (size_t)WeightTraits<KIND, DV, DR, TILE>::stage_bytes(G)}; }
-WeightKernel weight_kernel(int kind, const gva_config &c) {
+WeightKernel weight_kernel_t(int G, bool multi) {
+    return WeightKernel{multi ? weights_mma_kernel<KIND, DV, DR, TILE, true> : weights_mma_kernel<KIND, DV, DR, TILE, false>, TILE,
+                        (size_t)WeightTraits<KIND, DV, DR, TILE>::stage_bytes(G)};
+}
+WeightKernel weight_kernel(int kind, const gva_config &c, bool multi) {
     // a tile lies in one page; the bf16 tile of wide heads is kept to 32 tokens, so that a ring of several fits
     const bool t64 = c.page_size % 64 == 0;
-#define GVA_W(KIND_, DV_, DR_) (t64 ? weight_kernel_t<KIND_, DV_, DR_, 64>(c.G) : weight_kernel_t<KIND_, DV_, DR_, 32>(c.G))
+#define GVA_W(KIND_, DV_, DR_) (t64 ? weight_kernel_t<KIND_, DV_, DR_, 64>(c.G, multi) : weight_kernel_t<KIND_, DV_, DR_, 32>(c.G, multi))
 #define GVA_W_SHAPES(KIND_) \
     if (c.d_v == 64 && c.d_r == 16) return GVA_W(KIND_, 64, 16); \
     if (c.d_v == 64 && c.d_r == 0) return GVA_W(KIND_, 64, 0)
@@ -119,10 +122,10 @@ WeightKernel weight_kernel(int kind, const gva_config &c) {
     if (kind == kCacheBf16) {
         GVA_W_SHAPES(kCacheBf16);
         if (c.d_v == 64) return GVA_W(kCacheBf16, 64, 24);
-        return c.d_r == 32 ? weight_kernel_t<kCacheBf16, 128, 32, 32>(c.G) : weight_kernel_t<kCacheBf16, 128, 0, 32>(c.G);
+        return c.d_r == 32 ? weight_kernel_t<kCacheBf16, 128, 32, 32>(c.G, multi) : weight_kernel_t<kCacheBf16, 128, 0, 32>(c.G, multi);
     }
-    if (c.d_v == 64) return c.d_r == 16 ? weight_kernel_t<kCacheE4m3, 64, 16, 64>(c.G) : weight_kernel_t<kCacheE4m3, 64, 0, 64>(c.G);   // pages of 64 k tokens
-    return c.d_r == 32 ? weight_kernel_t<kCacheE4m3, 128, 32, 64>(c.G) : weight_kernel_t<kCacheE4m3, 128, 0, 64>(c.G);
+    if (c.d_v == 64) return c.d_r == 16 ? weight_kernel_t<kCacheE4m3, 64, 16, 64>(c.G, multi) : weight_kernel_t<kCacheE4m3, 64, 0, 64>(c.G, multi);   // pages of 64 k tokens
+    return c.d_r == 32 ? weight_kernel_t<kCacheE4m3, 128, 32, 64>(c.G, multi) : weight_kernel_t<kCacheE4m3, 128, 0, 64>(c.G, multi);
 #undef GVA_W_SHAPES
 #undef GVA_W
 }
@@ -145,15 +148,18 @@ int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_ab
     if (kind == kCacheF32)
         return launched(launch_pdl(c.d_v == 64 ? weights_f32_kernel<64> : weights_f32_kernel<128>, dim3((max_seq_len + kWeightTile - 1) / kWeightTile, B),
                                    dim3(256), 0, s, p, c.d_r));
-    const WeightKernel k = weight_kernel(kind, c);
+    const bool multi = cu_q != nullptr && max_q_len > 1;
+    const WeightKernel k = weight_kernel(kind, c, multi);
     const long long tiles = (long long)B * ((max_seq_len + k.tile - 1) / k.tile);
     const int grid = (int)std::min<long long>(tiles, h->sm_count);
     WeightLaunch l;
     l.teams = (int)std::min<long long>(std::max(1, kWeightConsumers / c.G), (tiles + grid - 1) / grid);
-    const size_t tail = (size_t)(B + 1) * 4 + 2048 + (size_t)l.teams * 2 * c.G * k.tile * 4;
+    // beside the ring: lengths, barriers and the sums of up to four tiles per team
+    const size_t tail = (size_t)(B + 1) * 4 + 2048 + (size_t)l.teams * 4 * c.G * k.tile * 4;
     ring(l.teams, k.stage, (size_t)h->smem_optin - tail, &l.nstage, &l.producers);
-    const size_t smem = l.nstage * k.stage + WeightTraits<kCacheQ4, 64, 0, 32>::tail_bytes(B, l.nstage, l.teams, c.G) +
-                        (size_t)l.teams * 2 * c.G * (k.tile - 32) * 4;
+    l.batch = l.nstage / l.teams;
+    const int sums = multi ? l.nstage : 2 * l.teams;
+    const size_t smem = l.nstage * k.stage + WeightTraits<kCacheQ4, 64, 0, 32>::tail_bytes(B, l.nstage, sums, c.G) + (size_t)sums * c.G * (k.tile - 32) * 4;
     if (smem > (size_t)h->smem_optin) return GVA_ERR_UNSUPPORTED;
     if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GVA_ERR_CUDA;
     return launched(launch_pdl(k.fn, dim3(grid), dim3(32 * (l.teams * c.G + l.producers)), smem, s, p, l));

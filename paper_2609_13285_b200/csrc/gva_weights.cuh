@@ -83,8 +83,7 @@ weights_f32_kernel(WeightParams p, int DR) {
 // Blocks, teams, ring and producers as in decode_q4_kernel; a team's warps hold one group each.  Scores come out of the
 // MMAs with the sum over a head's {hi, lo} columns in one lane; every lane adds up the weights of its head over the new
 // rows, four lanes join the group's heads, and the team's groups meet in shared memory (two buffers, one named barrier per
-// tile), where they are added in a fixed order.  A row's queries are kept in registers while a sequence has only
-// one; several rows are loaded for every tile, from L1.
+// tile), where they are added in a fixed order.  A single row's queries stay in registers while the sequence lasts.
 //   bf16 : values as they lie, queries as bf16 hi + lo (and lo's rest for the positional part, as in the 4-bit kernel)
 //   e4m3 : codes widened to f16 exactly, queries as f16 hi + lo, scaled by a power of two per head
 // A lane reads the d_v / 4 neighbouring dims [lane % 4 * d_v / 4, ...) of its rows in 16-byte loads: as in the 4-bit kernel the
@@ -97,8 +96,9 @@ struct WeightTraits {
     static constexpr int KR_ROW = KIND == kCacheE4m3 ? DR : 2 * DR, KR_BYTES = TILE * KR_ROW;
     static constexpr int CHUNKS = TILE / 16, DQ = DV + DR;
     __host__ __device__ static constexpr int stage_bytes(int G) { return G * (V_BYTES + SZ_BYTES) + KR_BYTES; }
-    __host__ __device__ static constexpr int tail_bytes(int B, int nstage, int teams, int G) {
-        return nstage * 32 + 16 + teams * 2 * G * TILE * 4 + (B + 1) * 4;
+    // sums: two tiles per team, or one per slot of the ring
+    __host__ __device__ static constexpr int tail_bytes(int B, int nstage, int sums, int G) {
+        return nstage * 32 + 32 + sums * G * TILE * 4 + (B + 1) * 4;
     }
 };
 
@@ -259,12 +259,247 @@ __device__ __forceinline__ void score_plain(const unsigned char *v, const unsign
     }
 }
 
+// ---- several new rows per sequence ----
+// Two rows at a time: the eight MMA columns are 2 rows x 4 heads, and the query's hi and lo parts go in as two MMAs on the same
+// values, so that whatever widening the values need is done once for both rows; both parts of a query are made by the
+// lane that holds its column, which is a quarter of the instructions that filling columns {hi, lo} takes.  A team takes up
+// to four tiles at once and loads every pair of rows once for all of them -- 32 lanes read 32 cache lines apart, from L2, since
+// the ring leaves L1 no room -- adding up in shared memory.  The blocks' ranges of tiles are cut by the rows that see them.
+template <int KIND, class T>
+struct PairQuery {
+    uint32_t hi[T::DV / 16][2], lo[T::DV / 16][2];
+    uint32_t rhi[T::DR > 0 ? (T::DR + 15) / 16 : 1][2], rlo[T::DR > 0 ? (T::DR + 15) / 16 : 1][2];
+    float unscale[2], sum[2], off[2];                        // of this lane's score columns 2 c, 2 c + 1
+};
+__device__ __forceinline__ void parts_f16(float a, float b, uint32_t &hi, uint32_t &lo) {
+    const __half2 h = __floats2half2_rn(a, b);
+    const float2 f = __half22float2(h);
+    hi = *reinterpret_cast<const uint32_t *>(&h);
+    lo = pack_half2(a - f.x, b - f.y);
+}
+__device__ __forceinline__ void parts_bf16(float a, float b, uint32_t &hi, uint32_t &lo) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    const float2 f = __bfloat1622float2(h);
+    const __nv_bfloat162 l = __floats2bfloat162_rn(a - f.x, b - f.y);
+    hi = *reinterpret_cast<const uint32_t *>(&h);
+    lo = *reinterpret_cast<const uint32_t *>(&l);
+}
+// q: row r's first head of the group; second: the row after it exists
+template <int KIND, class T>
+__device__ __forceinline__ void load_pair(PairQuery<KIND, T> &out, const float *q, const float *lse, int H, bool second, float factor, int lane) {
+    const int n = lane >> 2, c = lane & 3, row = second ? n >> 2 : 0, head = n & 3;
+    const float *src = q + ((size_t)row * H + head) * T::DQ, *rot = src + T::DV;
+    constexpr int FULL = T::DR / 16;
+    float v[T::DV / 4];
+    float top = 0.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < T::DV / 16; ++i) {
+        const float4 x = *reinterpret_cast<const float4 *>(src + c * (T::DV / 4) + 4 * i);
+        v[4 * i] = x.x * factor; v[4 * i + 1] = x.y * factor; v[4 * i + 2] = x.z * factor; v[4 * i + 3] = x.w * factor;
+    }
+    float up = 1.f;
+    if constexpr (KIND == kCacheBf16) {
+#pragma unroll
+        for (int j = 0; j < T::DV / 16; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) parts_bf16(v[4 * j + 2 * i], v[4 * j + 2 * i + 1], out.hi[j][i], out.lo[j][i]);
+    } else {
+        float w[KIND == kCacheE4m3 && T::DR > 0 ? T::DR / 4 : 1];
+#pragma unroll
+        for (int i = 0; i < T::DV / 4; ++i) {
+            top = fmaxf(top, fabsf(v[i]));
+            sum += v[i];
+        }
+        if constexpr (KIND == kCacheE4m3) {
+#pragma unroll
+            for (int i = 0; i < T::DR / 4; ++i) {
+                w[i] = rot[c * (T::DR / 4) + i] * factor;
+                top = fmaxf(top, fabsf(w[i]));
+            }
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        int e = (int)((__float_as_uint(top) >> 23) & 255u) - 126;
+        e = min(max(e, -100), 110);
+        if constexpr (KIND == kCacheQ4) {                    // as in load_q4_query
+            const float down = __uint_as_float((uint32_t)(127 - e + 10) << 23), down16 = 16.f * down;
+            up = __uint_as_float((uint32_t)(127 + e + 10) << 23);
+#pragma unroll
+            for (int i = 0; i < T::DV / 32; ++i) {
+                const float *x = v + 8 * i;
+                parts_f16(x[0] * down16, x[4] * down16, out.hi[2 * i][0], out.lo[2 * i][0]);
+                parts_f16(x[1] * down, x[5] * down, out.hi[2 * i][1], out.lo[2 * i][1]);
+                parts_f16(x[2] * down16, x[6] * down16, out.hi[2 * i + 1][0], out.lo[2 * i + 1][0]);
+                parts_f16(x[3] * down, x[7] * down, out.hi[2 * i + 1][1], out.lo[2 * i + 1][1]);
+            }
+        } else {
+            const float down = __uint_as_float((uint32_t)(127 - e + 6) << 23);
+            up = __uint_as_float((uint32_t)(127 + e - 6) << 23);
+#pragma unroll
+            for (int j = 0; j < T::DV / 16; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) parts_f16(v[4 * j + 2 * i] * down, v[4 * j + 2 * i + 1] * down, out.hi[j][i], out.lo[j][i]);
+#pragma unroll
+            for (int k = 0; k < FULL; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) parts_f16(w[4 * k + 2 * i] * down, w[4 * k + 2 * i + 1] * down, out.rhi[k][i], out.rlo[k][i]);
+        }
+    }
+    if constexpr (KIND != kCacheE4m3) {                      // bf16 positional keys, in the natural order
+#pragma unroll
+        for (int k = 0; k < FULL; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float2 x = *reinterpret_cast<const float2 *>(rot + 16 * k + 8 * i + 2 * c);
+                parts_bf16(x.x * factor, x.y * factor, out.rhi[k][i], out.rlo[k][i]);
+            }
+        if constexpr (T::DR % 16 == 8) {
+            const float2 x = *reinterpret_cast<const float2 *>(rot + 16 * FULL + 2 * c);
+            parts_bf16(x.x * factor, x.y * factor, out.rhi[FULL][0], out.rlo[FULL][0]);
+        }
+    }
+    const float l = lse[row * H + head], shift = l == -INFINITY ? -INFINITY : -l * kLog2e;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                            // from the column's lanes to the lanes that hold its scores
+        out.unscale[i] = __shfl_sync(0xffffffffu, up, 8 * c + 4 * i);
+        out.sum[i] = __shfl_sync(0xffffffffu, sum, 8 * c + 4 * i);
+        out.off[i] = __shfl_sync(0xffffffffu, shift, 8 * c + 4 * i);
+    }
+}
+
+// Scores of one chunk: x[0], x[1]: token row tok_lo, columns 2 c, 2 c + 1; x[2], x[3]: the row eight further.
+template <int KIND, class T>
+__device__ __forceinline__ void score_pair(const unsigned char *v, const unsigned char *kr_row, uint32_t kr, const __half2 *sz /* of row tok_lo */, int c, const PairQuery<KIND, T> &q, float (&x)[4]) {
+    float acc[4];
+    auto both = [&](bool first, const uint32_t (&f)[4], int j) {
+        if constexpr (KIND == kCacheBf16) {
+            if (first) mma_bf16_first(acc, f, q.lo[j][0], q.lo[j][1]);
+            else mma_bf16(acc, f, q.lo[j][0], q.lo[j][1]);
+            mma_bf16(acc, f, q.hi[j][0], q.hi[j][1]);
+        } else {
+            if (first) mma_f16_first(acc, f[0], f[1], f[2], f[3], q.lo[j][0], q.lo[j][1]);
+            else mma_f16_q4(acc, f[0], f[1], f[2], f[3], q.lo[j][0], q.lo[j][1]);
+            mma_f16_q4(acc, f[0], f[1], f[2], f[3], q.hi[j][0], q.hi[j][1]);
+        }
+    };
+    if constexpr (KIND == kCacheQ4) {
+#pragma unroll
+        for (int w = 0; w < T::DV / 32; w += 2) {
+            const uint2 a = *reinterpret_cast<const uint2 *>(v + 4 * w), b = *reinterpret_cast<const uint2 *>(v + 8 * T::ROW + 4 * w);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t lo = u ? a.y : a.x, hi = u ? b.y : b.x;
+                both(w + u == 0, {lo & 0x000f000fu, hi & 0x000f000fu, lo & 0x00f000f0u, hi & 0x00f000f0u}, 2 * (w + u));
+                const uint32_t l = lo >> 8, h = hi >> 8;
+                both(false, {l & 0x000f000fu, h & 0x000f000fu, l & 0x00f000f0u, h & 0x00f000f0u}, 2 * (w + u) + 1);
+            }
+        }
+    } else if constexpr (KIND == kCacheBf16) {
+#pragma unroll
+        for (int j = 0; j < T::DV / 32; ++j) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(v + 16 * j), b = *reinterpret_cast<const uint4 *>(v + 8 * T::ROW + 16 * j);
+            both(j == 0, {a.x, b.x, a.y, b.y}, 2 * j);
+            both(false, {a.z, b.z, a.w, b.w}, 2 * j + 1);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < T::DV / 64; ++j) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(v + 16 * j), b = *reinterpret_cast<const uint4 *>(v + 8 * T::ROW + 16 * j);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t f[4];
+                e4m3_words(w == 0 ? a.x : w == 1 ? a.y : w == 2 ? a.z : a.w, f[0], f[2]);
+                e4m3_words(w == 0 ? b.x : w == 1 ? b.y : w == 2 ? b.z : b.w, f[1], f[3]);
+                both(j == 0 && w == 0, f, 4 * j + w);
+            }
+        }
+    }
+    constexpr int FULL = T::DR / 16;
+    if constexpr (KIND == kCacheE4m3) {
+#pragma unroll
+        for (int u = 0; u < FULL; ++u) {
+            const unsigned char *row = kr_row + c * (T::DR / 4) + 4 * u;
+            uint32_t f[4];
+            e4m3_words(*reinterpret_cast<const uint32_t *>(row), f[0], f[2]);
+            e4m3_words(*reinterpret_cast<const uint32_t *>(row + 8 * T::KR_ROW), f[1], f[3]);
+            mma_f16_q4(acc, f[0], f[1], f[2], f[3], q.rlo[u][0], q.rlo[u][1]);
+            mma_f16_q4(acc, f[0], f[1], f[2], f[3], q.rhi[u][0], q.rhi[u][1]);
+        }
+    } else {
+        float rot[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < FULL; ++u) {
+            uint32_t f[4];
+            ldsm_x4(kr + 32 * u, f);
+            mma_bf16(rot, f, q.rlo[u][0], q.rlo[u][1]);
+            mma_bf16(rot, f, q.rhi[u][0], q.rhi[u][1]);
+        }
+        if constexpr (T::DR % 16 == 8) {
+            uint32_t t[2];
+            ldsm_x2(kr + 32 * FULL, t);
+            mma_bf16_k8(rot, t, q.rlo[FULL][0]);
+            mma_bf16_k8(rot, t, q.rhi[FULL][0]);
+        }
+        if constexpr (KIND == kCacheQ4) {
+            const float2 a = __half22float2(sz[0]), b = __half22float2(sz[8]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 z = i < 2 ? a : b;
+                x[i] = fmaf(acc[i] * q.unscale[i & 1], z.x, fmaf(z.y, q.sum[i & 1], rot[i]));
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] += rot[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = acc[i] * q.unscale[i & 1];
+}
+
+// The block's range of the tile list when a tile costs (rows + 1) / 2 + 1: block c of n takes the tiles whose cost starts in
+// [c, c + 1) total / n.  Called by one whole warp.
+__device__ __forceinline__ void weighted_range(const int *s_off, const int32_t *cu_q, int B, int max_q_len, int lane, int *out_lo, int *out_hi) {
+    auto weight = [&](int b) { return (min(max(cu_q[b + 1] - cu_q[b], 0), max_q_len) + 1) / 2 + 1; };
+    long long total = 0;
+    for (int b = lane; b < B; b += 32) total += (long long)(s_off[b + 1] - s_off[b]) * weight(b);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    int edge[2] = {s_off[B], s_off[B]};
+    long long before = 0;
+    for (int base = 0; base < B; base += 32) {
+        const int b = base + lane;
+        const int w = b < B ? weight(b) : 1, tiles = b < B ? s_off[b + 1] - s_off[b] : 0;
+        const long long mine = (long long)tiles * w;
+        long long incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        const long long start = before + incl - mine;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {                        // the first tile whose cost starts at or behind x
+            const long long x = ((long long)blockIdx.x + e) * total / gridDim.x;
+            const bool here = mine > 0 && x <= start + mine - w;     // (the first such sequence has it)
+            const int at = here ? s_off[b] + (int)((max(x - start, 0ll) + w - 1) / w) : 0;
+            const uint32_t who = __ballot_sync(0xffffffffu, here);
+            if (who) edge[e] = min(edge[e], __shfl_sync(0xffffffffu, at, __ffs(who) - 1));
+        }
+        before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    *out_lo = edge[0];
+    *out_hi = edge[1];
+}
+
 struct WeightLaunch {
     int teams, producers, nstage;   // see Q4Launch
+    int batch;                      // several rows: tiles a team takes at once, nstage / teams
 };
 constexpr int kWeightConsumers = 16;
 
-template <int KIND, int DV, int DR, int TILE>
+template <int KIND, int DV, int DR, int TILE, bool MULTI>
 __global__ void __launch_bounds__(32 * (kWeightConsumers + kQ4Producers), 1)
 weights_mma_kernel(WeightParams w, WeightLaunch L) {
     using T = WeightTraits<KIND, DV, DR, TILE>;
@@ -277,8 +512,9 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
     uint64_t *full_bar = reinterpret_cast<uint64_t *>(tail), *empty_bar = full_bar + nstage;
     TileMeta *s_meta = reinterpret_cast<TileMeta *>(empty_bar + nstage);
     volatile int *s_abort = reinterpret_cast<volatile int *>(s_meta + nstage);
-    float *s_sum = reinterpret_cast<float *>(s_meta + nstage) + 4;                       // [team][2][G][TILE]
-    int *s_off = reinterpret_cast<int *>(s_sum + L.teams * 2 * G * TILE);
+    int *s_edge = reinterpret_cast<int *>(s_meta + nstage) + 4;
+    float *s_sum = reinterpret_cast<float *>(s_edge + 4);                                // [team][2 or batch][G][TILE]
+    int *s_off = reinterpret_cast<int *>(s_sum + L.teams * (MULTI ? L.batch : 2) * G * TILE);
     if (tid == 0) {
         for (int s = 0; s < nstage; ++s) {
             mbar_init(smem_u32(&full_bar[s]), 1);
@@ -296,7 +532,22 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
     p.max_pages = w.max_pages;
     p.num_splits = 0;
     compute_tile_offsets<TILE>(p, s_off, min((long long)w.max_pages * w.P, (long long)w.stride));    // ends with a barrier
-    const BlockRange rg = block_range(p, s_off);
+    BlockRange rg;
+    if constexpr (MULTI) {
+        if (warp == 0) {
+            int lo, hi;
+            weighted_range(s_off, w.cu_q, w.B, w.max_q_len, lane, &lo, &hi);
+            if (lane == 0) {
+                s_edge[0] = lo;
+                s_edge[1] = hi;
+            }
+        }
+        __syncthreads();
+        rg.lo = s_edge[0];
+        rg.hi = s_edge[1];
+    } else {
+        rg = block_range(p, s_off);
+    }
     if (rg.lo >= rg.hi) return;
     if (warp >= G * L.teams) {
         const uint64_t pol = l2_policy_evict_first();
@@ -319,18 +570,88 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
     } else {
         const int team = warp / G, g = warp - team * G, c = lane & 3, r8 = lane >> 2;
         const int tok_lo = rowmap(r8), tok_hi = tok_lo + 8, head = g * kHeadsPerGroup + c;
-        using Query = std::conditional_t<KIND == kCacheQ4, Q4Query<QT>, PlainQuery<KIND, T>>;
-        Query q;
-        float *sums = s_sum + team * 2 * G * TILE;
+        using Single = std::conditional_t<KIND == kCacheQ4, Q4Query<QT>, PlainQuery<KIND, T>>;
+        std::conditional_t<MULTI, PairQuery<KIND, T>, Single> q;
+        float *sums = s_sum + team * (MULTI ? L.batch : 2) * G * TILE;
         int cur_b = -1, row0 = 0, rows = 0, buf = 0;
-        float off = 0.f;                                     // -lse in log2 units of the row in hand
-        auto take_row = [&](int r) {
-            load_query<KIND>(q, w.q + ((size_t)(row0 + r) * H + g * kHeadsPerGroup) * T::DQ, w.scale * kLog2e, lane);
-            const float lse = w.lse[(size_t)(row0 + r) * H + head];
-            off = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
-        };
+        float off = 0.f;                                     // -lse in log2 units (one row)
         const int n_tiles = rg.hi - rg.lo;
         bool dead = false;                                   // a wait ran out: only the team's barriers are still kept
+        if constexpr (MULTI) {
+            // the team's tiles of one round stand in slots team, team + teams, ... of the ring, all of it
+#pragma unroll 1
+            for (int i0 = team, parity = 0; i0 < n_tiles; i0 += L.teams * L.batch, parity ^= 1) {
+                const int n = min(L.batch, (n_tiles - i0 + L.teams - 1) / L.teams);
+                for (int t = lane; t < n * TILE; t += 32) sums[(t / TILE * G + g) * TILE + t % TILE] = 0.f;
+                __syncwarp();
+                for (int j = 0; j < n && !dead; ++j)
+                    if (!mbar_wait_bounded(smem_u32(&full_bar[team + j * L.teams]), parity, s_abort)) {
+                        if (!*s_abort && lane == 0) report_error(w.dev_status, GVA_ERR_TIMEOUT, 0);
+                        *s_abort = 1;
+                        dead = true;
+                    }
+#pragma unroll 1
+                for (int j0 = 0; j0 < n && !dead;) {         // tiles [j0, j1) of one sequence
+                    const int b = s_meta[team + j0 * L.teams].b;
+                    int j1 = j0 + 1;
+                    while (j1 < n && s_meta[team + j1 * L.teams].b == b) ++j1;
+                    row0 = w.cu_q[b];
+                    rows = min(max(w.cu_q[b + 1] - row0, 0), w.max_q_len);
+#pragma unroll 1
+                    for (int r = 0; r < rows; r += 2) {
+                        const bool second = r + 1 < rows;
+                        const size_t at = (size_t)(row0 + r) * H + g * kHeadsPerGroup;
+                        load_pair<KIND, T>(q, w.q + at * T::DQ, w.lse + at, H, second, w.scale * kLog2e, lane);
+#pragma unroll 1
+                        for (int j = j0; j < j1; ++j) {
+                            const int st = team + j * L.teams;
+                            const TileMeta meta = s_meta[st];
+                            // tokens of the tile that this lane's row sees; the later row sees one more
+                            const int seen = meta.len - (rows - 1 - r) - meta.t0;
+                            if (min(meta.n_valid, seen + 1) <= 0) continue;
+                            const int lim = c < 2 ? min(meta.n_valid, seen) : second ? min(meta.n_valid, seen + 1) : 0;
+                            const unsigned char *stage = smem + (size_t)st * stage_bytes;
+                            const unsigned char *vt = stage + (size_t)g * T::V_BYTES;
+                            const __half2 *szt = reinterpret_cast<const __half2 *>(stage + (size_t)G * T::V_BYTES + (size_t)g * T::SZ_BYTES);
+                            const unsigned char *krt = stage + (size_t)G * (T::V_BYTES + T::SZ_BYTES);
+                            float *mine = sums + (j * G + g) * TILE;
+#pragma unroll
+                            for (int k = 0; k < T::CHUNKS; ++k) {
+                                float x[4];
+                                score_pair<KIND, T>(vt + (k * 16 + tok_lo) * T::ROW + c * (T::ROW / 4), krt + (k * 16 + tok_lo) * T::KR_ROW,
+                                                    smem_u32(krt) + k * 16 * T::KR_ROW + kr_lane<QT>(lane), szt + k * 16 + tok_lo, c, q, x);
+                                // (what stands behind the sequence may be anything, a NaN included)
+                                float p0 = fast_exp2(x[0] + q.off[0]) + fast_exp2(x[1] + q.off[1]), p1 = fast_exp2(x[2] + q.off[0]) + fast_exp2(x[3] + q.off[1]);
+                                p0 = k * 16 + tok_lo < lim ? p0 : 0.f;
+                                p1 = k * 16 + tok_hi < lim ? p1 : 0.f;
+                                p0 += __shfl_xor_sync(0xffffffffu, p0, 1);       // the group's heads and the two rows
+                                p1 += __shfl_xor_sync(0xffffffffu, p1, 1);
+                                p0 += __shfl_xor_sync(0xffffffffu, p0, 2);
+                                p1 += __shfl_xor_sync(0xffffffffu, p1, 2);
+                                if (c < 2) mine[k * 16 + (c ? tok_hi : tok_lo)] += c ? p1 : p0;
+                            }
+                        }
+                    }
+                    j0 = j1;
+                }
+                if (G > 1) asm volatile("bar.sync %0, %1;\n" ::"r"(1 + team), "r"(32 * G) : "memory");   // (at most 8 teams then)
+                else __syncwarp();
+                for (int j = 0; j < n && !dead; ++j) {
+                    const TileMeta meta = s_meta[team + j * L.teams];
+                    const int here = min(TILE, meta.len - meta.t0);
+                    for (int t = g * 32 + lane; t < here; t += 32 * G) {
+                        float total = 0.f;
+                        for (int k = 0; k < G; ++k) total += sums[(j * G + k) * TILE + t];
+                        const size_t at = (size_t)meta.b * w.stride + meta.t0 + t;
+                        w.w_out[at] = w.w_in ? fmaf(w.decay, w.w_in[at], total) : total;
+                    }
+                }
+                if (G > 1) asm volatile("bar.sync %0, %1;\n" ::"r"(1 + team), "r"(32 * G) : "memory");   // the sums may be cleared again
+                else __syncwarp();
+                if (lane == 0 && !dead)
+                    for (int j = 0; j < n; ++j) mbar_arrive(smem_u32(&empty_bar[team + j * L.teams]));
+            }
+        } else {
 #pragma unroll 1
         for (int i = team, st = team, parity = 0; i < n_tiles; i += L.teams) {
             if (!dead && !mbar_wait_bounded(smem_u32(&full_bar[st]), parity, s_abort)) {
@@ -343,7 +664,11 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
                 cur_b = meta.b;
                 row0 = w.cu_q ? w.cu_q[cur_b] : cur_b;
                 rows = w.cu_q ? min(max(w.cu_q[cur_b + 1] - row0, 0), w.max_q_len) : 1;
-                if (rows == 1) take_row(0);
+                if (rows == 1) {
+                    load_query<KIND>(q, w.q + ((size_t)row0 * H + g * kHeadsPerGroup) * T::DQ, w.scale * kLog2e, lane);
+                    const float lse = w.lse[(size_t)row0 * H + head];
+                    off = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+                }
             }
             const unsigned char *stage = smem + (size_t)st * stage_bytes;
             const unsigned char *vt = stage + (size_t)g * T::V_BYTES;
@@ -352,11 +677,7 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
             float sum[T::CHUNKS][2];
 #pragma unroll
             for (int k = 0; k < T::CHUNKS; ++k) sum[k][0] = sum[k][1] = 0.f;
-#pragma unroll 1
-            for (int r = 0; r < rows && !dead; ++r) {
-                if (rows > 1) take_row(r);
-                const int lim = min(meta.n_valid, meta.len - (rows - 1 - r) - meta.t0);   // tokens of the tile this row sees
-                if (lim <= 0) continue;
+            if (rows > 0 && !dead) {
 #pragma unroll
                 for (int kk = 0; kk < T::CHUNKS; kk += 2) {
                     float x[2][2];
@@ -377,9 +698,8 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const float p0 = fast_exp2(x[k][0] + off), p1 = fast_exp2(x[k][1] + off);
-                        // (what stands behind the sequence may be anything, a NaN included)
-                        sum[kk + k][0] += (kk + k) * 16 + tok_lo < lim ? p0 : 0.f;
-                        sum[kk + k][1] += (kk + k) * 16 + tok_hi < lim ? p1 : 0.f;
+                        sum[kk + k][0] = (kk + k) * 16 + tok_lo < meta.n_valid ? p0 : 0.f;
+                        sum[kk + k][1] = (kk + k) * 16 + tok_hi < meta.n_valid ? p1 : 0.f;
                     }
                 }
             }
@@ -411,6 +731,7 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
                 st -= nstage;
                 parity ^= 1;
             }
+        }
         }
     }
     __syncthreads();                                         // shared memory stays until every warp is done with it

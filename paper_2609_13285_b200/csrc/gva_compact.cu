@@ -153,12 +153,20 @@ int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_ab
     const long long tiles = (long long)B * ((max_seq_len + k.tile - 1) / k.tile);
     const int grid = (int)std::min<long long>(tiles, h->sm_count);
     WeightLaunch l;
-    l.teams = (int)std::min<long long>(std::max(1, kWeightConsumers / c.G), (tiles + grid - 1) / grid);
+    l.teams = std::max(1, kWeightConsumers / c.G);
+    l.split = 1;
+    if (multi) {                                         // as many teams on the same tiles as there are pairs of rows for
+        l.split = l.teams;
+        while (l.split > (max_q_len + 1) / 2 || l.teams % l.split != 0) --l.split;
+    } else {
+        l.teams = (int)std::min<long long>(l.teams, (tiles + grid - 1) / grid);
+    }
+    const int leads = l.teams / l.split;
     // beside the ring: lengths, barriers and the sums of up to four tiles per team
     const size_t tail = (size_t)(B + 1) * 4 + 2048 + (size_t)l.teams * 4 * c.G * k.tile * 4;
-    ring(l.teams, k.stage, (size_t)h->smem_optin - tail, &l.nstage, &l.producers);
-    l.batch = l.nstage / l.teams;
-    const int sums = multi ? l.nstage : 2 * l.teams;
+    ring(leads, k.stage, (size_t)h->smem_optin - tail, &l.nstage, &l.producers);
+    l.batch = l.nstage / leads;
+    const int sums = multi ? l.batch * l.teams : 2 * l.teams;
     const size_t smem = l.nstage * k.stage + WeightTraits<kCacheQ4, 64, 0, 32>::tail_bytes(B, l.nstage, sums, c.G) + (size_t)sums * c.G * (k.tile - 32) * 4;
     if (smem > (size_t)h->smem_optin) return GVA_ERR_UNSUPPORTED;
     if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GVA_ERR_CUDA;

@@ -262,9 +262,10 @@ __device__ __forceinline__ void score_plain(const unsigned char *v, const unsign
 // ---- several new rows per sequence ----
 // Two rows at a time: the eight MMA columns are 2 rows x 4 heads, and the query's hi and lo parts go in as two MMAs on the same
 // values, so that whatever widening the values need is done once for both rows; both parts of a query are made by the
-// lane that holds its column, which is a quarter of the instructions that filling columns {hi, lo} takes.  A team takes up
-// to four tiles at once and loads every pair of rows once for all of them -- 32 lanes read 32 cache lines apart, from L2, since
-// the ring leaves L1 no room -- adding up in shared memory.  The blocks' ranges of tiles are cut by the rows that see them.
+// lane that holds its column, which is a quarter of the instructions that filling columns {hi, lo} takes.  A pair of rows is
+// loaded once for several tiles -- 32 lanes read 32 cache lines apart, from L2, since the ring leaves L1 no room --: the teams
+// take all tiles of the ring together and split the rows where there are enough, adding up in shared memory.  The blocks'
+// ranges of tiles are cut by the rows that see them.
 template <int KIND, class T>
 struct PairQuery {
     uint32_t hi[T::DV / 16][2], lo[T::DV / 16][2];
@@ -495,7 +496,8 @@ __device__ __forceinline__ void weighted_range(const int *s_off, const int32_t *
 
 struct WeightLaunch {
     int teams, producers, nstage;   // see Q4Launch
-    int batch;                      // several rows: tiles a team takes at once, nstage / teams
+    int split;                      // several rows: teams that share their tiles and split the rows; 1 otherwise
+    int batch;                      // several rows: tiles that such teams take at once, nstage / (teams / split)
 };
 constexpr int kWeightConsumers = 16;
 
@@ -514,11 +516,11 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
     volatile int *s_abort = reinterpret_cast<volatile int *>(s_meta + nstage);
     int *s_edge = reinterpret_cast<int *>(s_meta + nstage) + 4;
     float *s_sum = reinterpret_cast<float *>(s_edge + 4);                                // [team][2 or batch][G][TILE]
-    int *s_off = reinterpret_cast<int *>(s_sum + L.teams * (MULTI ? L.batch : 2) * G * TILE);
+    int *s_off = reinterpret_cast<int *>(s_sum + (MULTI ? L.batch : 2) * L.teams * G * TILE);
     if (tid == 0) {
         for (int s = 0; s < nstage; ++s) {
             mbar_init(smem_u32(&full_bar[s]), 1);
-            mbar_init(smem_u32(&empty_bar[s]), G);
+            mbar_init(smem_u32(&empty_bar[s]), G * L.split);
         }
         *s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -572,39 +574,41 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
         const int tok_lo = rowmap(r8), tok_hi = tok_lo + 8, head = g * kHeadsPerGroup + c;
         using Single = std::conditional_t<KIND == kCacheQ4, Q4Query<QT>, PlainQuery<KIND, T>>;
         std::conditional_t<MULTI, PairQuery<KIND, T>, Single> q;
-        float *sums = s_sum + team * (MULTI ? L.batch : 2) * G * TILE;
+        const int part = MULTI ? team % L.split : 0, lead = MULTI ? team / L.split : team, leads = L.teams / L.split;   // rows' part, tiles' part
+        const int GS = G * L.split;                          // partial sums per token
+        float *sums = s_sum + lead * (MULTI ? L.batch : 2) * GS * TILE;
         int cur_b = -1, row0 = 0, rows = 0, buf = 0;
         float off = 0.f;                                     // -lse in log2 units (one row)
         const int n_tiles = rg.hi - rg.lo;
         bool dead = false;                                   // a wait ran out: only the team's barriers are still kept
         if constexpr (MULTI) {
-            // the team's tiles of one round stand in slots team, team + teams, ... of the ring, all of it
+            // the tiles of one round stand in slots lead, lead + leads, ... of the ring, all of it
 #pragma unroll 1
-            for (int i0 = team, parity = 0; i0 < n_tiles; i0 += L.teams * L.batch, parity ^= 1) {
-                const int n = min(L.batch, (n_tiles - i0 + L.teams - 1) / L.teams);
-                for (int t = lane; t < n * TILE; t += 32) sums[(t / TILE * G + g) * TILE + t % TILE] = 0.f;
+            for (int i0 = lead, parity = 0; i0 < n_tiles; i0 += leads * L.batch, parity ^= 1) {
+                const int n = min(L.batch, (n_tiles - i0 + leads - 1) / leads);
+                for (int t = lane; t < n * TILE; t += 32) sums[(t / TILE * GS + part * G + g) * TILE + t % TILE] = 0.f;
                 __syncwarp();
                 for (int j = 0; j < n && !dead; ++j)
-                    if (!mbar_wait_bounded(smem_u32(&full_bar[team + j * L.teams]), parity, s_abort)) {
+                    if (!mbar_wait_bounded(smem_u32(&full_bar[lead + j * leads]), parity, s_abort)) {
                         if (!*s_abort && lane == 0) report_error(w.dev_status, GVA_ERR_TIMEOUT, 0);
                         *s_abort = 1;
                         dead = true;
                     }
 #pragma unroll 1
                 for (int j0 = 0; j0 < n && !dead;) {         // tiles [j0, j1) of one sequence
-                    const int b = s_meta[team + j0 * L.teams].b;
+                    const int b = s_meta[lead + j0 * leads].b;
                     int j1 = j0 + 1;
-                    while (j1 < n && s_meta[team + j1 * L.teams].b == b) ++j1;
+                    while (j1 < n && s_meta[lead + j1 * leads].b == b) ++j1;
                     row0 = w.cu_q[b];
                     rows = min(max(w.cu_q[b + 1] - row0, 0), w.max_q_len);
 #pragma unroll 1
-                    for (int r = 0; r < rows; r += 2) {
+                    for (int r = 2 * part; r < rows; r += 2 * L.split) {
                         const bool second = r + 1 < rows;
                         const size_t at = (size_t)(row0 + r) * H + g * kHeadsPerGroup;
                         load_pair<KIND, T>(q, w.q + at * T::DQ, w.lse + at, H, second, w.scale * kLog2e, lane);
 #pragma unroll 1
                         for (int j = j0; j < j1; ++j) {
-                            const int st = team + j * L.teams;
+                            const int st = lead + j * leads;
                             const TileMeta meta = s_meta[st];
                             // tokens of the tile that this lane's row sees; the later row sees one more
                             const int seen = meta.len - (rows - 1 - r) - meta.t0;
@@ -614,7 +618,7 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
                             const unsigned char *vt = stage + (size_t)g * T::V_BYTES;
                             const __half2 *szt = reinterpret_cast<const __half2 *>(stage + (size_t)G * T::V_BYTES + (size_t)g * T::SZ_BYTES);
                             const unsigned char *krt = stage + (size_t)G * (T::V_BYTES + T::SZ_BYTES);
-                            float *mine = sums + (j * G + g) * TILE;
+                            float *mine = sums + (j * GS + part * G + g) * TILE;
 #pragma unroll
                             for (int k = 0; k < T::CHUNKS; ++k) {
                                 float x[4];
@@ -634,22 +638,22 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
                     }
                     j0 = j1;
                 }
-                if (G > 1) asm volatile("bar.sync %0, %1;\n" ::"r"(1 + team), "r"(32 * G) : "memory");   // (at most 8 teams then)
+                if (GS > 1) asm volatile("bar.sync %0, %1;\n" ::"r"(1 + lead), "r"(32 * GS) : "memory");   // (at most 8 of them then)
                 else __syncwarp();
                 for (int j = 0; j < n && !dead; ++j) {
-                    const TileMeta meta = s_meta[team + j * L.teams];
+                    const TileMeta meta = s_meta[lead + j * leads];
                     const int here = min(TILE, meta.len - meta.t0);
-                    for (int t = g * 32 + lane; t < here; t += 32 * G) {
+                    for (int t = (part * G + g) * 32 + lane; t < here; t += 32 * GS) {
                         float total = 0.f;
-                        for (int k = 0; k < G; ++k) total += sums[(j * G + k) * TILE + t];
+                        for (int k = 0; k < GS; ++k) total += sums[(j * GS + k) * TILE + t];
                         const size_t at = (size_t)meta.b * w.stride + meta.t0 + t;
                         w.w_out[at] = w.w_in ? fmaf(w.decay, w.w_in[at], total) : total;
                     }
                 }
-                if (G > 1) asm volatile("bar.sync %0, %1;\n" ::"r"(1 + team), "r"(32 * G) : "memory");   // the sums may be cleared again
+                if (GS > 1) asm volatile("bar.sync %0, %1;\n" ::"r"(1 + lead), "r"(32 * GS) : "memory");   // the sums may be cleared again
                 else __syncwarp();
                 if (lane == 0 && !dead)
-                    for (int j = 0; j < n; ++j) mbar_arrive(smem_u32(&empty_bar[team + j * L.teams]));
+                    for (int j = 0; j < n; ++j) mbar_arrive(smem_u32(&empty_bar[lead + j * leads]));
             }
         } else {
 #pragma unroll 1

@@ -255,7 +255,9 @@ int gva_q4_append_chunk(gva_handle *h, const gva_q4_cache *cache, const float *v
     if (B < 0 || n_q < 0) return GVA_ERR_INVALID_ARG;
     if (B == 0 || n_q == 0) return GVA_OK;
     if (!cu_q || !aligned(cu_q, 4) || !ctx_lens) return GVA_ERR_INVALID_ARG;
-    return append_q4(h, cache, v_new, kr_new, cu_q, ctx_lens, first_pos ? first_pos : ctx_lens, B, n_q, kAppendQ4Rows, dev_status, stream);
+    // rows of a block: four shares of eight elements per thread
+    const int rows = kAppendQ4Threads * kAppendQ4Shares / (h->cfg.G * h->cfg.d_v / 8);
+    return append_q4(h, cache, v_new, kr_new, cu_q, ctx_lens, first_pos ? first_pos : ctx_lens, B, n_q, rows, dev_status, stream);
 }
 
 int gva_q4_widen(gva_handle *h, const gva_q4_cache *cache, const gva_cache *wide, const int32_t *starts, const int32_t *seq_lens,

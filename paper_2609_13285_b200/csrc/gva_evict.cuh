@@ -17,7 +17,7 @@ namespace gva {
 // select: one cluster of blocks per sequence finds the n-th key by a radix select (digits of 11, 11 and 10 bits from the
 // top, histograms in shared memory summed over the cluster), counts the ties that still fit, and writes weights and
 // positions of the slots that stay, zero and -1 for those that leave, and the lists of free slots and of survivors to move.
-// move: warps copy the rows of the moves, 16 bytes per lane and piece, weights and positions with them.
+// move: blocks copy the rows of the moves in 16-byte pieces, weights and positions with them.
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictBins = 2048;
 constexpr int kEvictKeysMax = 32768;     // keys of one block that are kept in shared memory; beyond, they are made again
@@ -67,7 +67,7 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
     namespace cg = cooperative_groups;
     grid_dependency_launch();
     extern __shared__ uint32_t s_keys[];                     // [keys_in_smem]
-    __shared__ int s_hist[kEvictBins];
+    __shared__ __align__(8) int s_hists[3][kEvictBins];                   // one per digit: a pass needs no second meeting of the cluster
     __shared__ int s_warp[32];
     __shared__ int s_share[4];                               // read by the other blocks of the cluster
     __shared__ int s_digit, s_rest;
@@ -117,16 +117,32 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
         }
         return;
     }
-    auto make_key = [&](int t) -> uint32_t {
-        const int at = pos ? pos[t] : t;
+    auto make_key = [&](float weight, int at) -> uint32_t {
         const bool safe = at < p.sinks || (p.recent > 0 && (long long)at >= (long long)next - p.recent);
-        return safe ? kEvictKeyInf : evict_key(w[t]);
+        return safe ? kEvictKeyInf : evict_key(weight);
     };
     const bool held = per_block <= keys_in_smem;
-    if (held)
-        for (int t = lo + tid; t < hi; t += kEvictThreads) s_keys[t - lo] = make_key(t);
+    if (held) {
+        constexpr int U = 8;                                 // a thread's weights and positions are asked for eight at a time
+        for (int t0 = lo + tid; t0 < hi; t0 += U * kEvictThreads) {
+            float ww[U];
+            int at[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = min(t0 + u * kEvictThreads, hi - 1);
+                ww[u] = w[t];
+                at[u] = pos ? pos[t] : t;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + u * kEvictThreads;
+                if (t < hi) s_keys[t - lo] = make_key(ww[u], at[u]);
+            }
+        }
+    }
+    for (int i = tid; i < 3 * kEvictBins; i += kEvictThreads) (&s_hists[0][0])[i] = 0;
     __syncthreads();
-    auto key_of = [&](int t) -> uint32_t { return held ? s_keys[t - lo] : make_key(t); };
+    auto key_of = [&](int t) -> uint32_t { return held ? s_keys[t - lo] : make_key(w[t], pos ? pos[t] : t); };
 
     // ---- the key of rank `keep`, from the top digit down ----
     uint32_t prefix = 0, mask = 0;
@@ -134,8 +150,7 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
     if (want > 0)
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, bins = 1 << bits;
-        for (int i = tid; i < kEvictBins; i += kEvictThreads) s_hist[i] = 0;
-        __syncthreads();
+        int *s_hist = s_hists[pass];
         for (int t0 = lo; t0 < hi; t0 += kEvictThreads) {
             const int t = t0 + tid;
             uint32_t key = 0;
@@ -159,10 +174,11 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
         int n0 = 0, n1 = 0;
         const int i0 = bins - 1 - 2 * tid, i1 = i0 - 1;
         if (i1 >= 0) {
+#pragma unroll 8
             for (int c = 0; c < C; ++c) {
-                const int *hist = cluster.map_shared_rank(s_hist, c);
-                n0 += hist[i0];
-                n1 += hist[i1];
+                const int2 n = *reinterpret_cast<const int2 *>(cluster.map_shared_rank(s_hist, c) + i1);
+                n0 += n.y;
+                n1 += n.x;
             }
         }
         int incl = n0 + n1;
@@ -183,7 +199,7 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
         prefix |= (uint32_t)s_digit << shift;
         mask |= (uint32_t)(bins - 1) << shift;
         want = s_rest;
-        cluster.sync();                                      // the histograms may be cleared again
+        __syncthreads();
     }
     const bool none = keep == 0;
 
@@ -234,71 +250,109 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
     cluster.sync();                                          // no block leaves while another still reads its shared memory
     {
         int seen = tie_base;
-        for (int t0 = w_lo; t0 < w_hi; t0 += 32) {
-            const int t = t0 + lane;
-            const uint32_t key = t < w_hi ? key_of(t) : 0;
-            const uint32_t tie = __ballot_sync(0xffffffffu, !none && t < w_hi && key == prefix), below = (1u << lane) - 1;
-            const bool kept = !none && t < w_hi && (key > prefix || (key == prefix && seen + __popc(tie & below) < want));
-            const bool hole = t < w_hi && t < keep && !kept, source = kept && t >= keep;
-            const uint32_t hm = __ballot_sync(0xffffffffu, hole), sm = __ballot_sync(0xffffffffu, source);
-            if (hole) p.holes[(size_t)b * p.move_stride + hole_base + __popc(hm & below)] = t;
-            if (source) p.sources[(size_t)b * p.move_stride + source_base + __popc(sm & below)] = t;
-            if (kept && t < keep) {
-                if (w_out != w) w_out[t] = w[t];
-                if (pos_out != pos) pos_out[t] = pos ? pos[t] : t;
-            } else if (t < w_hi && t >= keep && !kept) {     // leaves; the slot is behind the new end
-                w_out[t] = 0.f;
-                pos_out[t] = -1;
+        constexpr int U = 4;
+        for (int t00 = w_lo; t00 < w_hi; t00 += 32 * U) {
+            float ww[U];
+            int at[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {                    // what stays where it is, asked for ahead of the decisions
+                const int t = t00 + 32 * u + lane;
+                if (t < keep && t < w_hi) {
+                    if (w_out != w) ww[u] = w[t];
+                    if (pos_out != pos) at[u] = pos ? pos[t] : t;
+                }
             }
-            hole_base += __popc(hm);
-            source_base += __popc(sm);
-            seen += __popc(tie);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = t00 + 32 * u + lane;
+                const uint32_t key = t < w_hi ? key_of(t) : 0, below = (1u << lane) - 1;
+                const uint32_t tie = __ballot_sync(0xffffffffu, !none && t < w_hi && key == prefix);
+                const bool kept = !none && t < w_hi && (key > prefix || (key == prefix && seen + __popc(tie & below) < want));
+                const bool hole = t < w_hi && t < keep && !kept, source = kept && t >= keep;
+                const uint32_t hm = __ballot_sync(0xffffffffu, hole), sm = __ballot_sync(0xffffffffu, source);
+                if (hole) p.holes[(size_t)b * p.move_stride + hole_base + __popc(hm & below)] = t;
+                if (source) p.sources[(size_t)b * p.move_stride + source_base + __popc(sm & below)] = t;
+                if (kept && t < keep) {
+                    if (w_out != w) w_out[t] = ww[u];
+                    if (pos_out != pos) pos_out[t] = at[u];
+                } else if (t < w_hi && t >= keep && !kept) { // leaves; the slot is behind the new end
+                    w_out[t] = 0.f;
+                    pos_out[t] = -1;
+                }
+                hole_base += __popc(hm);
+                source_base += __popc(sm);
+                seen += __popc(tie);
+            }
         }
     }
 }
 
-// One cached row of a pool: `groups` segments of `bytes` each, `bytes` apart by a page's slots.
+// One cached row of a pool: G segments of v_bytes and sz, a page's slots apart, and one of kr_bytes.
 struct MovePools {
     uint8_t *v, *kr;             // kr: nullable
     uint32_t *sz;                // 4-bit only, else NULL
     int v_bytes, kr_bytes;       // bytes of a value row of one group, of a positional row (multiples of 16)
 };
-constexpr int kMoveThreads = 256;
+// A block looks up kMoveBatch moves at a time, and its threads then copy their pieces, four of a thread's in flight at once.
+constexpr int kMoveThreads = 256, kMoveBatch = 64;
 __global__ void __launch_bounds__(kMoveThreads)
 evict_move_kernel(EvictParams p, MovePools c, int G) {
     grid_dependency_launch();
+    __shared__ uint32_t s_to[kMoveBatch], s_from[kMoveBatch];                    // page * P + slot
+    __shared__ uint32_t s_page_to[kMoveBatch], s_page_from[kMoveBatch];
     grid_dependency_wait();
-    const int b = blockIdx.y, n = p.n_moves[b];
-    const int warp = blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31, warps = gridDim.x * (kMoveThreads / 32);
-    const int pv = c.v_bytes / 16, pk = c.kr ? c.kr_bytes / 16 : 0, pieces = G * pv + pk;
-    for (int i = warp; i < n; i += warps) {
-        const int to = p.holes[(size_t)b * p.move_stride + i], from = p.sources[(size_t)b * p.move_stride + i];
-        const size_t table = (size_t)b * p.max_pages;
-        const size_t page_to = p.block_table ? (size_t)p.block_table[table + to / p.P] : table + to / p.P;
-        const size_t page_from = p.block_table ? (size_t)p.block_table[table + from / p.P] : table + from / p.P;
-        const int slot_to = to % p.P, slot_from = from % p.P;
-        for (int e = lane; e < pieces; e += 32) {
-            if (e < G * pv) {
-                const int g = e / pv, k = e % pv;
-                *reinterpret_cast<uint4 *>(c.v + ((page_to * G + g) * p.P + slot_to) * c.v_bytes + 16 * k) =
-                    *reinterpret_cast<const uint4 *>(c.v + ((page_from * G + g) * p.P + slot_from) * c.v_bytes + 16 * k);
-            } else {
-                const int k = e - G * pv;
-                *reinterpret_cast<uint4 *>(c.kr + (page_to * p.P + slot_to) * c.kr_bytes + 16 * k) =
-                    *reinterpret_cast<const uint4 *>(c.kr + (page_from * p.P + slot_from) * c.kr_bytes + 16 * k);
-            }
-        }
-        if (c.sz && lane < G) c.sz[(page_to * G + lane) * p.P + slot_to] = c.sz[(page_from * G + lane) * p.P + slot_from];
-        if (lane == 31) {
-            const size_t row = (size_t)b * p.stride;
-            p.w_out[row + to] = p.w_in[row + from];
+    const int b = blockIdx.y, n = p.n_moves[b], tid = threadIdx.x;
+    const uint32_t pv = c.v_bytes / 16, values = G * pv, pk = c.kr ? c.kr_bytes / 16 : 0, per = values + pk + (c.sz ? G : 0);
+    for (int i0 = blockIdx.x * kMoveBatch; i0 < n; i0 += gridDim.x * kMoveBatch) {
+        const int here = min(kMoveBatch, n - i0);
+        if (tid < here) {
+            const int to = p.holes[(size_t)b * p.move_stride + i0 + tid], from = p.sources[(size_t)b * p.move_stride + i0 + tid];
+            const size_t table = (size_t)b * p.max_pages, row = (size_t)b * p.stride;
+            s_page_to[tid] = (uint32_t)(p.block_table ? (size_t)p.block_table[table + to / p.P] : table + to / p.P);
+            s_page_from[tid] = (uint32_t)(p.block_table ? (size_t)p.block_table[table + from / p.P] : table + from / p.P);
+            s_to[tid] = to % p.P;
+            s_from[tid] = from % p.P;
+            p.w_out[row + to] = p.w_in[row + from];          // (the two may be one buffer: sources lie behind all targets)
             p.w_out[row + from] = 0.f;
-        }
-        if (lane == 30) {
-            const size_t row = (size_t)b * p.stride;
             p.pos_out[row + to] = p.pos_in ? p.pos_in[row + from] : from;
             p.pos_out[row + from] = -1;
         }
+        __syncthreads();
+        constexpr int U = 4;
+        for (uint32_t e0 = tid; e0 < here * per; e0 += U * kMoveThreads) {
+            uint4 x[U];
+            uint8_t *dst[U];
+            int size[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t e = e0 + u * kMoveThreads, m = e / per, k = e - m * per;
+                size[u] = 0;
+                if (e < here * per) {
+                    const size_t to = s_page_to[m], from = s_page_from[m];
+                    if (k < values) {
+                        const uint32_t g = k / pv, piece = k - g * pv;
+                        x[u] = *reinterpret_cast<const uint4 *>(c.v + ((from * G + g) * p.P + s_from[m]) * c.v_bytes + 16 * piece);
+                        dst[u] = c.v + ((to * G + g) * p.P + s_to[m]) * c.v_bytes + 16 * piece;
+                        size[u] = 16;
+                    } else if (k < values + pk) {
+                        x[u] = *reinterpret_cast<const uint4 *>(c.kr + (from * p.P + s_from[m]) * c.kr_bytes + 16 * (k - values));
+                        dst[u] = c.kr + (to * p.P + s_to[m]) * c.kr_bytes + 16 * (k - values);
+                        size[u] = 16;
+                    } else {
+                        const uint32_t g = k - values - pk;
+                        x[u].x = c.sz[(from * G + g) * p.P + s_from[m]];
+                        dst[u] = reinterpret_cast<uint8_t *>(c.sz + (to * G + g) * p.P + s_to[m]);
+                        size[u] = 4;
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (size[u] == 16) *reinterpret_cast<uint4 *>(dst[u]) = x[u];
+                else if (size[u] == 4) *reinterpret_cast<uint32_t *>(dst[u]) = x[u].x;
+            }
+        }
+        __syncthreads();
     }
 }
 

@@ -34,10 +34,11 @@ int append_q4(gva_handle *h, const gva_q4_cache *cache, const float *v_new, cons
     std::memset(&p, 0, sizeof(p));
     p.c = q4_pools(cache);
     p.v_new = v_new; p.kr_new = kr_new; p.cu_q = cu_q; p.slot0 = slot0; p.pos0 = pos0;
-    p.B = B; p.n_q = n_q; p.G = c.G; p.d_v = c.d_v; p.d_r = c.d_r; p.P = c.page_size; p.rows = rows;
+    p.B = B; p.n_q = n_q; p.G = c.G; p.d_r = c.d_r; p.P = c.page_size; p.rows = rows;
+    p.per_row_inv = (uint32_t)(((1u << 20) + c.G * c.d_v / 8 - 1) / (c.G * c.d_v / 8));
     p.vec = aligned(v_new, 16) ? 1 : 0;
     p.dev_status = dev_status;
-    return launched(launch_pdl(append_q4_kernel, dim3((n_q + rows - 1) / rows), dim3(kAppendQ4Threads), 0,
+    return launched(launch_pdl(c.d_v == 64 ? append_q4_kernel<64> : append_q4_kernel<128>, dim3((n_q + rows - 1) / rows), dim3(kAppendQ4Threads), 0,
                                static_cast<cudaStream_t>(stream), p, h->rope));
 }
 
@@ -255,8 +256,9 @@ int gva_q4_append_chunk(gva_handle *h, const gva_q4_cache *cache, const float *v
     if (B < 0 || n_q < 0) return GVA_ERR_INVALID_ARG;
     if (B == 0 || n_q == 0) return GVA_OK;
     if (!cu_q || !aligned(cu_q, 4) || !ctx_lens) return GVA_ERR_INVALID_ARG;
-    // rows of a block: four shares of eight elements per thread
-    const int rows = kAppendQ4Threads * kAppendQ4Shares / (h->cfg.G * h->cfg.d_v / 8);
+    // rows of a block: up to four shares of eight elements per thread, as long as that leaves four blocks per SM
+    const int most = kAppendQ4Threads * kAppendQ4Shares / (h->cfg.G * h->cfg.d_v / 8);
+    const int rows = std::max(1, std::min(most, n_q / (4 * h->sm_count)));
     return append_q4(h, cache, v_new, kr_new, cu_q, ctx_lens, first_pos ? first_pos : ctx_lens, B, n_q, rows, dev_status, stream);
 }
 

@@ -37,8 +37,7 @@ __device__ __forceinline__ int locate_page(const int32_t *block_table, int num_p
 // ---- append -----------------------------------------------------------------------------------------------------
 // d_v / 8 neighbouring lanes hold one value row, eight elements each (two 16-byte loads), reduce minimum and maximum with
 // shuffles, and each writes its eight codes as one 32-bit word.  A block takes as many input rows as give every thread four such
-// shares, and asks for all of them before it looks up where they go, so that a block waits for memory twice, not eight times
-// (65536 rows of 8 x 128: 144 -> 70 us, 4.5 TB/s of rows in and codes out).  Its threads rotate the positional pairs in fp64.
+// shares, asks for all of them at once and looks up where they go while they are quantised.  Its threads rotate the positional pairs in fp64.
 // All comparisons against the borders z + (k + 1/2) s are exact in f32: 15 s and (k + 1/2) s have at most 16 significant
 // bits, and "x - z >= T" for an f32 number T holds exactly if it holds for x - z rounded down (max - z <= 15 s: up).
 struct AppendQ4Params {
@@ -47,7 +46,8 @@ struct AppendQ4Params {
     const int32_t *cu_q;        // nullable: one row per sequence
     const int32_t *slot0;       // per sequence: slot of its first row
     const int32_t *pos0;        // per sequence: position of its first row
-    int B, n_q, G, d_v, d_r, P, rows;
+    int B, n_q, G, d_r, P, rows;
+    uint32_t per_row_inv;       // ceil(2^20 / (G d_v / 8)): shares of a block (< 1024) are told apart into rows by a product
     int vec;                    // v_new is 16-byte aligned
     int32_t *dev_status;
 };
@@ -55,33 +55,58 @@ constexpr int kAppendQ4Threads = 256;
 constexpr int kAppendQ4Shares = 4;        // shares of eight elements per thread
 constexpr int kAppendQ4Rows = kAppendQ4Threads * kAppendQ4Shares / 8;   // rows of a block at most (G = 1, d_v = 64)
 
-// Nearest integer of 0 <= y < 2^22 (ties to even) as a float, and a small non-negative integer held in a float as bits: by adding
-// 2^23, which moves the integer into the low bits of the mantissa.
-__device__ __forceinline__ float nearest_int(float y) { return __fsub_rn(__fadd_rn(y, 8388608.f), 8388608.f); }
-__device__ __forceinline__ uint32_t int_bits(float c) { return __float_as_uint(__fadd_rn(c, 8388608.f)) & 0xffu; }
-
-__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], float z, float s, float inv_s) {
-    uint32_t word = 0;
+// The codes of eight elements (z <= x, x - z <= 15 s).  A code is the integer nearest to (x - z) / s, read out of the mantissa after
+// adding 2^23; the quotient is off by less than 3e-6, so a code is right unless its remainder comes within 2e-5 of a half:
+// those elements (one in 25000) are compared with their border as above.
+__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], float z, float s) {
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(inv) : "f"(s));
+    if (!(s > 0.f)) inv = 0.f;
+    float c[8], edge = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float d = __fsub_rd(x[i], z);                  // >= 0
-        float c = nearest_int(fminf(d * inv_s, 15.f));       // off by at most one
-        if (d < (c - 0.5f) * s) c -= 1.f;                    // (a product of <= 5 by 11 bits: exact)
-        else if (d >= (c + 0.5f) * s) c += 1.f;
-        c = fminf(fmaxf(c, 0.f), 15.f);
-        word |= int_bits(c) << (4 * i);
+        c[i] = __fsub_rn(__fmaf_rn(d, inv, 8388608.f), 8388608.f);
+        edge = fmaxf(edge, fabsf(__fmaf_rn(d, inv, -c[i])));
     }
-    return word;
+    if (edge > 0.5f - 2e-5f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = __fsub_rd(x[i], z);
+            if (d < (c[i] - 0.5f) * s) c[i] -= 1.f;          // (a product of <= 5 by 11 bits: exact)
+            else if (d >= (c[i] + 0.5f) * s) c[i] += 1.f;
+            c[i] = fminf(fmaxf(c[i], 0.f), 15.f);
+        }
+    }
+    // four codes as one number below 2^16, again in the mantissa
+    const float lo = fmaf(4096.f, c[3], fmaf(256.f, c[2], fmaf(16.f, c[1], c[0]))) + 8388608.f;
+    const float hi = fmaf(4096.f, c[7], fmaf(256.f, c[6], fmaf(16.f, c[5], c[4]))) + 8388608.f;
+    return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
+}
+// The smallest f16 number s with 15 s >= d, for 0 <= d <= 15 * 65504: from the product with 1 / 15, which is at most one step off;
+// 15 s is exact in f32.
+__device__ __forceinline__ __half step_for(float d) {
+    uint32_t u = __half_as_ushort(__float2half_ru(d * 0.066666667f));
+    if (15.f * __half2float(__ushort_as_half((unsigned short)u)) < d) ++u;
+    const uint32_t less = u > 0 ? u - 1 : 0;
+    if (15.f * __half2float(__ushort_as_half((unsigned short)less)) >= d) u = less;
+    return __ushort_as_half((unsigned short)u);
+}
+__device__ __forceinline__ float max_nan(float a, float b) {         // NaN if either is
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(a), "f"(b));
+    return y;
 }
 
+template <int DV>
 __global__ void __launch_bounds__(kAppendQ4Threads)
-append_q4_kernel(AppendQ4Params p, RopeTable rope) {
+append_q4_kernel(const __grid_constant__ AppendQ4Params p, const __grid_constant__ RopeTable rope) {     // (tables are indexed where they lie)
     grid_dependency_launch();
     __shared__ int s_page[kAppendQ4Rows], s_slot[kAppendQ4Rows], s_pos[kAppendQ4Rows];   // page -1: the row is not written
     grid_dependency_wait();
     const int tid = threadIdx.x, n0 = blockIdx.x * p.rows;
     const int total = p.cu_q ? min(p.n_q, p.cu_q[p.B]) : p.n_q;
-    const int L = p.d_v / 8;                                 // lanes per value row: 8 or 16
+    constexpr int L = DV / 8;                                // lanes per value row
     const int per_row = p.G * L;
     // a row of G d_v elements is per_row shares side by side: share e of the block lies at 8 e
     const int n_shares = min(p.rows, total - n0) * per_row;
@@ -132,7 +157,50 @@ append_q4_kernel(AppendQ4Params p, RopeTable rope) {
         s_slot[r] = slot;
         s_pos[r] = pos;
     }
+    uint32_t word[kAppendQ4Shares];
+    __half2 sz[kAppendQ4Shares];
+#pragma unroll
+    for (int u = 0; u < kAppendQ4Shares; ++u) {
+        if (u * kAppendQ4Threads >= n_shares) break;         // (the whole block)
+        float mn = x[u][0], mx = x[u][0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+            mn = fminf(mn, x[u][i]);
+            mx = max_nan(mx, x[u][i]);
+        }
+#pragma unroll
+        for (int o = 1; o < L; o <<= 1) {
+            mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+            mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        }
+        const bool nan = mx != mx;
+        if (!(mn >= -65504.f && mx <= 65504.f)) {            // (rare) what is beyond f16, and rows with a NaN, which are marked below
+            mn = fminf(fmaxf(mn, -65504.f), 65504.f);
+            mx = nan ? mn : fminf(fmaxf(mx, -65504.f), 65504.f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i] = nan ? mn : fminf(fmaxf(x[u][i], -65504.f), 65504.f);
+        }
+        const __half zh = __float2half_rd(mn);
+        const float z = __half2float(zh);
+        const __half sh = step_for(__fsub_ru(mx, z));
+        word[u] = quantise8(x[u], z, __half2float(sh));
+        sz[u] = __halves2half2(sh, zh);
+        if (nan) {
+            word[u] = 0;
+            sz[u] = __halves2half2(__float2half(0.f), __ushort_as_half(0x7fff));
+        }
+    }
     __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kAppendQ4Shares; ++u) {
+        const int e = u * kAppendQ4Threads + tid;
+        const int r = (int)(((uint32_t)e * p.per_row_inv) >> 20), l = e & (L - 1), g = (e - r * per_row) >> (L == 8 ? 3 : 4);
+        if (e < n_shares && s_page[r] >= 0) {
+            const size_t row = ((size_t)s_page[r] * p.G + g) * p.P + s_slot[r];
+            *reinterpret_cast<uint32_t *>(p.c.v + row * (DV / 2) + 4 * l) = word[u];
+            if (l == 0) p.c.sz[row] = sz[u];
+        }
+    }
     // positional pairs, from the last thread down
     const int pairs = p.d_r / 2;
     for (int e = kAppendQ4Threads - 1 - tid; e < p.rows * pairs; e += kAppendQ4Threads) {
@@ -143,37 +211,6 @@ append_q4_kernel(AppendQ4Params p, RopeTable rope) {
         rope_pair((double)kr[0], (double)kr[1], s_pos[r], rope.inv_freq[k], y0, y1);
         uint16_t *dst = p.c.kr + ((size_t)s_page[r] * p.P + s_slot[r]) * p.d_r + 2 * k;
         *reinterpret_cast<uint32_t *>(dst) = (uint32_t)double_to_bf16_bits(y0) | ((uint32_t)double_to_bf16_bits(y1) << 16);
-    }
-#pragma unroll
-    for (int u = 0; u < kAppendQ4Shares; ++u) {
-        const int e = u * kAppendQ4Threads + tid;
-        if (u * kAppendQ4Threads >= n_shares) break;         // (the whole block)
-        bool nan = false;
-        float mn = 65504.f, mx = -65504.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            nan |= x[u][i] != x[u][i];
-            x[u][i] = fminf(fmaxf(x[u][i], -65504.f), 65504.f);          // (a NaN becomes a number here; its row is marked below)
-            mn = fminf(mn, x[u][i]);
-            mx = fmaxf(mx, x[u][i]);
-        }
-        for (int o = 1; o < L; o <<= 1) {
-            mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        }
-        const uint32_t bad = __ballot_sync(0xffffffffu, nan), mine = (L == 8 ? 0xffu : 0xffffu) << ((tid & 31) / L * L);
-        nan = (bad & mine) != 0;
-        const __half zh = __float2half_rd(mn);
-        const float z = __half2float(zh);
-        const __half sh = __float2half_ru(__fdiv_ru(__fsub_ru(mx, z), 15.f));   // smallest f16 with 15 s >= max - z
-        const float s = __half2float(sh);
-        const int r = e / per_row, l = e % L, g = (e % per_row) / L;
-        if (e < n_shares && s_page[r] >= 0) {
-            const size_t row = ((size_t)s_page[r] * p.G + g) * p.P + s_slot[r];
-            const uint32_t word = s > 0.f ? quantise8(x[u], z, s, __frcp_rn(s)) : 0u;
-            *reinterpret_cast<uint32_t *>(p.c.v + row * (p.d_v / 2) + 4 * l) = nan ? 0u : word;
-            if (l == 0) p.c.sz[row] = nan ? __halves2half2(__float2half(0.f), __ushort_as_half(0x7fff)) : __halves2half2(sh, zh);
-        }
     }
 }
 

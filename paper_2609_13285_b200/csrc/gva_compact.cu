@@ -175,10 +175,10 @@ int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_ab
 }
 
 // Blocks per sequence of the eviction's selection: as many as leave the device with about one block per SM, eight (the
-// portable cluster size) at most, and no more than the longest sequence has work for.
-int evict_cluster(const gva_handle *h, int B, int max_seq_len) {
+// portable cluster size) at most.  Short sequences need them for the moves alone.
+int evict_cluster(const gva_handle *h, int B) {
     int c = 1;
-    while (c < 8 && 2 * c * B <= h->sm_count && c * 2 * kEvictThreads <= max_seq_len) c *= 2;
+    while (c < 8 && 2 * c * B <= h->sm_count) c *= 2;
     return c;
 }
 size_t evict_workspace(int B, int max_seq_len) {
@@ -211,8 +211,12 @@ int evict(gva_handle *h, const int32_t *block_table, int num_pages, int max_page
     p.holes = reinterpret_cast<int32_t *>(ws + align_up((size_t)B * 4, 256));
     p.sources = reinterpret_cast<int32_t *>(ws + align_up((size_t)B * 4, 256) + align_up((size_t)B * p.move_stride * 4, 256));
     p.dev_status = dev_status;
-    const int C = evict_cluster(h, B, max_seq_len);
-    const int per_block = ((max_seq_len + C - 1) / C + 1023) / 1024 * 1024;
+    // few moves: the cluster that has chosen moves the rows too, which saves a launch and its look-ups
+    int C = evict_cluster(h, B);
+    const int here = max_seq_len / 2 <= kEvictMoveHere * kMoveBatch * C ? 1 : 0;
+    if (max_seq_len <= kEvictAlone && !here) C = 1;
+    const int alone = max_seq_len <= kEvictAlone ? 1 : 0;
+    const int per_block = ((max_seq_len + (alone ? 1 : C) - 1) / (alone ? 1 : C) + 1023) / 1024 * 1024;
     const int held = std::min(per_block, kEvictKeysMax);
     const size_t smem = (size_t)held * 4;
     if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GVA_ERR_CUDA;
@@ -230,8 +234,8 @@ int evict(gva_handle *h, const int32_t *block_table, int num_pages, int max_page
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    int rc = launched(cudaLaunchKernelEx(&cfg, evict_select_kernel, p, held));
-    if (rc != GVA_OK) return rc;
+    int rc = launched(cudaLaunchKernelEx(&cfg, evict_select_kernel, p, pools, h->cfg.G, held, alone, here));
+    if (rc != GVA_OK || here) return rc;
     const int blocks = std::max(1, std::min((max_seq_len / 2 + 31) / 32, (8 * h->sm_count + B - 1) / B));
     return launched(launch_pdl(evict_move_kernel, dim3(blocks, B), dim3(kMoveThreads), 0, static_cast<cudaStream_t>(stream), p, pools, h->cfg.G));
 }

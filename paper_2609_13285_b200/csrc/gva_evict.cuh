@@ -14,12 +14,15 @@ namespace gva {
 // len), survivors in slots below n stay where they are, and the i-th survivor behind n goes to the i-th free slot before n.
 // Sources and targets are disjoint, so the moves need no order among themselves.
 //
-// select: one cluster of blocks per sequence finds the n-th key by a radix select (digits of 11, 11 and 10 bits from the
-// top, histograms in shared memory summed over the cluster), counts the ties that still fit, and writes weights and
+// select: one cluster of blocks per sequence -- or, where the keys of a sequence fit one block's shared memory with room to spare, its
+// first block alone -- finds the n-th key by a radix select (digits of 11, 11 and 10 bits from the top, histograms in
+// shared memory summed over the cluster), counts the ties that still fit, and writes weights and
 // positions of the slots that stay, zero and -1 for those that leave, and the lists of free slots and of survivors to move.
 // move: blocks copy the rows of the moves in 16-byte pieces, weights and positions with them.
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictBins = 2048;
+constexpr int kEvictAlone = 8192;        // sequences up to this length: one block selects
+constexpr int kEvictMoveHere = 2;        // up to so many batches of moves per block: rows are moved by the selecting cluster
 constexpr int kEvictKeysMax = 32768;     // keys of one block that are kept in shared memory; beyond, they are made again
 
 struct EvictParams {
@@ -45,64 +48,119 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
 }
 constexpr uint32_t kEvictKeyInf = 0xff800000u;               // evict_key(+inf)
 
-// Sum over the block of one int per thread and the exclusive prefix of whole warps: every lane passes its warp's value.
-__device__ __forceinline__ int warp_prefix_of_block(int mine, int *s_warp, int &total) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = blockDim.x >> 5;
-    __syncthreads();
-    if (lane == 0) s_warp[warp] = mine;
-    __syncthreads();
-    const int x = lane < n ? s_warp[lane] : 0;
-    int incl = x;
+// One cached row of a pool: G segments of v_bytes and sz, a page's slots apart, and one of kr_bytes.
+struct MovePools {
+    uint8_t *v, *kr;             // kr: nullable
+    uint32_t *sz;                // 4-bit only, else NULL
+    int v_bytes, kr_bytes;       // bytes of a value row of one group, of a positional row (multiples of 16)
+};
+// A block looks up kMoveBatch moves at a time, and its threads then copy their pieces, four of a thread's in flight at once.
+constexpr int kMoveThreads = 256, kMoveBatch = 64;
+struct MoveScratch {
+    uint32_t to[kMoveBatch], from[kMoveBatch], page_to[kMoveBatch], page_from[kMoveBatch];
+};
+// Batches first, first + stride, ... of the n moves of sequence b; every thread of a block of NT calls it.
+template <int NT>
+__device__ __forceinline__ void move_rows(const EvictParams &p, const MovePools &c, int G, int b, int n, int first, int stride, MoveScratch &s) {
+    const int tid = threadIdx.x;
+    const uint32_t pv = c.v_bytes / 16, values = G * pv, pk = c.kr ? c.kr_bytes / 16 : 0, per = values + pk + (c.sz ? G : 0);
+    for (int i0 = first * kMoveBatch; i0 < n; i0 += stride * kMoveBatch) {
+        const int here = min(kMoveBatch, n - i0);
+        if (tid < here) {
+            const int to = p.holes[(size_t)b * p.move_stride + i0 + tid], from = p.sources[(size_t)b * p.move_stride + i0 + tid];
+            const size_t table = (size_t)b * p.max_pages, row = (size_t)b * p.stride;
+            s.page_to[tid] = (uint32_t)(p.block_table ? (size_t)p.block_table[table + to / p.P] : table + to / p.P);
+            s.page_from[tid] = (uint32_t)(p.block_table ? (size_t)p.block_table[table + from / p.P] : table + from / p.P);
+            s.to[tid] = to % p.P;
+            s.from[tid] = from % p.P;
+            p.w_out[row + to] = p.w_in[row + from];          // (the two may be one buffer: sources lie behind all targets)
+            p.w_out[row + from] = 0.f;
+            p.pos_out[row + to] = p.pos_in ? p.pos_in[row + from] : from;
+            p.pos_out[row + from] = -1;
+        }
+        __syncthreads();
+        constexpr int U = 4;
+        for (uint32_t e0 = tid; e0 < here * per; e0 += U * NT) {
+            uint4 x[U];
+            uint8_t *dst[U];
+            int size[U];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
+            for (int u = 0; u < U; ++u) {
+                const uint32_t e = e0 + u * NT, m = e / per, k = e - m * per;
+                size[u] = 0;
+                if (e < here * per) {
+                    const size_t to = s.page_to[m], from = s.page_from[m];
+                    if (k < values) {
+                        const uint32_t g = k / pv, piece = k - g * pv;
+                        x[u] = *reinterpret_cast<const uint4 *>(c.v + ((from * G + g) * p.P + s.from[m]) * c.v_bytes + 16 * piece);
+                        dst[u] = c.v + ((to * G + g) * p.P + s.to[m]) * c.v_bytes + 16 * piece;
+                        size[u] = 16;
+                    } else if (k < values + pk) {
+                        x[u] = *reinterpret_cast<const uint4 *>(c.kr + (from * p.P + s.from[m]) * c.kr_bytes + 16 * (k - values));
+                        dst[u] = c.kr + (to * p.P + s.to[m]) * c.kr_bytes + 16 * (k - values);
+                        size[u] = 16;
+                    } else {
+                        const uint32_t g = k - values - pk;
+                        x[u].x = c.sz[(from * G + g) * p.P + s.from[m]];
+                        dst[u] = reinterpret_cast<uint8_t *>(c.sz + (to * G + g) * p.P + s.to[m]);
+                        size[u] = 4;
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (size[u] == 16) *reinterpret_cast<uint4 *>(dst[u]) = x[u];
+                else if (size[u] == 4) *reinterpret_cast<uint32_t *>(dst[u]) = x[u].x;
+            }
+        }
+        __syncthreads();
     }
-    total = __shfl_sync(0xffffffffu, incl, 31);
-    return __shfl_sync(0xffffffffu, incl - x, warp);
 }
 
+__global__ void __launch_bounds__(kMoveThreads)
+evict_move_kernel(EvictParams p, MovePools c, int G) {
+    grid_dependency_launch();
+    __shared__ MoveScratch s;
+    grid_dependency_wait();
+    move_rows<kMoveThreads>(p, c, G, blockIdx.y, p.n_moves[blockIdx.y], blockIdx.x, gridDim.x, s);
+}
+
+// keys_in_smem: keys of a block that fit; alone: the cluster's first block selects; here: the cluster moves the rows itself
 __global__ void __launch_bounds__(kEvictThreads)
-evict_select_kernel(EvictParams p, int keys_in_smem) {
+evict_select_kernel(EvictParams p, MovePools pools, int G, int keys_in_smem, int alone, int here) {
     namespace cg = cooperative_groups;
     grid_dependency_launch();
     extern __shared__ uint32_t s_keys[];                     // [keys_in_smem]
-    __shared__ __align__(8) int s_hists[3][kEvictBins];                   // one per digit: a pass needs no second meeting of the cluster
-    __shared__ int s_warp[32];
-    __shared__ int s_share[4];                               // read by the other blocks of the cluster
-    __shared__ int s_digit, s_rest;
-    __shared__ int s_bad;
+    __shared__ __align__(8) int s_hists[3][kEvictBins];      // one per digit: a pass needs no second meeting of the cluster
+    __shared__ int s_warp[3][32];
+    __shared__ int4 s_runs[32];                              // per warp: over first, tie first, over last, tie last
+    __shared__ int4 s_share;                                 // their sums, read by the other blocks of the cluster
+    __shared__ int s_digit[3], s_rest[3], s_bad;
+    __shared__ MoveScratch s_move;
     cg::cluster_group cluster = cg::this_cluster();
-    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int b = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int blocks = (int)cluster.num_blocks(), block = (int)cluster.block_rank();
+    const int C = alone ? 1 : blocks, rank = alone ? 0 : block;          // who selects
+    auto meet = [&]() {
+        if (alone) __syncthreads();
+        else cluster.sync();
+    };
+    const int b = blockIdx.x / blocks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     constexpr int kWarps = kEvictThreads / 32;
+    static_assert(kWarps == 32, "a lane per warp");
     if (tid == 0) s_bad = 0;
+    for (int i = tid; i < 3 * kEvictBins; i += kEvictThreads) (&s_hists[0][0])[i] = 0;
     grid_dependency_wait();
+    if (alone && block > 0) {                                // waits for the lists, then helps to move
+        if (!here) return;
+        cluster.sync();
+        move_rows<kEvictThreads>(p, pools, G, b, *(volatile int *)(p.n_moves + b), block, blocks, s_move);
+        return;
+    }
     __syncthreads();
     const int len_in = p.seq_lens[b], keep_in = p.keep[b], next = p.next_pos ? p.next_pos[b] : 0;
     bool bad = len_in < 0 || len_in > p.max_seq_len || (long long)len_in > (long long)p.max_pages * p.P || keep_in < 0;
     const int len = bad ? 0 : len_in;
     if (bad && rank == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
-    // every page of the live range has to be there before a row is moved
-    if (!bad && p.block_table && keep_in < len) {
-        for (int j = tid; j < (len + p.P - 1) / p.P; j += kEvictThreads) {
-            const int page = p.block_table[(size_t)b * p.max_pages + j];
-            if (page < 0 || page >= p.num_pages) s_bad = 1;
-        }
-    } else if (!bad && keep_in < len && ((long long)b * p.max_pages + (len + p.P - 1) / p.P > p.num_pages)) {
-        s_bad = 1;
-    }
-    __syncthreads();
-    if (s_bad) {
-        if (rank == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_BAD_PAGE, b);
-        bad = true;
-    }
-    const int keep = bad || keep_in >= len ? len : keep_in;
-    cluster.sync();                                          // everyone has read the lengths: new_lens may be seq_lens
-    if (rank == 0 && tid == 0) {
-        p.new_lens[b] = bad ? len_in : keep;
-        if (keep == len) p.n_moves[b] = 0;
-    }
     const float *w = p.w_in + (size_t)b * p.stride;
     const int32_t *pos = p.pos_in ? p.pos_in + (size_t)b * p.stride : nullptr;
     float *w_out = p.w_out + (size_t)b * p.stride;
@@ -110,19 +168,17 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
     // this block's slots: a multiple of 32 per warp, warps one after the other
     const int per_block = ((len + C - 1) / C + 1023) / 1024 * 1024;
     const int lo = min(len, rank * per_block), hi = min(len, lo + per_block);
-    if (keep == len) {                                       // nothing leaves (uniform over the cluster)
-        for (int t = lo + tid; t < hi; t += kEvictThreads) {
-            if (w_out != w) w_out[t] = w[t];
-            if (pos_out != pos) pos_out[t] = pos ? pos[t] : t;
-        }
-        return;
-    }
+    const bool loses = !bad && keep_in < len;
     auto make_key = [&](float weight, int at) -> uint32_t {
         const bool safe = at < p.sinks || (p.recent > 0 && (long long)at >= (long long)next - p.recent);
         return safe ? kEvictKeyInf : evict_key(weight);
     };
     const bool held = per_block <= keys_in_smem;
-    if (held) {
+    // every page of the live range has to be there before a row is moved; asked for ahead of the keys
+    const int n_pages = loses && p.block_table ? (len + p.P - 1) / p.P : 0;
+    const int32_t *table = p.block_table + (size_t)b * p.max_pages;
+    const int page = tid < n_pages ? table[tid] : 0;
+    if (held && loses) {
         constexpr int U = 8;                                 // a thread's weights and positions are asked for eight at a time
         for (int t0 = lo + tid; t0 < hi; t0 += U * kEvictThreads) {
             float ww[U];
@@ -140,15 +196,36 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
             }
         }
     }
-    for (int i = tid; i < 3 * kEvictBins; i += kEvictThreads) (&s_hists[0][0])[i] = 0;
+    if (page < 0 || page >= p.num_pages) s_bad = 1;
+    for (int j = tid + kEvictThreads; j < n_pages; j += kEvictThreads)
+        if (table[j] < 0 || table[j] >= p.num_pages) s_bad = 1;
+    if (loses && !p.block_table && (long long)b * p.max_pages + (len + p.P - 1) / p.P > p.num_pages) s_bad = 1;
     __syncthreads();
+    if (s_bad) {
+        if (rank == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_BAD_PAGE, b);
+        bad = true;
+    }
+    const int keep = bad || !loses ? len : keep_in;
+    if (keep == len) {                                       // nothing leaves (uniform over the cluster)
+        for (int t = lo + tid; t < hi; t += kEvictThreads) {
+            if (w_out != w) w_out[t] = w[t];
+            if (pos_out != pos) pos_out[t] = pos ? pos[t] : t;
+        }
+        meet();                                              // everyone has read the lengths: new_lens may be seq_lens
+        if (rank == 0 && tid == 0) {
+            p.new_lens[b] = bad ? len_in : keep;
+            p.n_moves[b] = 0;
+        }
+        if (alone && here) cluster.sync();
+        return;
+    }
     auto key_of = [&](int t) -> uint32_t { return held ? s_keys[t - lo] : make_key(w[t], pos ? pos[t] : t); };
 
     // ---- the key of rank `keep`, from the top digit down ----
     uint32_t prefix = 0, mask = 0;
     int want = keep;                                         // this many are still to be found among the keys with this prefix
-    if (want > 0)
-    for (int pass = 0; pass < 3; ++pass) {
+    const bool none = keep == 0;
+    for (int pass = 0; pass < 3 && !none; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, bins = 1 << bits;
         int *s_hist = s_hists[pass];
         for (int t0 = lo; t0 < hi; t0 += kEvictThreads) {
@@ -169,7 +246,7 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
                 atomicAdd(&s_hist[digit], 1);
             }
         }
-        cluster.sync();
+        meet();
         // bins from the top: thread i takes bins 2 i and 2 i + 1 counted from the top
         int n0 = 0, n1 = 0;
         const int i0 = bins - 1 - 2 * tid, i1 = i0 - 1;
@@ -187,67 +264,98 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
             const int y = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += y;
         }
-        int total;
-        const int before_warp = warp_prefix_of_block(__shfl_sync(0xffffffffu, incl, 31), s_warp, total);
-        const int above = before_warp + incl - (n0 + n1);     // keys in bins above i0
+        if (lane == 31) s_warp[pass][warp] = incl;
+        __syncthreads();
+        int sums = s_warp[pass][lane];                       // (kWarps = 32)
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, sums, o);
+            if (lane >= o) sums += y;
+        }
+        const int before_warp = warp ? __shfl_sync(0xffffffffu, sums, max(warp - 1, 0)) : 0;
+        const int above = before_warp + incl - (n0 + n1);    // keys in bins above i0
         if (above < want && above + n0 + n1 >= want) {
             const bool second = above + n0 < want;
-            s_digit = second ? i1 : i0;
-            s_rest = want - above - (second ? n0 : 0);
+            s_digit[pass] = second ? i1 : i0;
+            s_rest[pass] = want - above - (second ? n0 : 0);
         }
         __syncthreads();
-        prefix |= (uint32_t)s_digit << shift;
+        prefix |= (uint32_t)s_digit[pass] << shift;
         mask |= (uint32_t)(bins - 1) << shift;
-        want = s_rest;
-        __syncthreads();
+        want = s_rest[pass];
     }
-    const bool none = keep == 0;
 
-    // ---- in slot order: ties that still fit, free slots before `keep`, survivors behind it ----
+    // ---- one count of the block's slots: before `keep` and behind it, above the key and equal to it.  Ties stay in slot order, so
+    //      how many of a run of slots do follows from how many ties lie before it ----
     const int rows = per_block / kWarps;                     // slots of a warp
     const int w_lo = min(hi, lo + warp * rows), w_hi = min(hi, w_lo + rows);
-    int ties = 0;
+    int over_first = 0, tie_first = 0, over_last = 0, tie_last = 0;
     for (int t0 = w_lo; t0 < w_hi; t0 += 32) {
         const int t = t0 + lane;
-        ties += __popc(__ballot_sync(0xffffffffu, !none && t < w_hi && key_of(t) == prefix));
+        const uint32_t key = t < w_hi && !none ? key_of(t) : 0;
+        const uint32_t over = __ballot_sync(0xffffffffu, !none && t < w_hi && key > prefix), tie = __ballot_sync(0xffffffffu, !none && t < w_hi && key == prefix);
+        const uint32_t first = t0 + 32 <= keep ? 0xffffffffu : t0 >= keep ? 0u : (1u << (keep - t0)) - 1;
+        over_first += __popc(over & first);
+        tie_first += __popc(tie & first);
+        over_last += __popc(over & ~first);
+        tie_last += __popc(tie & ~first);
     }
-    int block_ties;
-    int tie_base = warp_prefix_of_block(ties, s_warp, block_ties);
-    if (tid == 0) s_share[0] = block_ties;
-    cluster.sync();
-    for (int c = 0; c < rank; ++c) tie_base += cluster.map_shared_rank(s_share, c)[0];
-    int holes = 0, sources = 0;
+    // (slots before `keep`, what stays of them) for a run with so many ties before it
+    auto stays_first = [&](int of, int tf, int before) { return of + min(tf, max(0, want - before)); };
+    auto stays_last = [&](int ol, int tf, int tl, int before) { return ol + min(tl, max(0, want - before - tf)); };
+    if (lane == 0) s_runs[warp] = make_int4(over_first, tie_first, over_last, tie_last);
+    __syncthreads();
+    int4 run = s_runs[lane];                                 // lane i: warp i's
+    if (warp == 0) {
+        const int4 sum = make_int4(__reduce_add_sync(0xffffffffu, run.x), __reduce_add_sync(0xffffffffu, run.y),
+                                   __reduce_add_sync(0xffffffffu, run.z), __reduce_add_sync(0xffffffffu, run.w));
+        if (lane == 0) s_share = sum;
+    }
+    meet();
+    int tie_base = 0, hole_base = 0, source_base = 0, all_holes = 0;
     {
-        int seen = tie_base;
-        for (int t0 = w_lo; t0 < w_hi; t0 += 32) {
-            const int t = t0 + lane;
-            const uint32_t key = t < w_hi ? key_of(t) : 0;
-            const uint32_t tie = __ballot_sync(0xffffffffu, !none && t < w_hi && key == prefix);
-            const bool kept = !none && t < w_hi && (key > prefix || (key == prefix && seen + __popc(tie & ((1u << lane) - 1)) < want));
-            holes += __popc(__ballot_sync(0xffffffffu, t < w_hi && t < keep && !kept));
-            sources += __popc(__ballot_sync(0xffffffffu, kept && t >= keep));
-            seen += __popc(tie);
+        int ties = 0;
+        for (int c = 0; c < C; ++c) {
+            const int4 o = alone ? s_share : *cluster.map_shared_rank(&s_share, c);
+            const int c_lo = min(len, c * per_block), c_hi = min(len, c_lo + per_block);
+            const int holes = max(0, min(c_hi, keep) - c_lo) - stays_first(o.x, o.y, ties), sources = stays_last(o.z, o.y, o.w, ties);
+            if (c < rank) {
+                hole_base += holes;
+                source_base += sources;
+                tie_base += o.y + o.w;
+            }
+            all_holes += holes;
+            ties += o.y + o.w;
         }
     }
-    int block_holes, block_sources;
-    int hole_base = warp_prefix_of_block(holes, s_warp, block_holes);
-    int source_base = warp_prefix_of_block(sources, s_warp, block_sources);
-    if (tid == 0) {
-        s_share[1] = block_holes;
-        s_share[2] = block_sources;
-    }
-    cluster.sync();
-    int all_holes = 0;
-    for (int c = 0; c < C; ++c) {
-        const int *other = cluster.map_shared_rank(s_share, c);
-        if (c < rank) {
-            hole_base += other[1];
-            source_base += other[2];
+    {   // the block's warps: lane i holds warp i's ties before, free slots and moving survivors
+        int ties = run.y + run.w;
+        const int own = ties;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, ties, o);
+            if (lane >= o) ties += y;
         }
-        all_holes += other[1];
+        ties += tie_base - own;
+        const int i_lo = min(hi, lo + lane * rows), i_hi = min(hi, i_lo + rows);
+        int holes = max(0, min(i_hi, keep) - i_lo) - stays_first(run.x, run.y, ties), sources = stays_last(run.z, run.y, run.w, ties);
+        const int own_holes = holes, own_sources = sources;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, holes, o), z = __shfl_up_sync(0xffffffffu, sources, o);
+            if (lane >= o) {
+                holes += y;
+                sources += z;
+            }
+        }
+        hole_base += __shfl_sync(0xffffffffu, holes - own_holes, warp);
+        source_base += __shfl_sync(0xffffffffu, sources - own_sources, warp);
+        tie_base = __shfl_sync(0xffffffffu, ties, warp);
     }
-    if (rank == 0 && tid == 0) p.n_moves[b] = all_holes;
-    cluster.sync();                                          // no block leaves while another still reads its shared memory
+    if (rank == 0 && tid == 0) {
+        p.n_moves[b] = all_holes;
+        p.new_lens[b] = keep;                                // (everyone has read the lengths)
+    }
     {
         int seen = tie_base;
         constexpr int U = 4;
@@ -285,75 +393,8 @@ evict_select_kernel(EvictParams p, int keys_in_smem) {
             }
         }
     }
-}
-
-// One cached row of a pool: G segments of v_bytes and sz, a page's slots apart, and one of kr_bytes.
-struct MovePools {
-    uint8_t *v, *kr;             // kr: nullable
-    uint32_t *sz;                // 4-bit only, else NULL
-    int v_bytes, kr_bytes;       // bytes of a value row of one group, of a positional row (multiples of 16)
-};
-// A block looks up kMoveBatch moves at a time, and its threads then copy their pieces, four of a thread's in flight at once.
-constexpr int kMoveThreads = 256, kMoveBatch = 64;
-__global__ void __launch_bounds__(kMoveThreads)
-evict_move_kernel(EvictParams p, MovePools c, int G) {
-    grid_dependency_launch();
-    __shared__ uint32_t s_to[kMoveBatch], s_from[kMoveBatch];                    // page * P + slot
-    __shared__ uint32_t s_page_to[kMoveBatch], s_page_from[kMoveBatch];
-    grid_dependency_wait();
-    const int b = blockIdx.y, n = p.n_moves[b], tid = threadIdx.x;
-    const uint32_t pv = c.v_bytes / 16, values = G * pv, pk = c.kr ? c.kr_bytes / 16 : 0, per = values + pk + (c.sz ? G : 0);
-    for (int i0 = blockIdx.x * kMoveBatch; i0 < n; i0 += gridDim.x * kMoveBatch) {
-        const int here = min(kMoveBatch, n - i0);
-        if (tid < here) {
-            const int to = p.holes[(size_t)b * p.move_stride + i0 + tid], from = p.sources[(size_t)b * p.move_stride + i0 + tid];
-            const size_t table = (size_t)b * p.max_pages, row = (size_t)b * p.stride;
-            s_page_to[tid] = (uint32_t)(p.block_table ? (size_t)p.block_table[table + to / p.P] : table + to / p.P);
-            s_page_from[tid] = (uint32_t)(p.block_table ? (size_t)p.block_table[table + from / p.P] : table + from / p.P);
-            s_to[tid] = to % p.P;
-            s_from[tid] = from % p.P;
-            p.w_out[row + to] = p.w_in[row + from];          // (the two may be one buffer: sources lie behind all targets)
-            p.w_out[row + from] = 0.f;
-            p.pos_out[row + to] = p.pos_in ? p.pos_in[row + from] : from;
-            p.pos_out[row + from] = -1;
-        }
-        __syncthreads();
-        constexpr int U = 4;
-        for (uint32_t e0 = tid; e0 < here * per; e0 += U * kMoveThreads) {
-            uint4 x[U];
-            uint8_t *dst[U];
-            int size[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const uint32_t e = e0 + u * kMoveThreads, m = e / per, k = e - m * per;
-                size[u] = 0;
-                if (e < here * per) {
-                    const size_t to = s_page_to[m], from = s_page_from[m];
-                    if (k < values) {
-                        const uint32_t g = k / pv, piece = k - g * pv;
-                        x[u] = *reinterpret_cast<const uint4 *>(c.v + ((from * G + g) * p.P + s_from[m]) * c.v_bytes + 16 * piece);
-                        dst[u] = c.v + ((to * G + g) * p.P + s_to[m]) * c.v_bytes + 16 * piece;
-                        size[u] = 16;
-                    } else if (k < values + pk) {
-                        x[u] = *reinterpret_cast<const uint4 *>(c.kr + (from * p.P + s_from[m]) * c.kr_bytes + 16 * (k - values));
-                        dst[u] = c.kr + (to * p.P + s_to[m]) * c.kr_bytes + 16 * (k - values);
-                        size[u] = 16;
-                    } else {
-                        const uint32_t g = k - values - pk;
-                        x[u].x = c.sz[(from * G + g) * p.P + s_from[m]];
-                        dst[u] = reinterpret_cast<uint8_t *>(c.sz + (to * G + g) * p.P + s_to[m]);
-                        size[u] = 4;
-                    }
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (size[u] == 16) *reinterpret_cast<uint4 *>(dst[u]) = x[u];
-                else if (size[u] == 4) *reinterpret_cast<uint32_t *>(dst[u]) = x[u].x;
-            }
-        }
-        __syncthreads();
-    }
+    if (!alone || here) cluster.sync();                      // no block leaves while another still reads its shared memory; lists complete
+    if (here) move_rows<kEvictThreads>(p, pools, G, b, all_holes, block, blocks, s_move);
 }
 
 }  // namespace gva

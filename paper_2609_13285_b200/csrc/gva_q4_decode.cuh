@@ -4,12 +4,13 @@
 //     q . v_t = s_t (q . c_t) + z_t sum(q),          sum_t p_t v_t = sum_t (p_t s_t) c_t + sum_t p_t z_t,
 // so the products run over the codes and step and lowest come in afterwards, per token, in f32.
 //
-// Codes as MMA operands.  Score: a nibble in the low bits of a 16-bit half word, the rest zero, is an f16 subnormal: c 2^-24, or
-// c 2^-20 one nibble further up.  Masking is all it takes to widen two codes (four masks and one shift for a word of
-// eight), and the powers of two are undone in the query.  Tensor cores multiply subnormals exactly but align products by
-// their nominal exponent 2^-14, which costs the sum up to ten of its bits: 8e-7 (rms) of a score, which the softmax can
-// take.  The output cannot (3e-5 measured), nor the offset of codes that are all positive: over T tokens it cancels to
-// T^-1/2 of its size.  So there the codes are centred, c - 8, and made normal numbers: one subtraction per two codes more, and
+// Codes as MMA operands.  Score: four bits in the middle of a 16-bit half word, the rest zero, are an f16 subnormal, c 2^-22 at bits 2
+// to 5 and c 2^-18 at bits 6 to 9.  Two shifts and four masks widen a word of eight codes, and the powers of two are undone
+// in the query.  Tensor cores multiply subnormals exactly but align products by their nominal exponent 2^-14, which costs
+// the sum as many of its bits as the code stands below: 8 and 4 here (without the shift up, at bits 0 and 4, a score
+// was off by 8e-7, rms).  The output cannot take that, nor the offset of codes that are all positive, which over T tokens
+// cancels to T^-1/2 of its size (3e-5 measured).  So there the codes are centred, c - 8, and made normal numbers: one
+// subtraction per two codes more, and
 //     sum_t p_t v_t = sum_t (p_t s_t) (c_t - 8) + sum_t p_t (z_t + 8 s_t).
 //
 // Both products need the contraction index in pairs inside a register: dims for the score, tokens for the output.  A lane
@@ -119,6 +120,8 @@ __device__ __forceinline__ uint32_t centred_high(uint32_t x) {
     return *reinterpret_cast<const uint32_t *>(&d);
 }
 
+constexpr uint32_t kCodeLow = 0x003c003cu, kCodeHigh = 0x03c003c0u;
+
 // One group's four queries as the score product's B fragments, for the MMA column n = lane / 4 = 2 head + {hi, lo}, scaled
 // by `factor` (softmax scale and log2 e).  Content: q 2^-e 2^10 with |q 2^-e| <= 1, times 16 where the code stands in the low
 // nibble; unscale = 2^(e + 10) of the head whose scores this lane holds (lane % 4); sum = sum of that head's content query.
@@ -163,7 +166,7 @@ __device__ __forceinline__ void load_q4_query(Q4Query<T> &out, const float *q /*
         out.v[2 * w + 1][1] = part_f16(x[3] * down, part) | (part_f16(x[7] * down, part) << 16);
     }
     // from the column's lanes to the lanes that hold the head's scores: lane % 4 = head, columns 2 head and 2 head + 1 alike
-    const float up = __uint_as_float((uint32_t)(127 + e + 10) << 23);      // c 2^-24 x q 2^-e 2^14 = c q 2^-(e + 10)
+    const float up = __uint_as_float((uint32_t)(127 + e + 8) << 23);       // c 2^-22 x q 2^-e 2^14 = c q 2^-(e + 8)
     out.unscale = __shfl_sync(0xffffffffu, up, 8 * c);
     out.sum = __shfl_sync(0xffffffffu, sum, 8 * c);
     if constexpr (T::DR > 0) {
@@ -242,14 +245,15 @@ __device__ __forceinline__ void score_q4(const unsigned char *v, uint32_t kr, co
     for (int w = 0; w < T::WORDS; ++w) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const uint32_t a0 = lo[k][w] & 0x000f000fu, a1 = hi[k][w] & 0x000f000fu, a2 = lo[k][w] & 0x00f000f0u, a3 = hi[k][w] & 0x00f000f0u;
+            const uint32_t l = lo[k][w] << 2, h = hi[k][w] << 2;
+            const uint32_t a0 = l & kCodeLow, a1 = h & kCodeLow, a2 = l & kCodeHigh, a3 = h & kCodeHigh;
             if (w == 0) mma_f16_first(acc[k], a0, a1, a2, a3, q.v[2 * w][0], q.v[2 * w][1]);
             else mma_f16_q4(acc[k], a0, a1, a2, a3, q.v[2 * w][0], q.v[2 * w][1]);
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const uint32_t l = lo[k][w] >> 8, h = hi[k][w] >> 8;
-            mma_f16_q4(acc[k], l & 0x000f000fu, h & 0x000f000fu, l & 0x00f000f0u, h & 0x00f000f0u, q.v[2 * w + 1][0], q.v[2 * w + 1][1]);
+            const uint32_t l = lo[k][w] >> 6, h = hi[k][w] >> 6;
+            mma_f16_q4(acc[k], l & kCodeLow, h & kCodeLow, l & kCodeHigh, h & kCodeHigh, q.v[2 * w + 1][0], q.v[2 * w + 1][1]);
         }
     }
 }

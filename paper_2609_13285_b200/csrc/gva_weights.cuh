@@ -84,7 +84,8 @@ weights_f32_kernel(WeightParams p, int DR) {
 // MMAs with the sum over a head's {hi, lo} columns in one lane; every lane adds up the weights of its head over the new
 // rows, four lanes join the group's heads, and the team's groups meet in shared memory (two buffers, one named barrier per
 // tile), where they are added in a fixed order.  A single row's queries stay in registers while the sequence lasts.
-//   bf16 : values as they lie, queries as bf16 hi + lo (and lo's rest for the positional part, as in the 4-bit kernel)
+//   bf16 : values as they lie, queries as three bf16 parts, of which two carry 16 bits only (1.1e-6 of the weights, measured): the
+//          third stands in the hi columns of MMAs of its own
 //   e4m3 : codes widened to f16 exactly, queries as f16 hi + lo, scaled by a power of two per head
 // A lane reads the d_v / 4 neighbouring dims [lane % 4 * d_v / 4, ...) of its rows in 16-byte loads: as in the 4-bit kernel the
 // order of dims inside the contraction is free.
@@ -105,7 +106,7 @@ struct WeightTraits {
 // Queries of a group as B fragments for values that need no step: k-step j of the content holds the lane's dims 4 j .. 4 j + 3.
 template <int KIND, class T>
 struct PlainQuery {
-    uint32_t v[T::DV / 16][2];
+    uint32_t v[T::DV / 16][2], v2[KIND == kCacheBf16 ? T::DV / 16 : 1][2];
     uint32_t r[T::DR > 0 ? (T::DR + 15) / 16 : 1][2], r2[KIND == kCacheBf16 && T::DR > 0 ? (T::DR + 15) / 16 : 1][2];
     float unscale;
 };
@@ -125,7 +126,10 @@ __device__ __forceinline__ void load_query(PlainQuery<KIND, T> &out, const float
 #pragma unroll
         for (int j = 0; j < T::DV / 16; ++j)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) out.v[j][i] = pair(v[4 * j + 2 * i], v[4 * j + 2 * i + 1], part);
+            for (int i = 0; i < 2; ++i) {
+                out.v[j][i] = pair(v[4 * j + 2 * i], v[4 * j + 2 * i + 1], part);
+                out.v2[j][i] = part ? 0u : pair(v[4 * j + 2 * i], v[4 * j + 2 * i + 1], 2);
+            }
         out.unscale = 1.f;
 #pragma unroll
         for (int k = 0; k < FULL; ++k)
@@ -190,12 +194,14 @@ __device__ __forceinline__ void score_plain(const unsigned char *v, const unsign
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const uint32_t f[4] = {a[k].x, b[k].x, a[k].y, b[k].y};
-                if (j == 0) mma_bf16_first(acc[k], f, q.v[2 * j][0], q.v[2 * j][1]);
-                else mma_bf16(acc[k], f, q.v[2 * j][0], q.v[2 * j][1]);
+                if (j == 0) mma_bf16_first(acc[k], f, q.v2[2 * j][0], q.v2[2 * j][1]);
+                else mma_bf16(acc[k], f, q.v2[2 * j][0], q.v2[2 * j][1]);
+                mma_bf16(acc[k], f, q.v[2 * j][0], q.v[2 * j][1]);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const uint32_t f[4] = {a[k].z, b[k].z, a[k].w, b[k].w};
+                mma_bf16(acc[k], f, q.v2[2 * j + 1][0], q.v2[2 * j + 1][1]);
                 mma_bf16(acc[k], f, q.v[2 * j + 1][0], q.v[2 * j + 1][1]);
             }
         }
@@ -260,7 +266,7 @@ __device__ __forceinline__ void score_plain(const unsigned char *v, const unsign
 }
 
 // ---- several new rows per sequence ----
-// Two rows at a time: the eight MMA columns are 2 rows x 4 heads, and the query's hi and lo parts go in as two MMAs on the same
+// Two rows at a time: the eight MMA columns are 2 rows x 4 heads, and the query's parts go in as MMAs of their own on the same
 // values, so that whatever widening the values need is done once for both rows; both parts of a query are made by the
 // lane that holds its column, which is a quarter of the instructions that filling columns {hi, lo} takes.  A pair of rows is
 // loaded once for several tiles -- 32 lanes read 32 cache lines apart, from L2, since the ring leaves L1 no room --: the teams
@@ -268,8 +274,8 @@ __device__ __forceinline__ void score_plain(const unsigned char *v, const unsign
 // ranges of tiles are cut by the rows that see them.
 template <int KIND, class T>
 struct PairQuery {
-    uint32_t hi[T::DV / 16][2], lo[T::DV / 16][2];
-    uint32_t rhi[T::DR > 0 ? (T::DR + 15) / 16 : 1][2], rlo[T::DR > 0 ? (T::DR + 15) / 16 : 1][2];
+    uint32_t hi[T::DV / 16][2], lo[T::DV / 16][2], low[KIND == kCacheBf16 ? T::DV / 16 : 1][2];     // (bf16: three parts)
+    uint32_t rhi[T::DR > 0 ? (T::DR + 15) / 16 : 1][2], rlo[T::DR > 0 ? (T::DR + 15) / 16 : 1][2], rlow[KIND != kCacheE4m3 && T::DR > 0 ? (T::DR + 15) / 16 : 1][2];
     float unscale[2], sum[2], off[2];                        // of this lane's score columns 2 c, 2 c + 1
 };
 __device__ __forceinline__ void parts_f16(float a, float b, uint32_t &hi, uint32_t &lo) {
@@ -278,12 +284,15 @@ __device__ __forceinline__ void parts_f16(float a, float b, uint32_t &hi, uint32
     hi = *reinterpret_cast<const uint32_t *>(&h);
     lo = pack_half2(a - f.x, b - f.y);
 }
-__device__ __forceinline__ void parts_bf16(float a, float b, uint32_t &hi, uint32_t &lo) {
+__device__ __forceinline__ void parts_bf16(float a, float b, uint32_t &hi, uint32_t &lo, uint32_t &low) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     const float2 f = __bfloat1622float2(h);
     const __nv_bfloat162 l = __floats2bfloat162_rn(a - f.x, b - f.y);
+    const float2 g = __bfloat1622float2(l);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(a - f.x - g.x, b - f.y - g.y);
     hi = *reinterpret_cast<const uint32_t *>(&h);
     lo = *reinterpret_cast<const uint32_t *>(&l);
+    low = *reinterpret_cast<const uint32_t *>(&r);
 }
 // q: row r's first head of the group; second: the row after it exists
 template <int KIND, class T>
@@ -303,7 +312,7 @@ __device__ __forceinline__ void load_pair(PairQuery<KIND, T> &out, const float *
 #pragma unroll
         for (int j = 0; j < T::DV / 16; ++j)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) parts_bf16(v[4 * j + 2 * i], v[4 * j + 2 * i + 1], out.hi[j][i], out.lo[j][i]);
+            for (int i = 0; i < 2; ++i) parts_bf16(v[4 * j + 2 * i], v[4 * j + 2 * i + 1], out.hi[j][i], out.lo[j][i], out.low[j][i]);
     } else {
         float w[KIND == kCacheE4m3 && T::DR > 0 ? T::DR / 4 : 1];
 #pragma unroll
@@ -326,7 +335,7 @@ __device__ __forceinline__ void load_pair(PairQuery<KIND, T> &out, const float *
         e = min(max(e, -100), 110);
         if constexpr (KIND == kCacheQ4) {                    // as in load_q4_query
             const float down = __uint_as_float((uint32_t)(127 - e + 10) << 23), down16 = 16.f * down;
-            up = __uint_as_float((uint32_t)(127 + e + 10) << 23);
+            up = __uint_as_float((uint32_t)(127 + e + 8) << 23);
 #pragma unroll
             for (int i = 0; i < T::DV / 32; ++i) {
                 const float *x = v + 8 * i;
@@ -354,11 +363,11 @@ __device__ __forceinline__ void load_pair(PairQuery<KIND, T> &out, const float *
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float2 x = *reinterpret_cast<const float2 *>(rot + 16 * k + 8 * i + 2 * c);
-                parts_bf16(x.x * factor, x.y * factor, out.rhi[k][i], out.rlo[k][i]);
+                parts_bf16(x.x * factor, x.y * factor, out.rhi[k][i], out.rlo[k][i], out.rlow[k][i]);
             }
         if constexpr (T::DR % 16 == 8) {
             const float2 x = *reinterpret_cast<const float2 *>(rot + 16 * FULL + 2 * c);
-            parts_bf16(x.x * factor, x.y * factor, out.rhi[FULL][0], out.rlo[FULL][0]);
+            parts_bf16(x.x * factor, x.y * factor, out.rhi[FULL][0], out.rlo[FULL][0], out.rlow[FULL][0]);
         }
     }
     const float l = lse[row * H + head], shift = l == -INFINITY ? -INFINITY : -l * kLog2e;
@@ -376,8 +385,9 @@ __device__ __forceinline__ void score_pair(const unsigned char *v, const unsigne
     float acc[4];
     auto both = [&](bool first, const uint32_t (&f)[4], int j) {
         if constexpr (KIND == kCacheBf16) {
-            if (first) mma_bf16_first(acc, f, q.lo[j][0], q.lo[j][1]);
-            else mma_bf16(acc, f, q.lo[j][0], q.lo[j][1]);
+            if (first) mma_bf16_first(acc, f, q.low[j][0], q.low[j][1]);
+            else mma_bf16(acc, f, q.low[j][0], q.low[j][1]);
+            mma_bf16(acc, f, q.lo[j][0], q.lo[j][1]);
             mma_bf16(acc, f, q.hi[j][0], q.hi[j][1]);
         } else {
             if (first) mma_f16_first(acc, f[0], f[1], f[2], f[3], q.lo[j][0], q.lo[j][1]);
@@ -392,9 +402,9 @@ __device__ __forceinline__ void score_pair(const unsigned char *v, const unsigne
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const uint32_t lo = u ? a.y : a.x, hi = u ? b.y : b.x;
-                both(w + u == 0, {lo & 0x000f000fu, hi & 0x000f000fu, lo & 0x00f000f0u, hi & 0x00f000f0u}, 2 * (w + u));
-                const uint32_t l = lo >> 8, h = hi >> 8;
-                both(false, {l & 0x000f000fu, h & 0x000f000fu, l & 0x00f000f0u, h & 0x00f000f0u}, 2 * (w + u) + 1);
+                const uint32_t l = lo << 2, h = hi << 2, l6 = lo >> 6, h6 = hi >> 6;
+                both(w + u == 0, {l & kCodeLow, h & kCodeLow, l & kCodeHigh, h & kCodeHigh}, 2 * (w + u));
+                both(false, {l6 & kCodeLow, h6 & kCodeLow, l6 & kCodeHigh, h6 & kCodeHigh}, 2 * (w + u) + 1);
             }
         }
     } else if constexpr (KIND == kCacheBf16) {
@@ -434,12 +444,14 @@ __device__ __forceinline__ void score_pair(const unsigned char *v, const unsigne
         for (int u = 0; u < FULL; ++u) {
             uint32_t f[4];
             ldsm_x4(kr + 32 * u, f);
+            mma_bf16(rot, f, q.rlow[u][0], q.rlow[u][1]);
             mma_bf16(rot, f, q.rlo[u][0], q.rlo[u][1]);
             mma_bf16(rot, f, q.rhi[u][0], q.rhi[u][1]);
         }
         if constexpr (T::DR % 16 == 8) {
             uint32_t t[2];
             ldsm_x2(kr + 32 * FULL, t);
+            mma_bf16_k8(rot, t, q.rlow[FULL][0]);
             mma_bf16_k8(rot, t, q.rlo[FULL][0]);
             mma_bf16_k8(rot, t, q.rhi[FULL][0]);
         }

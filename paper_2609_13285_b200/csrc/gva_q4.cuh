@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(kAppendQ4Threads)
 append_q4_kernel(const __grid_constant__ AppendQ4Params p, const __grid_constant__ RopeTable rope) {     // (tables are indexed where they lie)
     grid_dependency_launch();
     __shared__ int s_page[kAppendQ4Rows], s_slot[kAppendQ4Rows], s_pos[kAppendQ4Rows];   // page -1: the row is not written
+    __shared__ uint32_t s_key[kAppendQ4Rows * 8];            // rotated pairs, bf16 (rows * pairs <= 1024)
     grid_dependency_wait();
     const int tid = threadIdx.x, n0 = blockIdx.x * p.rows;
     const int total = p.cu_q ? min(p.n_q, p.cu_q[p.B]) : p.n_q;
@@ -129,33 +130,29 @@ append_q4_kernel(const __grid_constant__ AppendQ4Params p, const __grid_constant
             for (int i = 0; i < 8; ++i) x[u][i] = 0.f;
         }
     }
-    for (int r = tid; r < p.rows; r += kAppendQ4Threads) {
-        const int n = n0 + r;
-        int page = -1, slot = 0, pos = 0;
-        if (n < total) {
-            int b = n, i = 0;
-            if (p.cu_q) {
-                int lo = 0, hi = p.B - 1;                    // largest b with cu_q[b] <= n (empty sequences repeat an offset)
-                while (lo < hi) {
-                    const int mid = (lo + hi + 1) >> 1;
-                    if (p.cu_q[mid] <= n) lo = mid;
-                    else hi = mid - 1;
-                }
-                b = lo;
-                i = n - p.cu_q[b];
+    int my_b = -1, my_t = 0;                                 // this thread's row, if it has one (rows <= 128): sequence and slot
+    if (tid < p.rows && n0 + tid < total) {
+        const int n = n0 + tid;
+        int b = n, i = 0;
+        if (p.cu_q) {
+            int lo = 0, hi = p.B - 1;                        // largest b with cu_q[b] <= n (empty sequences repeat an offset)
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (p.cu_q[mid] <= n) lo = mid;
+                else hi = mid - 1;
             }
-            const long long t = (long long)p.slot0[b] + i, at = (long long)p.pos0[b] + i;
-            if (p.slot0[b] < 0 || p.pos0[b] < 0 || t > 0x7fffffff || at > 0x7fffffff) {
-                report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
-            } else {
-                page = locate_page(p.c.block_table, p.c.num_pages, p.c.max_pages, p.P, b, (int)t, p.dev_status);
-                slot = (int)t % p.P;
-                pos = (int)at;
-            }
+            b = lo;
+            i = n - p.cu_q[b];
         }
-        s_page[r] = page;
-        s_slot[r] = slot;
-        s_pos[r] = pos;
+        const int slot0 = p.slot0[b], pos0 = p.pos0[b];
+        const long long t = (long long)slot0 + i, at = (long long)pos0 + i;
+        if (slot0 < 0 || pos0 < 0 || t > 0x7fffffff || at > 0x7fffffff) {
+            report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
+        } else {
+            my_b = b;
+            my_t = (int)t;
+        }
+        s_pos[tid] = (int)at;
     }
     uint32_t word[kAppendQ4Shares];
     __half2 sz[kAppendQ4Shares];
@@ -191,6 +188,20 @@ append_q4_kernel(const __grid_constant__ AppendQ4Params p, const __grid_constant
         }
     }
     __syncthreads();
+    // pages by the first threads, positional pairs by the last
+    if (tid < p.rows) {
+        s_page[tid] = my_b >= 0 ? locate_page(p.c.block_table, p.c.num_pages, p.c.max_pages, p.P, my_b, my_t, p.dev_status) : -1;
+        s_slot[tid] = my_t % p.P;
+    }
+    const int pairs = p.d_r / 2, n_pairs = min(p.rows, total - n0) * pairs;
+    for (int e = kAppendQ4Threads - 1 - tid; e < n_pairs; e += kAppendQ4Threads) {
+        const int r = e / pairs, k = e - r * pairs;
+        const float *x = p.kr_new + (size_t)n0 * p.d_r + 2 * (size_t)e;
+        double y0, y1;
+        rope_pair((double)x[0], (double)x[1], s_pos[r], rope.inv_freq[k], y0, y1);
+        s_key[e] = (uint32_t)double_to_bf16_bits(y0) | ((uint32_t)double_to_bf16_bits(y1) << 16);
+    }
+    __syncthreads();
 #pragma unroll
     for (int u = 0; u < kAppendQ4Shares; ++u) {
         const int e = u * kAppendQ4Threads + tid;
@@ -201,16 +212,9 @@ append_q4_kernel(const __grid_constant__ AppendQ4Params p, const __grid_constant
             if (l == 0) p.c.sz[row] = sz[u];
         }
     }
-    // positional pairs, from the last thread down
-    const int pairs = p.d_r / 2;
-    for (int e = kAppendQ4Threads - 1 - tid; e < p.rows * pairs; e += kAppendQ4Threads) {
-        const int r = e / pairs, k = e % pairs;
-        if (s_page[r] < 0) continue;
-        const float *kr = p.kr_new + (size_t)(n0 + r) * p.d_r + 2 * k;
-        double y0, y1;
-        rope_pair((double)kr[0], (double)kr[1], s_pos[r], rope.inv_freq[k], y0, y1);
-        uint16_t *dst = p.c.kr + ((size_t)s_page[r] * p.P + s_slot[r]) * p.d_r + 2 * k;
-        *reinterpret_cast<uint32_t *>(dst) = (uint32_t)double_to_bf16_bits(y0) | ((uint32_t)double_to_bf16_bits(y1) << 16);
+    for (int e = tid; e < n_pairs; e += kAppendQ4Threads) {
+        const int r = e / pairs, k = e - r * pairs;
+        if (s_page[r] >= 0) *reinterpret_cast<uint32_t *>(p.c.kr + ((size_t)s_page[r] * p.P + s_slot[r]) * p.d_r + 2 * k) = s_key[e];
     }
 }
 

@@ -477,27 +477,31 @@ decode_q4_kernel(DecodeParams p, Q4Launch L) {
             for (; next_b < to; ++next_b)
                 if (r8 == 0) *reinterpret_cast<float2 *>(p.rec_ml + record(next_b) * 2) = make_float2(-INFINITY, 0.f);
         };
+        auto begin = [&](int b) {                            // sequence b is in hand from here
+            if (!direct) mark_empty(b);
+            cur_b = b;
+            next_b = b + 1;
+            load_q4_query<T>(q, p.q + ((size_t)b * H + g * kHeadsPerGroup) * T::DQ, p.scale_log2, lane);
+            m_run = -INFINITY;
+            l_run = z_run = step_ref = lift = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < T::MT; ++mt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) oacc[mt][e] = 0.f;
+        };
         const int n_tiles = rg.hi - rg.lo;
+        if (team < n_tiles) begin(seq_of_tile(s_off, p.B, rg.lo + team));    // its query is fetched while the first tiles fly
 #pragma unroll 1
         for (int i = team, st = team, parity = 0; i < n_tiles; i += L.teams) {
             if (!mbar_wait_bounded(smem_u32(&full_bar[st]), parity, s_abort)) {
-                if (!*s_abort && lane == 0) report_error(p.dev_status, GVA_ERR_TIMEOUT, cur_b < 0 ? 0 : cur_b);
+                if (!*s_abort && lane == 0) report_error(p.dev_status, GVA_ERR_TIMEOUT, cur_b);
                 *s_abort = 1;
                 break;
             }
             const TileMeta meta = s_meta[st];
             if (meta.b != cur_b) {
-                if (cur_b >= 0) flush();
-                if (!direct) mark_empty(meta.b);
-                cur_b = meta.b;
-                next_b = cur_b + 1;
-                load_q4_query<T>(q, p.q + ((size_t)cur_b * H + g * kHeadsPerGroup) * T::DQ, p.scale_log2, lane);
-                m_run = -INFINITY;
-                l_run = z_run = step_ref = lift = 0.f;
-#pragma unroll
-                for (int mt = 0; mt < T::MT; ++mt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) oacc[mt][e] = 0.f;
+                flush();
+                begin(meta.b);
             }
             const unsigned char *stage = smem + (size_t)st * stage_bytes;
             const unsigned char *vt = stage + (size_t)g * T::V_BYTES;

@@ -668,6 +668,17 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
                     for (int j = 0; j < n; ++j) mbar_arrive(smem_u32(&empty_bar[lead + j * leads]));
             }
         } else {
+        auto begin = [&](int b) {                            // sequence b is in hand from here
+            cur_b = b;
+            row0 = w.cu_q ? w.cu_q[b] : b;
+            rows = w.cu_q ? min(max(w.cu_q[b + 1] - row0, 0), w.max_q_len) : 1;
+            if (rows == 1) {
+                load_query<KIND>(q, w.q + ((size_t)row0 * H + g * kHeadsPerGroup) * T::DQ, w.scale * kLog2e, lane);
+                const float lse = w.lse[(size_t)row0 * H + head];
+                off = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
+            }
+        };
+        if (team < n_tiles) begin(seq_of_tile(s_off, w.B, rg.lo + team));        // its query is fetched while the first tiles fly
 #pragma unroll 1
         for (int i = team, st = team, parity = 0; i < n_tiles; i += L.teams) {
             if (!dead && !mbar_wait_bounded(smem_u32(&full_bar[st]), parity, s_abort)) {
@@ -676,16 +687,7 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
                 dead = true;
             }
             const TileMeta meta = dead ? TileMeta{cur_b, 0, 0, 0} : s_meta[st];
-            if (meta.b != cur_b) {
-                cur_b = meta.b;
-                row0 = w.cu_q ? w.cu_q[cur_b] : cur_b;
-                rows = w.cu_q ? min(max(w.cu_q[cur_b + 1] - row0, 0), w.max_q_len) : 1;
-                if (rows == 1) {
-                    load_query<KIND>(q, w.q + ((size_t)row0 * H + g * kHeadsPerGroup) * T::DQ, w.scale * kLog2e, lane);
-                    const float lse = w.lse[(size_t)row0 * H + head];
-                    off = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
-                }
-            }
+            if (meta.b != cur_b) begin(meta.b);
             const unsigned char *stage = smem + (size_t)st * stage_bytes;
             const unsigned char *vt = stage + (size_t)g * T::V_BYTES;
             const __half2 *szt = reinterpret_cast<const __half2 *>(stage + (size_t)G * T::V_BYTES + (size_t)g * T::SZ_BYTES);

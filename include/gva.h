@@ -414,8 +414,8 @@ int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, 
  *                       heads, of exp(scale * score(r, head, t) - lse[r][head]),        t < seq_lens[b]
  * i.e. the softmax weights of the attention whose lse is given (a row whose lse is -inf adds nothing).
  *   q_abs [rows][H][d_v+d_r], lse [rows][H] f32   as the attention call had and returned them
- *   cu_q  [B + 1] i32 or NULL    rows cu_q[b] .. cu_q[b+1] - 1 belong to sequence b, at most max_q_len are counted; row i of
- *                                q_len_b sees seq_lens[b] - (q_len_b - 1 - i) slots.  NULL: one row per sequence
+ *   cu_q  [B + 1] i32 or NULL    rows cu_q[b] .. cu_q[b+1] - 1 belong to sequence b, row i of q_len_b sees seq_lens[b] -
+ *                                (q_len_b - 1 - i) slots; rows beyond the first max_q_len add nothing.  NULL: one row per sequence
  *   decay                        >= 0, finite; 0: weights_in is not read
  *   weights_in / weights_out     [B][stride] f32, stride >= max_seq_len; weights_in may be NULL (zeros) or weights_out itself
  * Slots at or beyond seq_lens[b] keep what weights_out held.  seq_lens[b] < 0, beyond the block table or beyond stride ->

@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <mutex>
 
 #include "gva_evict.cuh"
 #include "gva_q4_decode.cuh"
@@ -25,6 +26,26 @@ Q4Pools q4_pools(const gva_q4_cache *c) {
     return Q4Pools{static_cast<uint8_t *>(c->v_pool), static_cast<__half2 *>(c->sz_pool), static_cast<uint16_t *>(c->kr_pool),
                    c->block_table, c->num_pages, c->max_pages_per_seq};
 }
+// Lets `fn` have `bytes` of dynamic shared memory on the handle's device; asked of the runtime once per kernel and device, not per call.
+int allow_smem(const gva_handle *h, const void *fn, size_t bytes) {
+    struct Entry { const void *fn; int device; size_t bytes; };
+    static std::mutex lock;
+    static Entry seen[256];
+    static int n = 0;
+    if (bytes <= 16 * 1024) return GVA_OK;               // every kernel may have 48 KB, its static shared memory (27 KB at most) included
+    std::lock_guard<std::mutex> hold(lock);
+    int i = 0;
+    while (i < n && (seen[i].fn != fn || seen[i].device != h->device)) ++i;
+    if (i < n && seen[i].bytes >= bytes) return GVA_OK;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return GVA_ERR_CUDA;
+    }
+    if (i < n) seen[i].bytes = bytes;
+    else if (n < 256) seen[n++] = Entry{fn, h->device, bytes};
+    return GVA_OK;
+}
+
 int append_q4(gva_handle *h, const gva_q4_cache *cache, const float *v_new, const float *kr_new, const int32_t *cu_q,
               const int32_t *slot0, const int32_t *pos0, int B, int n_q, int rows, int32_t *dev_status, void *stream) {
     if (!v_new || (h->cfg.d_r > 0 && !kr_new) || !aligned(v_new, 4) || !aligned(kr_new, 4) || !aligned(slot0, 4) || !aligned(pos0, 4))
@@ -50,7 +71,11 @@ struct Q4Kernel {
     size_t stage;
 };
 template <int DV, int DR, int TILE>
-Q4Kernel q4_kernel_t(int G) { return Q4Kernel{decode_q4_kernel<DV, DR, TILE>, TILE, (size_t)Q4Traits<DV, DR, TILE>::stage_bytes(G)}; }
+Q4Kernel q4_kernel_t(int G) {
+    constexpr int FEW = q4_consumers(DV, 1), MANY = q4_consumers(DV, 8);
+    return Q4Kernel{q4_consumers(DV, G) == FEW ? decode_q4_kernel<DV, DR, TILE, FEW> : decode_q4_kernel<DV, DR, TILE, MANY>, TILE,
+                    (size_t)Q4Traits<DV, DR, TILE>::stage_bytes(G)};
+}
 Q4Kernel q4_kernel(const gva_config &c) {
     const bool t64 = c.page_size % 64 == 0;              // a tile lies in one page
 #define GVA_Q4(DV_, DR_) (t64 ? q4_kernel_t<DV_, DR_, 64>(c.G) : q4_kernel_t<DV_, DR_, 32>(c.G))
@@ -84,7 +109,7 @@ Q4Plan q4_plan(const gva_handle *h, int B, int max_seq_len, int num_splits) {
         p.n_rec = p.grid;
     } else {
         p.grid = (int)std::min<long long>(tiles * B, h->sm_count);
-        p.teams = (int)std::min<long long>(std::max(1, q4_consumers(h->cfg.d_v) / h->cfg.G), std::max<long long>(1, (tiles * B + p.grid - 1) / p.grid));
+        p.teams = (int)std::min<long long>(q4_consumers(h->cfg.d_v, h->cfg.G) / h->cfg.G, std::max<long long>(1, (tiles * B + p.grid - 1) / p.grid));
         p.n_rec = (p.grid + B) * p.teams;
     }
     // the ring takes what the SM holds (one block per SM) or a third of it
@@ -139,7 +164,7 @@ int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_ab
     if (!q_abs || !lse || !seq_lens || !weights_out || stride < max_seq_len || !(decay >= 0.f) || std::isinf(decay)) return GVA_ERR_INVALID_ARG;
     if (!aligned(q_abs, 16) || !aligned(lse, 4) || !aligned(cu_q, 4) || !aligned(seq_lens, 4) || !aligned(weights_in, 4) || !aligned(weights_out, 4))
         return GVA_ERR_INVALID_ARG;
-    if (B > 8192) return GVA_ERR_UNSUPPORTED;
+    if (B > 8192 || (long long)B * ((stride + 31) / 32 + 1) >= (1ll << 30)) return GVA_ERR_UNSUPPORTED;     // (tiles are counted in 32 bits)
     const gva_config &c = h->cfg;
     p.q = q_abs; p.lse = lse; p.cu_q = cu_q; p.seq_lens = seq_lens; p.decay = decay; p.w_in = decay > 0.f ? weights_in : nullptr; p.w_out = weights_out;
     p.stride = stride; p.B = B; p.max_q_len = max_q_len; p.H = c.H; p.G = c.G; p.P = c.page_size;
@@ -170,7 +195,8 @@ int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_ab
     const int sums = multi ? l.batch * l.teams : 2 * l.teams;
     const size_t smem = l.nstage * k.stage + WeightTraits<kCacheQ4, 64, 0, 32>::tail_bytes(B, l.nstage, sums, c.G) + (size_t)sums * c.G * (k.tile - 32) * 4;
     if (smem > (size_t)h->smem_optin) return GVA_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GVA_ERR_CUDA;
+    const int rc = allow_smem(h, reinterpret_cast<const void *>(k.fn), smem);
+    if (rc != GVA_OK) return rc;
     return launched(launch_pdl(k.fn, dim3(grid), dim3(32 * (l.teams * c.G + l.producers)), smem, s, p, l));
 }
 
@@ -219,7 +245,8 @@ int evict(gva_handle *h, const int32_t *block_table, int num_pages, int max_page
     const int per_block = ((max_seq_len + (alone ? 1 : C) - 1) / (alone ? 1 : C) + 1023) / 1024 * 1024;
     const int held = std::min(per_block, kEvictKeysMax);
     const size_t smem = (size_t)held * 4;
-    if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GVA_ERR_CUDA;
+    int rc = allow_smem(h, reinterpret_cast<const void *>(evict_select_kernel), smem);
+    if (rc != GVA_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(B * C);
     cfg.blockDim = dim3(kEvictThreads);
@@ -234,7 +261,7 @@ int evict(gva_handle *h, const int32_t *block_table, int num_pages, int max_page
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    int rc = launched(cudaLaunchKernelEx(&cfg, evict_select_kernel, p, pools, h->cfg.G, held, alone, here));
+    rc = launched(cudaLaunchKernelEx(&cfg, evict_select_kernel, p, pools, h->cfg.G, held, alone, here));
     if (rc != GVA_OK || here) return rc;
     const int blocks = std::max(1, std::min((max_seq_len / 2 + 31) / 32, (8 * h->sm_count + B - 1) / B));
     return launched(launch_pdl(evict_move_kernel, dim3(blocks, B), dim3(kMoveThreads), 0, static_cast<cudaStream_t>(stream), p, pools, h->cfg.G));
@@ -332,7 +359,8 @@ int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, 
     l.producers = plan.producers;
     l.segments = plan.num_splits > 0 ? nullptr : reinterpret_cast<int2 *>(ws);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (cudaFuncSetAttribute(plan.k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan.smem) != cudaSuccess) return GVA_ERR_CUDA;
+    rc = allow_smem(h, reinterpret_cast<const void *>(plan.k.fn), plan.smem);
+    if (rc != GVA_OK) return rc;
     rc = launched(launch_pdl(plan.k.fn, dim3(plan.grid), dim3(32 * (plan.teams * c.G + plan.producers)), plan.smem, s, p, l));
     if (rc != GVA_OK || plan.num_splits == 1) return rc;
     const MergeParams m{p.rec_o, p.rec_ml, l.segments, out, lse, c.H, plan.num_splits, plan.teams};

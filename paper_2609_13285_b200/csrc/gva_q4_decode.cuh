@@ -24,7 +24,7 @@
 // p s by the largest step seen so far, which is followed like the running maximum.
 //
 // Blocks.  One block per SM streams a contiguous range of tiles through a ring of bulk copies: up to four producer warps, and
-// teams of G consumer warps, one warp per group, up to 16 consumers in all.  Team k takes tiles k, k + teams, ..., keeps its own
+// teams of G consumer warps, one warp per group, 12 to 16 consumers in all.  Team k takes tiles k, k + teams, ..., keeps its own
 // running softmax and writes its own partial records, so results do not depend on who is faster; a team that the
 // scheduler favours meets the end of the ring and waits there for the others, which evens them out (four blocks per SM with
 // equal ranges each ended between 45 and 69 us on the 1 M token batch, median 57).  All waits are bounded.
@@ -369,17 +369,13 @@ struct Q4Launch {
     int teams, producers, nstage;   // nstage: a multiple of both, see produce_tiles (a team likewise finds only its own tiles in a slot)
     int2 *segments;              // per sequence: first record group and their number, for the merge (balanced partition only)
 };
-#ifndef GVA_Q4_CONS64
-#define GVA_Q4_CONS64 16
-#endif
-#ifndef GVA_Q4_CONS128
-#define GVA_Q4_CONS128 16
-#endif
 constexpr int kQ4Producers = 4;           // producer warps of a block at most
-__host__ __device__ constexpr int q4_consumers(int d_v) { return d_v == 64 ? GVA_Q4_CONS64 : GVA_Q4_CONS128; }   // consumer warps of a block at most
+// Consumer warps of a block at most: 12, which leaves a thread 128 registers, where that is three teams or more, else 16 with 96
+// (1 M tokens, G = 4: 67 us with 12, 70 with 16, 75 with 8; wide heads, G = 8: 142 with 8, 133 with 16).
+__host__ __device__ constexpr int q4_consumers(int d_v, int G) { return d_v == 64 && G <= 4 ? 12 : 16; }
 
-template <int DV, int DR, int TILE>
-__global__ void __launch_bounds__(32 * (q4_consumers(DV) + kQ4Producers), 1)
+template <int DV, int DR, int TILE, int CONSUMERS>
+__global__ void __launch_bounds__(32 * (CONSUMERS + kQ4Producers), 1)
 decode_q4_kernel(DecodeParams p, Q4Launch L) {
     using T = Q4Traits<DV, DR, TILE>;
     grid_dependency_launch();

@@ -42,7 +42,7 @@ weights_f32_kernel(WeightParams p, int DR) {
         return;
     }
     const int row0 = p.cu_q ? p.cu_q[b] : b;
-    const int rows = p.cu_q ? min(max(p.cu_q[b + 1] - row0, 0), p.max_q_len) : 1;
+    const int q_len = p.cu_q ? p.cu_q[b + 1] - row0 : 1, rows = min(max(q_len, 0), p.max_q_len);
     const int DQ = DV + DR;
     constexpr int E = DV / 32;
     for (long long t0 = (long long)blockIdx.x * kWeightTile; t0 < len; t0 += (long long)gridDim.x * kWeightTile) {
@@ -58,7 +58,7 @@ weights_f32_kernel(WeightParams p, int DR) {
                     float v[E];
                     for (int e = 0; e < E; ++e) v[e] = static_cast<const float *>(p.v)[row * DV + lane * E + e];
                     for (int r = 0; r < rows; ++r) {
-                        if (t >= len - (rows - 1 - r)) continue;
+                        if (t >= len - (q_len - 1 - r)) continue;
                         for (int j = 0; j < kHeadsPerGroup; ++j) {
                             const int h = g * kHeadsPerGroup + j;
                             const float *q = p.q + ((size_t)(row0 + r) * p.H + h) * DQ;
@@ -462,13 +462,16 @@ __device__ __forceinline__ void score_pair(const unsigned char *v, const unsigne
                 const float2 z = i < 2 ? a : b;
                 x[i] = fmaf(acc[i] * q.unscale[i & 1], z.x, fmaf(z.y, q.sum[i & 1], rot[i]));
             }
-            return;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = (acc[i] + rot[i]) * q.unscale[i & 1];
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += rot[i];
+        return;
     }
+    if constexpr (KIND == kCacheE4m3) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = acc[i] * q.unscale[i & 1];
+        for (int i = 0; i < 4; ++i) x[i] = acc[i] * q.unscale[i & 1];
+    }
 }
 
 // The block's range of the tile list when a tile costs (rows + 1) / 2 + 1: block c of n takes the tiles whose cost starts in
@@ -589,7 +592,7 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
         const int part = MULTI ? team % L.split : 0, lead = MULTI ? team / L.split : team, leads = L.teams / L.split;   // rows' part, tiles' part
         const int GS = G * L.split;                          // partial sums per token
         float *sums = s_sum + lead * (MULTI ? L.batch : 2) * GS * TILE;
-        int cur_b = -1, row0 = 0, rows = 0, buf = 0;
+        int cur_b = -1, row0 = 0, q_len = 0, rows = 0, buf = 0;
         float off = 0.f;                                     // -lse in log2 units (one row)
         const int n_tiles = rg.hi - rg.lo;
         bool dead = false;                                   // a wait ran out: only the team's barriers are still kept
@@ -612,7 +615,8 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
                     int j1 = j0 + 1;
                     while (j1 < n && s_meta[lead + j1 * leads].b == b) ++j1;
                     row0 = w.cu_q[b];
-                    rows = min(max(w.cu_q[b + 1] - row0, 0), w.max_q_len);
+                    const int q_len = w.cu_q[b + 1] - row0;
+                    rows = min(max(q_len, 0), w.max_q_len);
 #pragma unroll 1
                     for (int r = 2 * part; r < rows; r += 2 * L.split) {
                         const bool second = r + 1 < rows;
@@ -623,7 +627,7 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
                             const int st = lead + j * leads;
                             const TileMeta meta = s_meta[st];
                             // tokens of the tile that this lane's row sees; the later row sees one more
-                            const int seen = meta.len - (rows - 1 - r) - meta.t0;
+                            const int seen = meta.len - (q_len - 1 - r) - meta.t0;
                             if (min(meta.n_valid, seen + 1) <= 0) continue;
                             const int lim = c < 2 ? min(meta.n_valid, seen) : second ? min(meta.n_valid, seen + 1) : 0;
                             const unsigned char *stage = smem + (size_t)st * stage_bytes;
@@ -671,7 +675,8 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
         auto begin = [&](int b) {                            // sequence b is in hand from here
             cur_b = b;
             row0 = w.cu_q ? w.cu_q[b] : b;
-            rows = w.cu_q ? min(max(w.cu_q[b + 1] - row0, 0), w.max_q_len) : 1;
+            q_len = w.cu_q ? w.cu_q[b + 1] - row0 : 1;
+            rows = min(max(q_len, 0), w.max_q_len);          // 0 or 1
             if (rows == 1) {
                 load_query<KIND>(q, w.q + ((size_t)row0 * H + g * kHeadsPerGroup) * T::DQ, w.scale * kLog2e, lane);
                 const float lse = w.lse[(size_t)row0 * H + head];
@@ -696,6 +701,7 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
 #pragma unroll
             for (int k = 0; k < T::CHUNKS; ++k) sum[k][0] = sum[k][1] = 0.f;
             if (rows > 0 && !dead) {
+                const int lim = min(meta.n_valid, meta.len - (q_len - 1) - meta.t0);      // (q_len > 1 where max_q_len cuts it off)
 #pragma unroll
                 for (int kk = 0; kk < T::CHUNKS; kk += 2) {
                     float x[2][2];
@@ -716,8 +722,8 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const float p0 = fast_exp2(x[k][0] + off), p1 = fast_exp2(x[k][1] + off);
-                        sum[kk + k][0] = (kk + k) * 16 + tok_lo < meta.n_valid ? p0 : 0.f;
-                        sum[kk + k][1] = (kk + k) * 16 + tok_hi < meta.n_valid ? p1 : 0.f;
+                        sum[kk + k][0] = (kk + k) * 16 + tok_lo < lim ? p0 : 0.f;
+                        sum[kk + k][1] = (kk + k) * 16 + tok_hi < lim ? p1 : 0.f;
                     }
                 }
             }

@@ -435,6 +435,17 @@ def test_decode_pages_beyond_four_gigabytes():
         check_decode(h, cache, queries(shape, 2, 38))
 
 
+def test_three_thousand_sequences():
+    shape, B = G1, 3000
+    lens = [b % 71 for b in range(B)]
+    cache = Cache(shape, lens, page=32, seed=46)
+    with Handle(shape, 32) as h:
+        check_decode(h, cache, queries(shape, B, 47))
+        check_decode(h, cache, queries(shape, B, 47), num_splits=2)
+    check_weights(shape, lens, "q4", [1 + b % 3 for b in range(B)], page=32)
+    check_evict(shape, lens, [40] * B, page=32)
+
+
 def test_decode_same_bits_every_time_and_on_a_side_stream():
     shape = wl.SHAPE_A
     cache = Cache(shape, [5000, 64, 1, 777], seed=39)
@@ -496,7 +507,7 @@ def test_bad_lengths_and_pages_are_reported_and_the_rest_is_right():
 
 
 # ---- gathered weights --------------------------------------------------------------------------------------------------
-def check_weights(shape, lens, kind, rows, page=64, paged=True, seed=50, decay=0.5, alias=False, cu=True, gain=1.5):
+def check_weights(shape, lens, kind, rows, page=64, paged=True, seed=50, decay=0.5, alias=False, cu=True, gain=1.5, most=None):
     cache = Cache(shape, lens, page=page, kind=kind, seed=seed, paged=paged)
     rng = np.random.default_rng(seed + 1)
     B, n = len(lens), sum(rows)
@@ -513,12 +524,15 @@ def check_weights(shape, lens, kind, rows, page=64, paged=True, seed=50, decay=0
                 m = lens[b] - (R - 1 - i)
                 if m > 0:
                     lse[cu_q[b] + i] = ref.attend(q[cu_q[b] + i].astype(np.float64), v[:m], kr[:m], h.scale)[1]
-            want[b, :lens[b]] = ref.gathered(q[cu_q[b]:cu_q[b + 1]].astype(np.float64), lse[cu_q[b]:cu_q[b + 1]].astype(np.float64), v, kr, h.scale, before[b, :lens[b]], decay)
+            counted = lse[cu_q[b]:cu_q[b + 1]].astype(np.float64)
+            if most is not None:
+                counted[most:] = -np.inf                                     # rows that max_q_len cuts off add nothing
+            want[b, :lens[b]] = ref.gathered(q[cu_q[b]:cu_q[b + 1]].astype(np.float64), counted, v, kr, h.scale, before[b, :lens[b]], decay)
         w_in = dev(before)
         w_out = w_in if alias else torch.full((B, stride), 7.0, device="cuda")
         status = torch.zeros(1, dtype=torch.int32, device="cuda")
         call = gb.gva_q4_attention_weights if kind == "q4" else gb.gva_attention_weights
-        call(h.h, cache.c, dev(q), dev(lse), ints(cu_q) if cu else None, ints(lens), decay, w_in, w_out, stride, B, max(max(rows), 1), max(max(lens), 1), status)
+        call(h.h, cache.c, dev(q), dev(lse), ints(cu_q) if cu else None, ints(lens), decay, w_in, w_out, stride, B, max(max(rows), 1) if most is None else most, max(max(lens), 1), status)
         got = w_out.cpu().numpy().astype(np.float64)
         assert int(status.item()) == 0
         # a weight is exp of a difference that is off by 5e-6 (see above) plus the rounding of lse to f32 (2^-24 of some 8)
@@ -548,6 +562,12 @@ def test_weights_page_sizes(page, paged, kind):
 def test_weights_of_one_long_sequence_and_of_many_short_ones():
     check_weights(wl.SHAPE_A, [20001], "q4", [2])
     check_weights(wl.SHAPE_A, [40 + b % 60 for b in range(400)], "q4", [1] * 400)
+
+
+@pytest.mark.parametrize("kind", ["q4", "bf16", "f32"])
+@pytest.mark.parametrize("most", [1, 2, 3])
+def test_weights_count_the_first_rows_where_there_are_more(kind, most):
+    check_weights(wl.SHAPE_A, [200, 64, 3], kind, [5, 1, 4], most=most)
 
 
 def test_weights_of_one_row_sum_to_the_number_of_heads():

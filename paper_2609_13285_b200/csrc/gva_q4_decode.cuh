@@ -568,26 +568,36 @@ decode_q4_kernel(DecodeParams p, Q4Launch L) {
                 pb0[k] = movmatrix_trans(s0);
                 pb1[k] = movmatrix_trans(s1);
             }
-            // ---- O^T += C_tile^T . (P s)^T ----
+            // ---- O^T += C_tile^T . (P s)^T.  A tile's products are summed from nothing and added to the running output in f32: the
+            //      MMA's own accumulation truncates, which over hundreds of steps came to 1.3e-6 of an output whose terms cancel ----
 #pragma unroll
-            for (int k = 0; k < T::CHUNKS; ++k) {
-                const unsigned char *row = vt + k * 16 * T::ROW + r8 * 4;
+            for (int h = 0; h < DV / 64; ++h) {              // words lane / 4 and, for d_v = 128, lane / 4 + 8
+                uint32_t half[2][T::CHUNKS][2];              // [low | high half words][chunk][pair of tokens], interleaved by token
 #pragma unroll
-                for (int h = 0; h < DV / 64; ++h) {          // words lane / 4 and, for d_v = 128, lane / 4 + 8
-                    uint32_t even[2], odd[2];                // [pair of tokens]: low and high half words interleaved by token
+                for (int k = 0; k < T::CHUNKS; ++k)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const uint32_t w0 = *reinterpret_cast<const uint32_t *>(row + (ta + 8 * u) * T::ROW + 32 * h);
-                        const uint32_t w1 = *reinterpret_cast<const uint32_t *>(row + (tb + 8 * u) * T::ROW + 32 * h);
-                        even[u] = __byte_perm(w0, w1, 0x5410);
-                        odd[u] = __byte_perm(w0, w1, 0x7632);
+                        const unsigned char *row = vt + k * 16 * T::ROW + r8 * 4 + 32 * h;
+                        const uint32_t w0 = *reinterpret_cast<const uint32_t *>(row + (ta + 8 * u) * T::ROW);
+                        const uint32_t w1 = *reinterpret_cast<const uint32_t *>(row + (tb + 8 * u) * T::ROW);
+                        half[0][k][u] = __byte_perm(w0, w1, 0x5410);
+                        half[1][k][u] = __byte_perm(w0, w1, 0x7632);
                     }
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {            // dims 8 word + 2 u and + 1
-                        const uint32_t e0 = u < 2 ? even[0] : odd[0], e1 = u < 2 ? even[1] : odd[1];
-                        const uint32_t f0 = u % 2 ? e0 >> 8 : e0, f1 = u % 2 ? e1 >> 8 : e1;
-                        mma_f16_q4(oacc[4 * h + u], centred_low(f0), centred_high(f0), centred_low(f1), centred_high(f1), pb0[k], pb1[k]);
-                    }
+                for (int u = 0; u < 4; u += 2) {             // dims 8 word + 2 u .. + 2 u + 3
+                    float acc[2][4];
+#pragma unroll
+                    for (int k = 0; k < T::CHUNKS; ++k)
+#pragma unroll
+                        for (int v = 0; v < 2; ++v) {
+                            const uint32_t e0 = half[u / 2][k][0], e1 = half[u / 2][k][1], f0 = v ? e0 >> 8 : e0, f1 = v ? e1 >> 8 : e1;
+                            if (k == 0) mma_f16_first(acc[v], centred_low(f0), centred_high(f0), centred_low(f1), centred_high(f1), pb0[k], pb1[k]);
+                            else mma_f16_q4(acc[v], centred_low(f0), centred_high(f0), centred_low(f1), centred_high(f1), pb0[k], pb1[k]);
+                        }
+#pragma unroll
+                    for (int v = 0; v < 2; ++v)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) oacc[4 * h + u + v][e] += acc[v][e];
                 }
             }
             __syncwarp();

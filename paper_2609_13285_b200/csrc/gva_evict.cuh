@@ -21,7 +21,8 @@ namespace gva {
 // move: blocks copy the rows of the moves in 16-byte pieces, weights and positions with them.
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictBins = 2048;
-constexpr int kEvictAlone = 8192;        // sequences up to this length: one block selects
+constexpr int kEvictAlone = 8192;        // sequences up to this length: one block selects (three of 1500: a cluster of eight took 7 us
+                                         // longer, for the histograms read from one another and the meetings)
 constexpr int kEvictMoveHere = 2;        // up to so many batches of moves per block: rows are moved by the selecting cluster
 constexpr int kEvictKeysMax = 32768;     // keys of one block that are kept in shared memory; beyond, they are made again
 

@@ -292,7 +292,7 @@ int gva_q4_append_chunk(gva_handle *h, const gva_q4_cache *cache, const float *v
     if (!cu_q || !aligned(cu_q, 4) || !ctx_lens) return GVA_ERR_INVALID_ARG;
     // rows of a block: up to four shares of eight elements per thread, as long as that leaves four blocks per SM (990 rows of
     // 4 x 64: 6.7 us with 32 rows to a block, 5.7 with one)
-    const int most = kAppendQ4Threads * kAppendQ4Shares / (h->cfg.G * h->cfg.d_v / 8);
+    const int most = append_q4_rows(h->cfg.d_v) / h->cfg.G;
     const int rows = std::max(1, std::min(most, n_q / (4 * h->sm_count)));
     return append_q4(h, cache, v_new, kr_new, cu_q, ctx_lens, first_pos ? first_pos : ctx_lens, B, n_q, rows, dev_status, stream);
 }

@@ -54,7 +54,10 @@ struct AppendQ4Params {
 };
 constexpr int kAppendQ4Threads = 256;
 constexpr int kAppendQ4Shares = 4;        // shares of eight elements per thread
-constexpr int kAppendQ4Rows = kAppendQ4Threads * kAppendQ4Shares / 8;   // rows of a block at most (G = 1, d_v = 64)
+// Rows of a block at most (G = 1), and the positional pairs that many rows can bring: 128 x 12 with d_v = 64, 64 x 16 with 128.
+__host__ __device__ constexpr int append_q4_rows(int d_v) { return kAppendQ4Threads * kAppendQ4Shares / (d_v / 8); }
+template <int DV>
+constexpr int kAppendQ4Pairs = append_q4_rows(DV) * widest_rope(DV) / 2;
 
 // The codes of eight elements (z <= x, x - z <= 15 s).  A code is the integer nearest to (x - z) / s, read out of the mantissa after
 // adding 2^23; the quotient is off by less than 3e-6, so a code is right unless its remainder comes within 2e-5 of a half:
@@ -103,8 +106,10 @@ template <int DV>
 __global__ void __launch_bounds__(kAppendQ4Threads)
 append_q4_kernel(const __grid_constant__ AppendQ4Params p, const __grid_constant__ RopeTable rope) {     // (tables are indexed where they lie)
     grid_dependency_launch();
-    __shared__ int s_page[kAppendQ4Rows], s_slot[kAppendQ4Rows], s_pos[kAppendQ4Rows];   // page -1: the row is not written
-    __shared__ uint32_t s_key[kAppendQ4Rows * 8];            // rotated pairs, bf16 (rows * pairs <= 1024)
+    constexpr int ROWS = append_q4_rows(DV);
+    __shared__ int s_page[ROWS], s_slot[ROWS], s_pos[ROWS];  // page -1: the row is not written
+    __shared__ uint32_t s_key[kAppendQ4Pairs<DV>];           // rotated pairs, bf16
+    static_assert(ROWS <= kAppendQ4Threads, "a thread per row");
     grid_dependency_wait();
     const int tid = threadIdx.x, n0 = blockIdx.x * p.rows;
     const int total = p.cu_q ? min(p.n_q, p.cu_q[p.B]) : p.n_q;
@@ -131,7 +136,7 @@ append_q4_kernel(const __grid_constant__ AppendQ4Params p, const __grid_constant
             for (int i = 0; i < 8; ++i) x[u][i] = 0.f;
         }
     }
-    int my_b = -1, my_t = 0;                                 // this thread's row, if it has one (rows <= 128): sequence and slot
+    int my_b = -1, my_t = 0;                                 // this thread's row, if it has one: sequence and slot
     if (tid < p.rows && n0 + tid < total) {
         const int n = n0 + tid;
         int b = n, i = 0;

@@ -7,6 +7,23 @@ namespace gva {
 
 constexpr int kMaxRopePairs = 16;   // d_r <= 32
 
+// The head widths that gva_create serves: of a value row and of the positional slice beside it.
+struct HeadWidths {
+    int d_v, d_r;
+};
+constexpr HeadWidths kHeadWidths[] = {{64, 16}, {64, 24}, {64, 0}, {128, 32}, {128, 0}};
+constexpr bool serves_widths(int d_v, int d_r) {
+    for (const HeadWidths &w : kHeadWidths)
+        if (w.d_v == d_v && w.d_r == d_r) return true;
+    return false;
+}
+constexpr int widest_rope(int d_v) {
+    int most = 0;
+    for (const HeadWidths &w : kHeadWidths)
+        if (w.d_v == d_v && w.d_r > most) most = w.d_r;
+    return most;
+}
+
 struct RopeTable {
     double inv_freq[kMaxRopePairs];   // base^(-2i/d_r), computed once on the host in fp64
 };

@@ -56,6 +56,16 @@ def rotate(x, pos, base=10000.0):
     return y
 
 
+def to_bf16_bits(y):
+    """float64 -> bf16 bit patterns, rounded once, to nearest even (by way of f32 one in 2^17 numbers would be rounded twice)."""
+    y = np.asarray(y, dtype=np.float64)
+    u = y.astype(np.float32).view(np.uint32) & np.uint32(0x7FFFFFFF)
+    low = u & np.uint32(0xFFFF0000)                       # the bf16 numbers on both sides of |y|
+    middle = (low | np.uint32(0x8000)).view(np.float32).astype(np.float64)
+    up = (np.abs(y) > middle) | ((np.abs(y) == middle) & ((low >> 16) & 1 == 1))
+    return ((low >> 16) + up + np.where(np.signbit(y), 0x8000, 0)).astype(np.uint16)
+
+
 def rows_of(pool, table, b, n, page):
     """Rows of slots 0 .. n - 1 of sequence b: pool [pages][G][page][d] -> [n][G][d], or [pages][page][d] -> [n][d]."""
     t = np.arange(n)

@@ -40,6 +40,19 @@ def test_codes_cover_every_row_and_are_the_nearest():
         assert np.array_equal(ref.unpack(ref.pack(c)), c)
 
 
+def test_bf16_of_f64_is_rounded_once():
+    from paper_2609_13285_b200 import workloads as wl
+    rng = np.random.default_rng(12)
+    x = np.concatenate([rng.standard_normal(20000) * 10.0 ** rng.uniform(-8, 8, 20000), [0.0, 1.0, -1.0, 1.00390625, 1.01171875, -1.01171875]])
+    a = wl.bf16_bits_to_f32(ref.to_bf16_bits(x)).astype(np.float64)
+    for step in (-1, 1):                                  # no neighbour is nearer
+        near = wl.bf16_bits_to_f32((ref.to_bf16_bits(x).astype(np.int32) + step).astype(np.uint16)).astype(np.float64)
+        assert np.all((np.abs(a - x) <= np.abs(near - x)) | (x == 0))
+    assert ref.to_bf16_bits([1.00390625, 1.01171875]).tolist() == [0x3F80, 0x3F82]           # ties go to the even pattern
+    just = 1.00390625 + 2.0 ** -40                        # over a border by less than f32 can hold
+    assert ref.to_bf16_bits([just, -just, 2 * 1.00390625 - just]).tolist() == [0x3F81, 0xBF81, 0x3F80]
+
+
 def test_a_row_with_a_nan_reads_as_nan():
     x = np.ones((2, 64), dtype=np.float32)
     x[1, 5] = np.nan

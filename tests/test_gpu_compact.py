@@ -20,6 +20,7 @@ TOL_MAX, TOL_REL = 2e-5, 1e-5
 EDGE = [0, 1, 31, 32, 33, 63, 64, 65, 127, 128, 129, 640, 641, 1000]
 SHAPES = [wl.SHAPE_A, wl.SHAPE_B, wl.SHAPE_C, wl.SHAPE_A0, wl.SHAPE_B0]
 G1 = wl.HeadShape(H=4, G=1, d_v=64, d_c=64, d_r=16)
+G1R = wl.HeadShape(H=4, G=1, d_v=64, d_c=64, d_r=24)
 G3 = wl.HeadShape(H=12, G=3, d_v=64, d_c=64, d_r=24)
 G8 = wl.HeadShape(H=32, G=8, d_v=64, d_c=64, d_r=16)
 G2W = wl.HeadShape(H=8, G=2, d_v=128, d_c=128, d_r=32)
@@ -236,6 +237,47 @@ def test_append_chunk_of_ragged_prompts(shape):
                                    len(ctx), n + 5, status)
             assert int(status.item()) == 0
             same_pools(cache.download(), expect_rows(cache, x, kr, places, pos))
+
+
+def check_chunk(shape, rows, seed, B=37, page=32, offset=0):
+    """A chunk large enough for `rows` input rows per block (a block takes n_q / (4 SMs), as many as its threads have shares
+    for at most), over ragged sequences whose borders lie inside blocks, empty ones among them, the last block cut short
+    by cu_q[B] < n_q."""
+    rng = np.random.default_rng(seed)
+    n_q = rows * 4 * torch.cuda.get_device_properties(0).multi_processor_count + 7
+    share = rng.random(B) * (rng.random(B) < 0.8)
+    q_lens = np.floor(share / share.sum() * (n_q - 5)).astype(np.int64)
+    q_lens[int(np.argmax(q_lens))] += n_q - 5 - q_lens.sum()
+    ctx = rng.integers(0, 100, B)
+    cache = Cache(shape, list(ctx + q_lens), page=page, seed=seed + 1)
+    n = int(q_lens.sum())
+    x = odd_rows(shape, n_q, seed + 2)
+    x[n:] = np.nan
+    kr = rng.standard_normal((n_q, shape.d_r)).astype(np.float32)
+    first = rng.integers(0, 100000, B)
+    cu = np.concatenate([[0], np.cumsum(q_lens)])
+    b = np.repeat(np.arange(B), q_lens)
+    i = np.arange(n) - cu[b]
+    pg, sl = cache.ids[b, (ctx[b] + i) // page], (ctx[b] + i) % page
+    want = [p.copy() for p in cache.pools]
+    c, st, z = ref.quantise(x[:n])
+    want[0][pg, :, sl] = ref.pack(c)
+    want[1][pg, :, sl] = np.stack([st, z], axis=-1)
+    if shape.d_r:
+        want[2][pg, sl] = ref.to_bf16_bits(ref.rotate(kr[:n], first[b] + i))
+    with Handle(shape, page) as h:
+        xs = torch.zeros(x.size + 1, device="cuda")
+        xs[offset:offset + x.size] = dev(x).reshape(-1)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        gb.gva_q4_append_chunk(h.h, cache.c, xs[offset:], dev(kr) if shape.d_r else None, ints(cu), ints(ctx), ints(first), B, n_q, status)
+        assert int(status.item()) == 0
+        same_pools(cache.download(), want)
+
+
+@pytest.mark.parametrize("rows", [85, 86, 127, 128, 130])
+def test_append_chunk_of_one_group_with_the_widest_positional_slice(rows):
+    # up to 128 rows to a block, 12 positional pairs to a row: 1020 pairs with 85 rows, 1032 with 86, 1536 at most
+    check_chunk(G1R, rows, 300 + rows)
 
 
 def test_append_reports_what_has_no_place_and_writes_the_rest():

@@ -344,11 +344,13 @@ merge_records_kernel(MergeParams p) {
             const size_t rh = (size_t)(first + min(r, count - 1)) * p.H + h;
             ml[u] = *reinterpret_cast<const float2 *>(p.rec_ml + rh * 2);
             o[u] = *reinterpret_cast<const float4 *>(p.rec_o + rh * DV + 4 * l);
-            if (r >= count) ml[u].x = -INFINITY;
+            if (r >= count) ml[u] = make_float2(-INFINITY, 0.f);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (ml[u].x == -INFINITY) continue;              // an empty range: its output is not written
+            // an empty range: its output is not written.  (Where all scores are NaN the maximum is -inf too, but the sum is NaN, which
+            // from here on stays in sum and outputs: 0 NaN = NaN)
+            if (ml[u].x == -INFINITY && ml[u].y == 0.f) continue;
             const float top = fmaxf(m, ml[u].x), f = exp2f(m - top), w = exp2f(ml[u].x - top);
             m = top;
             acc.x = fmaf(w, o[u].x, acc.x * f);

@@ -459,6 +459,32 @@ def test_decode_rows_with_nan_stay_with_their_head_and_sequence():
         assert np.isfinite(out[1]).all() and np.isfinite(np.delete(out[0], range(8, 12), axis=0)).all()
 
 
+@pytest.mark.parametrize("num_splits", [0, 1, 3, 40])
+@pytest.mark.parametrize("shape", [wl.SHAPE_A, wl.SHAPE_B])
+def test_decode_nan_is_carried_however_the_sequences_are_split(shape, num_splits):
+    # fifteen tiles each: a range of them holds nothing but what is NaN (a head's whole query, a row alone in the last tile, a
+    # group's whole sequence), and a NaN is not an empty range
+    lens = [900, 897, 900, 333]
+    cache = Cache(shape, lens, seed=130)
+    step = cache.pools[1]
+    step[cache.ids[1, 896 // 64], 2, 896 % 64, 1] = np.nan
+    step[cache.ids[2], 0, :, 1] = np.nan
+    cache.upload()
+    q = queries(shape, len(lens), 131)
+    q[0, 5, 7], q[0, 6, 3], q[0, 7, -1] = np.nan, np.inf, np.nan
+    nan = np.zeros((len(lens), shape.H), dtype=bool)
+    nan[0, 5:8], nan[1, 8:12], nan[2, 0:4] = True, True, True
+    with Handle(shape) as h:
+        out, lse, status = decode(h, cache, q, num_splits=num_splits)
+        assert status == 0
+        assert np.array_equal(np.isnan(lse), nan) and np.array_equal(np.isnan(out), np.broadcast_to(nan[..., None], out.shape))
+        for b, n in enumerate(lens):
+            o, l = ref.attend(np.nan_to_num(q[b].astype(np.float64), nan=0, posinf=0), *cache.values(b, n), h.scale)
+            live = ~nan[b]
+            assert np.max(np.abs(out[b, live] - o[live])) <= TOL_MAX
+            assert np.max(np.abs(lse[b, live] - l[live])) <= 1e-5 * np.max(np.abs(l[live]))
+
+
 def test_decode_pages_beyond_four_gigabytes():
     shape, page = wl.SHAPE_A, 64
     pages = (5 << 30) // (shape.G * page * shape.d_v // 2)

@@ -159,9 +159,9 @@ evict_select_kernel(EvictParams p, MovePools pools, int G, int keys_in_smem, int
     }
     __syncthreads();
     const int len_in = p.seq_lens[b], keep_in = p.keep[b], next = p.next_pos ? p.next_pos[b] : 0;
-    bool bad = len_in < 0 || len_in > p.max_seq_len || (long long)len_in > (long long)p.max_pages * p.P || keep_in < 0;
+    bool bad = len_in < 0 || len_in > p.max_seq_len || (long long)len_in > (long long)p.max_pages * p.P;
     const int len = bad ? 0 : len_in;
-    if (bad && rank == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
+    if ((bad || keep_in < 0) && rank == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
     const float *w = p.w_in + (size_t)b * p.stride;
     const int32_t *pos = p.pos_in ? p.pos_in + (size_t)b * p.stride : nullptr;
     float *w_out = p.w_out + (size_t)b * p.stride;
@@ -169,7 +169,7 @@ evict_select_kernel(EvictParams p, MovePools pools, int G, int keys_in_smem, int
     // this block's slots: a multiple of 32 per warp, warps one after the other
     const int per_block = ((len + C - 1) / C + 1023) / 1024 * 1024;
     const int lo = min(len, rank * per_block), hi = min(len, lo + per_block);
-    const bool loses = !bad && keep_in < len;
+    const bool loses = !bad && keep_in >= 0 && keep_in < len;            // (a negative budget: the sequence stays as it is)
     auto make_key = [&](float weight, int at) -> uint32_t {
         const bool safe = at < p.sinks || (p.recent > 0 && (long long)at >= (long long)next - p.recent);
         return safe ? kEvictKeyInf : evict_key(weight);

@@ -769,6 +769,28 @@ def test_evict_leaves_bad_sequences_alone():
                 assert all(np.array_equal(a[cache.table[b, j]].view(np.uint8), c[cache.table[b, j]].view(np.uint8)) for a, c in zip(got, cache.pools))
 
 
+@pytest.mark.parametrize("kind", ["q4", "bf16"])
+@pytest.mark.parametrize("T", [200, 20000])
+def test_evict_with_a_negative_budget_hands_weights_and_positions_on(kind, T):
+    # the sequence stays as it is, and so the outputs say, when they are other buffers than the inputs
+    shape = wl.SHAPE_A
+    cache = Cache(shape, [T, T - 7, 5], kind=kind, seed=140)
+    with Handle(shape) as h:
+        w, p = torch.rand(3, T, device="cuda"), torch.randint(0, 10 ** 6, (3, T), dtype=torch.int32, device="cuda")
+        w2, p2, new = torch.full_like(w, 9.0), torch.full_like(p, 9), ints([0, 0, 0])
+        ws = torch.empty(gb.gva_evict_workspace_bytes(h.h, 3, T), dtype=torch.uint8, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        call = gb.gva_q4_evict if kind == "q4" else gb.gva_evict
+        call(h.h, cache.c, w, p, ints([T, T - 7, 5]), ints([T, -3, -2 ** 31]), None, 0, 0, w2, p2, new, T, ws, 3, T, status)
+        code = int(status.item())
+        assert code & 0xFF == gb.GVA_ERR_SEQ_LEN and code >> 8 in (1, 2)
+        assert new.cpu().tolist() == [T, T - 7, 5]
+        for b, n in enumerate([T, T - 7, 5]):
+            assert torch.equal(w2[b, :n], w[b, :n]) and torch.equal(p2[b, :n], p[b, :n])
+            assert torch.all(w2[b, n:] == 9) and torch.all(p2[b, n:] == 9)
+        assert all(np.array_equal(g.view(np.uint8), q.view(np.uint8)) for g, q in zip(cache.download(), cache.pools))
+
+
 # ---- refusals ----------------------------------------------------------------------------------------------------------
 def test_refusals():
     shape = wl.SHAPE_A

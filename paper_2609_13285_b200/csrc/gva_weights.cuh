@@ -640,8 +640,9 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
                                 float x[4];
                                 score_pair<KIND, T>(vt + (k * 16 + tok_lo) * T::ROW + c * (T::ROW / 4), krt + (k * 16 + tok_lo) * T::KR_ROW,
                                                     smem_u32(krt) + k * 16 * T::KR_ROW + kr_lane<QT>(lane), szt + k * 16 + tok_lo, c, q, x);
-                                // (what stands behind the sequence may be anything, a NaN included)
-                                float p0 = fast_exp2(x[0] + q.off[0]) + fast_exp2(x[1] + q.off[1]), p1 = fast_exp2(x[2] + q.off[0]) + fast_exp2(x[3] + q.off[1]);
+                                // (scores may be anything, a NaN included, behind the sequence and where a head has no lse)
+                                auto weight = [&](float s, int i) { return q.off[i] == -INFINITY ? 0.f : fast_exp2(s + q.off[i]); };
+                                float p0 = weight(x[0], 0) + weight(x[1], 1), p1 = weight(x[2], 0) + weight(x[3], 1);
                                 p0 = k * 16 + tok_lo < lim ? p0 : 0.f;
                                 p1 = k * 16 + tok_hi < lim ? p1 : 0.f;
                                 p0 += __shfl_xor_sync(0xffffffffu, p0, 1);       // the group's heads and the two rows
@@ -701,7 +702,8 @@ weights_mma_kernel(WeightParams w, WeightLaunch L) {
 #pragma unroll
             for (int k = 0; k < T::CHUNKS; ++k) sum[k][0] = sum[k][1] = 0.f;
             if (rows > 0 && !dead) {
-                const int lim = min(meta.n_valid, meta.len - (q_len - 1) - meta.t0);      // (q_len > 1 where max_q_len cuts it off)
+                // (q_len > 1 where max_q_len cuts it off; a head without an lse adds nothing, not even a NaN score's NaN)
+                const int lim = off == -INFINITY ? 0 : min(meta.n_valid, meta.len - (q_len - 1) - meta.t0);
 #pragma unroll
                 for (int kk = 0; kk < T::CHUNKS; kk += 2) {
                     float x[2][2];

@@ -638,6 +638,44 @@ def test_weights_count_the_first_rows_where_there_are_more(kind, most):
     check_weights(wl.SHAPE_A, [200, 64, 3], kind, [5, 1, 4], most=most)
 
 
+@pytest.mark.parametrize("rows", [[1, 1, 1], [3, 2, 5]])
+@pytest.mark.parametrize("kind", ["q4", "bf16", "fp8", "f32"])
+@pytest.mark.parametrize("shape", [wl.SHAPE_A, wl.SHAPE_B])
+def test_weights_of_a_row_without_lse_add_nothing_whatever_its_query_holds(shape, kind, rows):
+    # lse = -inf marks a (row, head) that attended to nothing: its query may be what the buffer held before
+    lens = [200, 129, 77]
+    cache = Cache(shape, lens, kind=kind, seed=150)
+    rng = np.random.default_rng(151)
+    cu_q = np.concatenate([[0], np.cumsum(rows)])
+    n, stride = int(cu_q[-1]), 210
+    q, before = queries(shape, n, 152), rng.random((3, stride)).astype(np.float32)
+    with Handle(shape, dtype=DTYPE[kind]) as h:
+        lse, want = np.full((n, shape.H), -np.inf, dtype=np.float32), before.astype(np.float64)
+        dead = rng.random((n, shape.H)) < 0.3
+        dead[cu_q[0]:cu_q[1]] = True                                     # sequence 0: nothing at all is added
+        for b in range(3):
+            v, kr = cache.values(b, lens[b])
+            for i in range(rows[b]):
+                m = lens[b] - (rows[b] - 1 - i)
+                lse[cu_q[b] + i] = ref.attend(q[cu_q[b] + i].astype(np.float64), v[:m], kr[:m], h.scale)[1]
+        lse[dead] = -np.inf
+        for b in range(3):
+            v, kr = cache.values(b, lens[b])
+            at = slice(cu_q[b], cu_q[b + 1])
+            want[b, :lens[b]] = ref.gathered(q[at].astype(np.float64), lse[at].astype(np.float64), v, kr, h.scale, before[b, :lens[b]], 0.5)
+        q[dead] = rng.choice(np.array([np.nan, np.inf, 3e38], dtype=np.float32), (int(dead.sum()), 1))
+        w_out = torch.full((3, stride), 7.0, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        call = gb.gva_q4_attention_weights if kind == "q4" else gb.gva_attention_weights
+        call(h.h, cache.c, dev(q), dev(lse), ints(cu_q), ints(lens), 0.5, dev(before), w_out, stride, 3, max(rows), 200, status)
+        assert int(status.item()) == 0
+        got = w_out.cpu().numpy().astype(np.float64)
+        assert np.array_equal(got[0, :200], before[0, :200].astype(np.float64) / 2)
+        for b in range(3):
+            assert np.max(np.abs(got[b, :lens[b]] - want[b, :lens[b]]) / np.maximum(want[b, :lens[b]], 1e-3)) <= 4e-5
+            assert np.all(got[b, lens[b]:] == 7)
+
+
 def test_weights_of_one_row_sum_to_the_number_of_heads():
     got = check_weights(wl.SHAPE_A, [3000], "q4", [1], decay=0.0, gain=3.0)
     assert abs(got[0, :3000].sum() - 16) <= 1e-4

@@ -397,7 +397,8 @@ int gva_q4_append_chunk(gva_handle *h, const gva_q4_cache *cache, const float *v
 
 /* Slots starts[b] .. seq_lens[b] - 1 (starts NULL: from 0) of every sequence as rows of a bf16 cache with the same page size,
  * same slots: value rows z + s c rounded once, positional rows as they are.  Nothing else of the bf16 cache changes.
- * max_seq_len sizes the launch (longer sequences are widened whole).  The two caches must not share memory. */
+ * max_seq_len sizes the launch (longer sequences are widened whole, those beyond either block table to its end, with
+ * GVA_ERR_SEQ_LEN).  The two caches must not share memory. */
 int gva_q4_widen(gva_handle *h, const gva_q4_cache *cache, const gva_cache *wide, const int32_t *starts, const int32_t *seq_lens,
                  int B, int max_seq_len, int32_t *dev_status, void *stream);
 

@@ -245,11 +245,13 @@ widen_q4_kernel(WidenParams p) {
     __shared__ int s_src[kWidenTokens], s_dst[kWidenTokens], s_slot[kWidenTokens];
     grid_dependency_wait();
     const int b = blockIdx.y, tid = threadIdx.x;
-    const int start = p.starts ? p.starts[b] : 0, len = p.seq_lens[b];
-    if (start < 0 || len < 0) {
+    const int start = p.starts ? p.starts[b] : 0, len_in = p.seq_lens[b];
+    const long long room = (long long)min(p.c.max_pages, p.max_pages) * p.P;     // slots that both block tables have
+    if (start < 0 || len_in < 0 || len_in > room) {
         if (blockIdx.x == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
-        return;
+        if (start < 0 || len_in < 0) return;
     }
+    const int len = (int)min((long long)len_in, room);
     const int shift = p.d_v == 64 ? 3 : 4, L = 1 << shift;   // lanes per row
     for (long long t0 = start + (long long)blockIdx.x * kWidenTokens; t0 < len; t0 += (long long)gridDim.x * kWidenTokens) {
         const int n = (int)min((long long)kWidenTokens, len - t0);

@@ -347,6 +347,31 @@ def test_widen_rounds_each_value_once_and_leaves_the_rest(shape, page, paged):
             assert np.array_equal(got[0], v) and np.array_equal(got[1], k)
 
 
+@pytest.mark.parametrize("wide_pages", [4, 3])
+def test_widen_of_lengths_beyond_the_block_tables_stops_at_their_end(wide_pages):
+    shape, page = wl.SHAPE_A, 64
+    cache = Cache(shape, [200, 256, 256, 64, 256], seed=160)
+    wide = Cache(shape, [64 * wide_pages] * 5, kind="bf16", seed=161)
+    lens = [200, 2 ** 31 - 1, 257, 64, 2 ** 31 - 1]
+    starts = [0, 70, 0, 3, 2 ** 31 - 5]
+    with Handle(shape) as h:
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        gb.gva_q4_widen(h.h, cache.c, wide.c, ints(starts), ints(lens), 5, 256, status)
+        code = int(status.item())
+        assert code & 0xFF == gb.GVA_ERR_SEQ_LEN and code >> 8 in ((1, 2, 4) if wide_pages == 4 else (0, 1, 2, 4))
+        v, k = [p.copy() for p in wide.pools]
+        for b in range(5):
+            n = min(lens[b], page * wide_pages)
+            if starts[b] >= n:
+                continue
+            t = np.arange(starts[b], n)
+            val, _ = cache.values(b, n)
+            v[wide.ids[b, t // page], :, t % page] = wl.f32_to_bf16_bits(val[t].astype(np.float32))
+            k[wide.ids[b, t // page], t % page] = ref.rows_of(cache.pools[2], cache.ids, b, n, page)[t]
+        got = wide.download()
+        assert np.array_equal(got[0], v) and np.array_equal(got[1], k)
+
+
 # ---- decode ----------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("shape", SHAPES)
 @pytest.mark.parametrize("num_splits", [0, 1, 5, 40])

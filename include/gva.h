@@ -441,7 +441,7 @@ int gva_q4_attention_weights(gva_handle *h, const gva_q4_cache *cache, const flo
  *                                  slots at or beyond seq_lens[b] are left as they were
  *   keep [B] i32, next_pos [B] i32 (position of the sequence's next token; NULL if recent = 0)
  *   new_lens [B] i32               n; may be seq_lens itself
- *   max_seq_len                    upper bound on seq_lens[] (here a longer sequence is an error)
+ *   max_seq_len                    upper bound on seq_lens[] (here a longer sequence is an error), 2^30 at most
  *   workspace                      gva_evict_workspace_bytes(h, B, max_seq_len) bytes, 256-byte aligned
  * Pages must belong to one sequence only.  keep[b] < 0 or a bad length -> GVA_ERR_SEQ_LEN, a bad page in the live range of a
  * sequence that would lose tokens -> GVA_ERR_BAD_PAGE: that sequence stays as it is (a bad length: its outputs too), with

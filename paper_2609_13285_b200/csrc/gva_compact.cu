@@ -63,6 +63,9 @@ int append_q4(gva_handle *h, const gva_q4_cache *cache, const float *v_new, cons
                                static_cast<cudaStream_t>(stream), p, h->rope));
 }
 
+// (lengths may be up to 2^31 - 1: a rounding up in 32 bits would overflow)
+inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
 // ---- 4-bit decode: which kernel, which grid ----
 using Q4DecodeFn = void (*)(DecodeParams, Q4Launch);
 struct Q4Kernel {
@@ -103,7 +106,7 @@ struct Q4Plan {
 Q4Plan q4_plan(const gva_handle *h, int B, int max_seq_len, int num_splits) {
     Q4Plan p;
     p.k = q4_kernel(h->cfg);
-    const long long tiles = (max_seq_len + p.k.tile - 1) / p.k.tile;
+    const long long tiles = ceil_div(max_seq_len, p.k.tile);
     p.num_splits = num_splits > 0 ? num_splits : tiles <= (B >= h->sm_count ? 8 : 4) ? 1 : 0;
     if (p.num_splits > 0) {
         p.teams = 1;
@@ -111,7 +114,7 @@ Q4Plan q4_plan(const gva_handle *h, int B, int max_seq_len, int num_splits) {
         p.n_rec = p.grid;
     } else {
         p.grid = (int)std::min<long long>(tiles * B, h->sm_count);
-        p.teams = (int)std::min<long long>(q4_consumers(h->cfg.d_v, h->cfg.G) / h->cfg.G, std::max<long long>(1, (tiles * B + p.grid - 1) / p.grid));
+        p.teams = (int)std::min<long long>(q4_consumers(h->cfg.d_v, h->cfg.G) / h->cfg.G, std::max(1ll, ceil_div(tiles * B, p.grid)));
         p.n_rec = (p.grid + B) * p.teams;
     }
     // the ring takes what the SM holds (one block per SM) or a third of it
@@ -166,7 +169,7 @@ int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_ab
     if (!q_abs || !lse || !seq_lens || !weights_out || stride < max_seq_len || !(decay >= 0.f) || std::isinf(decay)) return GVA_ERR_INVALID_ARG;
     if (!aligned(q_abs, 16) || !aligned(lse, 4) || !aligned(cu_q, 4) || !aligned(seq_lens, 4) || !aligned(weights_in, 4) || !aligned(weights_out, 4))
         return GVA_ERR_INVALID_ARG;
-    if (B > 8192 || (long long)B * ((stride + 31) / 32 + 1) >= (1ll << 30)) return GVA_ERR_UNSUPPORTED;     // (tiles are counted in 32 bits)
+    if (B > 8192 || B * (ceil_div(stride, 32) + 1) >= (1ll << 30)) return GVA_ERR_UNSUPPORTED;     // (tiles are counted in 32 bits)
     const gva_config &c = h->cfg;
     p.q = q_abs; p.lse = lse; p.cu_q = cu_q; p.seq_lens = seq_lens; p.decay = decay; p.w_in = decay > 0.f ? weights_in : nullptr; p.w_out = weights_out;
     p.stride = stride; p.B = B; p.max_q_len = max_q_len; p.H = c.H; p.G = c.G; p.P = c.page_size;
@@ -174,11 +177,11 @@ int attention_weights(gva_handle *h, WeightParams p, int kind, const float *q_ab
     p.dev_status = dev_status;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (kind == kCacheF32)
-        return launched(launch_pdl(c.d_v == 64 ? weights_f32_kernel<64> : weights_f32_kernel<128>, dim3((max_seq_len + kWeightTile - 1) / kWeightTile, B),
+        return launched(launch_pdl(c.d_v == 64 ? weights_f32_kernel<64> : weights_f32_kernel<128>, dim3((unsigned)ceil_div(max_seq_len, kWeightTile), B),
                                    dim3(256), 0, s, p, c.d_r));
     const bool multi = cu_q != nullptr && max_q_len > 1;
     const WeightKernel k = weight_kernel(kind, c, multi);
-    const long long tiles = (long long)B * ((max_seq_len + k.tile - 1) / k.tile);
+    const long long tiles = B * ceil_div(max_seq_len, k.tile);
     const int grid = (int)std::min<long long>(tiles, h->sm_count);
     WeightLaunch l;
     l.teams = std::max(1, kWeightConsumers / c.G);
@@ -209,6 +212,8 @@ int evict_cluster(const gva_handle *h, int B) {
     while (c < 8 && 2 * c * B <= h->sm_count) c *= 2;
     return c;
 }
+// The kernels count slots in 32 bits, ahead of the one in hand.
+constexpr int kEvictMost = 1 << 30;
 size_t evict_workspace(int B, int max_seq_len) {
     const size_t stride = ((size_t)max_seq_len / 2 + 64) / 64 * 64;
     return align_up((size_t)B * 4, 256) + 2 * align_up((size_t)B * stride * 4, 256);
@@ -224,7 +229,7 @@ int evict(gva_handle *h, const int32_t *block_table, int num_pages, int max_page
     if (!aligned(weights_in, 4) || !aligned(positions_in, 4) || !aligned(seq_lens, 4) || !aligned(keep, 4) || !aligned(next_pos, 4) ||
         !aligned(weights_out, 4) || !aligned(positions_out, 4) || !aligned(new_lens, 4))
         return GVA_ERR_INVALID_ARG;
-    if (B > 8192) return GVA_ERR_UNSUPPORTED;
+    if (B > 8192 || max_seq_len > kEvictMost) return GVA_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < evict_workspace(B, max_seq_len)) return GVA_ERR_WORKSPACE;
     if (!aligned(workspace, 256)) return GVA_ERR_INVALID_ARG;
     EvictParams p;
@@ -319,7 +324,7 @@ int gva_q4_widen(gva_handle *h, const gva_q4_cache *cache, const gva_cache *wide
     p.seq_lens = seq_lens;
     p.G = c.G; p.d_v = c.d_v; p.d_r = c.d_r; p.P = c.page_size;
     p.dev_status = dev_status;
-    return launched(launch_pdl(widen_q4_kernel, dim3((max_seq_len + kWidenTokens - 1) / kWidenTokens, B), dim3(256), 0,
+    return launched(launch_pdl(widen_q4_kernel, dim3((unsigned)ceil_div(max_seq_len, kWidenTokens), B), dim3(256), 0,
                                static_cast<cudaStream_t>(stream), p));
 }
 
@@ -402,7 +407,7 @@ int gva_q4_attention_weights(gva_handle *h, const gva_q4_cache *cache, const flo
 }
 
 size_t gva_evict_workspace_bytes(const gva_handle *h, int B, int max_seq_len) {
-    if (!h || B < 0 || max_seq_len < 0 || B > 8192) return 0;
+    if (!h || B < 0 || max_seq_len < 0 || B > 8192 || max_seq_len > kEvictMost) return 0;
     return evict_workspace(B, max_seq_len);
 }
 

@@ -854,6 +854,32 @@ def test_evict_with_a_negative_budget_hands_weights_and_positions_on(kind, T):
         assert all(np.array_equal(g.view(np.uint8), q.view(np.uint8)) for g, q in zip(cache.download(), cache.pools))
 
 
+def test_bounds_up_to_the_largest_number():
+    """max_seq_len is a bound: one that nobody made an effort for gives what a close one gives."""
+    shape, most = wl.SHAPE_A, 2 ** 31 - 1
+    lens = [200, 70]
+    cache, wide = Cache(shape, lens, seed=170), [Cache(shape, lens, kind="bf16", seed=171) for _ in range(2)]
+    q = queries(shape, 2, 172)
+    with Handle(shape) as h:
+        check_decode(h, cache, q, max_len=most)
+        for w, bound in zip(wide, (most, 200)):
+            gb.gva_q4_widen(h.h, cache.c, w.c, None, ints(lens), 2, bound)
+        assert all(np.array_equal(a, b) for a, b in zip(wide[0].download(), wide[1].download()))
+        for bound in (2 ** 30 + 1, most):
+            assert gb.gva_evict_workspace_bytes(h.h, 1, bound) == 0
+            w, i, ws = torch.zeros(1, 200, device="cuda"), ints([200]), torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+            assert gb.gva_q4_evict(h.h, cache.c, w, None, i, i, None, 0, 0, w, i, i, bound, ws, 1, bound, check=False) == gb.GVA_ERR_UNSUPPORTED
+    row = torch.empty(most, device="cuda")
+    for kind in ("q4", "f32"):
+        one = Cache(shape, [200], kind=kind, seed=173)
+        with Handle(shape, dtype=DTYPE[kind]) as h:
+            call = gb.gva_q4_attention_weights if kind == "q4" else gb.gva_attention_weights
+            near, lse = torch.zeros(200, device="cuda"), torch.full((1, shape.H), 5.0, device="cuda")
+            call(h.h, one.c, dev(q[:1]), lse, None, ints([200]), 0.0, None, near, 200, 1, 1, 200)
+            call(h.h, one.c, dev(q[:1]), lse, None, ints([200]), 0.0, None, row, most, 1, 1, most)
+            assert torch.equal(row[:200], near) and float(near.sum()) > 0
+
+
 # ---- refusals ----------------------------------------------------------------------------------------------------------
 def test_refusals():
     shape = wl.SHAPE_A

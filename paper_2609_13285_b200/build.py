@@ -1,6 +1,7 @@
 """Builds libgva.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
 from __future__ import annotations
 
+import hashlib
 import os
 import subprocess
 import sys
@@ -25,8 +26,9 @@ def _files(source: str):
     return [os.path.join(CSRC, f) for f in [source] + SOURCES[source]]
 
 
-def _object(source: str) -> str:
-    return os.path.join(CSRC, source[:-3] + ".o")
+def _object(source: str, command) -> str:
+    """The object of a source, named after the command that makes it, so that other flags never find it."""
+    return os.path.join(CSRC, f"{source[:-3]}.{hashlib.sha256(' '.join(command).encode()).hexdigest()[:12]}.o")
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -39,23 +41,29 @@ def build(force: bool = False, verbose: bool = False) -> str:
     flags = arch + ["-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
     if os.path.exists(os.path.join(CSRC, "gva_decode_mma.cuh")):
         flags.append("-DGVA_WITH_MMA")
-    flags += os.environ.get("GVA_EXTRA_NVCC_FLAGS", "").split()   # e.g. tuning macros such as -DGVA_MMA_WPG64=1
-    if verbose:
-        flags += ["-Xptxas", "-v"]
+    extra = os.environ.get("GVA_EXTRA_NVCC_FLAGS", "").split()   # e.g. tuning macros such as -DGVA_MMA_WPG64=1
+    compile_ = [nvcc, "-c"] + flags + extra
+    objects = {f: _object(f, compile_) for f in SOURCES}
     jobs = []                                                     # the sources are compiled side by side
-    for f in SOURCES:
-        if force or not _newer(_object(f), _files(f)):
-            cmd = [nvcc, "-c"] + flags + [os.path.join(CSRC, f), "-o", _object(f)]
-            jobs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+    for f, obj in objects.items():
+        if force or verbose or not _newer(obj, _files(f)):
+            part = f"{obj[:-2]}.{os.getpid()}.o"                  # takes its name once it is whole
+            cmd = compile_ + (["-Xptxas", "-v"] if verbose else []) + [os.path.join(CSRC, f), "-o", part]
+            jobs.append((subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True), part, obj))
     failed = False
-    for job in jobs:
+    for job, part, obj in jobs:
         said = job.communicate()[0]
-        failed |= job.returncode != 0
         if verbose or job.returncode != 0:
             sys.stderr.write(said)
+        if job.returncode == 0:
+            os.replace(part, obj)
+        else:
+            failed = True
+            if os.path.exists(part):
+                os.unlink(part)
     if failed:
         raise RuntimeError("nvcc failed building libgva.so")
-    link = subprocess.run([nvcc] + arch + ["-shared"] + [_object(f) for f in SOURCES] + ["-o", LIB], capture_output=True, text=True)
+    link = subprocess.run([nvcc] + arch + extra + ["-shared"] + list(objects.values()) + ["-o", LIB], capture_output=True, text=True)
     if link.returncode != 0:
         sys.stderr.write(link.stdout + link.stderr)
         raise RuntimeError("nvcc failed linking libgva.so")

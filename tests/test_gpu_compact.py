@@ -280,6 +280,19 @@ def test_append_chunk_of_one_group_with_the_widest_positional_slice(rows):
     check_chunk(G1R, rows, 300 + rows)
 
 
+@pytest.mark.parametrize("rows,offset", [(2, 0), (5, 1), (1000, 0)])
+@pytest.mark.parametrize("shape", [wl.SHAPE_A, wl.SHAPE_C, G1, G3])
+def test_append_chunk_of_several_rows_per_block(shape, rows, offset):
+    # 1000: as many rows as a block takes, one more block than that needs
+    check_chunk(shape, min(rows, 8192 // (shape.G * shape.d_v) + 1), 400 + rows, offset=offset)
+
+
+@pytest.mark.parametrize("rows", [2, 1000])
+@pytest.mark.parametrize("shape", [wl.SHAPE_B, wl.SHAPE_A0, wl.SHAPE_B0, G8, G2W])
+def test_append_chunk_of_several_rows_per_block_on_the_other_shapes(shape, rows):
+    check_chunk(shape, min(rows, 8192 // (shape.G * shape.d_v) + 1), 500 + rows, B=19, page=64, offset=1 if rows == 2 else 0)
+
+
 def test_append_reports_what_has_no_place_and_writes_the_rest():
     shape = wl.SHAPE_A
     cache = Cache(shape, [64] * 5, seed=7, room=64)
@@ -319,6 +332,27 @@ def test_append_at_is_append_where_slot_and_position_agree_and_turns_by_position
         gb.gva_append_cache_at(h.h, b.c, dev(x), dev(kr), ints([4, 4000, -1]), ints([-1, 3, 3]), 3, status)
         assert int(status.item()) & 0xFF == gb.GVA_ERR_SEQ_LEN
         assert all(np.array_equal(p.view(np.uint8), q.view(np.uint8)) for p, q in zip(before, b.download()))
+
+
+@pytest.mark.parametrize("kind,shape", [(k, s) for k in ("bf16", "fp8", "f32") for s in SHAPES + [G3] if not (k == "fp8" and s.d_r == 24)])
+def test_append_at_on_every_head_shape(kind, shape):
+    # the row that append writes at its position, in any slot, and nothing else
+    rng = np.random.default_rng(110)
+    B, slots, pos = 5, [0, 63, 64, 130, 7], [500, 0, 77, 130, 400]
+    x, kr = rng.standard_normal((B, shape.G, shape.d_v)).astype(np.float32), rng.standard_normal((B, shape.d_r)).astype(np.float32)
+    with Handle(shape, dtype=DTYPE[kind]) as h:
+        near, far = Cache(shape, [140] * B, kind=kind, seed=111), Cache(shape, [501] * B, kind=kind, seed=112)
+        keys = dev(kr) if shape.d_r else None
+        gb.gva_append_cache(h.h, far.c, dev(x), keys, ints(pos), B)
+        gb.gva_append_cache_at(h.h, near.c, dev(x), keys, ints(slots), ints(pos), B)
+        got, at, want = near.download(), far.download(), [p.copy() for p in near.pools]
+        for b in range(B):
+            for w, f in zip(want, at):
+                row = ref.rows_of(f, far.ids, b, 501, 64)[pos[b]]
+                pg, sl = near.ids[b, slots[b] // 64], slots[b] % 64
+                if w.ndim == 4: w[pg, :, sl] = row
+                else: w[pg, sl] = row
+        assert all(np.array_equal(g.view(np.uint8), w.view(np.uint8)) for g, w in zip(got, want))
 
 
 # ---- widen -----------------------------------------------------------------------------------------------------------
@@ -721,6 +755,58 @@ def test_weights_report_bad_lengths_and_pages():
         assert (code & 0xFF, code >> 8) in {(gb.GVA_ERR_BAD_PAGE, 1), (gb.GVA_ERR_SEQ_LEN, 2)}
         got = w.cpu().numpy()
         assert np.all(got[2] == 3) and np.all(got[1, 128:192] == 1.5) and np.all(got[1, :128] > 1.5) and np.all(got[1, 192:300] > 1.5)
+
+
+@pytest.mark.parametrize("rows", [1, 5])
+@pytest.mark.parametrize("kind", ["q4", "bf16", "fp8", "f32"])
+@pytest.mark.parametrize("shape", [wl.SHAPE_A, wl.SHAPE_B, wl.SHAPE_B0])
+def test_every_bit_of_a_query_counts(shape, kind, rows):
+    """Cached dims alternate between 1 and -1 and a query holds two numbers near 2^12 on a pair of them (a positional pair in every
+    other head), so that a score is what their last bits leave.
+
+    A score is then off by A = 2^12 softmax_scale times: 2 * 2^-24 for the product of both numbers with the scale, their two
+    roundings to the operands (2^-22 each in two f16 parts, 2^-24 in f32 or three bf16 parts), and 2^-23 for each of the four
+    additions that meet them (an accumulator that truncates).  Two bf16 parts would be off by up to 2 * 2^-18 A."""
+    lens = [100, 64]
+    cache = Cache(shape, lens, kind=kind, seed=120)
+    plus = np.where(np.arange(shape.d_v) % 2 == 0, 1.0, -1.0).astype(np.float32)
+    plus_r = np.where(np.arange(shape.d_r) % 2 == 0, 1.0, -1.0).astype(np.float32)
+    cast = {"q4": wl.f32_to_bf16_bits, "bf16": wl.f32_to_bf16_bits, "fp8": wl.f32_to_e4m3_bits, "f32": lambda a: a}[kind]
+    if kind == "q4":
+        cache.pools[0][:] = 0x02                                           # value = -1 + 1 * (2 or 0)
+        cache.pools[1][..., 0], cache.pools[1][..., 1] = 1, -1
+    else:
+        cache.pools[0][:] = cast(plus)
+    cache.pools[-1][:] = cast(plus_r)
+    cache.upload()
+    rng, n = np.random.default_rng(121), 2 * rows
+    q = np.zeros((n, shape.H, shape.d_v + shape.d_r), dtype=np.float32)
+    for r in range(n):
+        for h in range(shape.H):
+            first, width = (shape.d_v, shape.d_r) if shape.d_r and h % 2 else (0, shape.d_v)
+            i, j = 2 * rng.integers(0, width // 2), 2 * rng.integers(0, width // 2) + 1
+            q[r, h, first + i] = 4096 * (1 + rng.random() / 64)
+            q[r, h, first + j] = q[r, h, first + i] + np.float32(rng.standard_normal())
+    cu_q = [0, rows, n]
+    with Handle(shape, dtype=DTYPE[kind]) as h:
+        off = 4200 * h.scale * (2 * 2.0 ** -24 + 2 * (2.0 ** -22 if kind in ("q4", "fp8") else 2.0 ** -24) + 4 * 2.0 ** -23)
+        lse, want = np.zeros((n, shape.H), dtype=np.float32), []
+        for b in range(2):
+            v, kr = cache.values(b, lens[b])
+            at = slice(cu_q[b], cu_q[b + 1])
+            want.append(ref.gathered(q[at].astype(np.float64), lse[at].astype(np.float64), v, kr, h.scale, np.zeros(lens[b]), 0.0))
+        w = torch.zeros(2, 100, device="cuda")
+        call = gb.gva_q4_attention_weights if kind == "q4" else gb.gva_attention_weights
+        call(h.h, cache.c, dev(q), dev(lse), ints(cu_q), ints(lens), 0.0, None, w, 100, 2, rows, 100)
+        got = w.cpu().numpy().astype(np.float64)
+        for b in range(2):
+            assert np.max(np.abs(got[b, :lens[b]] / want[b] - 1)) <= off
+        if kind == "q4" and rows == 1:                                     # the decode kernel's scores, by its lse
+            for splits in (1, 2):
+                _, got, _ = decode(h, cache, q, num_splits=splits)
+                for b in range(2):
+                    _, l = ref.attend(q[b].astype(np.float64), *cache.values(b, lens[b]), h.scale)
+                    assert np.max(np.abs(got[b] - l)) <= off + 2.0 ** -22 * np.max(np.abs(l))
 
 
 # ---- eviction ----------------------------------------------------------------------------------------------------------

@@ -364,7 +364,8 @@ int gva_decode_tokens_ragged(gva_handle *h, const gva_cache *cache, const float 
  * The 4-bit cache.  A value row x[0 .. d_v) of one token and group is held as d_v codes of 4 bits and two f16 numbers:
  *     lowest z = the largest f16 <= min x,   step s = the smallest f16 with z + 15 s >= max x,
  *     code c = the number of k in 0 .. 14 with x >= z + (k + 1/2) s,   value = z + s c,   hence |value - x| <= s / 2.
- * Elements beyond +-65504 are clamped first; a row with a NaN anywhere reads as NaN; a row of one value has s = 0.
+ * Elements beyond +-65504 are clamped first; a row with a NaN anywhere reads as NaN (and attention that sees it gives NaN, however
+ * the sequence is split); a row of one value has s = 0.
  * Positional keys are bf16.  A token takes G (d_v / 2 + 4) + 2 d_r bytes: 176 against the bf16 cache's 544 with H = 16,
  * G = 4, d_v = 64, d_r = 16.  The calls take a handle with cache_dtype = GVA_BF16 (GVA_ERR_UNSUPPORTED otherwise), which
  * serves bf16 caches beside it: gva_q4_widen brings tokens into bf16 pages for the calls that have no 4-bit form
@@ -396,15 +397,16 @@ int gva_q4_append_chunk(gva_handle *h, const gva_q4_cache *cache, const float *v
                         const int32_t *ctx_lens, const int32_t *first_pos, int B, int n_q, int32_t *dev_status, void *stream);
 
 /* Slots starts[b] .. seq_lens[b] - 1 (starts NULL: from 0) of every sequence as rows of a bf16 cache with the same page size,
- * same slots: value rows z + s c rounded once, positional rows as they are.  Nothing else of the bf16 cache changes.
+ * same slots: value rows z + s c, rounded to f32 and then to bf16, positional rows as they are.  Nothing else of the bf16 cache changes.
  * max_seq_len sizes the launch (longer sequences are widened whole, those beyond either block table to its end, with
  * GVA_ERR_SEQ_LEN).  The two caches must not share memory. */
 int gva_q4_widen(gva_handle *h, const gva_q4_cache *cache, const gva_cache *wide, const int32_t *starts, const int32_t *seq_lens,
                  int B, int max_seq_len, int32_t *dev_status, void *stream);
 
 /* Decode attention over the 4-bit cache: arguments, splitting, outputs and errors as gva_decode (a tile whose page is bad
- * counts as empty).  Queries and softmax weights enter the products as two f16 numbers each, accumulation is f32: the
- * result is that of f32 arithmetic on the cached values.  Bitwise reproducible for fixed arguments.
+ * counts as empty).  Content queries and softmax weights enter the products as two f16 numbers each (22 bits), positional queries as
+ * three bf16 numbers, accumulation is f32: measured against 64 bits the result is as far off as that of f32 arithmetic on the cached
+ * values (1.3e-7 of its size over 1 M tokens, 1.1e-7 in f32).  Bitwise reproducible for fixed arguments.
  * Workspace: at least gva_q4_decode_workspace_bytes(h, B, max_seq_len, num_splits) bytes, 256-byte aligned. */
 size_t gva_q4_decode_workspace_bytes(const gva_handle *h, int B, int max_seq_len, int num_splits);
 int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, const int32_t *seq_lens, float *out, float *lse,
@@ -413,7 +415,10 @@ int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, 
 /* The attention every cached token has received, added up:
  *   weights_out[b][t] = decay * weights_in[b][t] + sum over the new rows r of sequence b that see slot t, and over all
  *                       heads, of exp(scale * score(r, head, t) - lse[r][head]),        t < seq_lens[b]
- * i.e. the softmax weights of the attention whose lse is given (a row whose lse is -inf adds nothing).
+ * i.e. the softmax weights of the attention whose lse is given (where lse is -inf nothing is added, whatever q_abs holds there).
+ * Queries enter the score products as three bf16 numbers each (24 bits) over a bf16 cache, as two f16 numbers (22 bits) over e4m3 and
+ * 4 bits (there the positional part as three bf16), accumulation is f32; over an f32 cache all is f32.  Measured against 64 bits: 2e-7
+ * of the weights over bf16, 5e-7 over e4m3, 1e-7 in plain f32 arithmetic.
  *   q_abs [rows][H][d_v+d_r], lse [rows][H] f32   as the attention call had and returned them
  *   cu_q  [B + 1] i32 or NULL    rows cu_q[b] .. cu_q[b+1] - 1 belong to sequence b, row i of q_len_b sees seq_lens[b] -
  *                                (q_len_b - 1 - i) slots; rows beyond the first max_q_len add nothing.  NULL: one row per sequence

@@ -96,8 +96,11 @@ void ring(int teams, size_t stage, size_t room, int *nstage, int *producers) {
 // The launch for B sequences of at most max_seq_len tokens.  num_splits = 0: where every sequence is a few tiles at most, one
 // block per sequence, which writes the result itself -- there is nothing to merge; else the balanced partition, one
 // block per SM with as many teams as there are tiles for.  num_splits >= 1: blocks of one team, num_splits per sequence.
-// (One block each against balanced, us: 1 x 97 tokens 5.8 / 9.1, 8 x 250 8.0 / 9.3, 64 x 250 9.2 / 10.7, 8 x 500 11.1 / 9.5; with
-// more sequences than SMs, 200 x 500 15.6 / 19.2.)
+// One block each against balanced, us, narrow heads (G = 4, d_v = 64): in tiles of 64 tokens 64 x 256 9.2 / 11.6, 64 x 512 12.4 / 12.3,
+// 64 x 640 15.0 / 12.7; of 32 64 x 128 9.2 / 11.8, 64 x 256 9.6 / 11.7, 64 x 384 12.3 / 11.8; 200 sequences of 512 15.4 / 19.1 and 17.4 / 20.7.
+// Wide heads (G = 8, d_v = 128): 8 x 128 11.5 / 11.9, 8 x 256 16.1 / 12.0, 64 x 128 13.3 / 14.4, 64 x 256 21.4 / 17.2, 200 x 512 39.6 / 46.3:
+// there two tiles would be the better border.  The rule goes by max_seq_len, as every launch does: a captured graph that allows for long
+// sequences takes the balanced form for short ones too.
 struct Q4Plan {
     Q4Kernel k;
     int num_splits, grid, teams, nstage, producers, n_rec;

@@ -21,8 +21,10 @@ namespace gva {
 // move: blocks copy the rows of the moves in 16-byte pieces, weights and positions with them.
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictBins = 2048;
-constexpr int kEvictAlone = 8192;        // sequences up to this length: one block selects (three of 1500: a cluster of eight took 7 us
-                                         // longer, for the histograms read from one another and the meetings)
+// Sequences up to this length: one block selects, since a cluster has histograms to read from one another and to meet for them.  One
+// block against a cluster, us for a 4-bit eviction to three quarters: 1 x 1536 tokens 13.6 / 19.9, 1 x 4096 16.7 / 21.7,
+// 1 x 8192 21.6 / 21.6; 3 x 4096 17.1 / 22.2, 3 x 8192 22.7 / 22.9; 32 x 4096 20.0 / 21.6, 32 x 6000 23.0 / 22.9, 32 x 8192 26.4 / 24.4.
+constexpr int kEvictAlone = 8192;
 constexpr int kEvictMoveHere = 2;        // up to so many batches of moves per block: rows are moved by the selecting cluster
 constexpr int kEvictKeysMax = 32768;     // keys of one block that are kept in shared memory; beyond, they are made again
 

@@ -38,7 +38,7 @@ __device__ __forceinline__ int locate_page(const int32_t *block_table, int num_p
 // d_v / 8 neighbouring lanes hold one value row, eight elements each (two 16-byte loads), reduce minimum and maximum with
 // shuffles, and each writes its eight codes as one 32-bit word.  A block takes as many input rows as give every thread four such
 // shares, asks for all of them at once and looks up where they go while they are quantised (65536 rows of 8 x 128: 72 us, 4.4 TB/s
-// of rows in and codes out; bound by issue slots, some 190 instructions per share and warp).  Its threads rotate the positional pairs in fp64.
+// of rows in and codes out; issue slots 69 % busy with some 190 instructions per share and warp, no pipe above 46 %).  Its threads rotate the positional pairs in fp64.
 // All comparisons against the borders z + (k + 1/2) s are exact in f32: 15 s and (k + 1/2) s have at most 16 significant
 // bits, and "x - z >= T" for an f32 number T holds exactly if it holds for x - z rounded down (max - z <= 15 s: up).
 struct AppendQ4Params {
@@ -225,7 +225,7 @@ append_q4_kernel(const __grid_constant__ AppendQ4Params p, const __grid_constant
 }
 
 // ---- widen ------------------------------------------------------------------------------------------------------
-// Slots [starts[b], seq_lens[b]) of every sequence as bf16 rows of another cache: z + s c in f32, rounded once.  A block
+// Slots [starts[b], seq_lens[b]) of every sequence as bf16 rows of another cache: z + s c rounded to f32, then to bf16.  A block
 // takes 64 slots of one sequence; d_v / 8 lanes widen one row, 4 bytes in and 16 bytes out per lane, neighbouring slots of
 // a group one after the other, so that reads and writes run through a page's rows in order; four shares of a thread are asked
 // for at a time (64 K tokens of wide heads: 46 us, 3.9 TB/s; one share at a time 76).

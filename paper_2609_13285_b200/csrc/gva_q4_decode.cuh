@@ -124,7 +124,7 @@ constexpr uint32_t kCodeLow = 0x003c003cu, kCodeHigh = 0x03c003c0u;
 
 // One group's four queries as the score product's B fragments, for the MMA column n = lane / 4 = 2 head + {hi, lo}, scaled
 // by `factor` (softmax scale and log2 e).  Content: q 2^-e 2^10 with |q 2^-e| <= 1, times 16 where the code stands in the low
-// nibble; unscale = 2^(e + 10) of the head whose scores this lane holds (lane % 4); sum = sum of that head's content query.
+// nibble; unscale = 2^(e + 8) of the head whose scores this lane holds (lane % 4); sum = sum of that head's content query.
 // Position: the keys are bf16 and so are the query's parts, of which two carry 16 bits only (2^-17 of every term); the third
 // stands in r2, in the hi columns, for one more MMA per 16 tokens.
 template <class T>
@@ -153,7 +153,7 @@ __device__ __forceinline__ void load_q4_query(Q4Query<T> &out, const float *q /*
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    // 2^e >= top, with e held inside what keeps 2^-e 2^14 and 2^(e + 10) finite
+    // 2^e >= top, with e held inside what keeps 2^-e 2^14 and 2^(e + 8) finite
     int e = (int)((__float_as_uint(top) >> 23) & 255u) - 126;
     e = min(max(e, -100), 110);
     const float down = __uint_as_float((uint32_t)(127 - e + 10) << 23), down16 = 16.f * down;
@@ -371,7 +371,7 @@ struct Q4Launch {
 };
 constexpr int kQ4Producers = 4;           // producer warps of a block at most
 // Consumer warps of a block at most: 12, which leaves a thread 128 registers, where that is three teams or more, else 16 with 96
-// (1 M tokens, G = 4: 67 us with 12, 70 with 16, 75 with 8; wide heads, G = 8: 142 with 8, 133 with 16).
+// (1 M tokens, G = 4: 66.3 us with 12, 67.8 with 16, 75.4 with 8; 0.55 M tokens of wide heads, G = 8: 142.7 with 8, 136.7 with 16).
 __host__ __device__ constexpr int q4_consumers(int d_v, int G) { return d_v == 64 && G <= 4 ? 12 : 16; }
 
 template <int DV, int DR, int TILE, int CONSUMERS>

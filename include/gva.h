@@ -418,7 +418,7 @@ int gva_q4_decode(gva_handle *h, const gva_q4_cache *cache, const float *q_abs, 
  * i.e. the softmax weights of the attention whose lse is given (where lse is -inf nothing is added, whatever q_abs holds there).
  * Queries enter the score products as three bf16 numbers each (24 bits) over a bf16 cache, as two f16 numbers (22 bits) over e4m3 and
  * 4 bits (there the positional part as three bf16), accumulation is f32; over an f32 cache all is f32.  Measured against 64 bits: 2e-7
- * of the weights over bf16, 5e-7 over e4m3, 1e-7 in plain f32 arithmetic.
+ * of the weights, 1e-7 in plain f32 arithmetic.
  *   q_abs [rows][H][d_v+d_r], lse [rows][H] f32   as the attention call had and returned them
  *   cu_q  [B + 1] i32 or NULL    rows cu_q[b] .. cu_q[b+1] - 1 belong to sequence b, row i of q_len_b sees seq_lens[b] -
  *                                (q_len_b - 1 - i) slots; rows beyond the first max_q_len add nothing.  NULL: one row per sequence

@@ -184,6 +184,7 @@ template <int KIND, class T>
 __device__ __forceinline__ void score_plain(const unsigned char *v, const unsigned char *kr_row, uint32_t kr, int c, const PlainQuery<KIND, T> &q, float (&x)[2][2]) {
     float acc[2][4];
     if constexpr (KIND == kCacheBf16) {
+        float low[2][4];                                     // the third parts, apart: see score_pair
 #pragma unroll
         for (int j = 0; j < T::DV / 32; ++j) {
             uint4 a[2], b[2];
@@ -195,14 +196,15 @@ __device__ __forceinline__ void score_plain(const unsigned char *v, const unsign
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const uint32_t f[4] = {a[k].x, b[k].x, a[k].y, b[k].y};
-                if (j == 0) mma_bf16_first(acc[k], f, q.v2[2 * j][0], q.v2[2 * j][1]);
-                else mma_bf16(acc[k], f, q.v2[2 * j][0], q.v2[2 * j][1]);
-                mma_bf16(acc[k], f, q.v[2 * j][0], q.v[2 * j][1]);
+                if (j == 0) mma_bf16_first(low[k], f, q.v2[2 * j][0], q.v2[2 * j][1]);
+                else mma_bf16(low[k], f, q.v2[2 * j][0], q.v2[2 * j][1]);
+                if (j == 0) mma_bf16_first(acc[k], f, q.v[2 * j][0], q.v[2 * j][1]);
+                else mma_bf16(acc[k], f, q.v[2 * j][0], q.v[2 * j][1]);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const uint32_t f[4] = {a[k].z, b[k].z, a[k].w, b[k].w};
-                mma_bf16(acc[k], f, q.v2[2 * j + 1][0], q.v2[2 * j + 1][1]);
+                mma_bf16(low[k], f, q.v2[2 * j + 1][0], q.v2[2 * j + 1][1]);
                 mma_bf16(acc[k], f, q.v[2 * j + 1][0], q.v[2 * j + 1][1]);
             }
         }
@@ -213,7 +215,7 @@ __device__ __forceinline__ void score_plain(const unsigned char *v, const unsign
 #pragma unroll
             for (int k = 0; k < 2; ++k) ldsm_x4(kr + k * 16 * T::KR_ROW + 32 * u, f[k]);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) mma_bf16(acc[k], f[k], q.r2[u][0], q.r2[u][1]);
+            for (int k = 0; k < 2; ++k) mma_bf16(low[k], f[k], q.r2[u][0], q.r2[u][1]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) mma_bf16(acc[k], f[k], q.r[u][0], q.r[u][1]);
         }
@@ -222,10 +224,14 @@ __device__ __forceinline__ void score_plain(const unsigned char *v, const unsign
             for (int k = 0; k < 2; ++k) {
                 uint32_t t[2];
                 ldsm_x2(kr + k * 16 * T::KR_ROW + 32 * FULL, t);
-                mma_bf16_k8(acc[k], t, q.r2[FULL][0]);
+                mma_bf16_k8(low[k], t, q.r2[FULL][0]);
                 mma_bf16_k8(acc[k], t, q.r[FULL][0]);
             }
         }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[k][i] += low[k][i];
     } else {
 #pragma unroll
         for (int j = 0; j < T::DV / 64; ++j) {
@@ -383,18 +389,23 @@ __device__ __forceinline__ void load_pair(PairQuery<KIND, T> &out, const float *
 // Scores of one chunk: x[0], x[1]: token row tok_lo, columns 2 c, 2 c + 1; x[2], x[3]: the row eight further.
 template <int KIND, class T>
 __device__ __forceinline__ void score_pair(const unsigned char *v, const unsigned char *kr_row, uint32_t kr, const __half2 *sz /* of row tok_lo */, int c, const PairQuery<KIND, T> &q, float (&x)[4]) {
-    float acc[4];
-    auto both = [&](bool first, const uint32_t (&f)[4], int j) {
+    // The low parts have an accumulator of their own: every MMA truncates its sum to what it is aligned to, the largest of its terms.  Over
+    // codes that is 2^-14, the exponent that a subnormal counts for, which cuts up to eight bits more off.  (Eight rows, 700 tokens, against 64 bits: 4 bits 3.5e-7 -> 1.6e-7 rms, bf16 3.9e-7 -> 2.1e-7, e4m3 3.6e-7 ->
+    // 1.9e-7; two short chains of MMAs are faster than a long one besides: 1 M tokens in 4 bits 410 -> 384 us, bf16 483 -> 451, e4m3 398 -> 364.)
+    float acc[4], acc_lo[4];
+    auto mma = [&](float (&to)[4], bool first, const uint32_t (&f)[4], const uint32_t (&b)[2]) {
         if constexpr (KIND == kCacheBf16) {
-            if (first) mma_bf16_first(acc, f, q.low[j][0], q.low[j][1]);
-            else mma_bf16(acc, f, q.low[j][0], q.low[j][1]);
-            mma_bf16(acc, f, q.lo[j][0], q.lo[j][1]);
-            mma_bf16(acc, f, q.hi[j][0], q.hi[j][1]);
+            if (first) mma_bf16_first(to, f, b[0], b[1]);
+            else mma_bf16(to, f, b[0], b[1]);
         } else {
-            if (first) mma_f16_first(acc, f[0], f[1], f[2], f[3], q.lo[j][0], q.lo[j][1]);
-            else mma_f16_q4(acc, f[0], f[1], f[2], f[3], q.lo[j][0], q.lo[j][1]);
-            mma_f16_q4(acc, f[0], f[1], f[2], f[3], q.hi[j][0], q.hi[j][1]);
+            if (first) mma_f16_first(to, f[0], f[1], f[2], f[3], b[0], b[1]);
+            else mma_f16_q4(to, f[0], f[1], f[2], f[3], b[0], b[1]);
         }
+    };
+    auto both = [&](bool first, const uint32_t (&f)[4], int j) {
+        if constexpr (KIND == kCacheBf16) mma(acc_lo, first, f, q.low[j]);
+        mma(acc_lo, first && KIND != kCacheBf16, f, q.lo[j]);
+        mma(acc, first, f, q.hi[j]);
     };
     if constexpr (KIND == kCacheQ4) {
 #pragma unroll
@@ -436,8 +447,8 @@ __device__ __forceinline__ void score_pair(const unsigned char *v, const unsigne
             uint32_t f[4];
             e4m3_words(*reinterpret_cast<const uint32_t *>(row), f[0], f[2]);
             e4m3_words(*reinterpret_cast<const uint32_t *>(row + 8 * T::KR_ROW), f[1], f[3]);
-            mma_f16_q4(acc, f[0], f[1], f[2], f[3], q.rlo[u][0], q.rlo[u][1]);
-            mma_f16_q4(acc, f[0], f[1], f[2], f[3], q.rhi[u][0], q.rhi[u][1]);
+            mma(acc_lo, false, f, q.rlo[u]);
+            mma(acc, false, f, q.rhi[u]);
         }
     } else {
         float rot[4] = {0.f, 0.f, 0.f, 0.f};
@@ -461,17 +472,17 @@ __device__ __forceinline__ void score_pair(const unsigned char *v, const unsigne
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float2 z = i < 2 ? a : b;
-                x[i] = fmaf(acc[i] * q.unscale[i & 1], z.x, fmaf(z.y, q.sum[i & 1], rot[i]));
+                x[i] = fmaf((acc[i] + acc_lo[i]) * q.unscale[i & 1], z.x, fmaf(z.y, q.sum[i & 1], rot[i]));
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = (acc[i] + rot[i]) * q.unscale[i & 1];
+            for (int i = 0; i < 4; ++i) x[i] = (acc[i] + (acc_lo[i] + rot[i])) * q.unscale[i & 1];
         }
         return;
     }
     if constexpr (KIND == kCacheE4m3) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = acc[i] * q.unscale[i & 1];
+        for (int i = 0; i < 4; ++i) x[i] = (acc[i] + acc_lo[i]) * q.unscale[i & 1];
     }
 }
 
@@ -515,7 +526,7 @@ struct WeightLaunch {
     int split;                      // several rows: teams that share their tiles and split the rows; 1 otherwise
     int batch;                      // several rows: tiles that such teams take at once, nstage / (teams / split)
 };
-constexpr int kWeightConsumers = 16;      // warps of a block (12 with more registers: 56.2 against 50.5 us on the 1 M token batch, 89.7 against 84.1 with 32 rows)
+constexpr int kWeightConsumers = 16;      // warps of a block (12 with more registers: 56.2 against 50.4 us on the 1 M token batch, 81.0 against 80.6 with 32 rows)
 
 template <int KIND, int DV, int DR, int TILE, bool MULTI>
 __global__ void __launch_bounds__(32 * (kWeightConsumers + kQ4Producers), 1)

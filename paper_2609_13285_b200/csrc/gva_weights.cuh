@@ -390,8 +390,9 @@ __device__ __forceinline__ void load_pair(PairQuery<KIND, T> &out, const float *
 template <int KIND, class T>
 __device__ __forceinline__ void score_pair(const unsigned char *v, const unsigned char *kr_row, uint32_t kr, const __half2 *sz /* of row tok_lo */, int c, const PairQuery<KIND, T> &q, float (&x)[4]) {
     // The low parts have an accumulator of their own: every MMA truncates its sum to what it is aligned to, the largest of its terms.  Over
-    // codes that is 2^-14, the exponent that a subnormal counts for, which cuts up to eight bits more off.  (Eight rows, 700 tokens, against 64 bits: 4 bits 3.5e-7 -> 1.6e-7 rms, bf16 3.9e-7 -> 2.1e-7, e4m3 3.6e-7 ->
-    // 1.9e-7; two short chains of MMAs are faster than a long one besides: 1 M tokens in 4 bits 410 -> 384 us, bf16 483 -> 451, e4m3 398 -> 364.)
+    // codes that is 2^-14, the exponent that a subnormal counts for, which cuts up to eight bits more off.  (Eight rows, 700 tokens,
+    // against 64 bits, rms: 4 bits 3.5e-7 -> 1.6e-7, bf16 3.9e-7 -> 2.1e-7, e4m3 3.6e-7 -> 1.9e-7.  Two short chains of MMAs are also
+    // faster than a long one: 1 M tokens in 4 bits 410 -> 384 us, bf16 483 -> 451, e4m3 398 -> 364.)
     float acc[4], acc_lo[4];
     auto mma = [&](float (&to)[4], bool first, const uint32_t (&f)[4], const uint32_t (&b)[2]) {
         if constexpr (KIND == kCacheBf16) {

@@ -1196,3 +1196,58 @@ def test_a_captured_step_replays_on_new_lengths(kind):
             for a, b in zip(*results):
                 assert torch.equal(torch.nan_to_num(a.float(), nan=-77.0), torch.nan_to_num(b.float(), nan=-77.0))
         del graph
+
+
+def test_two_chains_at_once_on_two_streams_of_one_handle():
+    """append, decode, gather (one row and several), evict, widen: two batches on two streams, nothing shared but the handle; what
+    each leaves is what it leaves alone, bit for bit."""
+    shape, page, steps = wl.SHAPE_A, 64, 6
+    with Handle(shape, page) as h:
+        def batch(i):
+            B, T = (3, 1500) if i == 0 else (40, 260)
+            rng = np.random.default_rng(180 + i)
+            cache = Cache(shape, [T - 9 * (b % 5) for b in range(B)], seed=182 + i, room=64)
+            wide = Cache(shape, [1] * B, kind="bf16", seed=184 + i, room=cache.max_pages * page - 1)
+            stride = cache.max_pages * page
+            x = [dev(rng.standard_normal((B, 4, 64)).astype(np.float32)) for _ in range(steps)]
+            kr, q = dev(rng.standard_normal((B, 16)).astype(np.float32)), dev(queries(shape, 2 * B, 186 + i))
+            seq, pos, keep = ints(cache.lens), ints(np.array(cache.lens) + 100), ints([T // 2 + 3 * b for b in range(B)])
+            cu = ints(2 * np.arange(B + 1))
+            out, lse, lse2 = torch.zeros(B, 16, 64, device="cuda"), torch.zeros(B, 16, device="cuda"), torch.full((2 * B, 16), 6.0, device="cuda")
+            w, p = torch.zeros(B, stride, device="cuda"), torch.zeros(B, stride, dtype=torch.int32, device="cuda")
+            ws = torch.zeros(gb.gva_q4_decode_workspace_bytes(h.h, B, stride), dtype=torch.uint8, device="cuda")
+            ews = torch.zeros(gb.gva_evict_workspace_bytes(h.h, B, stride), dtype=torch.uint8, device="cuda")
+
+            def step(k):
+                gb.gva_q4_append(h.h, cache.c, x[k], kr, seq, pos, B)
+                seq.add_(1)
+                pos.add_(1)
+                gb.gva_q4_decode(h.h, cache.c, q, seq, out, lse, ws, B, stride)
+                gb.gva_q4_attention_weights(h.h, cache.c, q, lse, None, seq, 0.5, w, w, stride, B, 1, stride)
+                gb.gva_q4_attention_weights(h.h, cache.c, q, lse2, cu, seq, 1.0, w, w, stride, B, 2, stride)
+                if k % 2:
+                    gb.gva_q4_evict(h.h, cache.c, w, p, seq, keep, pos, 1, 3, w, p, seq, stride, ews, B, stride)
+                gb.gva_q4_widen(h.h, cache.c, wide.c, None, seq, B, stride)
+
+            def left():
+                return [t.clone() for t in (out, lse, w, p, seq, *cache.d, *wide.d)]
+            return step, left
+
+        alone = []
+        for i in range(2):
+            step, left = batch(i)
+            for k in range(steps):
+                step(k)
+            torch.cuda.synchronize()
+            alone.append(left())
+        both = [batch(i) for i in range(2)]
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        torch.cuda.synchronize()
+        for k in range(steps):
+            for (step, _), s in zip(both, streams):
+                with torch.cuda.stream(s):
+                    step(k)
+        torch.cuda.synchronize()
+        for want, (_, left) in zip(alone, both):
+            for a, b in zip(want, left()):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))

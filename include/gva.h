@@ -54,7 +54,9 @@ typedef enum {
     GVA_ERR_BAD_PAGE = 5,     /* [device] block-table entry outside [0, num_pages) in the live range     */
     GVA_ERR_SEQ_LEN = 6,      /* [device] seq_len < 0 or beyond max_pages_per_seq * page_size            */
     GVA_ERR_TIMEOUT = 7,      /* [device] a bounded wait on an asynchronous copy expired                 */
-    GVA_ERR_STATIC_LIMIT = 8  /* gva_decode_static: the request needs more than GVA_STATIC_SCRATCH_BYTES  */
+    GVA_ERR_STATIC_LIMIT = 8, /* gva_decode_static: the request needs more than GVA_STATIC_SCRATCH_BYTES  */
+    GVA_ERR_NO_ROOM = 9,      /* [device] gva_assign_pages: not enough free pages or rows for a sequence  */
+    GVA_ERR_TREE = 10         /* [device] a node's parent is not a node before it, or a tree has more nodes than max_q_len */
 } gva_status;
 
 /* Element type of the cache pools.  GVA_E4M3 stores every cache element as one byte (sign, 4 exponent bits with bias 7,
@@ -460,6 +462,131 @@ int gva_q4_evict(gva_handle *h, const gva_q4_cache *cache, const float *weights_
                  const int32_t *keep, const int32_t *next_pos, int sinks, int recent, float *weights_out, int32_t *positions_out,
                  int32_t *new_lens, int stride, void *workspace, size_t workspace_bytes, int B, int max_seq_len, int32_t *dev_status,
                  void *stream);
+
+/* ---- A step with drafted tokens: pages and slots, rows by slot map, attention of a tree, commit -----------------------
+ * (Not in the paper, whose steps add one token: this library's calls for serving programs that draft several continuations of
+ * every sequence as a tree, look at all of them in one step and keep the path the model agrees with.)  One step in order:
+ *   gva_assign_pages -> gva_tree_masks -> gva_absorb_query(q_pos = positions) -> gva_append_rows -> gva_decode_tree -> the rest of the
+ *   model -> gva_tree_commit;
+ * the first and gqa_append serve single tokens and prompts as well.  All of them want the handle's device to be the current
+ * one (GVA_ERR_INVALID_ARG otherwise), use no state of the handle on the device, and may be captured into CUDA graphs and
+ * replayed; calls on different streams may overlap as long as they share no workspace, no output and no page that one of them
+ * writes.  B is 8192 at most; num_pages * page_size is below 2^31. */
+
+/* Pages for the tokens that sequences are about to get, pages back from those that need fewer, and a position and a slot for every
+ * new row.  The free pages are a ring of num_pages entries: free_in / free_out [2] = (entry of the first free page, how many there
+ * are); pages are taken from its front in the order of sequences and returned to its end.
+ *   used     [B] i32   tokens that sequence b holds
+ *   want     [B] i32   tokens it is to have room for: used + new rows; fewer than used (0 once it is done) returns its pages
+ *   pages_in / pages_out [B] i32   pages in its row of the block table, before and after: ceil(want / page_size) afterwards
+ *   block_table [B][max_pages_per_seq]   entries pages_in[b] and on are filled in for pages taken; nothing else in it changes
+ *   new_lens [B]       want[b], or used[b] where the sequence was not served
+ *   cu_q     [B + 1]   rows cu_q[b] .. cu_q[b+1] - 1 are the new tokens of b, max(want - used, 0) of them
+ *   positions, slots [max_rows]   of every row: its position used[b] + i, and its place page * page_size + position % page_size
+ *                      (-1 if the block table holds a bad page there).  Rows at or beyond cu_q[B] are left as they were
+ * pages_out may be pages_in, new_lens may be used, free_out may be free_in; nothing else overlaps.
+ * Sequences that grow are served in order as long as free pages and rows suffice: the first that does not fit, and all growing
+ * ones after it, stay as they are (GVA_ERR_NO_ROOM with the index of one of them).  Pages returned by a call are there for the next one.
+ * used < 0, want < 0, pages_in outside [0, max_pages_per_seq], used beyond those pages or want beyond the block table -> GVA_ERR_SEQ_LEN,
+ * the sequence stays as it is.  A ring state outside its range -> GVA_ERR_BAD_PAGE, everything stays as it is; more pages returned
+ * than the ring has room for -> GVA_ERR_BAD_PAGE, those beyond it are lost.  Pages must belong to one sequence only. */
+int gva_assign_pages(gva_handle *h, const int32_t *used, const int32_t *want, const int32_t *pages_in, int32_t *pages_out, int32_t *block_table,
+                     int max_pages_per_seq, int num_pages, int32_t *free_ring, const int32_t *free_in, int32_t *free_out, int32_t *new_lens,
+                     int32_t *cu_q, int32_t *positions, int32_t *slots, int max_rows, int B, int32_t *dev_status, void *stream);
+
+/* What the nodes of trees see of one another.  Row cu_q[b] + i is node i of sequence b's tree; its parent is a node before it, or
+ * -1: a first token behind the context.
+ *   parents   [rows] i32   number of the parent within the tree, below the node's own; or -1
+ *   mask      [rows][mask_words] u32   bit j of a row (bit j % 32 of word j / 32) is set iff node j is the row's node or one of its ancestors
+ *   positions [rows] i32 or NULL   ctx_lens[b] + number of ancestors
+ * mask_words >= ceil(max_q_len / 32), 8 at most; max_q_len = nodes of a tree at most, 256 at most.  A tree with a bad parent or more
+ * than max_q_len nodes -> GVA_ERR_TREE, its rows are left as they were. */
+int gva_tree_masks(gva_handle *h, const int32_t *parents, const int32_t *cu_q, const int32_t *ctx_lens, uint32_t *mask, int mask_words,
+                   int32_t *positions, int B, int max_q_len, int32_t *dev_status, void *stream);
+
+/* How far a rotation turns: pair i of d_rot / 2 by position * f_i, with f_i from base^(-2 i / d_rot):
+ *   GVA_ROPE_PLAIN    f_i
+ *   GVA_ROPE_LINEAR   f_i / factor                                  (positions closer together)
+ *   GVA_ROPE_BASE     with base * factor^(d_rot / (d_rot - 2)) for base: the slowest pair by 1 / factor, the fastest as it was
+ *   GVA_ROPE_PARTS    f_i (g + (1 - g) / factor), g = (original_len f_i / 2 pi - low) / (high - low) held to [0, 1]: pairs that turn
+ *                     more than `high` times over the original context stay, those below `low` turns are divided
+ * Pair i is elements (2 i, 2 i + 1) (GVA_ROPE_PAIRS) or (i, i + d_rot / 2) (GVA_ROPE_HALVES) of the first d_rot; what is rotated is
+ * multiplied by magnitude.  factor >= 1 (unused with PLAIN); original_len > 0 and 0 <= low < high with PARTS, unused otherwise. */
+typedef enum { GVA_ROPE_PAIRS = 0, GVA_ROPE_HALVES = 1 } gva_rope_layout;
+typedef enum { GVA_ROPE_PLAIN = 0, GVA_ROPE_LINEAR = 1, GVA_ROPE_BASE = 2, GVA_ROPE_PARTS = 3 } gva_rope_scaling;
+typedef struct {
+    int32_t layout;        /* gva_rope_layout                                                            */
+    int32_t d_rot;         /* elements of a head that turn, even                                         */
+    int32_t scaling;       /* gva_rope_scaling                                                           */
+    int32_t original_len;  /* context that PARTS counts turns over                                       */
+    double base, factor, low, high;
+    float magnitude;       /* 1                                                                          */
+    int32_t reserved;      /* set to 0                                                                   */
+} gva_rope;
+/* [host] The f_i of a rotation: d_rot / 2 numbers. */
+int gva_rope_frequencies(const gva_rope *rope, double *inv_freq);
+/* [host] The rotation of the positional slice, for every call on this handle from now on that rotates one (absorb, appends of every kind,
+ * the projections, the fused steps); after gva_create it is PAIRS, PLAIN with cfg.rope_base.  d_rot = cfg.d_r, PAIRS and magnitude 1 only
+ * (GVA_ERR_UNSUPPORTED otherwise).  Calls that were captured before keep the rotation they were captured with. */
+int gva_set_rope(gva_handle *h, const gva_rope *rope);
+/* [host] The rotation of gqa_append on this handle; after gva_create it is PAIRS, PLAIN with cfg.rope_base over the whole head.
+ * d_rot a multiple of 8, cfg.d_v at most (GVA_ERR_UNSUPPORTED otherwise). */
+int gqa_set_rope(gva_handle *h, const gva_rope *rope);
+
+/* Rows of the matched GQA cache by slot map: keys are rotated to their positions and written with their values, queries are
+ * rotated for gqa_decode.  Any mixture of sequences, of single tokens and prompts.
+ *   q [n][H][d_h], k_new, v_new [n][G][d_h] f32   with q_stride, k_stride, v_stride elements from row to row (multiples of 4, so that one
+ *                      packed projection [n][H + 2 G][d_h] serves all three); q and q_out may both be NULL
+ *   pos, slots [n] i32 position and place page * page_size + slot of every row; slots < 0: a padded row, of which nothing is cached
+ *   q_out [n][H][d_h] f32   rotated queries of all rows, padded ones too; may be q where q_stride = H d_h
+ * The angle is reduced to a fraction of a turn in fp64, sine and cosine are f32, and so are the two products and the sum of an element;
+ * keys and values are rounded once to the cache dtype (nearest even; e4m3 saturates).  All pointers are 16-byte aligned
+ * (pos and slots 4).  A slot beyond the pool -> GVA_ERR_BAD_PAGE, pos < 0 with a slot -> GVA_ERR_SEQ_LEN, each with the row's
+ * number in the place of a sequence's: that row is not cached.  Two rows with the same slot leave either's elements.  cache->block_table
+ * and max_pages_per_seq are not used. */
+int gqa_append(gva_handle *h, const gqa_cache *cache, const float *q, int64_t q_stride, const float *k_new, int64_t k_stride,
+               const float *v_new, int64_t v_stride, const int32_t *pos, const int32_t *slots, float *q_out, int n,
+               int32_t *dev_status, void *stream);
+
+/* Rows of the GVA cache by slot map, any cache type: v_new [n][G][d_v], kr_new [n][d_r] f32 as gva_append_chunk takes them, pos, slots
+ * and errors as gqa_append.  A row is bit for bit what gva_append_cache_at writes for that slot and position. */
+int gva_append_rows(gva_handle *h, const gva_cache *cache, const float *v_new, const float *kr_new, const int32_t *pos, const int32_t *slots,
+                    int n, int32_t *dev_status, void *stream);
+
+/* Attention of drafted tokens over the cache, which already holds them: sequence b has ctx_lens[b] tokens of context in slots
+ * 0 .. ctx - 1 and its n_b = cu_q[b+1] - cu_q[b] nodes in slots ctx .. ctx + n_b - 1.  Node i sees the whole context and those nodes j whose
+ * bit is set in its row of the mask (gva_tree_masks, or any other mask: a chain, a prompt's causal order, none of the nodes).
+ *   q    [n_q][H][d_v+d_r]   absorbed queries with their rotated positional slice; bf16, or f32 over an f32 cache
+ *   mask [n_q][mask_words] u32, mask_words >= ceil(max_q_len / 32); bits at or beyond n_b are ignored
+ *   out  [n_q][H][d_v]       of q's type: rounded once.  A row that sees nothing gives 0
+ *   lse  [n_q][H] f32 or NULL   natural logarithm; -inf for a row that sees nothing
+ *   max_q_len, max_seq_len   upper bounds on n_b (256 at most) and on ctx_lens[b] + n_b
+ *   num_splits               0: all sequences' tiles in a row are cut into equal ranges; n: every 32 nodes' tiles into n ranges (64 at most)
+ * Over a bf16 cache the products are taken of the bf16 numbers as they are, accumulated in f32; softmax weights enter the value product
+ * rounded to bf16 (2^-9, as the output is; their sum is taken before), everything else is f32: measured against 64 bits the output is
+ * 1.4 times as far off as its own rounding.  Bitwise reproducible for fixed arguments.  What is cached for a node does not reach rows that do
+ * not see it, not even infinities and NaN; a row that sees a node with an infinity or NaN among a group's values has NaN in the heads of that
+ * group, in those elements or in all.
+ * n_b < 0 or > max_q_len, ctx_lens[b] < 0, or ctx_lens[b] + n_b beyond max_seq_len or the block table -> GVA_ERR_SEQ_LEN, the sequence's rows are left as
+ * they were; tokens of a page outside the pool count as absent (GVA_ERR_BAD_PAGE).  Rows at or beyond cu_q[B] are left as they were.
+ * Workspace: at least gva_decode_tree_workspace_bytes(...) bytes, 256-byte aligned. */
+size_t gva_decode_tree_workspace_bytes(const gva_handle *h, int B, int n_q, int max_q_len, int max_seq_len, int num_splits);
+int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const uint32_t *mask, int mask_words, const int32_t *cu_q,
+                    const int32_t *ctx_lens, void *out, float *lse, void *workspace, size_t workspace_bytes, int B, int n_q, int max_q_len,
+                    int max_seq_len, int num_splits, int32_t *dev_status, void *stream);
+
+/* The drafts that the model agrees with become part of their sequences.  Node 0 of a tree is the token that was chosen last, so it stays; of a
+ * node that stays the first child whose token is the one chosen after it stays too.
+ *   parents [rows] as gva_tree_masks;  tokens [rows] i32 the drafted tokens;  chosen [rows] i32 what the model says after each node
+ *   path     [rows]   row cu_q[b] + k: the k-th node that stays (0 first), -1 behind the last
+ *   new_lens [B]      ctx_lens[b] + number of nodes that stay; may be ctx_lens
+ *   last     [B]      the token chosen after the last of them (the next tree's node 0), -1 for a sequence without nodes
+ * Their rows move to slots ctx, ctx + 1, ... bit for bit (any cache type), so that slots are positions again; the slots behind them
+ * hold what is left of the tree and are the next append's.  A bad tree (see gva_tree_masks) -> GVA_ERR_TREE, ctx_lens[b] < 0 or a tree beyond
+ * the block table -> GVA_ERR_SEQ_LEN, a bad page among the rows that move -> GVA_ERR_BAD_PAGE: nothing of that sequence moves, new_lens[b] =
+ * ctx_lens[b], last[b] = -1 and its path is -1. */
+int gva_tree_commit(gva_handle *h, const gva_cache *cache, const int32_t *parents, const int32_t *tokens, const int32_t *chosen, const int32_t *cu_q,
+                    const int32_t *ctx_lens, int32_t *path, int32_t *new_lens, int32_t *last, int B, int max_q_len, int32_t *dev_status, void *stream);
 
 /* Geometry of the most recent gva_decode / gqa_decode launch on this handle (reporting only):
  * number of split-KV partitions launched (thread blocks of the decode kernel). */

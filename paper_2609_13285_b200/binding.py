@@ -17,16 +17,21 @@ LIB_PATH = os.environ.get("GVA_LIBRARY", os.path.join(_HERE, "libgva.so"))   # o
 GVA_OK = 0
 GVA_ERR_INVALID_ARG, GVA_ERR_UNSUPPORTED, GVA_ERR_WORKSPACE, GVA_ERR_CUDA = 1, 2, 3, 4
 GVA_ERR_BAD_PAGE, GVA_ERR_SEQ_LEN, GVA_ERR_TIMEOUT, GVA_ERR_STATIC_LIMIT = 5, 6, 7, 8
+GVA_ERR_NO_ROOM, GVA_ERR_TREE = 9, 10
 GVA_STATIC_SCRATCH_BYTES = 16 << 20
 GVA_F32, GVA_BF16, GVA_E4M3 = 0, 1, 2
 GVA_KERNEL_AUTO, GVA_KERNEL_FMA, GVA_KERNEL_MMA = 0, 1, 2
+GVA_ROPE_PAIRS, GVA_ROPE_HALVES = 0, 1
+GVA_ROPE_PLAIN, GVA_ROPE_LINEAR, GVA_ROPE_BASE, GVA_ROPE_PARTS = 0, 1, 2, 3
 
 EXPORTS = ["gva_create", "gva_destroy", "gva_decode_workspace_bytes", "gva_absorb_query", "gva_append_cache",
            "gva_decode", "gva_decode_static", "gqa_decode", "gva_decode_step", "gva_step_scratch_bytes", "gva_decode_step_host", "gva_input_width", "gva_pack_input_weights", "gva_pack_bf16",
            "gva_project_in", "gva_project_out", "gva_layer_step", "gva_last_num_splits", "gva_last_kernel", "gva_last_tile_tokens",
            "gva_status_string", "gva_append_chunk", "gva_prefill", "gva_decode_multi_workspace_bytes", "gva_decode_multi", "gva_decode_tokens_workspace_bytes", "gva_decode_tokens", "gva_decode_tokens_ragged",
            "gva_append_cache_at", "gva_q4_append", "gva_q4_append_chunk", "gva_q4_widen", "gva_q4_decode_workspace_bytes", "gva_q4_decode",
-           "gva_attention_weights", "gva_q4_attention_weights", "gva_evict_workspace_bytes", "gva_evict", "gva_q4_evict"]
+           "gva_attention_weights", "gva_q4_attention_weights", "gva_evict_workspace_bytes", "gva_evict", "gva_q4_evict",
+           "gva_assign_pages", "gva_tree_masks", "gva_rope_frequencies", "gva_set_rope", "gqa_set_rope", "gqa_append", "gva_append_rows",
+           "gva_decode_tree_workspace_bytes", "gva_decode_tree", "gva_tree_commit"]
 
 
 class GvaConfig(ctypes.Structure):
@@ -49,6 +54,12 @@ class GqaCache(ctypes.Structure):
 class GvaQ4Cache(ctypes.Structure):
     _fields_ = [("v_pool", ctypes.c_void_p), ("sz_pool", ctypes.c_void_p), ("kr_pool", ctypes.c_void_p),
                 ("block_table", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32)]
+
+
+class GvaRope(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("d_rot", ctypes.c_int32), ("scaling", ctypes.c_int32), ("original_len", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("magnitude", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 class GvaError(RuntimeError):
@@ -114,13 +125,25 @@ def load() -> ctypes.CDLL:
     lib.gva_evict_workspace_bytes.restype = sz
     lib.gva_evict.argtypes = [vp, pool, vp, vp, vp, vp, vp, ip, ip, vp, vp, vp, ip, vp, sz, ip, ip, vp, vp]
     lib.gva_q4_evict.argtypes = [vp, q4, vp, vp, vp, vp, vp, ip, ip, vp, vp, vp, ip, vp, sz, ip, ip, vp, vp]
+    rope, i64 = ctypes.POINTER(GvaRope), ctypes.c_int64
+    lib.gva_assign_pages.argtypes = [vp] + [vp] * 5 + [ip, ip] + [vp] * 7 + [ip, ip, vp, vp]
+    lib.gva_tree_masks.argtypes = [vp, vp, vp, vp, vp, ip, vp, ip, ip, vp, vp]
+    lib.gva_rope_frequencies.argtypes = [rope, vp]
+    lib.gva_set_rope.argtypes = [vp, rope]
+    lib.gqa_set_rope.argtypes = [vp, rope]
+    lib.gqa_append.argtypes = [vp, ctypes.POINTER(GqaCache), vp, i64, vp, i64, vp, i64, vp, vp, vp, ip, vp, vp]
+    lib.gva_append_rows.argtypes = [vp, pool, vp, vp, vp, vp, ip, vp, vp]
+    lib.gva_decode_tree_workspace_bytes.argtypes = [vp, ip, ip, ip, ip, ip]
+    lib.gva_decode_tree_workspace_bytes.restype = sz
+    lib.gva_decode_tree.argtypes = [vp, pool, vp, vp, ip, vp, vp, vp, vp, vp, sz, ip, ip, ip, ip, ip, vp, vp]
+    lib.gva_tree_commit.argtypes = [vp, pool] + [vp] * 8 + [ip, ip, vp, vp]
     for name in ("gva_last_num_splits", "gva_last_kernel", "gva_last_tile_tokens"):
         getattr(lib, name).argtypes = [vp]
     lib.gva_status_string.argtypes = [ip]
     lib.gva_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("gva_decode_workspace_bytes", "gva_step_scratch_bytes", "gva_status_string", "gva_pack_bf16",
-                        "gva_q4_decode_workspace_bytes", "gva_evict_workspace_bytes"):
+                        "gva_q4_decode_workspace_bytes", "gva_evict_workspace_bytes", "gva_decode_tree_workspace_bytes"):
             getattr(lib, name).restype = ip
     _lib = lib
     return lib
@@ -521,6 +544,92 @@ def gva_q4_evict(handle: int, cache: GvaQ4Cache, weights_in, positions_in, seq_l
                  workspace_bytes: Optional[int] = None, check: bool = True) -> int:
     return _evict("gva_q4_evict", handle, cache, weights_in, positions_in, seq_lens, keep, next_pos, sinks, recent, weights_out,
                   positions_out, new_lens, stride, workspace, B, max_seq_len, dev_status, workspace_bytes, check)
+
+
+# ---- a step with drafted tokens: pages and slots, rows by slot map, attention of a tree, commit ----
+
+def make_rope(*, layout: int = GVA_ROPE_PAIRS, d_rot: int, base: float = 10000.0, scaling: int = GVA_ROPE_PLAIN, factor: float = 1.0,
+              low: float = 0.0, high: float = 0.0, original_len: int = 0, magnitude: float = 1.0) -> GvaRope:
+    return GvaRope(int(layout), int(d_rot), int(scaling), int(original_len), float(base), float(factor), float(low), float(high),
+                   float(magnitude), 0)
+
+
+def gva_rope_frequencies(rope: GvaRope):
+    """The frequencies of a rotation (numpy float64 [d_rot / 2])."""
+    import numpy as np
+    out = np.empty(max(0, rope.d_rot // 2), dtype=np.float64)
+    _check(load().gva_rope_frequencies(ctypes.byref(rope), _np_ptr(out)), "gva_rope_frequencies")
+    return out
+
+
+def gva_set_rope(handle: int, rope: GvaRope) -> None:
+    _check(load().gva_set_rope(handle, ctypes.byref(rope)), "gva_set_rope")
+
+
+def gqa_set_rope(handle: int, rope: GvaRope) -> None:
+    _check(load().gqa_set_rope(handle, ctypes.byref(rope)), "gqa_set_rope")
+
+
+def gva_assign_pages(handle: int, used, want, pages_in, pages_out, block_table, max_pages_per_seq: int, num_pages: int, free_ring, free_in,
+                     free_out, new_lens, cu_q, positions, slots, max_rows: int, B: int, dev_status=None, check: bool = True) -> int:
+    rc = load().gva_assign_pages(handle, _ptr(used), _ptr(want), _ptr(pages_in), _ptr(pages_out), _ptr(block_table), int(max_pages_per_seq),
+                                 int(num_pages), _ptr(free_ring), _ptr(free_in), _ptr(free_out), _ptr(new_lens), _ptr(cu_q), _ptr(positions),
+                                 _ptr(slots), int(max_rows), int(B), _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gva_assign_pages")
+    return rc
+
+
+def gva_tree_masks(handle: int, parents, cu_q, ctx_lens, mask, mask_words: int, positions, B: int, max_q_len: int, dev_status=None,
+                   check: bool = True) -> int:
+    rc = load().gva_tree_masks(handle, _ptr(parents), _ptr(cu_q), _ptr(ctx_lens), _ptr(mask), int(mask_words), _ptr(positions), int(B),
+                               int(max_q_len), _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gva_tree_masks")
+    return rc
+
+
+def gqa_append(handle: int, cache: GqaCache, q, q_stride: int, k_new, k_stride: int, v_new, v_stride: int, pos, slots, q_out, n: int,
+               dev_status=None, check: bool = True) -> int:
+    rc = load().gqa_append(handle, ctypes.byref(cache), _ptr(q), int(q_stride), _ptr(k_new), int(k_stride), _ptr(v_new), int(v_stride),
+                           _ptr(pos), _ptr(slots), _ptr(q_out), int(n), _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gqa_append")
+    return rc
+
+
+def gva_append_rows(handle: int, cache: GvaCache, v_new, kr_new, pos, slots, n: int, dev_status=None, check: bool = True) -> int:
+    rc = load().gva_append_rows(handle, ctypes.byref(cache), _ptr(v_new), _ptr(kr_new), _ptr(pos), _ptr(slots), int(n), _ptr(dev_status),
+                                _stream())
+    if check:
+        _check(rc, "gva_append_rows")
+    return rc
+
+
+def gva_decode_tree_workspace_bytes(handle: int, B: int, n_q: int, max_q_len: int, max_seq_len: int, num_splits: int = 0) -> int:
+    return int(load().gva_decode_tree_workspace_bytes(handle, int(B), int(n_q), int(max_q_len), int(max_seq_len), int(num_splits)))
+
+
+def gva_decode_tree(handle: int, cache: GvaCache, q, mask, mask_words: int, cu_q, ctx_lens, out, lse, workspace, B: int, n_q: int,
+                    max_q_len: int, max_seq_len: int, num_splits: int = 0, dev_status=None, workspace_bytes: Optional[int] = None,
+                    check: bool = True) -> int:
+    """q and out are bf16 tensors (f32 over an f32 cache), mask int32 or uint32 words."""
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    rc = load().gva_decode_tree(handle, ctypes.byref(cache), _ptr(q), _ptr(mask), int(mask_words), _ptr(cu_q), _ptr(ctx_lens), _ptr(out),
+                                _ptr(lse), _ptr(workspace), wb, int(B), int(n_q), int(max_q_len), int(max_seq_len), int(num_splits),
+                                _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gva_decode_tree")
+    return rc
+
+
+def gva_tree_commit(handle: int, cache: GvaCache, parents, tokens, chosen, cu_q, ctx_lens, path, new_lens, last, B: int, max_q_len: int,
+                    dev_status=None, check: bool = True) -> int:
+    rc = load().gva_tree_commit(handle, ctypes.byref(cache), _ptr(parents), _ptr(tokens), _ptr(chosen), _ptr(cu_q), _ptr(ctx_lens),
+                                _ptr(path), _ptr(new_lens), _ptr(last), int(B), int(max_q_len), _ptr(dev_status), _stream())
+    if check:
+        _check(rc, "gva_tree_commit")
+    return rc
 
 
 def gva_last_num_splits(handle: int) -> int:

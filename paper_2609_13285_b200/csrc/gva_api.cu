@@ -371,6 +371,15 @@ int gva_create(gva_handle **out, const gva_config *cfg, int device) {
     h->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : (float)(1.0 / std::sqrt((double)(cfg->d_c + cfg->d_r)));
     for (int i = 0; i < kMaxRopePairs; ++i)
         h->rope.inv_freq[i] = (2 * i < cfg->d_r) ? std::pow(cfg->rope_base, -2.0 * (double)i / (double)cfg->d_r) : 0.0;
+    {
+        gva_rope r = {};
+        r.layout = GVA_ROPE_PAIRS;
+        r.d_rot = cfg->d_v;
+        r.scaling = GVA_ROPE_PLAIN;
+        r.base = cfg->rope_base;
+        r.magnitude = 1.f;
+        h->head_rope = head_rope(r);
+    }
     h->last_num_splits = 0;
     h->last_kernel = 0;
     h->last_tile = 0;
@@ -1115,6 +1124,8 @@ const char *gva_status_string(int status) {
         case GVA_ERR_SEQ_LEN: return "sequence length or position outside the block table";
         case GVA_ERR_TIMEOUT: return "bounded wait on an asynchronous copy expired";
         case GVA_ERR_STATIC_LIMIT: return "request exceeds the built-in scratch of gva_decode_static";
+        case GVA_ERR_NO_ROOM: return "not enough free pages or rows for a sequence";
+        case GVA_ERR_TREE: return "a node's parent is not a node before it, or the tree is larger than allowed for";
         default: return "unknown status";
     }
 }

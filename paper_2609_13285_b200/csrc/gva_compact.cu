@@ -3,7 +3,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <mutex>
 
 #include "gva_evict.cuh"
 #include "gva_q4_decode.cuh"
@@ -26,26 +25,6 @@ Q4Pools q4_pools(const gva_q4_cache *c) {
     return Q4Pools{static_cast<uint8_t *>(c->v_pool), static_cast<__half2 *>(c->sz_pool), static_cast<uint16_t *>(c->kr_pool),
                    c->block_table, c->num_pages, c->max_pages_per_seq};
 }
-// Lets `fn` have `bytes` of dynamic shared memory on the handle's device; asked of the runtime once per kernel and device, not per call.
-int allow_smem(const gva_handle *h, const void *fn, size_t bytes) {
-    struct Entry { const void *fn; int device; size_t bytes; };
-    static std::mutex lock;
-    static Entry seen[256];
-    static int n = 0;
-    if (bytes <= 16 * 1024) return GVA_OK;               // every kernel may have 48 KB, its static shared memory (27 KB at most) included
-    std::lock_guard<std::mutex> hold(lock);
-    int i = 0;
-    while (i < n && (seen[i].fn != fn || seen[i].device != h->device)) ++i;
-    if (i < n && seen[i].bytes >= bytes) return GVA_OK;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return GVA_ERR_CUDA;
-    }
-    if (i < n) seen[i].bytes = bytes;
-    else if (n < 256) seen[n++] = Entry{fn, h->device, bytes};
-    return GVA_OK;
-}
-
 int append_q4(gva_handle *h, const gva_q4_cache *cache, const float *v_new, const float *kr_new, const int32_t *cu_q,
               const int32_t *slot0, const int32_t *pos0, int B, int n_q, int rows, int32_t *dev_status, void *stream) {
     if (!v_new || (h->cfg.d_r > 0 && !kr_new) || !aligned(v_new, 4) || !aligned(kr_new, 4) || !aligned(slot0, 4) || !aligned(pos0, 4))

@@ -1,6 +1,8 @@
 // The handle behind the C ABI and the checks that its entry points share.
 #pragma once
 
+#include <mutex>
+
 #include "gva_rope.cuh"
 #ifdef GVA_WITH_MMA
 #include "gva_decode_mma.cuh"
@@ -14,6 +16,7 @@ struct gva_handle {
     int smem_per_sm;         // shared memory of one SM
     float scale;             // softmax scale of gva_decode
     gva::RopeTable rope;
+    gva::HeadRope head_rope; // rotation of gqa_append
     int last_num_splits;
     int last_kernel;
     int last_tile;
@@ -59,6 +62,26 @@ inline int launched(cudaError_t ce) {
     if (ce == cudaSuccess) return GVA_OK;
     (void)cudaGetLastError();
     return GVA_ERR_CUDA;
+}
+
+// Lets `fn` have `bytes` of dynamic shared memory on the handle's device; asked of the runtime once per kernel and device, not per call.
+inline int allow_smem(const gva_handle *h, const void *fn, size_t bytes) {
+    struct Entry { const void *fn; int device; size_t bytes; };
+    static std::mutex lock;
+    static Entry seen[256];
+    static int n = 0;
+    if (bytes <= 16 * 1024) return GVA_OK;               // every kernel may have 48 KB, its static shared memory (27 KB at most) included
+    std::lock_guard<std::mutex> hold(lock);
+    int i = 0;
+    while (i < n && (seen[i].fn != fn || seen[i].device != h->device)) ++i;
+    if (i < n && seen[i].bytes >= bytes) return GVA_OK;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return GVA_ERR_CUDA;
+    }
+    if (i < n) seen[i].bytes = bytes;
+    else if (n < 256) seen[n++] = Entry{fn, h->device, bytes};
+    return GVA_OK;
 }
 
 }  // namespace gva

@@ -1,0 +1,345 @@
+// The bookkeeping of a serving step on the device: pages given out and taken back with the rows' positions and slots, what the
+// drafted tokens of a tree see of one another, and the tokens of a tree that become part of their sequence.
+//
+// All three move a few kilobytes: what they cost is a launch and their chains of dependent steps, so each is one launch whose
+// chains are short (a scan of all sequences in every block rather than a pass for the scan and one for its use).
+#pragma once
+
+#include <cooperative_groups.h>
+
+#include "gva_common.cuh"
+
+namespace gva {
+
+constexpr int kTreeMost = 256;       // nodes of a tree
+
+// ---- pages ---------------------------------------------------------------------------------------------------
+struct AssignParams {
+    const int32_t *used, *want, *pages_in;   // [B]; new_lens may be used, pages_out may be pages_in
+    int32_t *pages_out, *block_table, *ring;
+    const int32_t *free_in;                  // [2] first entry of the ring that holds a free page, and how many do
+    int32_t *free_out, *new_lens, *cu_q, *positions, *slots;
+    int32_t *dev_status;
+    int max_pages, num_pages, max_rows, B, P;
+};
+constexpr int kAssignItems = 8;      // sequences of a thread: 1024 threads serve 8192
+
+// What a sequence asks for.
+struct Asks {
+    int used, pages, to, rows, take, give;
+    bool fine;
+};
+__device__ __forceinline__ Asks sequence_asks(const AssignParams &p, int b, bool sound) {
+    Asks a;
+    a.used = p.used[b];
+    a.pages = p.pages_in[b];
+    const int want = p.want[b];
+    a.fine = sound && a.used >= 0 && want >= 0 && a.pages >= 0 && a.pages <= p.max_pages && (long long)want <= (long long)p.max_pages * p.P &&
+             (long long)a.used <= (long long)a.pages * p.P;
+    a.to = a.fine ? (int)(((long long)want + p.P - 1) / p.P) : a.pages;
+    a.rows = a.fine ? max(want - a.used, 0) : 0;
+    a.take = max(a.to - a.pages, 0);
+    a.give = max(a.pages - a.to, 0);
+    return a;
+}
+// Largest b in [0, B) with off[b] <= x, for off non-decreasing, off[0] <= x.
+__device__ __forceinline__ int owner_of(const int *off, int B, int x) {
+    int lo = 0, hi = B - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (off[mid] <= x) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+// Inclusive sum over the block's threads of v, in place; s_part holds one word per warp.  Returns the block's total.
+__device__ __forceinline__ long long block_scan(long long &v, long long *s_part) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += y;
+    }
+    if (lane == 31) s_part[warp] = v;
+    __syncthreads();
+    long long w = lane < warps ? s_part[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += y;
+    }
+    const long long before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+    if (warp > 0) v += before;
+    const long long total = __shfl_sync(0xffffffffu, w, 31);
+    __syncthreads();
+    return total;
+}
+
+// One cluster.  Every block scans all sequences for itself (8 a thread at most) and keeps the offsets in shared memory; once all
+// of them have read the inputs -- outputs may be the same buffers -- they share out rows, taken and returned pages among
+// their threads, which find their sequence by bisection.  Growing sequences are served in order until one does not fit, so the
+// sums before a served one are sums over all growing ones before it, and what is served needs no second scan.
+__global__ void __launch_bounds__(1024)
+assign_pages_kernel(AssignParams p) {
+    grid_dependency_launch();
+    extern __shared__ int s_mem[];
+    int *s_row = s_mem, *s_take = s_row + p.B, *s_give = s_take + p.B, *s_used = s_give + p.B, *s_pages = s_used + p.B, *s_to = s_pages + p.B;
+    __shared__ long long s_part[32];
+    __shared__ int s_served[3];      // rows, pages taken, pages returned by growing sequences: of those served
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, nt = blockDim.x, rank = (int)cluster.block_rank(), wide = (int)cluster.num_blocks();
+    const int per = (p.B + nt - 1) / nt;
+    if (tid < 3) s_served[tid] = 0;
+    grid_dependency_wait();
+    const int first = p.free_in[0], count = p.free_in[1];
+    const bool sound = first >= 0 && first < p.num_pages && count >= 0 && count <= p.num_pages;    // else all stays as it is
+    if (!sound && rank == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_BAD_PAGE, 0);
+    Asks a[kAssignItems];
+    long long rows = 0, take = 0, give = 0, back = 0;
+#pragma unroll
+    for (int i = 0; i < kAssignItems; ++i) {
+        const int b = tid * per + i;
+        if (i >= per || b >= p.B) continue;
+        a[i] = sequence_asks(p, b, sound);
+        rows += a[i].rows;
+        take += a[i].take;
+        if (a[i].rows > 0) back += a[i].give;
+        else give += a[i].give;
+        if (!a[i].fine && sound && rank == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
+    }
+    long long rows_to = rows, take_to = take, give_to = give, back_to = back;
+    block_scan(rows_to, s_part);
+    block_scan(take_to, s_part);
+    const long long give_all = block_scan(give_to, s_part);
+    block_scan(back_to, s_part);
+    {
+        long long r = rows_to - rows, t = take_to - take, g = give_to - give, k = back_to - back;
+#pragma unroll
+        for (int i = 0; i < kAssignItems; ++i) {
+            const int b = tid * per + i;
+            if (i >= per || b >= p.B) continue;
+            const bool grows = a[i].rows > 0;
+            const bool served = !grows || (t + a[i].take <= count && r + a[i].rows <= p.max_rows);
+            // (sums past what is served are past what fits: cut off here and below)
+            s_row[b] = (int)min(r, (long long)p.max_rows);
+            s_take[b] = (int)min(t, (long long)count);
+            s_give[b] = (int)min(g, (long long)p.num_pages);
+            s_to[b] = (int)min(k, (long long)p.num_pages);     // (for a moment: returned before it by growing sequences)
+            s_used[b] = a[i].used;
+            s_pages[b] = a[i].pages;
+            r += a[i].rows;
+            t += a[i].take;
+            if (grows) k += a[i].give;
+            else g += a[i].give;
+            if (grows && served) {
+                atomicMax(&s_served[0], (int)r);
+                atomicMax(&s_served[1], (int)t);
+                atomicMax(&s_served[2], (int)min(k, (long long)p.num_pages));
+            }
+            if (!served) {
+                if (rank == 0) report_error(p.dev_status, GVA_ERR_NO_ROOM, b);
+                a[i].to = a[i].pages;
+                a[i].rows = -1;                                // stays as it is
+            }
+        }
+    }
+    __syncthreads();
+    const int n_rows = s_served[0], n_take = s_served[1], n_back = s_served[2];
+#pragma unroll
+    for (int i = 0; i < kAssignItems; ++i) {
+        const int b = tid * per + i;
+        if (i >= per || b >= p.B) continue;
+        s_row[b] = min(s_row[b], n_rows);
+        s_take[b] = min(s_take[b], n_take);
+        s_give[b] = (int)min((long long)s_give[b] + min(s_to[b], n_back), (long long)p.num_pages);
+        s_to[b] = a[i].to;
+    }
+    int want[kAssignItems];
+#pragma unroll
+    for (int i = 0; i < kAssignItems; ++i) {
+        const int b = tid * per + i;
+        if (i < per && b < p.B) want[i] = p.want[b];
+    }
+    const int n_give = (int)min(give_all + n_back, (long long)p.num_pages + 1);
+    // every block of the cluster has read its inputs (and this block's offsets are whole) before anything is written
+    cluster.sync();
+    if (rank == 0) {
+#pragma unroll
+        for (int i = 0; i < kAssignItems; ++i) {
+            const int b = tid * per + i;
+            if (i >= per || b >= p.B) continue;
+            p.pages_out[b] = a[i].to;
+            p.new_lens[b] = !a[i].fine || a[i].rows < 0 ? a[i].used : want[i];
+            p.cu_q[b] = s_row[b];
+        }
+        if (tid == 0) {
+            p.cu_q[p.B] = n_rows;
+            // a ring that would overflow held pages twice: it takes no more than fit
+            const int room = p.num_pages - count;
+            if (sound && n_give > room) report_error(p.dev_status, GVA_ERR_BAD_PAGE, 0);
+            p.free_out[0] = sound ? (int)(((long long)first + n_take) % p.num_pages) : first;
+            p.free_out[1] = sound ? count - n_take + min(n_give, room) : count;
+        }
+    }
+    const int me = rank * nt + tid, all = wide * nt;
+    for (int i = me; i < n_take; i += all) {                     // (none of these without a sound ring)
+        const int b = owner_of(s_take, p.B, i);
+        p.block_table[(size_t)b * p.max_pages + s_pages[b] + (i - s_take[b])] = p.ring[((long long)first + i) % p.num_pages];
+    }
+    for (int i = me; i < n_give && i < p.num_pages - count; i += all) {
+        const int b = owner_of(s_give, p.B, i);
+        const int page = p.block_table[(size_t)b * p.max_pages + s_to[b] + (i - s_give[b])];
+        if (page < 0 || page >= p.num_pages) report_error(p.dev_status, GVA_ERR_BAD_PAGE, b);
+        p.ring[((long long)first + count + i) % p.num_pages] = page;
+    }
+    for (int i = me; i < n_rows; i += all) {
+        const int b = owner_of(s_row, p.B, i);
+        const int t = s_used[b] + (i - s_row[b]), j = t / p.P;
+        const int page = j < s_pages[b] ? p.block_table[(size_t)b * p.max_pages + j]
+                                        : p.ring[((long long)first + s_take[b] + (j - s_pages[b])) % p.num_pages];
+        p.positions[i] = t;
+        p.slots[i] = page < 0 || page >= p.num_pages ? -1 : page * p.P + t % p.P;
+    }
+}
+
+// ---- trees ---------------------------------------------------------------------------------------------------
+// One block per sequence: bits of a node and its ancestors, and its position ctx + depth.  A thread walks up from its node
+// through the parents in shared memory: as many dependent steps as the tree is deep.
+struct TreeMaskParams {
+    const int32_t *parents, *cu_q, *ctx_lens;
+    uint32_t *mask;
+    int32_t *positions;              // nullable
+    int32_t *dev_status;
+    int words, most;                 // words of a row, nodes of a tree at most
+};
+// Loads a tree's parents (n of them) into s_parents; whether they are sound: the first -1 or any node's below its own number.
+__device__ __forceinline__ bool load_parents(const int32_t *parents, int n, int *s_parents) {
+    bool bad = false;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int par = parents[i];
+        bad |= par < -1 || par >= i;
+        s_parents[i] = par;
+    }
+    return !__syncthreads_or(bad);
+}
+__global__ void __launch_bounds__(kTreeMost)
+tree_masks_kernel(TreeMaskParams p) {
+    grid_dependency_launch();
+    __shared__ int s_parents[kTreeMost];
+    grid_dependency_wait();
+    const int b = blockIdx.x, r0 = p.cu_q[b], n = p.cu_q[b + 1] - r0;
+    if (n <= 0) return;
+    if (n > p.most || !load_parents(p.parents + r0, n, s_parents)) {
+        if (threadIdx.x == 0) report_error(p.dev_status, GVA_ERR_TREE, b);
+        return;
+    }
+    const int ctx = p.positions ? p.ctx_lens[b] : 0;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        uint32_t bits[kTreeMost / 32];
+#pragma unroll
+        for (int w = 0; w < kTreeMost / 32; ++w) bits[w] = 0;
+        int depth = -1;
+        for (int at = i; at >= 0; at = s_parents[at], ++depth)
+#pragma unroll
+            for (int w = 0; w < kTreeMost / 32; ++w) bits[w] |= (at >> 5) == w ? 1u << (at & 31) : 0u;
+        uint32_t *row = p.mask + (size_t)(r0 + i) * p.words;
+#pragma unroll
+        for (int w = 0; w < kTreeMost / 32; ++w)
+            if (w < p.words) row[w] = bits[w];
+        if (p.positions) p.positions[r0 + i] = ctx + depth;
+    }
+}
+
+// ---- commit --------------------------------------------------------------------------------------------------
+// One block per sequence.  Node 0 is accepted; of an accepted node the first child whose token is the one that was chosen
+// after it is.  Every node looks at once whether it is such a child (the smallest wins), then one thread walks.  The path's nodes
+// ascend, so rows only move down, and a row is overwritten by a row further along the path only: a thread that takes its
+// 16-byte column of all rows in the path's order, loads of a batch before its stores, never reads what it has written.
+struct TreeCommitParams {
+    uint8_t *v_pool, *kr_pool;       // kr_pool may be null
+    const int32_t *block_table;      // nullable
+    const int32_t *parents, *tokens, *chosen, *cu_q, *ctx_lens;    // new_lens may be ctx_lens
+    int32_t *path, *new_lens, *last;
+    int32_t *dev_status;
+    int v_bytes, kr_bytes;           // of a row
+    int G, P, num_pages, max_pages, most;
+};
+constexpr int kCommitThreads = 128, kCommitBatch = 8;
+__global__ void __launch_bounds__(kCommitThreads)
+tree_commit_kernel(TreeCommitParams p) {
+    grid_dependency_launch();
+    __shared__ int s_parents[kTreeMost], s_next[kTreeMost], s_path[kTreeMost], s_chosen[kTreeMost];
+    __shared__ int2 s_from[kTreeMost], s_to[kTreeMost];           // page and slot of every row of the path, and of where it goes
+    __shared__ int s_count;
+    grid_dependency_wait();
+    const int b = blockIdx.x, tid = threadIdx.x;
+    const int r0 = p.cu_q[b], n = max(p.cu_q[b + 1] - r0, 0), ctx = p.ctx_lens[b];
+    int code = GVA_OK;
+    if (ctx < 0 || (long long)ctx + n > (long long)p.max_pages * p.P) code = GVA_ERR_SEQ_LEN;
+    else if (n > p.most || !load_parents(p.parents + r0, n, s_parents)) code = GVA_ERR_TREE;
+    int count = 0;
+    if (code == GVA_OK && n > 0) {
+        for (int i = tid; i < n; i += kCommitThreads) {
+            s_next[i] = n;
+            s_chosen[i] = p.chosen[r0 + i];
+        }
+        __syncthreads();
+        for (int i = tid; i < n; i += kCommitThreads) {
+            const int par = s_parents[i];
+            if (par >= 0 && p.tokens[r0 + i] == s_chosen[par]) atomicMin(&s_next[par], i);
+        }
+        __syncthreads();
+        if (tid == 0) {
+            int k = 0;
+            for (int at = 0; at < n; at = s_next[at]) s_path[k++] = at;
+            s_count = k;
+        }
+        __syncthreads();
+        count = s_count;
+        bool bad = false;
+        for (int i = tid; i < count; i += kCommitThreads) {
+            auto place = [&](int t) {
+                const int j = t / p.P;
+                const long long page = p.block_table ? (long long)p.block_table[(size_t)b * p.max_pages + j] : (long long)b * p.max_pages + j;
+                bad |= page < 0 || page >= p.num_pages;
+                return make_int2((int)page, t - j * p.P);
+            };
+            if (s_path[i] == i) continue;
+            s_from[i] = place(ctx + s_path[i]);
+            s_to[i] = place(ctx + i);
+        }
+        if (__syncthreads_or(bad)) {
+            code = GVA_ERR_BAD_PAGE;
+            count = 0;
+        }
+    }
+    if (code != GVA_OK && tid == 0) report_error(p.dev_status, code, b);
+    for (int i = tid; i < n; i += kCommitThreads) p.path[r0 + i] = i < count ? s_path[i] : -1;
+    if (tid == 0) {
+        p.new_lens[b] = ctx + count;
+        p.last[b] = count > 0 ? s_chosen[s_path[count - 1]] : -1;
+    }
+    int begin = 0;                                                // the path's beginning stays where it is
+    while (begin < count && s_path[begin] == begin) ++begin;
+    if (begin == count) return;
+    const int v_cols = p.v_bytes / 16, cols = p.G * v_cols + (p.kr_pool ? p.kr_bytes / 16 : 0);
+    for (int c = tid; c < cols; c += kCommitThreads) {
+        const bool v = c < p.G * v_cols;
+        const int g = v ? c / v_cols : 0, at = (v ? c - g * v_cols : c - p.G * v_cols) * 16;
+        auto address = [&](const int2 &x) {
+            return v ? p.v_pool + (((size_t)x.x * p.G + g) * p.P + x.y) * p.v_bytes + at : p.kr_pool + ((size_t)x.x * p.P + x.y) * p.kr_bytes + at;
+        };
+        for (int i0 = begin; i0 < count; i0 += kCommitBatch) {
+            uint4 row[kCommitBatch];
+#pragma unroll
+            for (int u = 0; u < kCommitBatch; ++u)
+                if (i0 + u < count) row[u] = *reinterpret_cast<const uint4 *>(address(s_from[i0 + u]));
+#pragma unroll
+            for (int u = 0; u < kCommitBatch; ++u)
+                if (i0 + u < count) *reinterpret_cast<uint4 *>(address(s_to[i0 + u])) = row[u];
+        }
+    }
+}
+
+}  // namespace gva

@@ -1,5 +1,7 @@
-// RoPE in fp64 and the roundings of an append.
+// RoPE in fp64, its frequencies, and the roundings of an append.
 #pragma once
+
+#include <cmath>
 
 #include "gva_common.cuh"
 
@@ -27,6 +29,38 @@ constexpr int widest_rope(int d_v) {
 struct RopeTable {
     double inv_freq[kMaxRopePairs];   // base^(-2i/d_r), computed once on the host in fp64
 };
+
+// The rotation of whole GQA heads (gqa_append): the first d_rot elements, in pairs (2i, 2i+1) or halves (i, i + d_rot/2).
+constexpr int kMaxHeadPairs = 64;     // d_rot <= d_h <= 128
+struct HeadRope {
+    double turns[kMaxHeadPairs];      // frequency / 2 pi: whole turns fall away in fp64, what is left of an angle is exact in f32
+    int d_rot, halves;
+    float magnitude;
+};
+
+// The frequencies of a rotation (see gva_rope in gva.h), d_rot / 2 of them.
+inline void rope_frequencies(const gva_rope &r, double *f) {
+    const double kTwoPi = 6.283185307179586476925;
+    const double base = r.scaling == GVA_ROPE_BASE ? r.base * std::pow(r.factor, (double)r.d_rot / (r.d_rot - 2)) : r.base;
+    for (int i = 0; i < r.d_rot / 2; ++i) {
+        f[i] = std::pow(base, -2.0 * i / r.d_rot);
+        if (r.scaling == GVA_ROPE_LINEAR) f[i] /= r.factor;
+        if (r.scaling == GVA_ROPE_PARTS) {
+            const double turns = r.original_len * f[i] / kTwoPi;           // of this pair over the original context
+            const double kept = std::fmin(1.0, std::fmax(0.0, (turns - r.low) / (r.high - r.low)));
+            f[i] = f[i] * kept + f[i] / r.factor * (1.0 - kept);
+        }
+    }
+}
+inline HeadRope head_rope(const gva_rope &r) {
+    HeadRope h = {};
+    rope_frequencies(r, h.turns);
+    for (int i = 0; i < r.d_rot / 2; ++i) h.turns[i] /= 6.283185307179586476925;
+    h.d_rot = r.d_rot;
+    h.halves = r.layout == GVA_ROPE_HALVES;
+    h.magnitude = r.magnitude;
+    return h;
+}
 
 // fp64 -> bf16, round to nearest even without double rounding: truncate to f32 toward zero, fold
 // everything that was cut off into the f32's last mantissa bit (round to odd), then round that

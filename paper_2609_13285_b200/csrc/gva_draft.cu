@@ -6,7 +6,7 @@
 
 #include "gva_pages.cuh"
 #include "gva_rows.cuh"
-#include "gva_tree.cuh"
+#include "gva_tree_mma.cuh"
 #include "gva_handle.cuh"
 
 using namespace gva;
@@ -57,10 +57,13 @@ TreePlan tree_plan(const gva_handle *h, int B, int max_q_len, int max_seq_len, i
     t.strips = (int)std::max<long long>(1, ceil_div(max_q_len, kStripNodes));
     const long long tiles = std::max<long long>(1, ceil_div(max_seq_len, kTreeTile)), all = (long long)std::max(B, 1) * t.strips;
     t.num_splits = num_splits;
-    const int room = std::max(1, h->sm_count / c.G);
+    const bool mma = c.cache_dtype == GVA_BF16;
+    const TreeMma k = tree_mma(c);
+    const int room = std::max(1, h->sm_count * (mma ? k.blocks_per_sm : 1) / c.G);
     t.ranges = (int)std::min<long long>(all * (num_splits > 0 ? num_splits : tiles), room);
     t.records = num_splits == 1 ? 0 : num_splits > 0 ? all * num_splits : t.ranges + all;
-    t.smem = tree_fma_smem(B, c.d_v, c.d_r);
+    // (never more blocks on an SM than its 512 columns of tensor memory serve)
+    t.smem = mma ? std::max(k.fixed + (size_t)B * 4, (size_t)h->smem_per_sm / (k.blocks_per_sm + 1)) : tree_fma_smem(B, c.d_v, c.d_r);
     t.rec_o = align_up((size_t)(B + 1) * 4, 256);
     t.rec_ml = t.rec_o + align_up((size_t)t.records * c.G * kStripRows * c.d_v * 4, 256);
     t.total = t.rec_ml + align_up((size_t)t.records * c.G * kStripRows * 2 * 4, 256);
@@ -70,7 +73,6 @@ using TreeFmaFn = void (*)(TreeParams, int);
 TreeFmaFn tree_fma(const gva_config &c) {
     const bool wide = c.d_v == 128;
     if (c.cache_dtype == GVA_F32) return wide ? tree_fma_kernel<float, float, 128> : tree_fma_kernel<float, float, 64>;
-    if (c.cache_dtype == GVA_BF16) return wide ? tree_fma_kernel<__nv_bfloat16, __nv_bfloat16, 128> : tree_fma_kernel<__nv_bfloat16, __nv_bfloat16, 64>;
     return wide ? tree_fma_kernel<uint8_t, __nv_bfloat16, 128> : tree_fma_kernel<uint8_t, __nv_bfloat16, 64>;
 }
 }  // namespace
@@ -224,6 +226,7 @@ int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const 
     if (B == 0 || n_q == 0 || max_q_len == 0 || max_seq_len == 0) return GVA_OK;
     if (!q || !mask || !cu_q || !ctx_lens || !out || mask_words * 32ll < max_q_len) return GVA_ERR_INVALID_ARG;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(mask, 4) || !aligned(cu_q, 4) || !aligned(ctx_lens, 4) || !aligned(lse, 4)) return GVA_ERR_INVALID_ARG;
+    if (h->cfg.cache_dtype == GVA_BF16 && (uint64_t)cache->num_pages * h->cfg.G * h->cfg.page_size >= (1ull << 31)) return GVA_ERR_UNSUPPORTED;
     const TreePlan plan = tree_plan(h, B, max_q_len, max_seq_len, num_splits);
     if (!workspace || workspace_bytes < plan.total) return GVA_ERR_WORKSPACE;
     if (!aligned(workspace, 256)) return GVA_ERR_INVALID_ARG;
@@ -242,10 +245,20 @@ int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const 
     p.scale_log2 = h->scale * kLog2e;
     if (plan.smem > (size_t)h->smem_optin) return GVA_ERR_UNSUPPORTED;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const TreeFmaFn fn = tree_fma(c);
-    rc = allow_smem(h, reinterpret_cast<const void *>(fn), plan.smem);
-    if (rc != GVA_OK) return rc;
-    rc = launched(launch_pdl(fn, dim3(plan.ranges * c.G), dim3(kTreeFmaThreads), plan.smem, s, p, c.d_r));
+    const dim3 grid(plan.ranges * c.G);
+    if (c.cache_dtype == GVA_BF16) {
+        const TreeMma k = tree_mma(c);
+        CUtensorMap tm_v, tm_k;
+        if (!tree_maps(c, h->mma, p, k.drp, &tm_v, &tm_k)) return GVA_ERR_CUDA;
+        rc = allow_smem(h, reinterpret_cast<const void *>(k.fn), plan.smem);
+        if (rc != GVA_OK) return rc;
+        rc = launched(launch_pdl(k.fn, grid, dim3(kTreeMmaThreads), plan.smem, s, p, tm_v, tm_k));
+    } else {
+        const TreeFmaFn fn = tree_fma(c);
+        rc = allow_smem(h, reinterpret_cast<const void *>(fn), plan.smem);
+        if (rc != GVA_OK) return rc;
+        rc = launched(launch_pdl(fn, grid, dim3(kTreeFmaThreads), plan.smem, s, p, c.d_r));
+    }
     if (rc != GVA_OK || plan.num_splits == 1) return rc;
     auto merge = c.cache_dtype == GVA_F32 ? (c.d_v == 64 ? tree_merge_kernel<float, 64> : tree_merge_kernel<float, 128>)
                                           : (c.d_v == 64 ? tree_merge_kernel<__nv_bfloat16, 64> : tree_merge_kernel<__nv_bfloat16, 128>);

@@ -59,11 +59,11 @@ TreePlan tree_plan(const gva_handle *h, int B, int max_q_len, int max_seq_len, i
     t.num_splits = num_splits;
     const bool mma = c.cache_dtype == GVA_BF16;
     const TreeMma k = tree_mma(c);
-    const int room = std::max(1, h->sm_count * (mma ? k.blocks_per_sm : 1) / c.G);
+    const int room = std::max(1, h->sm_count / c.G);
     t.ranges = (int)std::min<long long>(all * (num_splits > 0 ? num_splits : tiles), room);
     t.records = num_splits == 1 ? 0 : num_splits > 0 ? all * num_splits : t.ranges + all;
-    // (never more blocks on an SM than its 512 columns of tensor memory serve)
-    t.smem = mma ? std::max(k.fixed + (size_t)B * 4, (size_t)h->smem_per_sm / (k.blocks_per_sm + 1)) : tree_fma_smem(B, c.d_v, c.d_r);
+    // (never more blocks on an SM than its 512 columns of tensor memory serve: one)
+    t.smem = mma ? std::max(k.fixed + (size_t)B * 4, (size_t)h->smem_per_sm / 2) : tree_fma_smem(B, c.d_v, c.d_r);
     t.rec_o = align_up((size_t)(B + 1) * 4, 256);
     t.rec_ml = t.rec_o + align_up((size_t)t.records * c.G * kStripRows * c.d_v * 4, 256);
     t.total = t.rec_ml + align_up((size_t)t.records * c.G * kStripRows * 2 * 4, 256);
@@ -252,7 +252,7 @@ int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const 
         if (!tree_maps(c, h->mma, p, k.drp, &tm_v, &tm_k)) return GVA_ERR_CUDA;
         rc = allow_smem(h, reinterpret_cast<const void *>(k.fn), plan.smem);
         if (rc != GVA_OK) return rc;
-        rc = launched(launch_pdl(k.fn, grid, dim3(kTreeMmaThreads), plan.smem, s, p, tm_v, tm_k));
+        rc = launched(launch_pdl(k.fn, grid, dim3(k.threads), plan.smem, s, p, tm_v, tm_k));
     } else {
         const TreeFmaFn fn = tree_fma(c);
         rc = allow_smem(h, reinterpret_cast<const void *>(fn), plan.smem);

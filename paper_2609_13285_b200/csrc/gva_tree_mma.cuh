@@ -1,12 +1,18 @@
 // gva_decode_tree over a bf16 cache on the 5th-generation tensor cores (tcgen05 + tensor memory), sm_100a.
 //
-// A block works on one value group: the strip's 128 rows (32 nodes x 4 heads) are the M of every MMA, a tile of 64 cached tokens
-// is the N of the score product and the K of the value product, so one tile in shared memory feeds both.
-//   warps 0-3   softmax: a thread owns a row = a lane of tensor memory
-//   warp 4      issues the value products, warp 5 the score products (and owns the tensor memory), warp 6 fetches the tiles
-// The running number of a tile over the block's pieces decides its stage, its score buffer and every barrier's phase; the loader runs
-// ahead over pieces, so the ring does not drain where a sequence ends.
-//   S[t & 1] = Q K^T (Q from tensor memory)  ->  weights as bf16 pairs over the first half of the row's S  ->  O += P V
+// A block (one per SM) works on one value group: the strip's 128 rows (32 nodes x 4 heads) are the M of every MMA, a tile of 64
+// cached tokens is the N of the score product and the K of the value product, so one tile in shared memory feeds both.
+//   NWG groups of 4 warps   softmax: tile t is group t % NWG's, a thread owns a row = a lane of tensor memory
+//   4 more warps            issuer of the value products, issuer of the score products (owns the tensor memory), two loaders
+//   S[t % NWG] = Q K^T (Q from tensor memory)  ->  weights as bf16 pairs in P[t % NWG]  ->  O += P V
+// A tile's way through the softmax is a chain of some 1500 cycles (waits, tensor-memory round trips, 64 exponentials a thread) against
+// 360 (d_v = 64) or 725 that its bytes take from memory: four (three) tiles are on their way side by side.  They share one O, so
+// they share the rows' softmax references too: those go from tile to tile through shared memory in the tiles' order (`turn`), which is
+// a short step as long as no maximum moves one.  Sums stay with each group, relative to the reference they were made with.
+// Few nodes leave rows of the MMA unused, and its time is the same: up to 16 nodes are laid out twice, and each copy weighs its half
+// of every tile's tokens and has zeros for the others -- a sequence of its own, joined with the other at the end.
+// The running number of a tile over the block's pieces decides its stage, its group and every barrier's phase; loader and query run
+// ahead over pieces.
 // Rules as in the prefill kernel: tcgen05.ld / .st never sit in a per-lane branch; no barrier is waited on by parity two phases
 // late; every wait is bounded.
 #pragma once
@@ -15,10 +21,33 @@
 
 namespace gva {
 
-constexpr int kTreeMmaThreads = 224;
+// 16 consecutive f32 columns of this thread's tensor-memory lane.
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]),
+                   "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+                 : "r"(addr)
+                 : "memory");
+    tmem_ld_wait();
+}
+// Bounded wait of a whole warp, straight-line where the phase is complete already, as it mostly is: 30 cycles (220 with one lane waiting
+// and the others behind a shuffle).
+constexpr uint32_t kWarpPolls = 1u << 25;       // 40 cycles each: about a second
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+    for (uint32_t it = 0; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity));)
+        if ((++it & 1023u) == 0 && (it >= kWarpPolls || __any_sync(0xffffffffu, *abort_flag))) return false;
+    return true;
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(yes));
+    return yes != 0;
+}
+
 template <int DV, int DR>
 struct TreeTraits {
-    static constexpr int NSTAGE = DV == 64 ? 6 : 5;
+    static constexpr int NWG = DV == 64 ? 4 : 3;
+    static constexpr int NSTAGE = 8;                             // (a power of two)
     static constexpr int BOXES = DV / 64;
     static constexpr int DRP = (DR + 15) / 16 * 16;              // d_r = 24 occupies 32: the box reads zeros behind the row
     static constexpr int KR_ROW = DRP * 2;
@@ -26,47 +55,65 @@ struct TreeTraits {
     static constexpr int V_BYTES = BOXES * VBOX_BYTES;
     static constexpr int KR_BYTES = kTreeTile * KR_ROW;
     static constexpr int STAGE_BYTES = V_BYTES + ((KR_BYTES + 1023) & ~1023);
-    // Tensor memory: two score buffers, O, the query.  d_v = 64: 256 columns, two blocks on an SM; d_v = 128: 336 of 512, one block.
-    static constexpr int TMEM_COLS = DV == 64 ? 256 : 512, BLOCKS_PER_SM = 512 / TMEM_COLS;
-    static constexpr int COL_S = 0, COL_O = 2 * kTreeTile, COL_Q = COL_O + DV;
-    static_assert(COL_Q + (DV + DRP) / 2 <= TMEM_COLS, "scores, O and the query must fit the allocation");
-    static constexpr int OFF_BAR = NSTAGE * STAGE_BYTES, N_BARS = 2 * NSTAGE + 8;
-    static constexpr int OFF_WORDS = OFF_BAR + N_BARS * 8;      // tensor-memory address, abort flag, 4 words of bad rows, a flag per stage
-    static constexpr int OFF_SEQ = OFF_WORDS + (6 + NSTAGE) * 4;
+    static constexpr int TMEM_COLS = 512;
+    static constexpr int COL_S = 0, COL_P = NWG * kTreeTile, COL_O = COL_P + NWG * kTreeTile / 2, COL_Q = COL_O + DV;
+    static_assert(COL_Q + (DV + DRP) / 2 <= TMEM_COLS, "scores, weights, O and the query must fit the allocation");
+    static constexpr int SOFTMAX = NWG * 128, THREADS = SOFTMAX + 128;
+    // Registers: d_v = 64 launches 640 threads with 96 each; the softmax warps, which hold a row of scores, take 104 and the others 56
+    // (512 x 104 + 128 x 56 is less than 640 x 96).  d_v = 128: 512 threads with up to 128.
+    static constexpr bool SHARE_REGS = DV == 64;
+    static constexpr int PART = 16, JOIN_LD = 20;                // columns of O at a time in the join of copies; f32 of a row there, padded
+    static constexpr int OFF_JOIN = NSTAGE * STAGE_BYTES, OFF_REF = OFF_JOIN + NWG * kStripRows * JOIN_LD * 4;
+    static constexpr int OFF_SUM = OFF_REF + 2 * kStripRows * 4, OFF_BAR = OFF_SUM + 2 * SOFTMAX * 4;
+    static constexpr int N_BARS = 2 * NSTAGE + 8 * NWG + 6;
+    static constexpr int OFF_WORDS = OFF_BAR + N_BARS * 8;       // tensor-memory address, abort flag, a flag per stage, bad rows of a group's tile
+    static constexpr int OFF_SEQ = OFF_WORDS + (2 + NSTAGE + 4 * NWG) * 4;
     static constexpr size_t smem_bytes(int B) { return 1024 + OFF_SEQ + (size_t)(B + 1) * 4; }
 };
 
 template <int DV, int DR>
-__global__ void __launch_bounds__(kTreeMmaThreads, TreeTraits<DV, DR>::BLOCKS_PER_SM)
+__global__ void __launch_bounds__(TreeTraits<DV, DR>::THREADS, 1)
 tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_k) {
     using T = TreeTraits<DV, DR>;
-    constexpr int NS = T::NSTAGE, KS_V = DV / 16, KS_S = KS_V + T::DRP / 16, KS_O = kTreeTile / 16;
+    constexpr int NS = T::NSTAGE, NWG = T::NWG, KS_V = DV / 16, KS_S = KS_V + T::DRP / 16, KS_O = kTreeTile / 16;
+    constexpr uint32_t kAll = 0xffffffffu;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int c = blockIdx.x / p.G, g = blockIdx.x - c * p.G;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t s_base = smem_u32(smem), bar0 = s_base + T::OFF_BAR;
-    auto kv_full = [&](int s) { return bar0 + 8u * s; };
-    auto kv_empty = [&](int s) { return bar0 + 8u * (NS + s); };
-    auto s_full = [&](int t) { return bar0 + 8u * (2 * NS + (t & 1)); };
-    auto p_full = [&](int t) { return bar0 + 8u * (2 * NS + 2 + (t & 1)); };      // (one per score buffer: see the prefill kernel)
-    const uint32_t q_ready = bar0 + 8u * (2 * NS + 4), o_full = bar0 + 8u * (2 * NS + 5), drain_o = bar0 + 8u * (2 * NS + 6), drain_s = bar0 + 8u * (2 * NS + 7);
+    auto kv_full = [&](int t) { return bar0 + 8u * (t & (NS - 1)); };                 // by a tile's running number
+    auto kv_empty = [&](int t) { return bar0 + 8u * (NS + (t & (NS - 1))); };
+    auto kv_phase = [](int t) { return (uint32_t)(t / NS) & 1u; };
+    auto s_full = [&](int w) { return bar0 + 8u * (2 * NS + w); };                    // by the group
+    auto s_free = [&](int w) { return bar0 + 8u * (2 * NS + NWG + w); };
+    auto p_full = [&](int w) { return bar0 + 8u * (2 * NS + 2 * NWG + w); };
+    auto met = [&](int w) { return bar0 + 8u * (2 * NS + 3 * NWG + w); };
+    auto turn = [&](int w, int quarter) { return bar0 + 8u * (2 * NS + 4 * NWG + 4 * w + quarter); };
+    const uint32_t bar1 = bar0 + 8u * (2 * NS + 8 * NWG);
+    const uint32_t q_ready = bar1, o_full = bar1 + 8, o_free = bar1 + 16, met_all = bar1 + 24, drain_o = bar1 + 32, drain_s = bar1 + 40;
     uint32_t *s_tmem = reinterpret_cast<uint32_t *>(smem + T::OFF_WORDS);
     volatile int *s_abort = reinterpret_cast<volatile int *>(s_tmem + 1);
-    volatile uint32_t *s_bad = s_tmem + 2, *s_flag = s_tmem + 6;
+    volatile uint32_t *s_flag = s_tmem + 2, *s_bad = s_tmem + 2 + NS;
+    volatile float *s_ref = reinterpret_cast<volatile float *>(smem + T::OFF_REF), *s_sum = reinterpret_cast<volatile float *>(smem + T::OFF_SUM);
     int *s_off = reinterpret_cast<int *>(smem + T::OFF_SEQ);
 
     if (tid == 0) {
-        for (int s = 0; s < NS; ++s) {
-            mbar_init(kv_full(s), 1);
-            mbar_init(kv_empty(s), 1);
+        for (int i = 0; i < NS; ++i) {
+            mbar_init(kv_full(i), 1);
+            mbar_init(kv_empty(i), 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(s_full(i), 1);
-            mbar_init(p_full(i), kStripRows);
+        for (int w = 0; w < NWG; ++w) {
+            mbar_init(s_full(w), 2);                    // the score product, and its issuer (who has seen the stage's flag)
+            mbar_init(s_free(w), 4);                    // one arrival per warp: 32 lanes' would be handled one after the other
+            mbar_init(p_full(w), 4);
+            mbar_init(met(w), 4);
+            for (int i = 0; i < 4; ++i) mbar_init(turn(w, i), 1);
         }
-        mbar_init(q_ready, kStripRows);
+        mbar_init(q_ready, 4);
         mbar_init(o_full, 1);
+        mbar_init(o_free, 4 * NWG);
+        mbar_init(met_all, 4 * NWG);
         mbar_init(drain_o, 1);
         mbar_init(drain_s, 1);
         *s_abort = 0;
@@ -74,337 +121,443 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
         asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&tm_v)) : "memory");
         asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&tm_k)) : "memory");
     }
-    if (warp == 5) {
+    if (warp == 4 * NWG + 1) {
         tmem_alloc(smem_u32(s_tmem), T::TMEM_COLS);
         tmem_relinquish();
     }
     grid_dependency_wait();
     tree_offsets(p, s_off);
     if (blockIdx.x == 0)
-        for (int b = tid; b <= p.B; b += kTreeMmaThreads) p.offsets[b] = s_off[b];
+        for (int b = tid; b <= p.B; b += T::THREADS) p.offsets[b] = s_off[b];
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
     TreePieces pieces(p, s_off, c);
     TreePiece pc;
-    int t = 0;                                          // running number of a tile, and of a piece that has any
-    uint32_t n_pc = 0;
+    uint32_t n_pc = 0;                                  // running number of a piece
     bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) { return warp_wait(bar, parity & 1u, s_abort); };
+    // Arrivals of whole warps, by one lane: the barrier unit takes lanes one after the other.
+    auto arrive = [&](uint32_t bar) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+    };
 
-    if (warp < 4) {
+    if (warp < 4 * NWG) {
         // ========================================= softmax: one row per thread =========================================
-        const uint32_t lane_base = tmem + ((uint32_t)(warp * 32) << 16), o_addr = lane_base + T::COL_O;
-        while (ok && pieces.next(p, s_off, pc)) {
-            // Up to 16 nodes are two warps' rows.  The second block on an SM (its tensor memory starts at column 256) takes the lanes of
-            // the upper two warps for them, so that the two blocks' softmax runs on different quarters of the SM.
-            const int lw = warp - ((tmem & 0xffffu) >= 256 && pc.nv <= 16 ? 2 : 0);
-            const bool dead = lw < 0 || lw * 8 >= pc.nv;
-            const int tok = lw * 8 + (lane >> 2), h = g * kHeadsPerGroup + (lane & 3);
-            const bool live = !dead && tok < pc.nv;
-            const size_t node = (size_t)pc.s.r0 + pc.n0 + (live ? tok : 0), row_h = node * p.H + h;
-            const size_t rec = pc.rec >= 0 ? record_row(p, pc.rec, g, live ? tok * kHeadsPerGroup + (lane & 3) : 0) : 0;
-            if (pc.lo >= pc.hi) {                       // more splits than tiles: weighs nothing in the merge
-                if (live) *reinterpret_cast<float2 *>(p.rec_ml + rec * 2) = make_float2(-INFINITY, 0.f);
-                continue;
+        if constexpr (T::SHARE_REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;\n");
+        const int w = warp >> 2, quarter = warp & 3, r = tid & (kStripRows - 1), hl = lane & 3, h = g * kHeadsPerGroup + hl;
+        const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16), o_addr = lane_base + T::COL_O;
+        const uint32_t s_addr = lane_base + T::COL_S + w * kTreeTile, p_addr = lane_base + T::COL_P + w * (kTreeTile / 2);
+        float *s_join = reinterpret_cast<float *>(smem + T::OFF_JOIN) + w * kStripRows * T::JOIN_LD;
+        uint32_t n_tiles = 0;                           // tiles that this group has had: the next one's number is n_tiles * NWG + w
+        uint32_t n_met = 0;
+        // The group's warps meet; false: one of them has given up.  (Not a hardware barrier, on which the others would wait for good.)
+        auto meet = [&]() {
+            arrive(met(w));
+            return wait(met(w), n_met++);
+        };
+        // A row's node of a piece: its copy, whether there is one, its number.
+        auto copies_of = [](const TreePiece &x) { return x.nv <= 16 ? 2 : 1; };
+        auto node_of = [&](const TreePiece &x) { return (quarter & (4 / copies_of(x) - 1)) * 8 + (lane >> 2); };
+        // The next piece with any tile; one without (more splits than tiles) weighs nothing in the merge.
+        auto next_piece = [&](TreePiece &x) {
+            while (pieces.next(p, s_off, x)) {
+                if (x.lo < x.hi) return true;
+                if (w == 0 && r / 4 < x.nv) *reinterpret_cast<float2 *>(p.rec_ml + record_row(p, x.rec, g, r) * 2) = make_float2(-INFINITY, 0.f);
             }
-            // (the last score product of the piece before has been waited for: nothing reads the old query any more)
-            if (!dead) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + row_h * (DV + DR));
-                uint4 x[(DV + T::DRP) / 8];
+            return false;
+        };
+        // The query's rows into tensor memory, once the score products before are done, and fresh references.
+        auto stage_query = [&](const TreePiece &x, uint32_t number, uint32_t last_tile, bool any) {
+            const int tok = node_of(x);
+            const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) +
+                                                               (((size_t)x.s.r0 + x.n0 + min(tok, x.nv - 1)) * p.H + h) * (DV + DR));
+            constexpr int N = (DV + T::DRP) / 8, HALF = (N + 1) / 2;
 #pragma unroll
-                for (int i = 0; i < (DV + T::DRP) / 8; ++i) x[i] = live && i * 8 < DV + DR ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+            for (int half = 0; half < 2; ++half) {
+                uint4 v[HALF];
 #pragma unroll
-                for (int i = 0; i < (DV + T::DRP) / 8; ++i) {
-                    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-                    tmem_st4_nowait(lane_base + T::COL_Q + i * 4, w);
+                for (int i = 0; i < HALF; ++i) {
+                    const int at = half * HALF + i;
+                    v[i] = tok < x.nv && at * 8 < DV + DR ? __ldg(src + at) : make_uint4(0, 0, 0, 0);
                 }
-                tmem_st_wait();
-                tc_fence_before();
+                if (half == 0) {
+                    if (any && !wait(s_full(last_tile % NWG), last_tile / NWG)) return false;
+                    tc_fence_after();
+                }
+#pragma unroll
+                for (int i = 0; i < HALF; ++i) {
+                    if (half * HALF + i >= N) continue;
+                    const uint32_t words[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                    tmem_st4_nowait(lane_base + T::COL_Q + (half * HALF + i) * 4, words);
+                }
             }
-            mbar_arrive(q_ready);
-            float m_run = -INFINITY, l_run = 0.f;       // softmax reference (log2 domain) and sum relative to it
+            s_ref[(number & 1) * kStripRows + r] = -INFINITY;
+            tmem_st_wait();
+            tc_fence_before();
+            arrive(q_ready);
+            return true;
+        };
+        // One tile of a row: `chunks` times 32 of its columns, from col0 on.  Of two chunks the first is loaded again for its weights: the
+        // registers hold 32 scores at a time.  (One copy of this code for all cases: it has to stay in the instruction caches.)
+        float sum = 0.f, sum_ref = -INFINITY;           // this group's sum, and the reference it is relative to
+        auto softmax_tile = [&](int chunks, int col0, uint64_t bits, bool edge, bool first) -> bool {
+            const int t = (int)(n_tiles * NWG) + w;
+            float s[32], m_tile = -INFINITY;
+            auto load = [&](int chunk) {
+                tmem_ld32_nowait(s_addr + col0 + chunk * 32, s);
+                tmem_ld_wait();
+                if (edge) {
+                    const uint32_t seen = (uint32_t)(bits >> (col0 + chunk * 32));
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) s[k] = (seen >> k) & 1 ? s[k] : -INFINITY;
+                }
+            };
+            tc_fence_after();
+#pragma unroll 1
+            for (int i = 0; i < chunks; ++i) {
+                load(i);
+                float mx[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mx[k] = max3(s[k], s[k + 4], s[k + 8]);
+#pragma unroll
+                for (int j = 12; j + 8 <= 32; j += 8)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[j + k], s[j + 4 + k]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], s[28 + k]);
+                m_tile = max3(m_tile, fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            }
+            m_tile *= p.scale_log2;
+            // The reference as the tile before leaves it.  It moves only when a tile's maximum exceeds it by more than 2^8: weights stay
+            // below 256, the quotient is the same, and O in tensor memory is rescaled only then, once the value product before is done.
+            // (tcgen05.ld / .st take whole warps: rows that stay multiply by 1.)
+            if (t > 0 && !wait(turn(w == 0 ? NWG - 1 : w - 1, quarter), w == 0 ? n_tiles - 1 : n_tiles)) return false;
+            float ref = s_ref[(n_pc & 1) * kStripRows + r];
+            const bool move = m_tile > ref + kRescaleLog2;
+            if (__any_sync(kAll, move)) {
+                if (!first) {
+                    if (!wait(kv_empty(t - 1), kv_phase(t - 1))) return false;
+                    tc_fence_after();
+                    const float alpha = move ? fast_exp2(ref - m_tile) : 1.f;
+#pragma unroll 1
+                    for (int part = 0; part < DV / 16; ++part) {
+                        float o[16];
+                        uint32_t words[16];
+                        tmem_ld16(o_addr + part * 16, o);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) words[i] = __float_as_uint(o[i] * alpha);
+                        tmem_st16_nowait(o_addr + part * 16, words);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                }
+                if (move) s_ref[(n_pc & 1) * kStripRows + r] = ref = m_tile;
+            }
+            arrive(turn(w, quarter));
+            if (sum_ref != ref) {
+                sum *= fast_exp2(sum_ref - ref);
+                sum_ref = ref;
+            }
+            if (t >= NWG && !wait(kv_empty(t - NWG), kv_phase(t - NWG))) return false;      // the group's weights before have been used
+            tc_fence_after();
+            const float nm = ref == -INFINITY ? 0.f : -ref;                          // nothing seen yet: all weights 0, not NaN
+            const uint64_t sc2 = f2_pack(p.scale_log2, p.scale_log2), nm2 = f2_pack(nm, nm);
+            uint64_t sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+#pragma unroll 1
+            for (int i = chunks - 1;;) {
+                uint32_t pk[16];
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) {
+                    float a, b;
+                    f2_unpack(f2_fma(f2_pack(s[k], s[k + 1]), sc2, nm2), a, b);
+                    a = fast_exp2(a);
+                    b = fast_exp2(b);
+                    sum2[(k >> 1) & 1] = f2_add(sum2[(k >> 1) & 1], f2_pack(a, b));
+                    pk[k >> 1] = pack_bf16(a, b);
+                }
+                tmem_st16_nowait(p_addr + (col0 + i * 32) / 2, pk);
+                if (--i < 0) break;
+                load(i);
+            }
+            tc_fence_before();
+            arrive(s_free(w));
+            float sa, sb;
+            f2_unpack(f2_add(sum2[0], sum2[1]), sa, sb);
+            sum += sa + sb;
+            tmem_st_wait();
+            tc_fence_before();
+            arrive(p_full(w));
+            return true;
+        };
+
+        bool have = next_piece(pc);
+        uint32_t t_base = 0;                            // running number of the piece's first tile
+        if (have && w == 0) ok = stage_query(pc, 0, 0, false);
+        while (have && ok) {
+            const int copies = copies_of(pc), copy = quarter * copies / 4, tok = node_of(pc);
+            const bool live = tok < pc.nv;
+            const size_t node = (size_t)pc.s.r0 + pc.n0 + (live ? tok : 0), row_h = node * p.H + h;
+            if (copies > 1) {                           // the other copy's tokens weigh nothing
+                const uint32_t none[32] = {};
+                tmem_st32u_nowait(p_addr, none);
+                tmem_st_wait();
+            }
+            sum = 0.f;
+            sum_ref = -INFINITY;
             bool poison = false;
-            for (int j = pc.lo; j < pc.hi; ++j, ++t) {
-                const int st = t % NS, t0 = j * kTreeTile;
-                if (!__all_sync(0xffffffffu, mbar_wait_spin(s_full(t), (t >> 1) & 1, s_abort))) { ok = false; break; }
-                // (complete since before the score product; waited for by every thread because it also publishes the stage's flag)
-                if (!__all_sync(0xffffffffu, mbar_wait_spin(kv_full(st), (t / NS) & 1, s_abort))) { ok = false; break; }
+            const uint32_t t_end = t_base + (uint32_t)(pc.hi - pc.lo);
+            for (; n_tiles * NWG + w < t_end; ++n_tiles) {
+                const int t = (int)(n_tiles * NWG) + w, st = t & (NS - 1), t0 = (pc.lo + (int)(t - t_base)) * kTreeTile;
+                if (!wait(s_full(w), n_tiles)) { ok = false; break; }
                 const uint32_t flag = s_flag[st];
                 const bool edge = t0 + kTreeTile > pc.s.ctx || flag != 0;            // the same for the whole block
                 uint64_t bits = ~0ull;
                 if (edge) {
                     // Value rows that P multiplies by 0 must not be NaN or infinite: those behind the end and of bad pages become zeros, and
                     // so do drafted tokens' rows with such an element (a row that sees one is made NaN at the end instead).
-                    if (tid < kTreeTile) {
-                        unsigned char *v = smem + st * T::STAGE_BYTES + tid * 128;
-                        bool zero = t0 + tid >= pc.s.total || ((flag >> (tid >> 5)) & 1), bad = false;
-                        if (!zero && t0 + tid >= pc.s.ctx) {
-#pragma unroll
+                    volatile uint32_t *bad_rows = s_bad + w * 4 + (n_tiles & 1) * 2; // (two sets: a slow reader of the tile before)
+                    if (r < kTreeTile) {
+                        unsigned char *v = smem + st * T::STAGE_BYTES + r * 128;
+                        bool zero = t0 + r >= pc.s.total || ((flag >> (r >> 5)) & 1), bad = false;
+                        if (!zero && t0 + r >= pc.s.ctx) {
+#pragma unroll 1
                             for (int bx = 0; bx < T::BOXES; ++bx)
-#pragma unroll
+#pragma unroll 2
                                 for (int i = 0; i < 8; ++i) {
                                     const uint4 x = *reinterpret_cast<const uint4 *>(v + bx * T::VBOX_BYTES + i * 16);
-                                    auto odd = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
+                                    auto odd = [](uint32_t y) { return (y & 0x7f80u) == 0x7f80u || (y & 0x7f800000u) == 0x7f800000u; };
                                     bad |= odd(x.x) || odd(x.y) || odd(x.z) || odd(x.w);
                                 }
                         }
                         if (zero || bad)
-#pragma unroll
+#pragma unroll 1
                             for (int bx = 0; bx < T::BOXES; ++bx)
-#pragma unroll
+#pragma unroll 2
                                 for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(v + bx * T::VBOX_BYTES + i * 16) = make_uint4(0, 0, 0, 0);
-                        const uint32_t all = __ballot_sync(0xffffffffu, bad);
-                        if (lane == 0) s_bad[(t & 1) * 2 + warp] = all;              // (two sets: a slow reader of the tile before)
+                        const uint32_t all = __ballot_sync(kAll, bad);
+                        if (lane == 0) bad_rows[quarter] = all;
                     }
                     fence_async_smem();
-                    asm volatile("bar.sync 1, 128;\n" ::: "memory");
+                    if (!meet()) { ok = false; break; }
                     if (live) {
                         bits = tree_window(p.mask + node * p.words, p.words, t0 - pc.s.ctx);
                         const int n = pc.s.total - t0;
                         if (n < kTreeTile) bits &= (1ull << n) - 1;
                         if (flag & 1) bits &= ~0xffffffffull;
                         if (flag & 2) bits &= 0xffffffffull;
-                        poison |= (bits & (s_bad[(t & 1) * 2] | ((uint64_t)s_bad[(t & 1) * 2 + 1] << 32))) != 0;
+                        poison |= (bits & (bad_rows[0] | ((uint64_t)bad_rows[1] << 32))) != 0;
                     }
                 }
-                if (dead) {                             // keeps the protocol going; nothing reads its rows
-                    mbar_arrive(p_full(t));
-                    continue;
-                }
-                tc_fence_after();
-                const uint32_t s_addr = lane_base + T::COL_S + (t & 1) * kTreeTile;
-                float s[kTreeTile];
-                {
-                    float lo[32], hi[32];
-                    tmem_ld32_nowait(s_addr, lo);
-                    tmem_ld32_nowait(s_addr + 32, hi);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) { s[i] = lo[i]; s[32 + i] = hi[i]; }
-                }
-                if (edge) {
-                    const uint32_t b0 = (uint32_t)bits, b1 = (uint32_t)(bits >> 32);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        s[i] = (b0 >> i) & 1 ? s[i] : -INFINITY;
-                        s[32 + i] = (b1 >> i) & 1 ? s[32 + i] : -INFINITY;
-                    }
-                }
-                uint32_t pk[kTreeTile / 2];
-                float tile_sum = 0.f;
-                auto weights = [&](float m_ref) {       // and their sum, relative to the reference
-                    const float nm = m_ref == -INFINITY ? 0.f : -m_ref;              // nothing seen yet: all weights 0, not NaN
-                    const uint64_t sc2 = f2_pack(p.scale_log2, p.scale_log2), nm2 = f2_pack(nm, nm);
-                    uint64_t sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
-#pragma unroll
-                    for (int i = 0; i < kTreeTile; i += 2) {
-                        float a, b;
-                        f2_unpack(f2_fma(f2_pack(s[i], s[i + 1]), sc2, nm2), a, b);
-                        a = fast_exp2(a);
-                        b = fast_exp2(b);
-                        sum2[(i >> 1) & 1] = f2_add(sum2[(i >> 1) & 1], f2_pack(a, b));
-                        pk[i >> 1] = pack_bf16(a, b);
-                    }
-                    float sa, sb;
-                    f2_unpack(f2_add(sum2[0], sum2[1]), sa, sb);
-                    tile_sum = sa + sb;
-                };
-                // As in the prefill kernel: weights against the present reference while the maximum is reduced; a tile whose maximum
-                // exceeds it by more than 2^8 is done again.
-                if (j > pc.lo) weights(m_run);
-                float mx[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mx[k] = max3(s[k], s[k + 4], s[k + 8]);
-#pragma unroll
-                for (int i = 12; i + 8 <= kTreeTile; i += 8)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[i + k], s[i + 4 + k]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], s[kTreeTile - 4 + k]);
-                const float m_tile = max3(mx[0], mx[1], fmaxf(mx[2], mx[3])) * p.scale_log2;
-                const bool move = m_tile > m_run + kRescaleLog2;
-                if (j == pc.lo || __any_sync(0xffffffffu, move)) {
-                    float alpha = 1.f;
-                    if (move) {
-                        alpha = fast_exp2(m_run - m_tile);
-                        l_run *= alpha;
-                        m_run = m_tile;
-                    }
-                    if (j > pc.lo) {                    // the piece's O so far, once the value product before has landed
-                        if (!__all_sync(0xffffffffu, mbar_wait_spin(kv_empty((t - 1) % NS), ((t - 1) / NS) & 1, s_abort))) { ok = false; break; }
-                        tc_fence_after();
-                        const uint64_t al2 = f2_pack(alpha, alpha);
-#pragma unroll
-                        for (int part = 0; part < DV / 32; ++part) {
-                            float o[32];
-                            tmem_ld32_nowait(o_addr + part * 32, o);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) f2_unpack(f2_mul(f2_pack(o[i], o[i + 1]), al2), o[i], o[i + 1]);
-                            tmem_st32(o_addr + part * 32, o);
-                        }
-                    }
-                    weights(m_run);
-                }
-                tmem_st32u_nowait(s_addr, pk);
-                l_run += tile_sum;
-                tmem_st_wait();
-                tc_fence_before();
-                mbar_arrive(p_full(t));
+                const bool first = (uint32_t)t == t_base;
+                ok = softmax_tile(2 / copies, copy * 32, bits, edge, first);
+                if (!ok) break;
             }
-            if (ok && !__all_sync(0xffffffffu, mbar_wait_spin(o_full, n_pc & 1, s_abort))) ok = false;
-            ++n_pc;
-            if (!ok || dead) continue;
+            TreePiece nx;
+            const bool more = next_piece(nx);
+            if (ok && more && w == 0) ok = stage_query(nx, n_pc + 1, t_end - 1, true);
+            ok = ok && wait(o_full, n_pc);
+            if (!__all_sync(kAll, ok)) { ok = false; break; }
+            // All value products are done, so all references are final: sums relative to them from every group, then the copies' shares.
+            const uint32_t set = n_pc & 1;
+            volatile float *refs = s_ref + set * kStripRows, *sums = s_sum + set * T::SOFTMAX;
+            const float own_ref = refs[r];
+            sums[tid] = poison ? __int_as_float(0x7fc00000) : sum == 0.f ? 0.f : sum * fast_exp2(sum_ref - own_ref);
+            arrive(met_all);
+            if (!wait(met_all, n_pc)) { ok = false; break; }
+            float m = -INFINITY, l = 0.f, share = 1.f;
+            {
+                const int rows = kStripRows / copies, r0 = r & (rows - 1);
+                for (int k = 0; k < copies; ++k) m = fmaxf(m, refs[r0 + k * rows]);
+                const float ref = m == -INFINITY ? 0.f : m;
+                for (int k = 0; k < copies; ++k) {
+                    float x = 0.f;
+#pragma unroll
+                    for (int i = 0; i < NWG; ++i) x += sums[i * kStripRows + r0 + k * rows];
+                    l += x == 0.f ? 0.f : fast_exp2(refs[r0 + k * rows] - ref) * x;
+                }
+                if (copies > 1) share = own_ref == -INFINITY ? 0.f : fast_exp2(own_ref - ref);
+            }
+            const size_t rec = pc.rec >= 0 ? record_row(p, pc.rec, g, live ? tok * kHeadsPerGroup + hl : 0) : 0;
+            if (w == 0 && live && copy == 0) {
+                if (pc.rec >= 0) *reinterpret_cast<float2 *>(p.rec_ml + rec * 2) = make_float2(m, l);
+                else if (p.lse) p.lse[row_h] = tree_lse(m, l);
+            }
+            const float inv = (pc.rec < 0 ? tree_inverse(l) : 1.f) * share;
             tc_fence_after();
-            if (poison) l_run = __int_as_float(0x7fc00000);
-            const float inv = pc.rec < 0 ? tree_inverse(l_run) : 1.f;
+#pragma unroll 1
+            for (int part = w; part < DV / T::PART; part += NWG) {
+                float o[T::PART];
+                tmem_ld16(o_addr + part * T::PART, o);
 #pragma unroll
-            for (int part = 0; part < DV / 32; ++part) {
-                float o[32];
-                tmem_ld32_nowait(o_addr + part * 32, o);
-                tmem_ld_wait();
-                if (live) {
+                for (int i = 0; i < T::PART; ++i) o[i] *= inv;
+                if (copies > 1) {
+                    if (copy > 0)
+#pragma unroll
+                        for (int i = 0; i < T::PART; i += 4)
+                            *reinterpret_cast<float4 *>(s_join + r * T::JOIN_LD + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    if (!meet()) { ok = false; break; }
+                    if (copy == 0)
+                        for (int k = 1; k < copies; ++k)
+#pragma unroll
+                            for (int i = 0; i < T::PART; i += 4) {
+                                const float4 x = *reinterpret_cast<const float4 *>(s_join + (r + k * (kStripRows / copies)) * T::JOIN_LD + i);
+                                o[i] += x.x;
+                                o[i + 1] += x.y;
+                                o[i + 2] += x.z;
+                                o[i + 3] += x.w;
+                            }
+                    if (!meet()) { ok = false; break; }
+                }
+                if (live && copy == 0) {
                     if (pc.rec < 0) {
-                        uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row_h * DV + part * 32);
+                        uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + row_h * DV + part * T::PART);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8)
-                            dst[i / 8] = make_uint4(pack_bf16(o[i] * inv, o[i + 1] * inv), pack_bf16(o[i + 2] * inv, o[i + 3] * inv),
-                                                    pack_bf16(o[i + 4] * inv, o[i + 5] * inv), pack_bf16(o[i + 6] * inv, o[i + 7] * inv));
+                        for (int i = 0; i < T::PART; i += 8)
+                            dst[i / 8] = make_uint4(pack_bf16(o[i], o[i + 1]), pack_bf16(o[i + 2], o[i + 3]), pack_bf16(o[i + 4], o[i + 5]), pack_bf16(o[i + 6], o[i + 7]));
                     } else {
-                        float4 *dst = reinterpret_cast<float4 *>(p.rec_o + rec * DV + part * 32);
+                        float4 *dst = reinterpret_cast<float4 *>(p.rec_o + rec * DV + part * T::PART);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) dst[i / 4] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        for (int i = 0; i < T::PART; i += 4) dst[i / 4] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                     }
                 }
             }
-            if (live) {
-                if (pc.rec >= 0) *reinterpret_cast<float2 *>(p.rec_ml + rec * 2) = make_float2(m_run, l_run);
-                else if (p.lse) p.lse[row_h] = tree_lse(m_run, l_run);
-            }
+            tc_fence_before();
+            arrive(o_free);
+            t_base = t_end;
+            ++n_pc;
+            pc = nx;
+            have = more;
         }
-        if (!ok && !*s_abort) {
-            report_error(p.dev_status, GVA_ERR_TIMEOUT, pc.b);
-            *s_abort = 1;
-        }
-        tc_fence_before();
-    } else if (warp == 6) {
-        // ==================================== loader: one lane issues, all look pages up ====================================
-        const bool whole = p.P % kTreeTile == 0;        // a tile lies in one page; else its two halves do, each in its own
-        const uint64_t stream = l2_policy_evict_first();
-        while (ok && pieces.next(p, s_off, pc)) {
-            for (int base = pc.lo; base < pc.hi && ok; base += 32) {
-                int page0 = -1, page1 = -1;             // (-2: a half behind the sequence's end)
-                if (base + lane < pc.hi) {
-                    const int t0 = (base + lane) * kTreeTile;
-                    auto look = [&](int at) {
-                        const long long page = tree_page(p, pc.b, at / p.P);
-                        return page < 0 || page >= p.num_pages ? -1 : (int)page;
-                    };
-                    page0 = look(t0);
-                    if (!whole) page1 = t0 + 32 < pc.s.total ? look(t0 + 32) : -2;
-                    if (page0 == -1 || (!whole && page1 == -1)) report_error(p.dev_status, GVA_ERR_BAD_PAGE, pc.b);
-                }
-                const int n = min(32, pc.hi - base);
-                for (int i = 0; i < n && ok; ++i, ++t) {
-                    const int pg0 = __shfl_sync(0xffffffffu, page0, i), pg1 = __shfl_sync(0xffffffffu, page1, i);
-                    if (lane == 0) {
-                        const int st = t % NS;
-                        if (t >= NS) ok = mbar_wait_sleepy(kv_empty(st), ((t / NS) - 1) & 1, s_abort);
-                        if (ok) {
-                            const int at = ((base + i) * kTreeTile) % p.P;
-                            const uint32_t dst = s_base + st * T::STAGE_BYTES;
-                            s_flag[st] = whole ? (pg0 < 0 ? 3u : 0u) : (pg0 < 0 ? 1u : 0u) | (pg1 == -1 ? 2u : 0u);
-                            const int boxes = (pg0 >= 0 ? 1 : 0) + (!whole && pg1 >= 0 ? 1 : 0);
-                            const uint32_t bytes = (uint32_t)(T::V_BYTES + T::KR_BYTES) / (whole ? 1 : 2) * boxes;
-                            if (boxes == 0) mbar_arrive(kv_full(st));
-                            else mbar_expect_tx(kv_full(st), bytes);
-                            auto fetch = [&](int page, int slot, int row) {
+    } else {
+        if constexpr (T::SHARE_REGS) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
+        int t = 0;                                      // running number of a tile
+        if (warp >= 4 * NWG + 2) {
+            // ========================== loaders: of even and of odd tiles; all lanes look pages up, one issues ==========================
+            const bool whole = p.P % kTreeTile == 0;    // a tile lies in one page; else its two halves do, each in its own
+            const uint64_t stream = l2_policy_evict_first();
+            while (ok && pieces.next(p, s_off, pc)) {
+                for (int base = pc.lo; base < pc.hi && ok; base += 32) {
+                    // rows of the pools where a lane's tile begins (its halves, where they lie apart); -1: a bad page, -2: nothing there
+                    int v0 = -2, k0 = -2, v1 = -2, k1 = -2;
+                    if (base + lane < pc.hi) {
+                        auto look = [&](int at, int &v, int &k) {
+                            const int j = at / p.P, slot = at - j * p.P;
+                            const long long page = tree_page(p, pc.b, j);
+                            const bool bad = page < 0 || page >= p.num_pages;
+                            if (bad) report_error(p.dev_status, GVA_ERR_BAD_PAGE, pc.b);
+                            v = bad ? -1 : ((int)page * p.G + g) * p.P + slot;
+                            k = (int)page * p.P + slot;
+                        };
+                        const int t0 = (base + lane) * kTreeTile;
+                        look(t0, v0, k0);
+                        if (!whole && t0 + 32 < pc.s.total) look(t0 + 32, v1, k1);
+                    }
+                    const int n = min(32, pc.hi - base);
+                    for (int i = 0; i < n; ++i, ++t) {
+                        if ((t ^ warp) & 1) continue;
+                        const int va = __shfl_sync(kAll, v0, i), ka = __shfl_sync(kAll, k0, i), vb = __shfl_sync(kAll, v1, i), kb = __shfl_sync(kAll, k1, i);
+                        if (t >= NS && !wait(kv_empty(t), kv_phase(t) ^ 1u)) { ok = false; break; }
+                        const uint32_t full = kv_full(t), dst = s_base + (t & (NS - 1)) * T::STAGE_BYTES;
+                        if (elect_one()) {
+                            s_flag[t & (NS - 1)] = (va == -1 ? (whole ? 3u : 1u) : 0u) | (vb == -1 ? 2u : 0u);
+                            const uint32_t half = (uint32_t)(T::V_BYTES + T::KR_BYTES) / 2, bytes = (va >= 0 ? (whole ? 2 * half : half) : 0u) + (vb >= 0 ? half : 0u);
+                            if (bytes == 0) mbar_arrive(full);
+                            else mbar_expect_tx(full, bytes);
+                            if (va >= 0) {
 #pragma unroll
-                                for (int bx = 0; bx < T::BOXES; ++bx)
-                                    tma_load_2d_stream(dst + bx * T::VBOX_BYTES + row * 128, &tm_v, bx * 64, (page * p.G + g) * p.P + slot, kv_full(st), stream);
-                                if constexpr (DR > 0) tma_load_2d(dst + T::V_BYTES + row * T::KR_ROW, &tm_k, 0, page * p.P + slot, kv_full(st));
-                            };
-                            if (pg0 >= 0) fetch(pg0, at, 0);
-                            if (!whole && pg1 >= 0) fetch(pg1, (at + 32) % p.P, 32);
+                                for (int bx = 0; bx < T::BOXES; ++bx) tma_load_2d_stream(dst + bx * T::VBOX_BYTES, &tm_v, bx * 64, va, full, stream);
+                                if constexpr (DR > 0) tma_load_2d(dst + T::V_BYTES, &tm_k, 0, ka, full);
+                            }
+                            if (vb >= 0) {
+#pragma unroll
+                                for (int bx = 0; bx < T::BOXES; ++bx) tma_load_2d_stream(dst + bx * T::VBOX_BYTES + 32 * 128, &tm_v, bx * 64, vb, full, stream);
+                                if constexpr (DR > 0) tma_load_2d(dst + T::V_BYTES + 32 * T::KR_ROW, &tm_k, 0, kb, full);
+                            }
                         }
+                        __syncwarp();
                     }
-                    ok = __shfl_sync(0xffffffffu, ok, 0);
                 }
-            }
-        }
-        if (lane == 0) {
-            if (!ok && !*s_abort) {
-                report_error(p.dev_status, GVA_ERR_TIMEOUT, pc.b);
-                *s_abort = 1;
             }
             // copies in flight must land before the block's shared memory is released
-            for (int k = max(0, t - NS); k < t; ++k)
-                for (int it = 0; it < kDrainPolls && !mbar_try_wait(kv_full(k % NS), (k / NS) & 1); ++it) {}
-        }
-    } else if (lane == 0) {
-        // ======================================= MMA issuers: one thread per product =======================================
-        constexpr uint32_t hi128 = (1024u >> 4) | (1u << 14) | ((uint32_t)kSwz128 << 29);        // (descriptors as in the prefill kernel)
-        constexpr uint32_t hikr = ((8u * T::KR_ROW) >> 4) | (1u << 14) | ((uint32_t)(T::KR_ROW == 32 ? kSwz32 : kSwz64) << 29);
-        constexpr uint32_t lo_k = (16u >> 4) << 16, lo_mn = ((uint32_t)T::VBOX_BYTES >> 4) << 16;
-        const uint32_t a_st = (s_base & 0x3FFFFu) >> 4;
-        auto mk = [](uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); };
-        int issued = 0;
-        if (warp == 5) {
-            constexpr uint32_t idesc = umma_idesc(kStripRows, kTreeTile, false);
-            while (ok && pieces.next(p, s_off, pc)) {
-                if (pc.lo >= pc.hi) continue;
-                if (!mbar_wait_spin(q_ready, n_pc & 1, s_abort)) { ok = false; break; }
-                ++n_pc;
-                for (int j = pc.lo; j < pc.hi; ++j, ++t) {
-                    // S[t & 1] also holds the weights of tile t - 2: its value product must have completed
-                    if (!mbar_wait_spin(kv_full(t % NS), (t / NS) & 1, s_abort)) { ok = false; break; }
-                    if (t >= 2 && !mbar_wait_spin(kv_empty((t - 2) % NS), ((t - 2) / NS) & 1, s_abort)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t vb = a_st + (uint32_t)(t % NS) * (T::STAGE_BYTES >> 4), d = tmem + T::COL_S + (t & 1) * kTreeTile;
+            if (!ok || *s_abort)
+                for (int k = max(0, t - NS); k < t; ++k)   // (the other loader's too, once they are issued: a bounded wait)
+                    for (int it = 0; it < kDrainPolls && !mbar_try_wait(kv_full(k), kv_phase(k)); ++it) {}
+        } else if (warp < 4 * NWG + 2) {
+            // ================================= MMA issuers: a warp per product, one elected lane issues =================================
+            constexpr uint32_t hi128 = (1024u >> 4) | (1u << 14) | ((uint32_t)kSwz128 << 29);    // (descriptors as in the prefill kernel)
+            constexpr uint32_t hikr = ((8u * T::KR_ROW) >> 4) | (1u << 14) | ((uint32_t)(T::KR_ROW == 32 ? kSwz32 : kSwz64) << 29);
+            constexpr uint32_t lo_k = (16u >> 4) << 16, lo_mn = ((uint32_t)T::VBOX_BYTES >> 4) << 16;
+            const uint32_t a_st = (s_base & 0x3FFFFu) >> 4;
+            auto mk = [](uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); };
+            int w = 0;
+            uint32_t round = 0;                         // t = round * NWG + w
+            if (warp == 4 * NWG + 1) {
+                constexpr uint32_t idesc = umma_idesc(kStripRows, kTreeTile, false);
+                while (ok && pieces.next(p, s_off, pc)) {
+                    if (pc.lo >= pc.hi) continue;
+                    if (!wait(q_ready, n_pc)) { ok = false; break; }
+                    ++n_pc;
+                    for (int j = pc.lo; j < pc.hi; ++j, ++t) {
+                        if (!wait(kv_full(t), kv_phase(t))) { ok = false; break; }
+                        if (round > 0 && !wait(s_free(w), round - 1)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t vb = a_st + (uint32_t)(t & (NS - 1)) * (T::STAGE_BYTES >> 4), d = tmem + T::COL_S + w * kTreeTile;
+                        if (elect_one()) {
 #pragma unroll
-                    for (int ks = 0; ks < KS_S; ++ks) {
-                        const uint32_t off = ks < KS_V ? ((ks >> 2) * T::VBOX_BYTES + (ks & 3) * 32) >> 4 : (T::V_BYTES >> 4) + (uint32_t)(ks - KS_V) * 2;
-                        umma_bf16_ts(d, tmem + T::COL_Q + ks * 8, mk((vb + off) | lo_k, ks < KS_V ? hi128 : hikr), idesc, ks > 0);
+                            for (int ks = 0; ks < KS_S; ++ks) {
+                                const uint32_t off = ks < KS_V ? ((ks >> 2) * T::VBOX_BYTES + (ks & 3) * 32) >> 4 : (T::V_BYTES >> 4) + (uint32_t)(ks - KS_V) * 2;
+                                umma_bf16_ts(d, tmem + T::COL_Q + ks * 8, mk((vb + off) | lo_k, ks < KS_V ? hi128 : hikr), idesc, ks > 0);
+                            }
+                            umma_commit(s_full(w));
+                            mbar_arrive(s_full(w));
+                        }
+                        __syncwarp();
+                        if (++w == NWG) { w = 0; ++round; }
                     }
-                    umma_commit(s_full(t));
-                    issued = 1;
                 }
-            }
-        } else {
-            constexpr uint32_t idesc = umma_idesc(kStripRows, DV, true);
-            while (ok && pieces.next(p, s_off, pc)) {
-                if (pc.lo >= pc.hi) continue;
-                for (int j = pc.lo; j < pc.hi; ++j, ++t) {
-                    // every row has stored its weights of tile t and finished any rescaling of O
-                    if (!mbar_wait_spin(p_full(t), (t >> 1) & 1, s_abort)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t vb = a_st + (uint32_t)(t % NS) * (T::STAGE_BYTES >> 4);
+            } else {
+                constexpr uint32_t idesc = umma_idesc(kStripRows, DV, true);
+                while (ok && pieces.next(p, s_off, pc)) {
+                    if (pc.lo >= pc.hi) continue;
+                    for (int j = pc.lo; j < pc.hi; ++j, ++t) {
+                        // every row has stored its weights of tile t and finished any rescaling of O; of a new piece, the one before has been read
+                        if (!wait(p_full(w), round)) { ok = false; break; }
+                        if (j == pc.lo && n_pc > 0 && !wait(o_free, n_pc - 1)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t vb = a_st + (uint32_t)(t & (NS - 1)) * (T::STAGE_BYTES >> 4), a = tmem + T::COL_P + w * (kTreeTile / 2);
+                        if (elect_one()) {
 #pragma unroll
-                    for (int ks = 0; ks < KS_O; ++ks)
-                        umma_bf16_ts(tmem + T::COL_O, tmem + T::COL_S + (t & 1) * kTreeTile + ks * 8, mk((vb + ks * (16 * 128 >> 4)) | lo_mn, hi128), idesc,
-                                     (j > pc.lo || ks > 0) ? 1u : 0u);
-                    umma_commit(kv_empty(t % NS));
-                    issued = 1;
+                            for (int ks = 0; ks < KS_O; ++ks)
+                                umma_bf16_ts(tmem + T::COL_O, a + ks * 8, mk((vb + ks * (16 * 128 >> 4)) | lo_mn, hi128), idesc, (j > pc.lo || ks > 0) ? 1u : 0u);
+                            umma_commit(kv_empty(t));
+                            if (j + 1 == pc.hi) umma_commit(o_full);
+                        }
+                        __syncwarp();
+                        if (++w == NWG) { w = 0; ++round; }
+                    }
+                    ++n_pc;
                 }
-                if (ok) umma_commit(o_full);
+            }
+            // nothing issued here may still be running (or about to signal a barrier) when the block ends
+            if (t > 0) {
+                const uint32_t dr = warp == 4 * NWG + 1 ? drain_s : drain_o;
+                if (elect_one()) umma_commit(dr);
+                __syncwarp();
+                for (int it = 0; it < kDrainPolls * 16 && !mbar_try_wait(dr, 0); ++it) {}
             }
         }
-        if (!ok && !*s_abort) {
-            report_error(p.dev_status, GVA_ERR_TIMEOUT, pc.b);
-            *s_abort = 1;
-        }
-        // nothing issued by this thread may still be running (or about to signal a barrier) when the block ends
-        if (issued) {
-            const uint32_t dr = warp == 5 ? drain_s : drain_o;
-            umma_commit(dr);
-            for (int it = 0; it < kDrainPolls * 16 && !mbar_try_wait(dr, 0); ++it) {}
-        }
-        tc_fence_before();
     }
+    if (!ok && lane == 0 && !*s_abort) {
+        report_error(p.dev_status, GVA_ERR_TIMEOUT, pc.b);
+        *s_abort = 1;
+    }
+    tc_fence_before();
     grid_dependency_launch();
     __syncthreads();
-    if (warp == 5) {
+    if (warp == 4 * NWG + 1) {
         tc_fence_after();
         tmem_dealloc(tmem, T::TMEM_COLS);
     }
@@ -414,11 +567,11 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
 using TreeMmaFn = void (*)(TreeParams, CUtensorMap, CUtensorMap);
 struct TreeMma {
     TreeMmaFn fn;
-    int blocks_per_sm, drp;
+    int threads, drp;
     size_t fixed;                    // shared memory without the offsets of sequences
 };
 template <int DV, int DR>
-TreeMma tree_mma_t() { return TreeMma{tree_mma_kernel<DV, DR>, TreeTraits<DV, DR>::BLOCKS_PER_SM, TreeTraits<DV, DR>::DRP, TreeTraits<DV, DR>::smem_bytes(0)}; }
+TreeMma tree_mma_t() { return TreeMma{tree_mma_kernel<DV, DR>, TreeTraits<DV, DR>::THREADS, TreeTraits<DV, DR>::DRP, TreeTraits<DV, DR>::smem_bytes(0)}; }
 inline TreeMma tree_mma(const gva_config &c) {
     if (c.d_v == 64) return c.d_r == 16 ? tree_mma_t<64, 16>() : c.d_r == 24 ? tree_mma_t<64, 24>() : tree_mma_t<64, 0>();
     return c.d_r == 32 ? tree_mma_t<128, 32>() : tree_mma_t<128, 0>();

@@ -40,7 +40,7 @@ int rows_per_block(const gva_handle *h, int n, int most) { return (int)std::min<
 
 // ---- the tree's launch ----
 struct TreePlan {
-    int strips, ranges, num_splits;
+    int tile, strips, ranges, num_splits;
     long long records;
     size_t smem, rec_o, rec_ml, total;       // shared memory of a block; workspace: offsets, records, their maxima and sums
 };
@@ -48,14 +48,15 @@ int tree_status(const gva_handle *h, int B, int n_q, int max_q_len, int max_seq_
     if (!h || B < 0 || n_q < 0 || max_q_len < 0 || max_seq_len < 0 || num_splits < 0) return GVA_ERR_INVALID_ARG;
     if (B > 8192 || max_q_len > kTreeMost || num_splits > 64) return GVA_ERR_UNSUPPORTED;
     const long long strips = ceil_div(max_q_len, kStripNodes) * B;
-    if (strips * std::max<long long>(ceil_div(max_seq_len, kTreeTile), num_splits) >= (1ll << 30)) return GVA_ERR_UNSUPPORTED;   // (tiles are counted in 32 bits)
+    if (strips * std::max<long long>(ceil_div(max_seq_len, kTreeFmaTile), num_splits) >= (1ll << 30)) return GVA_ERR_UNSUPPORTED;   // (tiles are counted in 32 bits)
     return GVA_OK;
 }
 TreePlan tree_plan(const gva_handle *h, int B, int max_q_len, int max_seq_len, int num_splits) {
     const gva_config &c = h->cfg;
     TreePlan t;
     t.strips = (int)std::max<long long>(1, ceil_div(max_q_len, kStripNodes));
-    const long long tiles = std::max<long long>(1, ceil_div(max_seq_len, kTreeTile)), all = (long long)std::max(B, 1) * t.strips;
+    t.tile = c.cache_dtype == GVA_BF16 ? kTreeTile : kTreeFmaTile;
+    const long long tiles = std::max<long long>(1, ceil_div(max_seq_len, t.tile)), all = (long long)std::max(B, 1) * t.strips;
     t.num_splits = num_splits;
     const bool mma = c.cache_dtype == GVA_BF16;
     const TreeMma k = tree_mma(c);
@@ -241,7 +242,7 @@ int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const 
     p.rec_ml = reinterpret_cast<float *>(ws + plan.rec_ml);
     p.B = B; p.H = c.H; p.G = c.G; p.P = c.page_size; p.num_pages = cache->num_pages; p.max_pages = cache->max_pages_per_seq; p.words = mask_words;
     p.max_q_len = max_q_len; p.max_seq_len = max_seq_len;
-    p.strips = plan.strips; p.ranges = plan.ranges; p.num_splits = plan.num_splits;
+    p.tile = plan.tile; p.strips = plan.strips; p.ranges = plan.ranges; p.num_splits = plan.num_splits;
     p.scale_log2 = h->scale * kLog2e;
     if (plan.smem > (size_t)h->smem_optin) return GVA_ERR_UNSUPPORTED;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -5,7 +5,7 @@
 //     s_ij = q~_i,h . v_j,g + q^rope_i,h . k^rope_j,   o_i,h = softmax_j(s_ij / sqrt(d_qk)) V_g,   j < ctx or bit (j - ctx).
 //
 // Work: a sequence's nodes are cut into strips of at most 32 (x 4 heads of a group = 128 rows, the M of one MMA), the strip's
-// cache into tiles of 64 tokens.  All strips' tiles in a row, sequence by sequence, are the flat list; it is cut into equal
+// cache into tiles of 64 or 128 tokens.  All strips' tiles in a row, sequence by sequence, are the flat list; it is cut into equal
 // ranges, each of which G neighbouring blocks share, one per value group (they read the same positional keys).  A piece = what
 // a range holds of one strip.  A strip in one piece is written at once; the pieces of others leave unnormalised (O, m, l)
 // records that tree_merge_kernel joins.
@@ -15,7 +15,7 @@
 
 namespace gva {
 
-constexpr int kStripNodes = 32, kStripRows = kStripNodes * kHeadsPerGroup, kTreeTile = 64;
+constexpr int kStripNodes = 32, kStripRows = kStripNodes * kHeadsPerGroup;
 
 struct TreeParams {
     const void *q;               // [n_q][H][d_v + d_r]
@@ -29,6 +29,7 @@ struct TreeParams {
     float *rec_o, *rec_ml;       // workspace records [..][G][128][d_v], [..][G][128][2]
     int B, H, G, P, num_pages, max_pages, words;
     int max_q_len, max_seq_len;
+    int tile;                    // tokens of a tile
     int strips;                  // of a sequence at most
     int ranges;                  // balanced form: ranges of the flat list; uniform form: blocks (of a group) that share the pieces
     int num_splits;              // 0: balanced; n: every strip in n pieces
@@ -50,7 +51,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams &p, int b, bool say
     if (!fine) s.n = 0;
     s.total = (int)total;
     s.strips = (s.n + kStripNodes - 1) / kStripNodes;
-    s.tiles = s.n > 0 ? (s.total + kTreeTile - 1) / kTreeTile : 0;
+    s.tiles = s.n > 0 ? (s.total + p.tile - 1) / p.tile : 0;
     s.per_strip = s.strips > 0 ? (s.n + s.strips - 1) / s.strips : 0;     // nodes, shared out evenly
     return s;
 }
@@ -104,7 +105,7 @@ struct TreePieces {
             step = c;
         }
     }
-    __device__ __forceinline__ bool next(const TreeParams &p, const int *s_off, TreePiece &t) {
+    __device__ __noinline__ bool next(const TreeParams &p, const int *s_off, TreePiece &t) {      // (rare, and large: 64-bit divisions)
         if (x >= end) return false;
         if (p.num_splits > 0) {
             const int strip = x / p.num_splits, k = x - strip * p.num_splits;
@@ -153,7 +154,7 @@ __device__ __forceinline__ float tree_lse(float m, float l) { return (m + log2f(
 
 // ---- CUDA cores: f32 and e4m3 caches ------------------------------------------------------------------------
 // 256 threads, two per row: each scores 16 of 32 tokens, holds half of the row's output in registers.
-constexpr int kTreeFmaThreads = 256, kTreeFmaTokens = 32;
+constexpr int kTreeFmaThreads = 256, kTreeFmaTokens = 32, kTreeFmaTile = 64;
 inline size_t tree_fma_smem(int B, int d_v, int d_r) {
     return (size_t)(kStripRows + kTreeFmaTokens) * (d_v + d_r + 4) * 4 + (size_t)kStripRows * (kTreeFmaTokens + 1) * 4 + (size_t)(B + 1) * 4;
 }
@@ -189,7 +190,7 @@ tree_fma_kernel(TreeParams p, int d_r) {
         float m = -INFINITY, l = 0.f, acc[DV / 2];
 #pragma unroll
         for (int i = 0; i < DV / 2; ++i) acc[i] = 0.f;
-        for (int t0 = t.lo * kTreeTile; t0 < min(t.hi * kTreeTile, t.s.total); t0 += kTreeFmaTokens) {
+        for (int t0 = t.lo * kTreeFmaTile; t0 < min(t.hi * kTreeFmaTile, t.s.total); t0 += kTreeFmaTokens) {
             const long long page = tree_page(p, t.b, t0 / p.P);           // 32 tokens lie in one page
             if (page < 0 || page >= p.num_pages) {                        // counts as empty
                 if (tid == 0) report_error(p.dev_status, GVA_ERR_BAD_PAGE, t.b);

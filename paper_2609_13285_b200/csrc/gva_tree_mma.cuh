@@ -1,14 +1,15 @@
 // gva_decode_tree over a bf16 cache on the 5th-generation tensor cores (tcgen05 + tensor memory), sm_100a.
 //
-// A block (one per SM) works on one value group: the strip's 128 rows (32 nodes x 4 heads) are the M of every MMA, a tile of 64
+// A block (one per SM) works on one value group: the strip's 128 rows (32 nodes x 4 heads) are the M of every MMA, a tile of 128
 // cached tokens is the N of the score product and the K of the value product, so one tile in shared memory feeds both.
-//   NWG groups of 4 warps   softmax: tile t is group t % NWG's, a thread owns a row = a lane of tensor memory
-//   4 more warps            issuer of the value products, issuer of the score products (owns the tensor memory), two loaders
-//   S[t % NWG] = Q K^T (Q from tensor memory)  ->  weights as bf16 pairs in P[t % NWG]  ->  O += P V
-// A tile's way through the softmax is a chain of some 1500 cycles (waits, tensor-memory round trips, 64 exponentials a thread) against
-// 360 (d_v = 64) or 725 that its bytes take from memory: four (three) tiles are on their way side by side.  They share one O, so
-// they share the rows' softmax references too: those go from tile to tile through shared memory in the tiles' order (`turn`), which is
-// a short step as long as no maximum moves one.  Sums stay with each group, relative to the reference they were made with.
+//   2 groups of 4 warps   softmax: tile t is group t % 2's, a thread owns a row = a lane of tensor memory
+//   4 more warps          issuer of the value products, issuer of the score products (owns the tensor memory), two loaders
+//   S[t % 2] = Q K^T (Q from tensor memory, d_v = 128: shared memory)  ->  weights as bf16 pairs in P[t % 2]  ->  O += P V
+// What bounds it is neither bytes nor a pipe but every role's chain of steps per tile: a wait that is complete already takes 150
+// cycles, an MMA 40 to 60 to issue, a tile in all some 600 for each issuer and 1500 and more for the softmax.  Hence large tiles (64
+// tokens with four groups: 180 us for 1 M narrow tokens, 16 nodes), and two of them side by side.  They share one O, so they share the
+// rows' softmax references too: those go from tile to tile through shared memory in the tiles' order (`turn`), which is a short step as
+// long as no maximum moves one.  Sums stay with each group, relative to the reference they were made with.
 // Few nodes leave rows of the MMA unused, and its time is the same: up to 16 nodes are laid out twice, and each copy weighs its half
 // of every tile's tokens and has zeros for the others -- a sequence of its own, joined with the other at the end.
 // The running number of a tile over the block's pieces decides its stage, its group and every barrier's phase; loader and query run
@@ -30,13 +31,21 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
                  : "memory");
     tmem_ld_wait();
 }
-// Bounded wait of a whole warp, straight-line where the phase is complete already, as it mostly is: 30 cycles (220 with one lane waiting
-// and the others behind a shuffle).
-constexpr uint32_t kWarpPolls = 1u << 25;       // 40 cycles each: about a second
+// Bounded wait of a whole warp, straight-line where the phase is complete already, as it mostly is (with one lane waiting and the others
+// behind a shuffle it took 100 cycles more).
+constexpr uint32_t kWarpPolls = 1u << 24;       // 100 cycles each: about a second
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
     for (uint32_t it = 0; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity));)
         if ((++it & 1023u) == 0 && (it >= kWarpPolls || __any_sync(0xffffffffu, *abort_flag))) return false;
     return true;
+}
+// Both of two phases: what they cost when complete overlaps.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t bar2, uint32_t parity2, volatile int *abort_flag) {
+    for (uint32_t it = 0;;) {
+        const bool one = mbar_try_wait(bar, parity), two = mbar_try_wait(bar2, parity2);
+        if (__all_sync(0xffffffffu, one && two)) return true;
+        if ((++it & 1023u) == 0 && (it >= kWarpPolls || __any_sync(0xffffffffu, *abort_flag))) return false;
+    }
 }
 __device__ __forceinline__ bool elect_one() {
     uint32_t yes;
@@ -44,30 +53,33 @@ __device__ __forceinline__ bool elect_one() {
     return yes != 0;
 }
 
+constexpr int kTreeTile = 128;
 template <int DV, int DR>
 struct TreeTraits {
-    static constexpr int NWG = DV == 64 ? 4 : 3;
-    static constexpr int NSTAGE = 8;                             // (a power of two)
+    static constexpr int NWG = 2;
+    static constexpr int NSTAGE = DV == 64 ? 6 : 3;
     static constexpr int BOXES = DV / 64;
     static constexpr int DRP = (DR + 15) / 16 * 16;              // d_r = 24 occupies 32: the box reads zeros behind the row
     static constexpr int KR_ROW = DRP * 2;
     static constexpr int VBOX_BYTES = kTreeTile * 128;
     static constexpr int V_BYTES = BOXES * VBOX_BYTES;
     static constexpr int KR_BYTES = kTreeTile * KR_ROW;
-    static constexpr int STAGE_BYTES = V_BYTES + ((KR_BYTES + 1023) & ~1023);
+    static constexpr int STAGE_BYTES = V_BYTES + KR_BYTES;
+    // Tensor memory: scores and weights of each group, O, and for d_v = 64 the query.  For d_v = 128 it is in shared memory: at 128
+    // columns a product the operand's bytes keep up with the tensor core.
+    static constexpr bool Q_TMEM = DV == 64;
     static constexpr int TMEM_COLS = 512;
     static constexpr int COL_S = 0, COL_P = NWG * kTreeTile, COL_O = COL_P + NWG * kTreeTile / 2, COL_Q = COL_O + DV;
-    static_assert(COL_Q + (DV + DRP) / 2 <= TMEM_COLS, "scores, weights, O and the query must fit the allocation");
+    static_assert(COL_Q + (Q_TMEM ? (DV + DRP) / 2 : 0) <= TMEM_COLS, "scores, weights, O and the query must fit the allocation");
     static constexpr int SOFTMAX = NWG * 128, THREADS = SOFTMAX + 128;
-    // Registers: d_v = 64 launches 640 threads with 96 each; the softmax warps, which hold a row of scores, take 104 and the others 56
-    // (512 x 104 + 128 x 56 is less than 640 x 96).  d_v = 128: 512 threads with up to 128.
-    static constexpr bool SHARE_REGS = DV == 64;
+    static constexpr int QBOX_BYTES = kStripRows * 128, Q_BYTES = Q_TMEM ? 0 : BOXES * QBOX_BYTES + kStripRows * KR_ROW;
     static constexpr int PART = 16, JOIN_LD = 20;                // columns of O at a time in the join of copies; f32 of a row there, padded
-    static constexpr int OFF_JOIN = NSTAGE * STAGE_BYTES, OFF_REF = OFF_JOIN + NWG * kStripRows * JOIN_LD * 4;
+    static constexpr int OFF_Q = NSTAGE * STAGE_BYTES, OFF_QR = OFF_Q + BOXES * QBOX_BYTES, OFF_JOIN = OFF_Q + Q_BYTES;
+    static constexpr int OFF_REF = OFF_JOIN + NWG * (kStripRows / 2) * JOIN_LD * 4;
     static constexpr int OFF_SUM = OFF_REF + 2 * kStripRows * 4, OFF_BAR = OFF_SUM + 2 * SOFTMAX * 4;
     static constexpr int N_BARS = 2 * NSTAGE + 8 * NWG + 6;
     static constexpr int OFF_WORDS = OFF_BAR + N_BARS * 8;       // tensor-memory address, abort flag, a flag per stage, bad rows of a group's tile
-    static constexpr int OFF_SEQ = OFF_WORDS + (2 + NSTAGE + 4 * NWG) * 4;
+    static constexpr int OFF_SEQ = OFF_WORDS + (2 + NSTAGE + 8 * NWG) * 4;
     static constexpr size_t smem_bytes(int B) { return 1024 + OFF_SEQ + (size_t)(B + 1) * 4; }
 };
 
@@ -82,9 +94,8 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t s_base = smem_u32(smem), bar0 = s_base + T::OFF_BAR;
-    auto kv_full = [&](int t) { return bar0 + 8u * (t & (NS - 1)); };                 // by a tile's running number
-    auto kv_empty = [&](int t) { return bar0 + 8u * (NS + (t & (NS - 1))); };
-    auto kv_phase = [](int t) { return (uint32_t)(t / NS) & 1u; };
+    auto kv_full = [&](int st) { return bar0 + 8u * st; };                            // by the stage
+    auto kv_empty = [&](int st) { return bar0 + 8u * (NS + st); };
     auto s_full = [&](int w) { return bar0 + 8u * (2 * NS + w); };                    // by the group
     auto s_free = [&](int w) { return bar0 + 8u * (2 * NS + NWG + w); };
     auto p_full = [&](int w) { return bar0 + 8u * (2 * NS + 2 * NWG + w); };
@@ -136,6 +147,15 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
     TreePieces pieces(p, s_off, c);
     TreePiece pc;
     uint32_t n_pc = 0;                                  // running number of a piece
+    int st = 0;                                         // stage of a tile, and the parity of its round through the ring
+    uint32_t ph = 0;
+    auto advance = [&](int by) {
+        st += by;
+        if (st >= NS) {
+            st -= NS;
+            ph ^= 1u;
+        }
+    };
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) { return warp_wait(bar, parity & 1u, s_abort); };
     // Arrivals of whole warps, by one lane: the barrier unit takes lanes one after the other.
@@ -146,12 +166,14 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
 
     if (warp < 4 * NWG) {
         // ========================================= softmax: one row per thread =========================================
-        if constexpr (T::SHARE_REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;\n");
         const int w = warp >> 2, quarter = warp & 3, r = tid & (kStripRows - 1), hl = lane & 3, h = g * kHeadsPerGroup + hl;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16), o_addr = lane_base + T::COL_O;
         const uint32_t s_addr = lane_base + T::COL_S + w * kTreeTile, p_addr = lane_base + T::COL_P + w * (kTreeTile / 2);
-        float *s_join = reinterpret_cast<float *>(smem + T::OFF_JOIN) + w * kStripRows * T::JOIN_LD;
+        float *s_join = reinterpret_cast<float *>(smem + T::OFF_JOIN) + w * (kStripRows / 2) * T::JOIN_LD;
         uint32_t n_tiles = 0;                           // tiles that this group has had: the next one's number is n_tiles * NWG + w
+        advance(w);                                     // (its first tile's stage)
+        int st_own = 0;                                 // stage and phase of the tile before
+        uint32_t ph_own = 0;
         uint32_t n_met = 0;
         // The group's warps meet; false: one of them has given up.  (Not a hardware barrier, on which the others would wait for good.)
         auto meet = [&]() {
@@ -190,106 +212,61 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
 #pragma unroll
                 for (int i = 0; i < HALF; ++i) {
                     if (half * HALF + i >= N) continue;
+                    const int at = half * HALF + i;
                     const uint32_t words[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                    tmem_st4_nowait(lane_base + T::COL_Q + (half * HALF + i) * 4, words);
+                    if constexpr (T::Q_TMEM) tmem_st4_nowait(lane_base + T::COL_Q + at * 4, words);
+                    else if (at < DV / 8) *reinterpret_cast<uint4 *>(smem + T::OFF_Q + (at >> 3) * T::QBOX_BYTES + swz128(r, at & 7)) = v[i];
+                    else *reinterpret_cast<uint4 *>(smem + T::OFF_QR + swz_kr<T::KR_ROW>(r, at - DV / 8)) = v[i];
                 }
             }
             s_ref[(number & 1) * kStripRows + r] = -INFINITY;
-            tmem_st_wait();
+            if constexpr (T::Q_TMEM) tmem_st_wait();
+            else fence_async_smem();
             tc_fence_before();
             arrive(q_ready);
             return true;
         };
-        // One tile of a row: `chunks` times 32 of its columns, from col0 on.  Of two chunks the first is loaded again for its weights: the
-        // registers hold 32 scores at a time.  (One copy of this code for all cases: it has to stay in the instruction caches.)
         float sum = 0.f, sum_ref = -INFINITY;           // this group's sum, and the reference it is relative to
-        auto softmax_tile = [&](int chunks, int col0, uint64_t bits, bool edge, bool first) -> bool {
-            const int t = (int)(n_tiles * NWG) + w;
-            float s[32], m_tile = -INFINITY;
-            auto load = [&](int chunk) {
-                tmem_ld32_nowait(s_addr + col0 + chunk * 32, s);
-                tmem_ld_wait();
-                if (edge) {
-                    const uint32_t seen = (uint32_t)(bits >> (col0 + chunk * 32));
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) s[k] = (seen >> k) & 1 ? s[k] : -INFINITY;
-                }
-            };
-            tc_fence_after();
+        bool poison = false;
+        // A tile that drafted tokens, the sequence's end or a bad page reach into: which of its tokens the row sees.  Value rows that P
+        // multiplies by 0 must not be NaN or infinite: those behind the end and of bad pages become zeros, and so do drafted tokens' rows
+        // with such an element (a row that sees one is made NaN at the end instead).
+        auto edge_tile = [&](int st, int t0, uint32_t flag, bool live, size_t node, int half0, int halves, uint64_t (&bits)[2]) -> bool {
+            volatile uint32_t *bad_rows = s_bad + w * 8 + (n_tiles & 1) * 4;         // (two sets: a slow reader of the tile before)
+            unsigned char *v = smem + st * T::STAGE_BYTES + r * 128;
+            const bool zero = t0 + r >= pc.s.total || ((flag >> quarter) & 1);
+            bool bad = false;
+            if (!zero && t0 + r >= pc.s.ctx) {
 #pragma unroll 1
-            for (int i = 0; i < chunks; ++i) {
-                load(i);
-                float mx[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mx[k] = max3(s[k], s[k + 4], s[k + 8]);
-#pragma unroll
-                for (int j = 12; j + 8 <= 32; j += 8)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[j + k], s[j + 4 + k]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], s[28 + k]);
-                m_tile = max3(m_tile, fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-            }
-            m_tile *= p.scale_log2;
-            // The reference as the tile before leaves it.  It moves only when a tile's maximum exceeds it by more than 2^8: weights stay
-            // below 256, the quotient is the same, and O in tensor memory is rescaled only then, once the value product before is done.
-            // (tcgen05.ld / .st take whole warps: rows that stay multiply by 1.)
-            if (t > 0 && !wait(turn(w == 0 ? NWG - 1 : w - 1, quarter), w == 0 ? n_tiles - 1 : n_tiles)) return false;
-            float ref = s_ref[(n_pc & 1) * kStripRows + r];
-            const bool move = m_tile > ref + kRescaleLog2;
-            if (__any_sync(kAll, move)) {
-                if (!first) {
-                    if (!wait(kv_empty(t - 1), kv_phase(t - 1))) return false;
-                    tc_fence_after();
-                    const float alpha = move ? fast_exp2(ref - m_tile) : 1.f;
-#pragma unroll 1
-                    for (int part = 0; part < DV / 16; ++part) {
-                        float o[16];
-                        uint32_t words[16];
-                        tmem_ld16(o_addr + part * 16, o);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) words[i] = __float_as_uint(o[i] * alpha);
-                        tmem_st16_nowait(o_addr + part * 16, words);
+                for (int bx = 0; bx < T::BOXES; ++bx)
+#pragma unroll 2
+                    for (int i = 0; i < 8; ++i) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(v + bx * T::VBOX_BYTES + i * 16);
+                        auto odd = [](uint32_t y) { return (y & 0x7f80u) == 0x7f80u || (y & 0x7f800000u) == 0x7f800000u; };
+                        bad |= odd(x.x) || odd(x.y) || odd(x.z) || odd(x.w);
                     }
-                    tmem_st_wait();
-                    tc_fence_before();
-                }
-                if (move) s_ref[(n_pc & 1) * kStripRows + r] = ref = m_tile;
             }
-            arrive(turn(w, quarter));
-            if (sum_ref != ref) {
-                sum *= fast_exp2(sum_ref - ref);
-                sum_ref = ref;
-            }
-            if (t >= NWG && !wait(kv_empty(t - NWG), kv_phase(t - NWG))) return false;      // the group's weights before have been used
-            tc_fence_after();
-            const float nm = ref == -INFINITY ? 0.f : -ref;                          // nothing seen yet: all weights 0, not NaN
-            const uint64_t sc2 = f2_pack(p.scale_log2, p.scale_log2), nm2 = f2_pack(nm, nm);
-            uint64_t sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+            if (zero || bad)
 #pragma unroll 1
-            for (int i = chunks - 1;;) {
-                uint32_t pk[16];
-#pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                    float a, b;
-                    f2_unpack(f2_fma(f2_pack(s[k], s[k + 1]), sc2, nm2), a, b);
-                    a = fast_exp2(a);
-                    b = fast_exp2(b);
-                    sum2[(k >> 1) & 1] = f2_add(sum2[(k >> 1) & 1], f2_pack(a, b));
-                    pk[k >> 1] = pack_bf16(a, b);
-                }
-                tmem_st16_nowait(p_addr + (col0 + i * 32) / 2, pk);
-                if (--i < 0) break;
-                load(i);
+                for (int bx = 0; bx < T::BOXES; ++bx)
+#pragma unroll 2
+                    for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(v + bx * T::VBOX_BYTES + i * 16) = make_uint4(0, 0, 0, 0);
+            const uint32_t all = __ballot_sync(kAll, bad);
+            if (lane == 0) bad_rows[quarter] = all;
+            fence_async_smem();
+            if (!meet()) return false;
+#pragma unroll 1
+            for (int k = 0; k < halves; ++k) {
+                const int from = (half0 + k) * 64, n = pc.s.total - t0 - from;       // tokens of this half of the tile
+                uint64_t seen = live ? tree_window(p.mask + node * p.words, p.words, t0 + from - pc.s.ctx) : 0;
+                if (n < 64) seen = n <= 0 ? 0 : seen & ((1ull << n) - 1);
+                const uint32_t gone = flag >> ((half0 + k) * 2);
+                if (gone & 1) seen &= ~0xffffffffull;
+                if (gone & 2) seen &= 0xffffffffull;
+                poison |= (seen & (bad_rows[(half0 + k) * 2] | ((uint64_t)bad_rows[(half0 + k) * 2 + 1] << 32))) != 0;
+                if (k == 0) bits[0] = seen;
+                else bits[1] = seen;
             }
-            tc_fence_before();
-            arrive(s_free(w));
-            float sa, sb;
-            f2_unpack(f2_add(sum2[0], sum2[1]), sa, sb);
-            sum += sa + sb;
-            tmem_st_wait();
-            tc_fence_before();
-            arrive(p_full(w));
             return true;
         };
 
@@ -302,58 +279,128 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             const size_t node = (size_t)pc.s.r0 + pc.n0 + (live ? tok : 0), row_h = node * p.H + h;
             if (copies > 1) {                           // the other copy's tokens weigh nothing
                 const uint32_t none[32] = {};
-                tmem_st32u_nowait(p_addr, none);
+                tmem_st32u_nowait(p_addr + (1 - copy) * 32, none);
                 tmem_st_wait();
             }
             sum = 0.f;
             sum_ref = -INFINITY;
-            bool poison = false;
+            poison = false;
             const uint32_t t_end = t_base + (uint32_t)(pc.hi - pc.lo);
+            const int first = pc.lo, ctx = pc.s.ctx, halves = 2 / copies, half0 = copy;                              // of a tile: those whose tokens this copy weighs
             for (; n_tiles * NWG + w < t_end; ++n_tiles) {
-                const int t = (int)(n_tiles * NWG) + w, st = t & (NS - 1), t0 = (pc.lo + (int)(t - t_base)) * kTreeTile;
+                const int t = (int)(n_tiles * NWG) + w, t0 = (first + (int)(t - t_base)) * kTreeTile;
                 if (!wait(s_full(w), n_tiles)) { ok = false; break; }
+                tc_fence_after();
+                // The row's scores, 64 columns at a time: of two such halves the first is loaded again for its weights.
                 const uint32_t flag = s_flag[st];
-                const bool edge = t0 + kTreeTile > pc.s.ctx || flag != 0;            // the same for the whole block
-                uint64_t bits = ~0ull;
-                if (edge) {
-                    // Value rows that P multiplies by 0 must not be NaN or infinite: those behind the end and of bad pages become zeros, and
-                    // so do drafted tokens' rows with such an element (a row that sees one is made NaN at the end instead).
-                    volatile uint32_t *bad_rows = s_bad + w * 4 + (n_tiles & 1) * 2; // (two sets: a slow reader of the tile before)
-                    if (r < kTreeTile) {
-                        unsigned char *v = smem + st * T::STAGE_BYTES + r * 128;
-                        bool zero = t0 + r >= pc.s.total || ((flag >> (r >> 5)) & 1), bad = false;
-                        if (!zero && t0 + r >= pc.s.ctx) {
-#pragma unroll 1
-                            for (int bx = 0; bx < T::BOXES; ++bx)
-#pragma unroll 2
-                                for (int i = 0; i < 8; ++i) {
-                                    const uint4 x = *reinterpret_cast<const uint4 *>(v + bx * T::VBOX_BYTES + i * 16);
-                                    auto odd = [](uint32_t y) { return (y & 0x7f80u) == 0x7f80u || (y & 0x7f800000u) == 0x7f800000u; };
-                                    bad |= odd(x.x) || odd(x.y) || odd(x.z) || odd(x.w);
-                                }
-                        }
-                        if (zero || bad)
-#pragma unroll 1
-                            for (int bx = 0; bx < T::BOXES; ++bx)
-#pragma unroll 2
-                                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(v + bx * T::VBOX_BYTES + i * 16) = make_uint4(0, 0, 0, 0);
-                        const uint32_t all = __ballot_sync(kAll, bad);
-                        if (lane == 0) bad_rows[quarter] = all;
+                float s[64], m_tile = -INFINITY;
+                auto load = [&](int half) {
+                    float lo[32], hi[32];
+                    tmem_ld32_nowait(s_addr + half * 64, lo);
+                    tmem_ld32_nowait(s_addr + half * 64 + 32, hi);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) { s[k] = lo[k]; s[32 + k] = hi[k]; }
+                };
+                auto free_scores = [&]() {              // the score product after the next may have their place
+                    tc_fence_before();
+                    arrive(s_free(w));
+                };
+                load(half0);
+                if (halves == 1) free_scores();
+                const bool edge = t0 + kTreeTile > ctx || flag != 0;                 // the same for the whole block
+                uint64_t bits[2] = {~0ull, ~0ull};
+                if (edge && !edge_tile(st, t0, flag, live, node, half0, halves, bits)) { ok = false; break; }
+                auto hide = [&](uint64_t seen) {
+                    const uint32_t b0 = (uint32_t)seen, b1 = (uint32_t)(seen >> 32);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        s[k] = (b0 >> k) & 1 ? s[k] : -INFINITY;
+                        s[32 + k] = (b1 >> k) & 1 ? s[32 + k] : -INFINITY;
                     }
-                    fence_async_smem();
-                    if (!meet()) { ok = false; break; }
-                    if (live) {
-                        bits = tree_window(p.mask + node * p.words, p.words, t0 - pc.s.ctx);
-                        const int n = pc.s.total - t0;
-                        if (n < kTreeTile) bits &= (1ull << n) - 1;
-                        if (flag & 1) bits &= ~0xffffffffull;
-                        if (flag & 2) bits &= 0xffffffffull;
-                        poison |= (bits & (bad_rows[0] | ((uint64_t)bad_rows[1] << 32))) != 0;
-                    }
+                };
+#pragma unroll 1
+                for (int i = 0;;) {
+                    if (edge) hide(i == 0 ? bits[0] : bits[1]);
+                    float mx[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mx[k] = max3(s[k], s[k + 4], s[k + 8]);
+#pragma unroll
+                    for (int j = 12; j + 8 <= 64; j += 8)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[j + k], s[j + 4 + k]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], s[60 + k]);
+                    m_tile = max3(m_tile, fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    if (++i == halves) break;
+                    load(i);
                 }
-                const bool first = (uint32_t)t == t_base;
-                ok = softmax_tile(2 / copies, copy * 32, bits, edge, first);
-                if (!ok) break;
+                m_tile *= p.scale_log2;
+                // The reference as the tile before leaves it.  It moves only when a tile's maximum exceeds it by more than 2^8: weights stay
+                // below 256, the quotient is the same, and O in tensor memory is rescaled only then, once the value product before is done.
+                // (tcgen05.ld / .st take whole warps: rows that stay multiply by 1.)  Asked for together: whether the group's weights
+                // before (long done, mostly) have been used.
+                const uint32_t turn1 = w == 0 ? n_tiles - 1 : n_tiles;
+                if (t > 0 && !(n_tiles == 0 ? wait(turn(1 - w, quarter), turn1)
+                                            : warp_wait(turn(1 - w, quarter), turn1 & 1u, kv_empty(st_own), ph_own, s_abort))) { ok = false; break; }
+                float ref = s_ref[(n_pc & 1) * kStripRows + r];
+                const bool move = m_tile > ref + kRescaleLog2;
+                if (__any_sync(kAll, move)) {
+                    if ((uint32_t)t != t_base) {
+                        const int before = st == 0 ? NS - 1 : st - 1;                // stage of the tile before, and its phase
+                        if (!wait(kv_empty(before), st == 0 ? ph ^ 1u : ph)) { ok = false; break; }
+                        tc_fence_after();
+                        const float alpha = move ? fast_exp2(ref - m_tile) : 1.f;
+#pragma unroll 1
+                        for (int part = 0; part < DV / 16; ++part) {
+                            float o[16];
+                            uint32_t words[16];
+                            tmem_ld16(o_addr + part * 16, o);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) words[i] = __float_as_uint(o[i] * alpha);
+                            tmem_st16_nowait(o_addr + part * 16, words);
+                        }
+                        tmem_st_wait();
+                        tc_fence_before();
+                    }
+                    if (move) s_ref[(n_pc & 1) * kStripRows + r] = ref = m_tile;
+                }
+                arrive(turn(w, quarter));
+                tc_fence_after();
+                if (sum_ref != ref) {
+                    sum *= fast_exp2(sum_ref - ref);
+                    sum_ref = ref;
+                }
+                const float nm = ref == -INFINITY ? 0.f : -ref;                      // nothing seen yet: all weights 0, not NaN
+                const uint64_t sc2 = f2_pack(p.scale_log2, p.scale_log2), nm2 = f2_pack(nm, nm);
+                uint64_t sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+#pragma unroll 1
+                for (int i = halves - 1;;) {
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int k = 0; k < 64; k += 2) {
+                        float a, b;
+                        f2_unpack(f2_fma(f2_pack(s[k], s[k + 1]), sc2, nm2), a, b);
+                        a = fast_exp2(a);
+                        b = fast_exp2(b);
+                        sum2[(k >> 1) & 1] = f2_add(sum2[(k >> 1) & 1], f2_pack(a, b));
+                        pk[k >> 1] = pack_bf16(a, b);
+                    }
+                    tmem_st32u_nowait(p_addr + (half0 + i) * 32, pk);
+                    if (--i < 0) break;
+                    load(i);
+                    free_scores();
+                    if (edge) hide(bits[0]);
+                }
+                float sa, sb;
+                f2_unpack(f2_add(sum2[0], sum2[1]), sa, sb);
+                sum += sa + sb;
+                tmem_st_wait();
+                tc_fence_before();
+                arrive(p_full(w));
+                st_own = st;
+                ph_own = ph;
+                advance(NWG);
             }
             TreePiece nx;
             const bool more = next_piece(nx);
@@ -397,18 +444,17 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                     if (copy > 0)
 #pragma unroll
                         for (int i = 0; i < T::PART; i += 4)
-                            *reinterpret_cast<float4 *>(s_join + r * T::JOIN_LD + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                            *reinterpret_cast<float4 *>(s_join + (r - kStripRows / 2) * T::JOIN_LD + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                     if (!meet()) { ok = false; break; }
                     if (copy == 0)
-                        for (int k = 1; k < copies; ++k)
 #pragma unroll
-                            for (int i = 0; i < T::PART; i += 4) {
-                                const float4 x = *reinterpret_cast<const float4 *>(s_join + (r + k * (kStripRows / copies)) * T::JOIN_LD + i);
-                                o[i] += x.x;
-                                o[i + 1] += x.y;
-                                o[i + 2] += x.z;
-                                o[i + 3] += x.w;
-                            }
+                        for (int i = 0; i < T::PART; i += 4) {
+                            const float4 x = *reinterpret_cast<const float4 *>(s_join + r * T::JOIN_LD + i);
+                            o[i] += x.x;
+                            o[i + 1] += x.y;
+                            o[i + 2] += x.z;
+                            o[i + 3] += x.w;
+                        }
                     if (!meet()) { ok = false; break; }
                 }
                 if (live && copy == 0) {
@@ -432,49 +478,44 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             have = more;
         }
     } else {
-        if constexpr (T::SHARE_REGS) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
         int t = 0;                                      // running number of a tile
         if (warp >= 4 * NWG + 2) {
             // ========================== loaders: of even and of odd tiles; all lanes look pages up, one issues ==========================
-            const bool whole = p.P % kTreeTile == 0;    // a tile lies in one page; else its two halves do, each in its own
+            const int rows = p.P % 64 == 0 ? 64 : 32, boxes = kTreeTile / rows;      // a box of that many rows lies in one page
             const uint64_t stream = l2_policy_evict_first();
+            const uint32_t box_bytes = (uint32_t)rows * (T::BOXES * 128 + T::KR_ROW);
             while (ok && pieces.next(p, s_off, pc)) {
-                for (int base = pc.lo; base < pc.hi && ok; base += 32) {
-                    // rows of the pools where a lane's tile begins (its halves, where they lie apart); -1: a bad page, -2: nothing there
-                    int v0 = -2, k0 = -2, v1 = -2, k1 = -2;
-                    if (base + lane < pc.hi) {
-                        auto look = [&](int at, int &v, int &k) {
-                            const int j = at / p.P, slot = at - j * p.P;
-                            const long long page = tree_page(p, pc.b, j);
-                            const bool bad = page < 0 || page >= p.num_pages;
-                            if (bad) report_error(p.dev_status, GVA_ERR_BAD_PAGE, pc.b);
-                            v = bad ? -1 : ((int)page * p.G + g) * p.P + slot;
-                            k = (int)page * p.P + slot;
-                        };
-                        const int t0 = (base + lane) * kTreeTile;
-                        look(t0, v0, k0);
-                        if (!whole && t0 + 32 < pc.s.total) look(t0 + 32, v1, k1);
+                for (int base = pc.lo; base < pc.hi && ok; base += 32 / boxes) {
+                    // rows of the pools where a lane's box begins; -1: a bad page, -2: nothing there
+                    int v0 = -2, k0 = 0;
+                    const int at = base * kTreeTile + lane * rows;
+                    if (base + lane / boxes < pc.hi && at < pc.s.total) {
+                        const int j = at / p.P, slot = at - j * p.P;
+                        const long long page = tree_page(p, pc.b, j);
+                        const bool bad = page < 0 || page >= p.num_pages;
+                        if (bad) report_error(p.dev_status, GVA_ERR_BAD_PAGE, pc.b);
+                        v0 = bad ? -1 : ((int)page * p.G + g) * p.P + slot;
+                        k0 = (int)page * p.P + slot;
                     }
-                    const int n = min(32, pc.hi - base);
-                    for (int i = 0; i < n; ++i, ++t) {
+                    const uint32_t bad_boxes = __ballot_sync(kAll, v0 == -1), good_boxes = __ballot_sync(kAll, v0 >= 0);
+                    const int n = min(32 / boxes, pc.hi - base);
+                    for (int i = 0; i < n; ++i, ++t, advance(1)) {
                         if ((t ^ warp) & 1) continue;
-                        const int va = __shfl_sync(kAll, v0, i), ka = __shfl_sync(kAll, k0, i), vb = __shfl_sync(kAll, v1, i), kb = __shfl_sync(kAll, k1, i);
-                        if (t >= NS && !wait(kv_empty(t), kv_phase(t) ^ 1u)) { ok = false; break; }
-                        const uint32_t full = kv_full(t), dst = s_base + (t & (NS - 1)) * T::STAGE_BYTES;
+                        if (t >= NS && !wait(kv_empty(st), ph ^ 1u)) { ok = false; break; }
+                        const uint32_t mine = (1u << boxes) - 1, full = kv_full(st), dst = s_base + st * T::STAGE_BYTES;
+                        const uint32_t bad = (bad_boxes >> (i * boxes)) & mine, good = (good_boxes >> (i * boxes)) & mine;
                         if (elect_one()) {
-                            s_flag[t & (NS - 1)] = (va == -1 ? (whole ? 3u : 1u) : 0u) | (vb == -1 ? 2u : 0u);
-                            const uint32_t half = (uint32_t)(T::V_BYTES + T::KR_BYTES) / 2, bytes = (va >= 0 ? (whole ? 2 * half : half) : 0u) + (vb >= 0 ? half : 0u);
-                            if (bytes == 0) mbar_arrive(full);
-                            else mbar_expect_tx(full, bytes);
-                            if (va >= 0) {
+                            // the flag: a bit for 32 tokens
+                            s_flag[st] = rows == 32 ? bad : (bad & 1 ? 3u : 0u) | (bad & 2 ? 12u : 0u);
+                            if (good == 0) mbar_arrive(full);
+                            else mbar_expect_tx(full, __popc(good) * box_bytes);
+                        }
+                        for (int k = 0; k < boxes; ++k) {
+                            const int va = __shfl_sync(kAll, v0, i * boxes + k), ka = __shfl_sync(kAll, k0, i * boxes + k);
+                            if (va >= 0 && elect_one()) {
 #pragma unroll
-                                for (int bx = 0; bx < T::BOXES; ++bx) tma_load_2d_stream(dst + bx * T::VBOX_BYTES, &tm_v, bx * 64, va, full, stream);
-                                if constexpr (DR > 0) tma_load_2d(dst + T::V_BYTES, &tm_k, 0, ka, full);
-                            }
-                            if (vb >= 0) {
-#pragma unroll
-                                for (int bx = 0; bx < T::BOXES; ++bx) tma_load_2d_stream(dst + bx * T::VBOX_BYTES + 32 * 128, &tm_v, bx * 64, vb, full, stream);
-                                if constexpr (DR > 0) tma_load_2d(dst + T::V_BYTES + 32 * T::KR_ROW, &tm_k, 0, kb, full);
+                                for (int bx = 0; bx < T::BOXES; ++bx) tma_load_2d_stream(dst + bx * T::VBOX_BYTES + k * rows * 128, &tm_v, bx * 64, va, full, stream);
+                                if constexpr (DR > 0) tma_load_2d(dst + T::V_BYTES + k * rows * T::KR_ROW, &tm_k, 0, ka, full);
                             }
                         }
                         __syncwarp();
@@ -483,14 +524,14 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             }
             // copies in flight must land before the block's shared memory is released
             if (!ok || *s_abort)
-                for (int k = max(0, t - NS); k < t; ++k)   // (the other loader's too, once they are issued: a bounded wait)
-                    for (int it = 0; it < kDrainPolls && !mbar_try_wait(kv_full(k), kv_phase(k)); ++it) {}
+                for (int k = 0; k < min(t, NS); ++k)    // (the last tile of every stage, the other loader's too: bounded waits)
+                    for (int it = 0; it < kDrainPolls && !mbar_try_wait(kv_full(k), ((t - 1 - k) / NS) & 1); ++it) {}
         } else if (warp < 4 * NWG + 2) {
             // ================================= MMA issuers: a warp per product, one elected lane issues =================================
             constexpr uint32_t hi128 = (1024u >> 4) | (1u << 14) | ((uint32_t)kSwz128 << 29);    // (descriptors as in the prefill kernel)
             constexpr uint32_t hikr = ((8u * T::KR_ROW) >> 4) | (1u << 14) | ((uint32_t)(T::KR_ROW == 32 ? kSwz32 : kSwz64) << 29);
             constexpr uint32_t lo_k = (16u >> 4) << 16, lo_mn = ((uint32_t)T::VBOX_BYTES >> 4) << 16;
-            const uint32_t a_st = (s_base & 0x3FFFFu) >> 4;
+            const uint32_t a_st = (s_base & 0x3FFFFu) >> 4, a_q = ((s_base + T::OFF_Q) & 0x3FFFFu) >> 4;
             auto mk = [](uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); };
             int w = 0;
             uint32_t round = 0;                         // t = round * NWG + w
@@ -500,16 +541,19 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                     if (pc.lo >= pc.hi) continue;
                     if (!wait(q_ready, n_pc)) { ok = false; break; }
                     ++n_pc;
-                    for (int j = pc.lo; j < pc.hi; ++j, ++t) {
-                        if (!wait(kv_full(t), kv_phase(t))) { ok = false; break; }
-                        if (round > 0 && !wait(s_free(w), round - 1)) { ok = false; break; }
+                    const int first = pc.lo, end = pc.hi;
+                    for (int j = first; j < end; ++j, ++t, advance(1)) {
+                        if (!(round == 0 ? wait(kv_full(st), ph) : warp_wait(kv_full(st), ph, s_free(w), (round - 1) & 1u, s_abort))) { ok = false; break; }
                         tc_fence_after();
-                        const uint32_t vb = a_st + (uint32_t)(t & (NS - 1)) * (T::STAGE_BYTES >> 4), d = tmem + T::COL_S + w * kTreeTile;
+                        const uint32_t vb = a_st + (uint32_t)st * (T::STAGE_BYTES >> 4), d = tmem + T::COL_S + w * kTreeTile;
                         if (elect_one()) {
 #pragma unroll
                             for (int ks = 0; ks < KS_S; ++ks) {
                                 const uint32_t off = ks < KS_V ? ((ks >> 2) * T::VBOX_BYTES + (ks & 3) * 32) >> 4 : (T::V_BYTES >> 4) + (uint32_t)(ks - KS_V) * 2;
-                                umma_bf16_ts(d, tmem + T::COL_Q + ks * 8, mk((vb + off) | lo_k, ks < KS_V ? hi128 : hikr), idesc, ks > 0);
+                                const uint64_t k_desc = mk((vb + off) | lo_k, ks < KS_V ? hi128 : hikr);
+                                const uint32_t q_off = ks < KS_V ? ((ks >> 2) * T::QBOX_BYTES + (ks & 3) * 32) >> 4 : (uint32_t)(T::OFF_QR - T::OFF_Q) / 16 + (uint32_t)(ks - KS_V) * 2;
+                                if constexpr (T::Q_TMEM) umma_bf16_ts(d, tmem + T::COL_Q + ks * 8, k_desc, idesc, ks > 0);
+                                else umma_bf16(d, mk((a_q + q_off) | lo_k, ks < KS_V ? hi128 : hikr), k_desc, idesc, ks > 0);
                             }
                             umma_commit(s_full(w));
                             mbar_arrive(s_full(w));
@@ -522,18 +566,19 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                 constexpr uint32_t idesc = umma_idesc(kStripRows, DV, true);
                 while (ok && pieces.next(p, s_off, pc)) {
                     if (pc.lo >= pc.hi) continue;
-                    for (int j = pc.lo; j < pc.hi; ++j, ++t) {
+                    const int first = pc.lo, end = pc.hi;
+                    for (int j = first; j < end; ++j, ++t, advance(1)) {
                         // every row has stored its weights of tile t and finished any rescaling of O; of a new piece, the one before has been read
                         if (!wait(p_full(w), round)) { ok = false; break; }
-                        if (j == pc.lo && n_pc > 0 && !wait(o_free, n_pc - 1)) { ok = false; break; }
+                        if (j == first && n_pc > 0 && !wait(o_free, n_pc - 1)) { ok = false; break; }
                         tc_fence_after();
-                        const uint32_t vb = a_st + (uint32_t)(t & (NS - 1)) * (T::STAGE_BYTES >> 4), a = tmem + T::COL_P + w * (kTreeTile / 2);
+                        const uint32_t vb = a_st + (uint32_t)st * (T::STAGE_BYTES >> 4), a = tmem + T::COL_P + w * (kTreeTile / 2);
                         if (elect_one()) {
 #pragma unroll
                             for (int ks = 0; ks < KS_O; ++ks)
-                                umma_bf16_ts(tmem + T::COL_O, a + ks * 8, mk((vb + ks * (16 * 128 >> 4)) | lo_mn, hi128), idesc, (j > pc.lo || ks > 0) ? 1u : 0u);
-                            umma_commit(kv_empty(t));
-                            if (j + 1 == pc.hi) umma_commit(o_full);
+                                umma_bf16_ts(tmem + T::COL_O, a + ks * 8, mk((vb + ks * (16 * 128 >> 4)) | lo_mn, hi128), idesc, (j > first || ks > 0) ? 1u : 0u);
+                            umma_commit(kv_empty(st));
+                            if (j + 1 == end) umma_commit(o_full);
                         }
                         __syncwarp();
                         if (++w == NWG) { w = 0; ++round; }
@@ -576,9 +621,9 @@ inline TreeMma tree_mma(const gva_config &c) {
     if (c.d_v == 64) return c.d_r == 16 ? tree_mma_t<64, 16>() : c.d_r == 24 ? tree_mma_t<64, 24>() : tree_mma_t<64, 0>();
     return c.d_r == 32 ? tree_mma_t<128, 32>() : tree_mma_t<128, 0>();
 }
-// Maps of the values (boxes of 64 dims by a tile or half a tile) and of the positional keys.
+// Maps of the values (boxes of 64 dims by the tokens that lie in one page) and of the positional keys.
 inline bool tree_maps(const gva_config &c, const MmaHostState &st, const TreeParams &p, int drp, CUtensorMap *v, CUtensorMap *k) {
-    const uint32_t rows = c.page_size % kTreeTile == 0 ? kTreeTile : kTreeTile / 2;
+    const uint32_t rows = c.page_size % 64 == 0 ? 64 : 32;
     if (!encode_map(st, v, p.v_pool, c.d_v, (uint64_t)p.num_pages * c.G * c.page_size, 64, rows, CU_TENSOR_MAP_SWIZZLE_128B)) return false;
     if (c.d_r == 0) {
         *k = *v;                     // (never used)

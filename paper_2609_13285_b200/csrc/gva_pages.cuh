@@ -21,6 +21,7 @@ struct AssignParams {
     int32_t *free_out, *new_lens, *cu_q, *positions, *slots;
     int32_t *dev_status;
     int max_pages, num_pages, max_rows, B, P;
+    int rows_here;                           // 1: the rows' positions and slots too; 0: assign_rows_kernel follows
 };
 constexpr int kAssignItems = 8;      // sequences of a thread: 1024 threads serve 8192
 
@@ -52,26 +53,53 @@ __device__ __forceinline__ int owner_of(const int *off, int B, int x) {
     }
     return lo;
 }
-// Inclusive sum over the block's threads of v, in place; s_part holds one word per warp.  Returns the block's total.
-__device__ __forceinline__ long long block_scan(long long &v, long long *s_part) {
+// Largest b in [0, B) with off[b] <= x, by a whole warp: 32 candidates at a time (B <= 8192: three trips to memory at most).
+__device__ __forceinline__ int warp_owner_of(const int32_t *off, int B, int x) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = B;                                   // the answer is in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 31) / 32, at = lo + lane * step;
+        const unsigned below = __ballot_sync(0xffffffffu, lane * step < n && off[at] <= x);      // (a prefix of the lanes, the first among them)
+        const int k = 31 - __clz(below);
+        n = min(step, lo + n - (lo + k * step));
+        lo += k * step;
+    }
+    return lo;
+}
+// Inclusive sums over the block's threads of four values, in place; s_part holds 4 x 32 words.  The last value's total is returned.
+struct Sums {
+    long long v[4];
+};
+__device__ __forceinline__ long long block_scan(Sums &x, int wanted, long long (*s_part)[32]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += y;
-    }
-    if (lane == 31) s_part[warp] = v;
-    __syncthreads();
-    long long w = lane < warps ? s_part[lane] : 0;
+    for (int o = 1; o < 32; o <<= 1)
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, w, o);
-        if (lane >= o) w += y;
-    }
-    const long long before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
-    if (warp > 0) v += before;
-    const long long total = __shfl_sync(0xffffffffu, w, 31);
+        for (int i = 0; i < 4; ++i) {
+            const long long y = __shfl_up_sync(0xffffffffu, x.v[i], o);
+            if (lane >= o) x.v[i] += y;
+        }
+    if (lane == 31)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_part[i][warp] = x.v[i];
     __syncthreads();
+    long long w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = lane < warps ? s_part[i][lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long y = __shfl_up_sync(0xffffffffu, w[i], o);
+            if (lane >= o) w[i] += y;
+        }
+    long long total = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const long long before = __shfl_sync(0xffffffffu, w[i], (warp + 31) & 31), all = __shfl_sync(0xffffffffu, w[i], 31);
+        if (warp > 0) x.v[i] += before;
+        if (i == wanted) total = all;
+    }
     return total;
 }
 
@@ -84,7 +112,7 @@ assign_pages_kernel(AssignParams p) {
     grid_dependency_launch();
     extern __shared__ int s_mem[];
     int *s_row = s_mem, *s_take = s_row + p.B, *s_give = s_take + p.B, *s_used = s_give + p.B, *s_pages = s_used + p.B, *s_to = s_pages + p.B;
-    __shared__ long long s_part[32];
+    __shared__ long long s_part[4][32];
     __shared__ int s_served[3];      // rows, pages taken, pages returned by growing sequences: of those served
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
@@ -108,13 +136,10 @@ assign_pages_kernel(AssignParams p) {
         else give += a[i].give;
         if (!a[i].fine && sound && rank == 0) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
     }
-    long long rows_to = rows, take_to = take, give_to = give, back_to = back;
-    block_scan(rows_to, s_part);
-    block_scan(take_to, s_part);
-    const long long give_all = block_scan(give_to, s_part);
-    block_scan(back_to, s_part);
+    Sums to = {{rows, take, give, back}};
+    const long long give_all = block_scan(to, 2, s_part);
     {
-        long long r = rows_to - rows, t = take_to - take, g = give_to - give, k = back_to - back;
+        long long r = to.v[0] - rows, t = to.v[1] - take, g = to.v[2] - give, k = to.v[3] - back;
 #pragma unroll
         for (int i = 0; i < kAssignItems; ++i) {
             const int b = tid * per + i;
@@ -193,13 +218,41 @@ assign_pages_kernel(AssignParams p) {
         if (page < 0 || page >= p.num_pages) report_error(p.dev_status, GVA_ERR_BAD_PAGE, b);
         p.ring[((long long)first + count + i) % p.num_pages] = page;
     }
-    for (int i = me; i < n_rows; i += all) {
+    for (int i = p.rows_here ? me : n_rows; i < n_rows; i += all) {
         const int b = owner_of(s_row, p.B, i);
         const int t = s_used[b] + (i - s_row[b]), j = t / p.P;
         const int page = j < s_pages[b] ? p.block_table[(size_t)b * p.max_pages + j]
                                         : p.ring[((long long)first + s_take[b] + (j - s_pages[b])) % p.num_pages];
         p.positions[i] = t;
         p.slots[i] = page < 0 || page >= p.num_pages ? -1 : page * p.P + t % p.P;
+    }
+}
+
+// Positions and slots of many rows, from what assign_pages_kernel has left: 0.2 M rows of 48 prompts in all of the GPU's blocks take 6 us,
+// in the one cluster 29.  A block has 1024 rows in a row, of as few sequences as these lie in.
+constexpr int kAssignRows = 1024, kAssignRowThreads = 256;
+__global__ void __launch_bounds__(kAssignRowThreads)
+assign_rows_kernel(AssignParams p) {
+    grid_dependency_launch();
+    __shared__ int s_b[2];
+    grid_dependency_wait();
+    const int r0 = blockIdx.x * kAssignRows, total = p.cu_q[p.B];
+    if (r0 >= total) return;
+    const int end = min(r0 + kAssignRows, total), warp = threadIdx.x >> 5;
+    if (warp < 2) {
+        const int b = warp_owner_of(p.cu_q, p.B, warp == 0 ? r0 : end - 1);
+        if ((threadIdx.x & 31) == 0) s_b[warp] = b;
+    }
+    __syncthreads();
+    const int b0 = s_b[0], n = s_b[1] - b0 + 1;
+#pragma unroll
+    for (int k = 0; k < kAssignRows / kAssignRowThreads; ++k) {
+        const int i = r0 + k * kAssignRowThreads + threadIdx.x;
+        if (i >= end) continue;
+        const int b = b0 + owner_of(p.cu_q + b0, n, i), t = p.new_lens[b] - (p.cu_q[b + 1] - i), j = t / p.P;
+        const int page = p.block_table[(size_t)b * p.max_pages + j];
+        p.positions[i] = t;
+        p.slots[i] = page < 0 || page >= p.num_pages ? -1 : page * p.P + (t - j * p.P);
     }
 }
 
@@ -271,23 +324,35 @@ tree_commit_kernel(TreeCommitParams p) {
     grid_dependency_launch();
     __shared__ int s_parents[kTreeMost], s_next[kTreeMost], s_path[kTreeMost], s_chosen[kTreeMost];
     __shared__ int2 s_from[kTreeMost], s_to[kTreeMost];           // page and slot of every row of the path, and of where it goes
-    __shared__ int s_count;
+    __shared__ int s_count, s_page[kTreeMost / 32 + 1];          // (pages of 32 tokens at least)
     grid_dependency_wait();
     const int b = blockIdx.x, tid = threadIdx.x;
     const int r0 = p.cu_q[b], n = max(p.cu_q[b + 1] - r0, 0), ctx = p.ctx_lens[b];
     int code = GVA_OK;
     if (ctx < 0 || (long long)ctx + n > (long long)p.max_pages * p.P) code = GVA_ERR_SEQ_LEN;
-    else if (n > p.most || !load_parents(p.parents + r0, n, s_parents)) code = GVA_ERR_TREE;
-    int count = 0;
-    if (code == GVA_OK && n > 0) {
-        for (int i = tid; i < n; i += kCommitThreads) {
-            s_next[i] = n;
+    else if (n > p.most) code = GVA_ERR_TREE;
+    int count = 0, token[kTreeMost / kCommitThreads];
+    if (code == GVA_OK) {                                         // everything the walk needs, in one trip
+#pragma unroll
+        for (int k = 0; k < kTreeMost / kCommitThreads; ++k) {
+            const int i = tid + k * kCommitThreads;
+            if (i >= n) continue;
+            token[k] = p.tokens[r0 + i];
             s_chosen[i] = p.chosen[r0 + i];
+            s_next[i] = n;
         }
-        __syncthreads();
-        for (int i = tid; i < n; i += kCommitThreads) {
-            const int par = s_parents[i];
-            if (par >= 0 && p.tokens[r0 + i] == s_chosen[par]) atomicMin(&s_next[par], i);
+        const int first = ctx / p.P, pages = n > 0 ? (ctx + n - 1) / p.P - first + 1 : 0;
+        for (int j = tid; j < pages; j += kCommitThreads) {
+            const long long page = p.block_table ? (long long)p.block_table[(size_t)b * p.max_pages + first + j] : (long long)b * p.max_pages + first + j;
+            s_page[j] = page < 0 || page >= p.num_pages ? -1 : (int)page;
+        }
+        if (!load_parents(p.parents + r0, n, s_parents)) code = GVA_ERR_TREE;
+    }
+    if (code == GVA_OK && n > 0) {
+#pragma unroll
+        for (int k = 0; k < kTreeMost / kCommitThreads; ++k) {
+            const int i = tid + k * kCommitThreads, par = i < n ? s_parents[i] : -1;
+            if (par >= 0 && token[k] == s_chosen[par]) atomicMin(&s_next[par], i);
         }
         __syncthreads();
         if (tid == 0) {
@@ -300,10 +365,9 @@ tree_commit_kernel(TreeCommitParams p) {
         bool bad = false;
         for (int i = tid; i < count; i += kCommitThreads) {
             auto place = [&](int t) {
-                const int j = t / p.P;
-                const long long page = p.block_table ? (long long)p.block_table[(size_t)b * p.max_pages + j] : (long long)b * p.max_pages + j;
-                bad |= page < 0 || page >= p.num_pages;
-                return make_int2((int)page, t - j * p.P);
+                const int j = t / p.P, page = s_page[j - ctx / p.P];
+                bad |= page < 0;
+                return make_int2(page, t - j * p.P);
             };
             if (s_path[i] == i) continue;
             s_from[i] = place(ctx + s_path[i]);

@@ -11,6 +11,7 @@
 // records that tree_merge_kernel joins.
 #pragma once
 
+#include "gva_pages.cuh"
 #include "gva_prefill.cuh"
 
 namespace gva {
@@ -273,6 +274,8 @@ tree_fma_kernel(TreeParams p, int d_r) {
 }
 
 // ---- merge: a warp per (node, head) whose strip was cut ---------------------------------------------------------
+// A chain of trips to memory, so each is made once: the sequence by 32 candidates at a time, the pieces' maxima and sums by a lane each,
+// four pieces' outputs at a time.
 template <typename OT, int DV>
 __global__ void __launch_bounds__(256)
 tree_merge_kernel(TreeParams p, int rows) {
@@ -280,9 +283,8 @@ tree_merge_kernel(TreeParams p, int rows) {
     grid_dependency_wait();
     const int x = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int node = x / p.H, h = x - node * p.H;
-    if (node >= rows) return;
-    if (node >= p.cu_q[p.B]) return;
-    const int b = seq_of_tile(p.cu_q, p.B, node);
+    if (node >= min(rows, p.cu_q[p.B])) return;
+    const int b = warp_owner_of(p.cu_q, p.B, node);
     const TreeSeq s = tree_seq(p, b, false);
     if (s.n <= 0) return;
     const int strip = (node - s.r0) / s.per_strip, row = (node - s.r0 - strip * s.per_strip) * kHeadsPerGroup + h % kHeadsPerGroup;
@@ -298,21 +300,42 @@ tree_merge_kernel(TreeParams p, int rows) {
     }
     if (count == 1) return;
     const int g = h / kHeadsPerGroup;
+    const size_t step = (size_t)p.G * kStripRows, r0 = record_row(p, first, g, row);      // from a piece's row to the next one's
     float m = -INFINITY;
-    for (int k = 0; k < count; ++k) m = fmaxf(m, p.rec_ml[record_row(p, first + k, g, row) * 2]);
+    for (int k = lane; k < count; k += 32) m = fmaxf(m, p.rec_ml[(r0 + k * step) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     const float ref = m == -INFINITY ? 0.f : m;
     float acc[DV / 32], l = 0.f;
 #pragma unroll
     for (int i = 0; i < DV / 32; ++i) acc[i] = 0.f;
-    for (int k = 0; k < count; ++k) {
-        const size_t r = record_row(p, first + k, g, row);
-        const float2 ml = *reinterpret_cast<const float2 *>(p.rec_ml + r * 2);
-        if (ml.y == 0.f) continue;                                        // an empty piece left its O unwritten
-        const float w = fast_exp2(ml.x - ref);
-        l = fmaf(w, ml.y, l);
+    for (int k0 = 0; k0 < count; k0 += 32) {
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (k0 + lane < count) ml = *reinterpret_cast<const float2 *>(p.rec_ml + (r0 + (k0 + lane) * step) * 2);
+        const float own = ml.y == 0.f ? 0.f : fast_exp2(ml.x - ref);                       // (0: an empty piece, which left its O unwritten)
+        l = fmaf(own, ml.y, l);
+        const int n = min(32, count - k0);
+        for (int k = 0; k < n; k += 4) {
+            float w[4], o[4][DV / 32];
 #pragma unroll
-        for (int i = 0; i < DV / 32; ++i) acc[i] = fmaf(w, p.rec_o[r * DV + lane * (DV / 32) + i], acc[i]);
+            for (int u = 0; u < 4; ++u) {
+                w[u] = __shfl_sync(0xffffffffu, own, (k + u) & 31);
+                if (k + u >= n) w[u] = 0.f;
+#pragma unroll
+                for (int i = 0; i < DV / 32; i += 2) {
+                    const float2 y = w[u] != 0.f ? *reinterpret_cast<const float2 *>(p.rec_o + (r0 + (k0 + k + u) * step) * DV + lane * (DV / 32) + i) : make_float2(0.f, 0.f);
+                    o[u][i] = y.x;
+                    o[u][i + 1] = y.y;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < DV / 32; ++i) acc[i] = fmaf(w[u], o[u][i], acc[i]);
+        }
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     const float inv = tree_inverse(l);
     OT *dst = static_cast<OT *>(p.out) + ((size_t)node * p.H + h) * DV + lane * (DV / 32);
 #pragma unroll

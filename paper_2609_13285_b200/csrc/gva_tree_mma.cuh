@@ -1,13 +1,13 @@
 // gva_decode_tree over a bf16 cache on the 5th-generation tensor cores (tcgen05 + tensor memory), sm_100a.
 //
 // A block (one per SM) works on one value group: the strip's 128 rows (32 nodes x 4 heads) are the M of every MMA, a tile of 128
-// cached tokens is the N of the score product and the K of the value product, so one tile in shared memory feeds both.
-//   2 groups of 4 warps   softmax: tile t is group t % 2's, a thread owns a row = a lane of tensor memory
+// (d_v = 128: 64) cached tokens is the N of the score product and the K of the value product, so one tile in shared memory feeds both.
+//   NWG = 2 (3) groups of 4 warps   softmax: tile t is group t % NWG's, a thread owns a row = a lane of tensor memory
 //   4 more warps          issuer of the value products, issuer of the score products (owns the tensor memory), two loaders
-//   S[t % 2] = Q K^T (Q from tensor memory, d_v = 128: shared memory)  ->  weights as bf16 pairs in P[t % 2]  ->  O += P V
+//   S[t % NWG] = Q K^T (Q from tensor memory)  ->  weights as bf16 pairs in P[t % NWG]  ->  O += P V
 // What bounds it is neither bytes nor a pipe but every role's chain of steps per tile: a wait that is complete already takes 150
-// cycles, an MMA 40 to 60 to issue, a tile in all some 600 for each issuer and 1500 and more for the softmax.  Hence large tiles (64
-// tokens with four groups: 180 us for 1 M narrow tokens, 16 nodes), and two of them side by side.  They share one O, so they share the
+// cycles, an MMA 40 to 60 to issue, a tile in all some 600 for each issuer and 1500 and more for the softmax.  Hence large tiles for
+// narrow heads (of 64 tokens with four groups: 180 us for 1 M tokens, 16 nodes), and several of them side by side.  They share one O, so they share the
 // rows' softmax references too: those go from tile to tile through shared memory in the tiles' order (`turn`), which is a short step as
 // long as no maximum moves one.  Sums stay with each group, relative to the reference they were made with.
 // Few nodes leave rows of the MMA unused, and its time is the same: up to 16 nodes are laid out twice, and each copy weighs its half
@@ -53,28 +53,26 @@ __device__ __forceinline__ bool elect_one() {
     return yes != 0;
 }
 
-constexpr int kTreeTile = 128;
+constexpr int tree_mma_tile(int d_v) { return d_v == 64 ? 128 : 64; }
 template <int DV, int DR>
 struct TreeTraits {
-    static constexpr int NWG = 2;
-    static constexpr int NSTAGE = DV == 64 ? 6 : 3;
+    static constexpr int TILE = tree_mma_tile(DV), HALF = TILE / 2;    // tokens of a tile, and of what a copy of two weighs
+    static constexpr int NWG = DV == 64 ? 2 : 3;
+    static constexpr int NSTAGE = DV == 64 ? 6 : 8;
     static constexpr int BOXES = DV / 64;
     static constexpr int DRP = (DR + 15) / 16 * 16;              // d_r = 24 occupies 32: the box reads zeros behind the row
     static constexpr int KR_ROW = DRP * 2;
-    static constexpr int VBOX_BYTES = kTreeTile * 128;
+    static constexpr int VBOX_BYTES = TILE * 128;
     static constexpr int V_BYTES = BOXES * VBOX_BYTES;
-    static constexpr int KR_BYTES = kTreeTile * KR_ROW;
-    static constexpr int STAGE_BYTES = V_BYTES + KR_BYTES;
-    // Tensor memory: scores and weights of each group, O, and for d_v = 64 the query.  For d_v = 128 it is in shared memory: at 128
-    // columns a product the operand's bytes keep up with the tensor core.
-    static constexpr bool Q_TMEM = DV == 64;
+    static constexpr int KR_BYTES = TILE * KR_ROW;
+    static constexpr int STAGE_BYTES = V_BYTES + ((KR_BYTES + 1023) & ~1023);
+    // Tensor memory columns: scores and weights of each group, O, the query.
     static constexpr int TMEM_COLS = 512;
-    static constexpr int COL_S = 0, COL_P = NWG * kTreeTile, COL_O = COL_P + NWG * kTreeTile / 2, COL_Q = COL_O + DV;
-    static_assert(COL_Q + (Q_TMEM ? (DV + DRP) / 2 : 0) <= TMEM_COLS, "scores, weights, O and the query must fit the allocation");
+    static constexpr int COL_S = 0, COL_P = NWG * TILE, COL_O = COL_P + NWG * TILE / 2, COL_Q = COL_O + DV;
+    static_assert(COL_Q + (DV + DRP) / 2 <= TMEM_COLS, "scores, weights, O and the query must fit the allocation");
     static constexpr int SOFTMAX = NWG * 128, THREADS = SOFTMAX + 128;
-    static constexpr int QBOX_BYTES = kStripRows * 128, Q_BYTES = Q_TMEM ? 0 : BOXES * QBOX_BYTES + kStripRows * KR_ROW;
     static constexpr int PART = 16, JOIN_LD = 20;                // columns of O at a time in the join of copies; f32 of a row there, padded
-    static constexpr int OFF_Q = NSTAGE * STAGE_BYTES, OFF_QR = OFF_Q + BOXES * QBOX_BYTES, OFF_JOIN = OFF_Q + Q_BYTES;
+    static constexpr int OFF_JOIN = NSTAGE * STAGE_BYTES;
     static constexpr int OFF_REF = OFF_JOIN + NWG * (kStripRows / 2) * JOIN_LD * 4;
     static constexpr int OFF_SUM = OFF_REF + 2 * kStripRows * 4, OFF_BAR = OFF_SUM + 2 * SOFTMAX * 4;
     static constexpr int N_BARS = 2 * NSTAGE + 8 * NWG + 6;
@@ -87,7 +85,7 @@ template <int DV, int DR>
 __global__ void __launch_bounds__(TreeTraits<DV, DR>::THREADS, 1)
 tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_k) {
     using T = TreeTraits<DV, DR>;
-    constexpr int NS = T::NSTAGE, NWG = T::NWG, KS_V = DV / 16, KS_S = KS_V + T::DRP / 16, KS_O = kTreeTile / 16;
+    constexpr int NS = T::NSTAGE, NWG = T::NWG, KS_V = DV / 16, KS_S = KS_V + T::DRP / 16, KS_O = T::TILE / 16;
     constexpr uint32_t kAll = 0xffffffffu;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int c = blockIdx.x / p.G, g = blockIdx.x - c * p.G;
@@ -168,7 +166,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
         // ========================================= softmax: one row per thread =========================================
         const int w = warp >> 2, quarter = warp & 3, r = tid & (kStripRows - 1), hl = lane & 3, h = g * kHeadsPerGroup + hl;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16), o_addr = lane_base + T::COL_O;
-        const uint32_t s_addr = lane_base + T::COL_S + w * kTreeTile, p_addr = lane_base + T::COL_P + w * (kTreeTile / 2);
+        const uint32_t s_addr = lane_base + T::COL_S + w * T::TILE, p_addr = lane_base + T::COL_P + w * (T::TILE / 2);
         float *s_join = reinterpret_cast<float *>(smem + T::OFF_JOIN) + w * (kStripRows / 2) * T::JOIN_LD;
         uint32_t n_tiles = 0;                           // tiles that this group has had: the next one's number is n_tiles * NWG + w
         advance(w);                                     // (its first tile's stage)
@@ -214,14 +212,11 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                     if (half * HALF + i >= N) continue;
                     const int at = half * HALF + i;
                     const uint32_t words[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                    if constexpr (T::Q_TMEM) tmem_st4_nowait(lane_base + T::COL_Q + at * 4, words);
-                    else if (at < DV / 8) *reinterpret_cast<uint4 *>(smem + T::OFF_Q + (at >> 3) * T::QBOX_BYTES + swz128(r, at & 7)) = v[i];
-                    else *reinterpret_cast<uint4 *>(smem + T::OFF_QR + swz_kr<T::KR_ROW>(r, at - DV / 8)) = v[i];
+                    tmem_st4_nowait(lane_base + T::COL_Q + at * 4, words);
                 }
             }
             s_ref[(number & 1) * kStripRows + r] = -INFINITY;
-            if constexpr (T::Q_TMEM) tmem_st_wait();
-            else fence_async_smem();
+            tmem_st_wait();
             tc_fence_before();
             arrive(q_ready);
             return true;
@@ -234,9 +229,9 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
         auto edge_tile = [&](int st, int t0, uint32_t flag, bool live, size_t node, int half0, int halves, uint64_t (&bits)[2]) -> bool {
             volatile uint32_t *bad_rows = s_bad + w * 8 + (n_tiles & 1) * 4;         // (two sets: a slow reader of the tile before)
             unsigned char *v = smem + st * T::STAGE_BYTES + r * 128;
-            const bool zero = t0 + r >= pc.s.total || ((flag >> quarter) & 1);
+            const bool mine = r < T::TILE, zero = mine && (t0 + r >= pc.s.total || ((flag >> quarter) & 1));
             bool bad = false;
-            if (!zero && t0 + r >= pc.s.ctx) {
+            if (mine && !zero && t0 + r >= pc.s.ctx) {
 #pragma unroll 1
                 for (int bx = 0; bx < T::BOXES; ++bx)
 #pragma unroll 2
@@ -257,19 +252,26 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             if (!meet()) return false;
 #pragma unroll 1
             for (int k = 0; k < halves; ++k) {
-                const int from = (half0 + k) * 64, n = pc.s.total - t0 - from;       // tokens of this half of the tile
-                uint64_t seen = live ? tree_window(p.mask + node * p.words, p.words, t0 + from - pc.s.ctx) : 0;
+                const int from = (half0 + k) * T::HALF, n = pc.s.total - t0 - from;  // tokens of this half of the tile
+                uint64_t seen = live ? tree_window(p.mask + node * p.words, p.words, t0 + from - pc.s.ctx) : 0, bad_here = 0;
                 if (n < 64) seen = n <= 0 ? 0 : seen & ((1ull << n) - 1);
-                const uint32_t gone = flag >> ((half0 + k) * 2);
-                if (gone & 1) seen &= ~0xffffffffull;
-                if (gone & 2) seen &= 0xffffffffull;
-                poison |= (seen & (bad_rows[(half0 + k) * 2] | ((uint64_t)bad_rows[(half0 + k) * 2 + 1] << 32))) != 0;
+#pragma unroll
+                for (int i = 0; i < T::HALF / 32; ++i) {
+                    const int word = (half0 + k) * (T::HALF / 32) + i;
+                    if ((flag >> word) & 1) seen &= ~(0xffffffffull << (32 * i));
+                    bad_here |= (uint64_t)bad_rows[word] << (32 * i);
+                }
+                poison |= (seen & bad_here) != 0;
                 if (k == 0) bits[0] = seen;
                 else bits[1] = seen;
             }
             return true;
         };
 
+        auto store_words = [](uint32_t addr, const uint32_t (&x)[T::HALF / 2]) {
+            if constexpr (T::HALF == 64) tmem_st32u_nowait(addr, x);
+            else tmem_st16_nowait(addr, x);
+        };
         bool have = next_piece(pc);
         uint32_t t_base = 0;                            // running number of the piece's first tile
         if (have && w == 0) ok = stage_query(pc, 0, 0, false);
@@ -278,8 +280,8 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             const bool live = tok < pc.nv;
             const size_t node = (size_t)pc.s.r0 + pc.n0 + (live ? tok : 0), row_h = node * p.H + h;
             if (copies > 1) {                           // the other copy's tokens weigh nothing
-                const uint32_t none[32] = {};
-                tmem_st32u_nowait(p_addr + (1 - copy) * 32, none);
+                const uint32_t none[T::HALF / 2] = {};
+                store_words(p_addr + (1 - copy) * (T::HALF / 2), none);
                 tmem_st_wait();
             }
             sum = 0.f;
@@ -288,35 +290,39 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             const uint32_t t_end = t_base + (uint32_t)(pc.hi - pc.lo);
             const int first = pc.lo, ctx = pc.s.ctx, halves = 2 / copies, half0 = copy;                              // of a tile: those whose tokens this copy weighs
             for (; n_tiles * NWG + w < t_end; ++n_tiles) {
-                const int t = (int)(n_tiles * NWG) + w, t0 = (first + (int)(t - t_base)) * kTreeTile;
+                const int t = (int)(n_tiles * NWG) + w, t0 = (first + (int)(t - t_base)) * T::TILE;
                 if (!wait(s_full(w), n_tiles)) { ok = false; break; }
                 tc_fence_after();
-                // The row's scores, 64 columns at a time: of two such halves the first is loaded again for its weights.
+                // The row's scores, half a tile at a time: of two halves the first is loaded again for its weights.
                 const uint32_t flag = s_flag[st];
-                float s[64], m_tile = -INFINITY;
+                float s[T::HALF], m_tile = -INFINITY;
                 auto load = [&](int half) {
-                    float lo[32], hi[32];
-                    tmem_ld32_nowait(s_addr + half * 64, lo);
-                    tmem_ld32_nowait(s_addr + half * 64 + 32, hi);
-                    tmem_ld_wait();
+                    if constexpr (T::HALF == 64) {
+                        float lo[32], hi[32];
+                        tmem_ld32_nowait(s_addr + half * 64, lo);
+                        tmem_ld32_nowait(s_addr + half * 64 + 32, hi);
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) { s[k] = lo[k]; s[32 + k] = hi[k]; }
+                        for (int k = 0; k < 32; ++k) { s[k] = lo[k]; s[32 + k] = hi[k]; }
+                    } else {
+                        tmem_ld32(s_addr + half * 32, s);
+                    }
                 };
-                auto free_scores = [&]() {              // the score product after the next may have their place
+                auto free_scores = [&]() {              // the score product after the next NWG - 1 may have their place
                     tc_fence_before();
                     arrive(s_free(w));
                 };
                 load(half0);
                 if (halves == 1) free_scores();
-                const bool edge = t0 + kTreeTile > ctx || flag != 0;                 // the same for the whole block
+                const bool edge = t0 + T::TILE > ctx || flag != 0;                   // the same for the whole block
                 uint64_t bits[2] = {~0ull, ~0ull};
                 if (edge && !edge_tile(st, t0, flag, live, node, half0, halves, bits)) { ok = false; break; }
                 auto hide = [&](uint64_t seen) {
-                    const uint32_t b0 = (uint32_t)seen, b1 = (uint32_t)(seen >> 32);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        s[k] = (b0 >> k) & 1 ? s[k] : -INFINITY;
-                        s[32 + k] = (b1 >> k) & 1 ? s[32 + k] : -INFINITY;
+                    for (int j = 0; j < T::HALF; j += 32) {
+                        const uint32_t word = (uint32_t)(seen >> j);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) s[j + k] = (word >> k) & 1 ? s[j + k] : -INFINITY;
                     }
                 };
 #pragma unroll 1
@@ -326,11 +332,11 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
 #pragma unroll
                     for (int k = 0; k < 4; ++k) mx[k] = max3(s[k], s[k + 4], s[k + 8]);
 #pragma unroll
-                    for (int j = 12; j + 8 <= 64; j += 8)
+                    for (int j = 12; j + 8 <= T::HALF; j += 8)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[j + k], s[j + 4 + k]);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], s[60 + k]);
+                    for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], s[T::HALF - 4 + k]);
                     m_tile = max3(m_tile, fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                     if (++i == halves) break;
                     load(i);
@@ -340,9 +346,10 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                 // below 256, the quotient is the same, and O in tensor memory is rescaled only then, once the value product before is done.
                 // (tcgen05.ld / .st take whole warps: rows that stay multiply by 1.)  Asked for together: whether the group's weights
                 // before (long done, mostly) have been used.
+                const int w1 = w == 0 ? NWG - 1 : w - 1;
                 const uint32_t turn1 = w == 0 ? n_tiles - 1 : n_tiles;
-                if (t > 0 && !(n_tiles == 0 ? wait(turn(1 - w, quarter), turn1)
-                                            : warp_wait(turn(1 - w, quarter), turn1 & 1u, kv_empty(st_own), ph_own, s_abort))) { ok = false; break; }
+                if (t > 0 && !(n_tiles == 0 ? wait(turn(w1, quarter), turn1)
+                                            : warp_wait(turn(w1, quarter), turn1 & 1u, kv_empty(st_own), ph_own, s_abort))) { ok = false; break; }
                 float ref = s_ref[(n_pc & 1) * kStripRows + r];
                 const bool move = m_tile > ref + kRescaleLog2;
                 if (__any_sync(kAll, move)) {
@@ -376,9 +383,9 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                 uint64_t sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
 #pragma unroll 1
                 for (int i = halves - 1;;) {
-                    uint32_t pk[32];
+                    uint32_t pk[T::HALF / 2];
 #pragma unroll
-                    for (int k = 0; k < 64; k += 2) {
+                    for (int k = 0; k < T::HALF; k += 2) {
                         float a, b;
                         f2_unpack(f2_fma(f2_pack(s[k], s[k + 1]), sc2, nm2), a, b);
                         a = fast_exp2(a);
@@ -386,7 +393,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                         sum2[(k >> 1) & 1] = f2_add(sum2[(k >> 1) & 1], f2_pack(a, b));
                         pk[k >> 1] = pack_bf16(a, b);
                     }
-                    tmem_st32u_nowait(p_addr + (half0 + i) * 32, pk);
+                    store_words(p_addr + (half0 + i) * (T::HALF / 2), pk);
                     if (--i < 0) break;
                     load(i);
                     free_scores();
@@ -481,14 +488,14 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
         int t = 0;                                      // running number of a tile
         if (warp >= 4 * NWG + 2) {
             // ========================== loaders: of even and of odd tiles; all lanes look pages up, one issues ==========================
-            const int rows = p.P % 64 == 0 ? 64 : 32, boxes = kTreeTile / rows;      // a box of that many rows lies in one page
+            const int rows = p.P % 64 == 0 ? 64 : 32, boxes = T::TILE / rows;      // a box of that many rows lies in one page
             const uint64_t stream = l2_policy_evict_first();
             const uint32_t box_bytes = (uint32_t)rows * (T::BOXES * 128 + T::KR_ROW);
             while (ok && pieces.next(p, s_off, pc)) {
                 for (int base = pc.lo; base < pc.hi && ok; base += 32 / boxes) {
                     // rows of the pools where a lane's box begins; -1: a bad page, -2: nothing there
                     int v0 = -2, k0 = 0;
-                    const int at = base * kTreeTile + lane * rows;
+                    const int at = base * T::TILE + lane * rows;
                     if (base + lane / boxes < pc.hi && at < pc.s.total) {
                         const int j = at / p.P, slot = at - j * p.P;
                         const long long page = tree_page(p, pc.b, j);
@@ -531,12 +538,12 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             constexpr uint32_t hi128 = (1024u >> 4) | (1u << 14) | ((uint32_t)kSwz128 << 29);    // (descriptors as in the prefill kernel)
             constexpr uint32_t hikr = ((8u * T::KR_ROW) >> 4) | (1u << 14) | ((uint32_t)(T::KR_ROW == 32 ? kSwz32 : kSwz64) << 29);
             constexpr uint32_t lo_k = (16u >> 4) << 16, lo_mn = ((uint32_t)T::VBOX_BYTES >> 4) << 16;
-            const uint32_t a_st = (s_base & 0x3FFFFu) >> 4, a_q = ((s_base + T::OFF_Q) & 0x3FFFFu) >> 4;
+            const uint32_t a_st = (s_base & 0x3FFFFu) >> 4;
             auto mk = [](uint32_t lo, uint32_t hi) { return (uint64_t)lo | ((uint64_t)hi << 32); };
             int w = 0;
             uint32_t round = 0;                         // t = round * NWG + w
             if (warp == 4 * NWG + 1) {
-                constexpr uint32_t idesc = umma_idesc(kStripRows, kTreeTile, false);
+                constexpr uint32_t idesc = umma_idesc(kStripRows, T::TILE, false);
                 while (ok && pieces.next(p, s_off, pc)) {
                     if (pc.lo >= pc.hi) continue;
                     if (!wait(q_ready, n_pc)) { ok = false; break; }
@@ -545,15 +552,13 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                     for (int j = first; j < end; ++j, ++t, advance(1)) {
                         if (!(round == 0 ? wait(kv_full(st), ph) : warp_wait(kv_full(st), ph, s_free(w), (round - 1) & 1u, s_abort))) { ok = false; break; }
                         tc_fence_after();
-                        const uint32_t vb = a_st + (uint32_t)st * (T::STAGE_BYTES >> 4), d = tmem + T::COL_S + w * kTreeTile;
+                        const uint32_t vb = a_st + (uint32_t)st * (T::STAGE_BYTES >> 4), d = tmem + T::COL_S + w * T::TILE;
                         if (elect_one()) {
 #pragma unroll
                             for (int ks = 0; ks < KS_S; ++ks) {
                                 const uint32_t off = ks < KS_V ? ((ks >> 2) * T::VBOX_BYTES + (ks & 3) * 32) >> 4 : (T::V_BYTES >> 4) + (uint32_t)(ks - KS_V) * 2;
                                 const uint64_t k_desc = mk((vb + off) | lo_k, ks < KS_V ? hi128 : hikr);
-                                const uint32_t q_off = ks < KS_V ? ((ks >> 2) * T::QBOX_BYTES + (ks & 3) * 32) >> 4 : (uint32_t)(T::OFF_QR - T::OFF_Q) / 16 + (uint32_t)(ks - KS_V) * 2;
-                                if constexpr (T::Q_TMEM) umma_bf16_ts(d, tmem + T::COL_Q + ks * 8, k_desc, idesc, ks > 0);
-                                else umma_bf16(d, mk((a_q + q_off) | lo_k, ks < KS_V ? hi128 : hikr), k_desc, idesc, ks > 0);
+                                umma_bf16_ts(d, tmem + T::COL_Q + ks * 8, k_desc, idesc, ks > 0);
                             }
                             umma_commit(s_full(w));
                             mbar_arrive(s_full(w));
@@ -572,7 +577,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                         if (!wait(p_full(w), round)) { ok = false; break; }
                         if (j == first && n_pc > 0 && !wait(o_free, n_pc - 1)) { ok = false; break; }
                         tc_fence_after();
-                        const uint32_t vb = a_st + (uint32_t)st * (T::STAGE_BYTES >> 4), a = tmem + T::COL_P + w * (kTreeTile / 2);
+                        const uint32_t vb = a_st + (uint32_t)st * (T::STAGE_BYTES >> 4), a = tmem + T::COL_P + w * (T::TILE / 2);
                         if (elect_one()) {
 #pragma unroll
                             for (int ks = 0; ks < KS_O; ++ks)

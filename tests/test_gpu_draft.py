@@ -450,7 +450,7 @@ def test_what_is_out_of_sight_may_hold_anything(kind, bad):
     shape, ctx, sizes = wl.SHAPE_A, [70, 0], [40, 6]
     with Handle(shape, dtype=DTYPE[kind]) as h:
         c, q, see = tree_case(shape, ctx, sizes, kind=kind, seed=3)
-        clean, clean_lse = check_tree(h, c, q, see, ctx, sizes)
+        without = {k: check_tree(h, c, q, see, ctx, sizes, k) for k in (0, 2)}
         slot = lambda b, t: (c.ids[b, t // 64], t % 64)  # noqa: E731
         pg, at = slot(0, 70 + 5)
         c.d[0][pg, 2, at, 17] = dev(np.array([wl.f32_to_bf16_bits(np.float32([bad]))[0]]).view(np.int16))[0] if kind == "bf16" else bad
@@ -458,6 +458,7 @@ def test_what_is_out_of_sight_may_hold_anything(kind, bad):
         c.d[1][pg, at, 4] = dev(np.array([wl.f32_to_bf16_bits(np.float32([bad]))[0]]).view(np.int16))[0] if kind == "bf16" else bad
         for num_splits in (0, 2):
             out, lse, status = tree(h, c, q, see, ctx, sizes, num_splits)
+            clean, clean_lse = without[num_splits]
             assert status == 0
             hit = np.zeros(out.shape[:2], dtype=bool)
             hit[:40, 8:12] = see[0][:, 5][:, None]

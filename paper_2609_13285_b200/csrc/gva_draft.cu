@@ -42,7 +42,7 @@ int rows_per_block(const gva_handle *h, int n, int most) { return (int)std::min<
 struct TreePlan {
     int tile, strips, ranges, num_splits;
     long long records;
-    size_t smem, rec_o, rec_ml, total;       // shared memory of a block; workspace: offsets, records, their maxima and sums
+    size_t smem, rec_o, rec_ml, total;       // shared memory of a block; workspace: entries, records, their maxima and sums
 };
 int tree_status(const gva_handle *h, int B, int n_q, int max_q_len, int max_seq_len, int num_splits) {
     if (!h || B < 0 || n_q < 0 || max_q_len < 0 || max_seq_len < 0 || num_splits < 0) return GVA_ERR_INVALID_ARG;
@@ -67,9 +67,9 @@ TreePlan tree_plan(const gva_handle *h, int B, int max_q_len, int max_seq_len, i
     t.records = num_splits == 1 ? 0 : num_splits > 0 ? all * num_splits : t.ranges + all;
     // (never more blocks on an SM than its 512 columns of tensor memory serve: one)
     t.smem = mma ? std::max(k.fixed + (size_t)B * 4, (size_t)h->smem_per_sm / 2) : tree_fma_smem(B, c.d_v, c.d_r);
-    t.rec_o = align_up((size_t)(B + 1) * 4, 256);
+    t.rec_o = t.num_splits == 1 ? 0 : align_up((size_t)all * sizeof(int4), 256);
     t.rec_ml = t.rec_o + align_up((size_t)t.records * c.G * kStripRows * c.d_v * 4, 256);
-    t.total = t.rec_ml + align_up((size_t)t.records * c.G * kStripRows * 2 * 4, 256);
+    t.total = std::max<size_t>(256, t.rec_ml + align_up((size_t)t.records * c.G * kStripRows * 2 * 4, 256));
     return t;
 }
 using TreeFmaFn = void (*)(TreeParams, int);
@@ -243,7 +243,7 @@ int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const 
     std::memset(&p, 0, sizeof(p));
     p.q = q; p.mask = mask; p.cu_q = cu_q; p.ctx_lens = ctx_lens; p.block_table = cache->block_table;
     p.v_pool = cache->v_pool; p.kr_pool = cache->kr_pool; p.out = out; p.lse = lse; p.dev_status = dev_status;
-    p.offsets = reinterpret_cast<int32_t *>(ws);
+    p.entries = reinterpret_cast<int4 *>(ws);
     p.rec_o = reinterpret_cast<float *>(ws + plan.rec_o);
     p.rec_ml = reinterpret_cast<float *>(ws + plan.rec_ml);
     p.B = B; p.H = c.H; p.G = c.G; p.P = c.page_size; p.num_pages = cache->num_pages; p.max_pages = cache->max_pages_per_seq; p.words = mask_words;
@@ -267,9 +267,15 @@ int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const 
         rc = launched(launch_pdl(fn, grid, dim3(kTreeFmaThreads), plan.smem, s, p, c.d_r));
     }
     if (rc != GVA_OK || plan.num_splits == 1) return rc;
-    auto merge = c.cache_dtype == GVA_F32 ? (c.d_v == 64 ? tree_merge_kernel<float, 64> : tree_merge_kernel<float, 128>)
-                                          : (c.d_v == 64 ? tree_merge_kernel<__nv_bfloat16, 64> : tree_merge_kernel<__nv_bfloat16, 128>);
-    return launched(launch_pdl(merge, dim3((unsigned)ceil_div((long long)n_q * c.H, 8)), dim3(256), 0, s, p, n_q));
+    // many pieces a strip: a block per node with the pieces side by side; few: a warp per node
+    const bool wide = plan.ranges >= 8 * plan.strips * B || plan.num_splits >= 8;
+    const int nodes = std::min(max_q_len, kStripNodes);
+    const dim3 merge_grid((unsigned)(B * plan.strips), c.H, wide ? nodes : (nodes + 7) / 8);
+#define GVA_MERGE(OT_, DV_) (wide ? tree_merge_kernel<OT_, DV_, true> : tree_merge_kernel<OT_, DV_, false>)
+    auto merge = c.cache_dtype == GVA_F32 ? (c.d_v == 64 ? GVA_MERGE(float, 64) : GVA_MERGE(float, 128))
+                                          : (c.d_v == 64 ? GVA_MERGE(__nv_bfloat16, 64) : GVA_MERGE(__nv_bfloat16, 128));
+#undef GVA_MERGE
+    return launched(launch_pdl(merge, merge_grid, dim3(256), 0, s, p, n_q));
 }
 
 int gva_tree_commit(gva_handle *h, const gva_cache *cache, const int32_t *parents, const int32_t *tokens, const int32_t *chosen, const int32_t *cu_q,

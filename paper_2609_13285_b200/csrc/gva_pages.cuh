@@ -331,7 +331,7 @@ tree_commit_kernel(TreeCommitParams p) {
     int code = GVA_OK;
     if (ctx < 0 || (long long)ctx + n > (long long)p.max_pages * p.P) code = GVA_ERR_SEQ_LEN;
     else if (n > p.most) code = GVA_ERR_TREE;
-    int count = 0, token[kTreeMost / kCommitThreads];
+    int count = 0; int token[kTreeMost / kCommitThreads];
     if (code == GVA_OK) {                                         // everything the walk needs, in one trip
 #pragma unroll
         for (int k = 0; k < kTreeMost / kCommitThreads; ++k) {

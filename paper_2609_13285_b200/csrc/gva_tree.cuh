@@ -11,7 +11,6 @@
 // records that tree_merge_kernel joins.
 #pragma once
 
-#include "gva_pages.cuh"
 #include "gva_prefill.cuh"
 
 namespace gva {
@@ -26,7 +25,7 @@ struct TreeParams {
     void *out;                   // [n_q][H][d_v]
     float *lse;                  // [n_q][H], nullable
     int32_t *dev_status;
-    int32_t *offsets;            // workspace [B + 1]: the flat list's offsets, for the merge
+    int4 *entries;               // workspace [B][strips]: a strip's first record, its records, first node, nodes -- for the merge
     float *rec_o, *rec_ml;       // workspace records [..][G][128][d_v], [..][G][128][2]
     int B, H, G, P, num_pages, max_pages, words;
     int max_q_len, max_seq_len;
@@ -153,6 +152,28 @@ __device__ __forceinline__ size_t record_row(const TreeParams &p, int rec, int g
 __device__ __forceinline__ float tree_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
 __device__ __forceinline__ float tree_lse(float m, float l) { return (m + log2f(l)) * kLn2; }
 
+// What the merge has to know of every strip, written by threads [0, nt) of one block of the attention kernel, so that a block of the
+// merge finds its work in one trip to memory: it is a chain of trips and little else.
+__device__ __forceinline__ void tree_publish(const TreeParams &p, const int *s_off, int tid, int nt) {
+    if (p.num_splits == 1) return;
+    const int total = s_off[p.B], n = p.num_splits > 0 ? 0 : partitions_in_use(total, p.ranges);
+    for (int e = tid; e < p.B * p.strips; e += nt) {
+        const int b = e / p.strips, strip = e - b * p.strips;
+        const TreeSeq s = tree_seq(p, b, false);
+        int4 x = make_int4(0, 0, 0, 0);
+        if (strip < s.strips) {
+            const int n0 = strip * s.per_strip;
+            if (p.num_splits > 0) {
+                x = make_int4(e * p.num_splits, p.num_splits, s.r0 + n0, min(s.per_strip, s.n - n0));
+            } else {
+                const int lo = s_off[b] + strip * s.tiles, c0 = range_owner(lo, total, n), c1 = range_owner(lo + s.tiles - 1, total, n);
+                x = make_int4(c0 + e, c0 == c1 ? 0 : c1 - c0 + 1, s.r0 + n0, min(s.per_strip, s.n - n0));
+            }
+        }
+        p.entries[e] = x;
+    }
+}
+
 // ---- CUDA cores: f32 and e4m3 caches ------------------------------------------------------------------------
 // 256 threads, two per row: each scores 16 of 32 tokens, holds half of the row's output in registers.
 constexpr int kTreeFmaThreads = 256, kTreeFmaTokens = 32, kTreeFmaTile = 64;
@@ -175,8 +196,7 @@ tree_fma_kernel(TreeParams p, int d_r) {
     grid_dependency_wait();
     tree_offsets(p, s_off);
     const int tid = threadIdx.x, c = blockIdx.x / p.G, g = blockIdx.x % p.G;
-    if (blockIdx.x == 0)
-        for (int b = tid; b <= p.B; b += kTreeFmaThreads) p.offsets[b] = s_off[b];
+    if (blockIdx.x == 0) tree_publish(p, s_off, tid, kTreeFmaThreads);
     const CT *v_pool = static_cast<const CT *>(p.v_pool), *kr_pool = static_cast<const CT *>(p.kr_pool);
     const QT *q = static_cast<const QT *>(p.q);
     QT *out = static_cast<QT *>(p.out);
@@ -273,77 +293,102 @@ tree_fma_kernel(TreeParams p, int d_r) {
     }
 }
 
-// ---- merge: a warp per (node, head) whose strip was cut ---------------------------------------------------------
-// A chain of trips to memory, so each is made once: the sequence by 32 candidates at a time, the pieces' maxima and sums by a lane each,
-// four pieces' outputs at a time.
-template <typename OT, int DV>
+// ---- merge -----------------------------------------------------------------------------------------------------
+// A block per strip and head and eight nodes of it, a warp each; or (WIDE: few strips in many pieces) one node, the pieces side by side:
+// DV / 4 threads read a piece's row.  In both the pieces' weights are made first, one by each lane or thread.
+template <typename OT, int DV, bool WIDE>
 __global__ void __launch_bounds__(256)
 tree_merge_kernel(TreeParams p, int rows) {
     grid_dependency_launch();
+    constexpr int kMost = 256;                                            // pieces whose weights are held at a time (WIDE)
+    __shared__ float s_w[WIDE ? kMost : 1], s_part[WIDE ? 8 : 1], s_o[WIDE ? 256 / (DV / 4) : 1][WIDE ? DV : 1];
     grid_dependency_wait();
-    const int x = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int node = x / p.H, h = x - node * p.H;
-    if (node >= min(rows, p.cu_q[p.B])) return;
-    const int b = warp_owner_of(p.cu_q, p.B, node);
-    const TreeSeq s = tree_seq(p, b, false);
-    if (s.n <= 0) return;
-    const int strip = (node - s.r0) / s.per_strip, row = (node - s.r0 - strip * s.per_strip) * kHeadsPerGroup + h % kHeadsPerGroup;
-    int first, count;
-    if (p.num_splits > 0) {
-        first = (b * p.strips + strip) * p.num_splits;
-        count = p.num_splits;
-    } else {
-        const int total = p.offsets[p.B], n = partitions_in_use(total, p.ranges);
-        const int lo = p.offsets[b] + strip * s.tiles, c0 = range_owner(lo, total, n), c1 = range_owner(lo + s.tiles - 1, total, n);
-        first = c0 + b * p.strips + strip;
-        count = c1 - c0 + 1;
-    }
-    if (count == 1) return;
-    const int g = h / kHeadsPerGroup;
-    const size_t step = (size_t)p.G * kStripRows, r0 = record_row(p, first, g, row);      // from a piece's row to the next one's
-    float m = -INFINITY;
+    const int4 e = p.entries[blockIdx.x];
+    const int h = blockIdx.y, g = h / kHeadsPerGroup, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, count = e.y;
+    const int tok = WIDE ? blockIdx.z : blockIdx.z * 8 + warp;
+    if (count == 0 || tok >= e.w || e.z + tok >= rows) return;
+    const size_t step = (size_t)p.G * kStripRows, r0 = record_row(p, e.x, g, tok * kHeadsPerGroup + h % kHeadsPerGroup);   // from a piece's row to the next one's
+    const size_t row = (size_t)(e.z + tok) * p.H + h;
+    OT *out = static_cast<OT *>(p.out) + row * DV;
+    // (log-sum-exp over the pieces: every lane has the pieces lane, lane + 32, ...)
+    float m = -INFINITY, l = 0.f;
     for (int k = lane; k < count; k += 32) m = fmaxf(m, p.rec_ml[(r0 + k * step) * 2]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     const float ref = m == -INFINITY ? 0.f : m;
-    float acc[DV / 32], l = 0.f;
+    auto weight = [&](int k) {                                            // 0: an empty piece, which left its O unwritten
+        const float2 ml = *reinterpret_cast<const float2 *>(p.rec_ml + (r0 + k * step) * 2);
+        const float w = ml.y == 0.f ? 0.f : fast_exp2(ml.x - ref);
+        l = fmaf(w, ml.y, l);
+        return w;
+    };
+    if constexpr (WIDE) {
+        constexpr int PT = DV / 4, PP = 256 / PT;                         // threads of a row, pieces side by side
+        const int c = threadIdx.x % PT, pp = threadIdx.x / PT;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k0 = 0; k0 < count; k0 += kMost) {
+            __syncthreads();
+            if (k0 + (int)threadIdx.x < count) s_w[threadIdx.x] = weight(k0 + threadIdx.x);
+            __syncthreads();
+            const int n = min(kMost, count - k0);
+#pragma unroll 4
+            for (int k = pp; k < n; k += PP) {
+                const float w = s_w[k];
+                if (w == 0.f) continue;
+                const float4 x = *reinterpret_cast<const float4 *>(p.rec_o + (r0 + (k0 + k) * step) * DV + c * 4);
+                acc.x = fmaf(w, x.x, acc.x);
+                acc.y = fmaf(w, x.y, acc.y);
+                acc.z = fmaf(w, x.z, acc.z);
+                acc.w = fmaf(w, x.w, acc.w);
+            }
+        }
+        *reinterpret_cast<float4 *>(&s_o[pp][c * 4]) = acc;
 #pragma unroll
-    for (int i = 0; i < DV / 32; ++i) acc[i] = 0.f;
-    for (int k0 = 0; k0 < count; k0 += 32) {
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (k0 + lane < count) ml = *reinterpret_cast<const float2 *>(p.rec_ml + (r0 + (k0 + lane) * step) * 2);
-        const float own = ml.y == 0.f ? 0.f : fast_exp2(ml.x - ref);                       // (0: an empty piece, which left its O unwritten)
-        l = fmaf(own, ml.y, l);
-        const int n = min(32, count - k0);
-        for (int k = 0; k < n; k += 4) {
-            float w[4], o[4][DV / 32];
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (lane == 0) s_part[warp] = l;
+        __syncthreads();
+        if (threadIdx.x >= PT) return;
+        l = 0.f;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                w[u] = __shfl_sync(0xffffffffu, own, (k + u) & 31);
-                if (k + u >= n) w[u] = 0.f;
+        for (int i = 0; i < 8; ++i) l += s_part[i];
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int i = 0; i < DV / 32; i += 2) {
-                    const float2 y = w[u] != 0.f ? *reinterpret_cast<const float2 *>(p.rec_o + (r0 + (k0 + k + u) * step) * DV + lane * (DV / 32) + i) : make_float2(0.f, 0.f);
-                    o[u][i] = y.x;
-                    o[u][i + 1] = y.y;
+        for (int i = 0; i < PP; ++i) {
+            const float4 x = *reinterpret_cast<const float4 *>(&s_o[i][c * 4]);
+            acc = make_float4(acc.x + x.x, acc.y + x.y, acc.z + x.z, acc.w + x.w);
+        }
+        const float inv = tree_inverse(l);
+        store_out4(out + c * 4, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    } else {
+        constexpr int E = DV / 32;
+        float acc[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) acc[i] = 0.f;
+        for (int k0 = 0; k0 < count; k0 += 32) {
+            const float own = k0 + lane < count ? weight(k0 + lane) : 0.f;
+            const int n = min(32, count - k0);
+#pragma unroll 4
+            for (int k = 0; k < n; ++k) {
+                const float w = __shfl_sync(0xffffffffu, own, k);
+                if (w == 0.f) continue;
+#pragma unroll
+                for (int i = 0; i < E; i += 2) {
+                    const float2 x = *reinterpret_cast<const float2 *>(p.rec_o + (r0 + (k0 + k) * step) * DV + lane * E + i);
+                    acc[i] = fmaf(w, x.x, acc[i]);
+                    acc[i + 1] = fmaf(w, x.y, acc[i + 1]);
                 }
             }
+        }
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        const float inv = tree_inverse(l);
 #pragma unroll
-                for (int i = 0; i < DV / 32; ++i) acc[i] = fmaf(w[u], o[u][i], acc[i]);
+        for (int i = 0; i < E; i += 2) {
+            if constexpr (sizeof(OT) == 2) *reinterpret_cast<uint32_t *>(out + lane * E + i) = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
+            else *reinterpret_cast<float2 *>(out + lane * E + i) = make_float2(acc[i] * inv, acc[i + 1] * inv);
         }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    const float inv = tree_inverse(l);
-    OT *dst = static_cast<OT *>(p.out) + ((size_t)node * p.H + h) * DV + lane * (DV / 32);
-#pragma unroll
-    for (int i = 0; i < DV / 32; i += 2) {
-        if constexpr (sizeof(OT) == 2) *reinterpret_cast<uint32_t *>(dst + i) = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
-        else *reinterpret_cast<float2 *>(dst + i) = make_float2(acc[i] * inv, acc[i + 1] * inv);
-    }
-    if (p.lse && lane == 0) p.lse[(size_t)node * p.H + h] = tree_lse(m, l);
+    if (p.lse && (WIDE ? threadIdx.x : lane) == 0) p.lse[row] = tree_lse(m, l);
 }
 
 }  // namespace gva

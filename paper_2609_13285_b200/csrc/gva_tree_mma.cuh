@@ -71,7 +71,7 @@ struct TreeTraits {
     static constexpr int COL_S = 0, COL_P = NWG * TILE, COL_O = COL_P + NWG * TILE / 2, COL_Q = COL_O + DV;
     static_assert(COL_Q + (DV + DRP) / 2 <= TMEM_COLS, "scores, weights, O and the query must fit the allocation");
     static constexpr int SOFTMAX = NWG * 128, THREADS = SOFTMAX + 128;
-    static constexpr int PART = 16, JOIN_LD = 20;                // columns of O at a time in the join of copies; f32 of a row there, padded
+    static constexpr int PART = 32, JOIN_LD = 36;                // columns of O at a time in the join of copies; f32 of a row there, padded
     static constexpr int OFF_JOIN = NSTAGE * STAGE_BYTES;
     static constexpr int OFF_REF = OFF_JOIN + NWG * (kStripRows / 2) * JOIN_LD * 4;
     static constexpr int OFF_SUM = OFF_REF + 2 * kStripRows * 4, OFF_BAR = OFF_SUM + 2 * SOFTMAX * 4;
@@ -136,14 +136,12 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
     }
     grid_dependency_wait();
     tree_offsets(p, s_off);
-    if (blockIdx.x == 0)
-        for (int b = tid; b <= p.B; b += T::THREADS) p.offsets[b] = s_off[b];
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
     TreePieces pieces(p, s_off, c);
-    TreePiece pc;
+    TreePiece pc = {};
     uint32_t n_pc = 0;                                  // running number of a piece
     int st = 0;                                         // stage of a tile, and the parity of its round through the ring
     uint32_t ph = 0;
@@ -272,6 +270,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             if constexpr (T::HALF == 64) tmem_st32u_nowait(addr, x);
             else tmem_st16_nowait(addr, x);
         };
+        if (blockIdx.x == 0 && w == NWG - 1) tree_publish(p, s_off, r, kStripRows);     // (its first tile comes last)
         bool have = next_piece(pc);
         uint32_t t_base = 0;                            // running number of the piece's first tile
         if (have && w == 0) ok = stage_query(pc, 0, 0, false);
@@ -444,7 +443,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
 #pragma unroll 1
             for (int part = w; part < DV / T::PART; part += NWG) {
                 float o[T::PART];
-                tmem_ld16(o_addr + part * T::PART, o);
+                tmem_ld32(o_addr + part * T::PART, o);
 #pragma unroll
                 for (int i = 0; i < T::PART; ++i) o[i] *= inv;
                 if (copies > 1) {
@@ -462,7 +461,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                             o[i + 2] += x.z;
                             o[i + 3] += x.w;
                         }
-                    if (!meet()) { ok = false; break; }
+                    if (part + NWG < DV / T::PART && !meet()) { ok = false; break; }     // (else the next piece's meetings do)
                 }
                 if (live && copy == 0) {
                     if (pc.rec < 0) {

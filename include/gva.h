@@ -560,15 +560,16 @@ int gva_append_rows(gva_handle *h, const gva_cache *cache, const float *v_new, c
  *   mask [n_q][mask_words] u32, mask_words >= ceil(max_q_len / 32); bits at or beyond n_b are ignored
  *   out  [n_q][H][d_v]       of q's type: rounded once.  A row that sees nothing gives 0
  *   lse  [n_q][H] f32 or NULL   natural logarithm; -inf for a row that sees nothing
- *   max_q_len, max_seq_len   upper bounds on n_b (256 at most) and on ctx_lens[b] + n_b
+ *   n_q                      rows that q, mask, out and lse hold: at least cu_q[B]
+ *   max_q_len, max_seq_len   upper bounds on n_b (256 at most) and on ctx_lens[b] + n_b (2^30 at most)
  *   num_splits               0: all sequences' tiles in a row are cut into equal ranges; n: every 32 nodes' tiles into n ranges (64 at most)
  * Over a bf16 cache the products are taken of the bf16 numbers as they are, accumulated in f32; softmax weights enter the value product
- * rounded to bf16 (2^-9, as the output is; their sum is taken before), everything else is f32: measured against 64 bits the output is
- * 1.4 times as far off as its own rounding.  Bitwise reproducible for fixed arguments.  What is cached for a node does not reach rows that do
+ * rounded to bf16 (2^-8 at most, as the output; their sum is taken before), everything else is f32: over a thousand tokens and more the output is
+ * as far off as its own rounding makes it (1.7e-3 of its size), over a hundred 1.1 times.  Over e4m3 and f32 caches all is f32 but the output's type.  Bitwise reproducible for fixed arguments.  What is cached for a node does not reach rows that do
  * not see it, not even infinities and NaN; a row that sees a node with an infinity or NaN among a group's values has NaN in the heads of that
  * group, in those elements or in all.
- * n_b < 0 or > max_q_len, ctx_lens[b] < 0, or ctx_lens[b] + n_b beyond max_seq_len or the block table -> GVA_ERR_SEQ_LEN, the sequence's rows are left as
- * they were; tokens of a page outside the pool count as absent (GVA_ERR_BAD_PAGE).  Rows at or beyond cu_q[B] are left as they were.
+ * n_b < 0 or > max_q_len, rows outside [0, n_q), ctx_lens[b] < 0, or ctx_lens[b] + n_b beyond max_seq_len or the block table -> GVA_ERR_SEQ_LEN, the
+ * sequence's rows are left as they were; tokens of a page outside the pool count as absent (GVA_ERR_BAD_PAGE).  Rows at or beyond cu_q[B] are left as they were.
  * Workspace: at least gva_decode_tree_workspace_bytes(...) bytes, 256-byte aligned. */
 size_t gva_decode_tree_workspace_bytes(const gva_handle *h, int B, int n_q, int max_q_len, int max_seq_len, int num_splits);
 int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const uint32_t *mask, int mask_words, const int32_t *cu_q,

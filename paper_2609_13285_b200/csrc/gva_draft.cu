@@ -46,7 +46,7 @@ struct TreePlan {
 };
 int tree_status(const gva_handle *h, int B, int n_q, int max_q_len, int max_seq_len, int num_splits) {
     if (!h || B < 0 || n_q < 0 || max_q_len < 0 || max_seq_len < 0 || num_splits < 0) return GVA_ERR_INVALID_ARG;
-    if (B > 8192 || max_q_len > kTreeMost || num_splits > 64) return GVA_ERR_UNSUPPORTED;
+    if (B > 8192 || max_q_len > kTreeMost || num_splits > 64 || max_seq_len > (1 << 30)) return GVA_ERR_UNSUPPORTED;
     const long long strips = ceil_div(max_q_len, kStripNodes) * B;
     if (strips * std::max<long long>(ceil_div(max_seq_len, kTreeFmaTile), num_splits) >= (1ll << 30)) return GVA_ERR_UNSUPPORTED;   // (tiles are counted in 32 bits)
     return GVA_OK;
@@ -178,13 +178,14 @@ int gva_assign_pages(gva_handle *h, const int32_t *used, const int32_t *want, co
     p.dev_status = dev_status;
     p.max_pages = max_pages_per_seq; p.num_pages = num_pages; p.max_rows = max_rows; p.B = B; p.P = h->cfg.page_size;
     // Up to 8192 rows the kernel's threads have one row each, in a cluster of up to eight blocks; more rows get a kernel of their own
-    // (256 trees, 5000 rows: 7.0 us with it, 5.4 in the cluster; 0.2 M rows of 48 prompts 8.3 and 33).
+    // (in the cluster and apart, us: 5000 rows of 256 trees 6.8 and 12.3, 0.2 M rows of 48 prompts 33 and 9.3).
     p.rows_here = max_rows <= 8192 ? 1 : 0;
-    const int work = std::max(B, p.rows_here ? max_rows : 1024);
+    const int work = (int)std::max<long long>(B, p.rows_here ? max_rows : std::max<long long>(1024, ceil_div(max_rows, p.P)));   // (as many pages taken, at least)
     const int threads = work <= 128 ? 128 : work <= 256 ? 256 : work <= 512 ? 512 : 1024;
-    const int blocks = !p.rows_here || work <= 1024 ? 1 : work <= 2048 ? 2 : work <= 4096 ? 4 : 8;
+    const int blocks = work <= 1024 ? 1 : work <= 2048 ? 2 : work <= 4096 ? 4 : 8;
     const size_t smem = (size_t)6 * B * 4;
-    rc = allow_smem(h, reinterpret_cast<const void *>(assign_pages_kernel), smem);
+    void (*const fn)(AssignParams) = B <= threads ? assign_pages_kernel<1> : assign_pages_kernel<kAssignItems>;
+    rc = allow_smem(h, reinterpret_cast<const void *>(fn), smem);
     if (rc != GVA_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
@@ -199,7 +200,7 @@ int gva_assign_pages(gva_handle *h, const int32_t *used, const int32_t *want, co
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    rc = launched(cudaLaunchKernelEx(&cfg, assign_pages_kernel, p));
+    rc = launched(cudaLaunchKernelEx(&cfg, fn, p));
     if (rc != GVA_OK || p.rows_here) return rc;
     return launched(launch_pdl(assign_rows_kernel, dim3((unsigned)ceil_div(max_rows, kAssignRows)), dim3(kAssignRowThreads), 0, cfg.stream, p));
 }
@@ -247,7 +248,7 @@ int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const 
     p.rec_o = reinterpret_cast<float *>(ws + plan.rec_o);
     p.rec_ml = reinterpret_cast<float *>(ws + plan.rec_ml);
     p.B = B; p.H = c.H; p.G = c.G; p.P = c.page_size; p.num_pages = cache->num_pages; p.max_pages = cache->max_pages_per_seq; p.words = mask_words;
-    p.max_q_len = max_q_len; p.max_seq_len = max_seq_len;
+    p.n_q = n_q; p.max_q_len = max_q_len; p.max_seq_len = max_seq_len;
     p.tile = plan.tile; p.strips = plan.strips; p.ranges = plan.ranges; p.num_splits = plan.num_splits;
     p.scale_log2 = h->scale * kLog2e;
     if (plan.smem > (size_t)h->smem_optin) return GVA_ERR_UNSUPPORTED;
@@ -275,7 +276,7 @@ int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const 
     auto merge = c.cache_dtype == GVA_F32 ? (c.d_v == 64 ? GVA_MERGE(float, 64) : GVA_MERGE(float, 128))
                                           : (c.d_v == 64 ? GVA_MERGE(__nv_bfloat16, 64) : GVA_MERGE(__nv_bfloat16, 128));
 #undef GVA_MERGE
-    return launched(launch_pdl(merge, merge_grid, dim3(256), 0, s, p, n_q));
+    return launched(launch_pdl(merge, merge_grid, dim3(256), 0, s, p));
 }
 
 int gva_tree_commit(gva_handle *h, const gva_cache *cache, const int32_t *parents, const int32_t *tokens, const int32_t *chosen, const int32_t *cu_q,
@@ -284,7 +285,7 @@ int gva_tree_commit(gva_handle *h, const gva_cache *cache, const int32_t *parent
     if (rc != GVA_OK) return rc;
     if (B < 0 || max_q_len < 0) return GVA_ERR_INVALID_ARG;
     if (B == 0) return GVA_OK;
-    if (!cu_q || !ctx_lens || !new_lens || !last || (max_q_len > 0 && (!parents || !tokens || !chosen || !path))) return GVA_ERR_INVALID_ARG;
+    if (!cu_q || !ctx_lens || !new_lens || !last || !parents || !tokens || !chosen || !path) return GVA_ERR_INVALID_ARG;
     if (!aligned(parents, 4) || !aligned(tokens, 4) || !aligned(chosen, 4) || !aligned(cu_q, 4) || !aligned(ctx_lens, 4) || !aligned(path, 4) || !aligned(new_lens, 4) ||
         !aligned(last, 4))
         return GVA_ERR_INVALID_ARG;

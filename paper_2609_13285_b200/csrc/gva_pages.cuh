@@ -23,7 +23,7 @@ struct AssignParams {
     int max_pages, num_pages, max_rows, B, P;
     int rows_here;                           // 1: the rows' positions and slots too; 0: assign_rows_kernel follows
 };
-constexpr int kAssignItems = 8;      // sequences of a thread: 1024 threads serve 8192
+constexpr int kAssignItems = 8;      // sequences of a thread at most: 1024 threads serve 8192
 
 // What a sequence asks for.
 struct Asks {
@@ -103,10 +103,11 @@ __device__ __forceinline__ long long block_scan(Sums &x, int wanted, long long (
     return total;
 }
 
-// One cluster.  Every block scans all sequences for itself (8 a thread at most) and keeps the offsets in shared memory; once all
+// One cluster.  Every block scans all sequences for itself (ITEMS a thread) and keeps the offsets in shared memory; once all
 // of them have read the inputs -- outputs may be the same buffers -- they share out rows, taken and returned pages among
 // their threads, which find their sequence by bisection.  Growing sequences are served in order until one does not fit, so the
 // sums before a served one are sums over all growing ones before it, and what is served needs no second scan.
+template <int ITEMS>
 __global__ void __launch_bounds__(1024)
 assign_pages_kernel(AssignParams p) {
     grid_dependency_launch();
@@ -123,10 +124,10 @@ assign_pages_kernel(AssignParams p) {
     const int first = p.free_in[0], count = p.free_in[1];
     const bool sound = first >= 0 && first < p.num_pages && count >= 0 && count <= p.num_pages;    // else all stays as it is
     if (!sound && rank == 0 && tid == 0) report_error(p.dev_status, GVA_ERR_BAD_PAGE, 0);
-    Asks a[kAssignItems];
+    Asks a[ITEMS];
     long long rows = 0, take = 0, give = 0, back = 0;
 #pragma unroll
-    for (int i = 0; i < kAssignItems; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         const int b = tid * per + i;
         if (i >= per || b >= p.B) continue;
         a[i] = sequence_asks(p, b, sound);
@@ -139,9 +140,10 @@ assign_pages_kernel(AssignParams p) {
     Sums to = {{rows, take, give, back}};
     const long long give_all = block_scan(to, 2, s_part);
     {
+        int most_rows = 0, most_take = 0, most_back = 0;        // of this thread's sequences that are served
         long long r = to.v[0] - rows, t = to.v[1] - take, g = to.v[2] - give, k = to.v[3] - back;
 #pragma unroll
-        for (int i = 0; i < kAssignItems; ++i) {
+        for (int i = 0; i < ITEMS; ++i) {
             const int b = tid * per + i;
             if (i >= per || b >= p.B) continue;
             const bool grows = a[i].rows > 0;
@@ -158,9 +160,9 @@ assign_pages_kernel(AssignParams p) {
             if (grows) k += a[i].give;
             else g += a[i].give;
             if (grows && served) {
-                atomicMax(&s_served[0], (int)r);
-                atomicMax(&s_served[1], (int)t);
-                atomicMax(&s_served[2], (int)min(k, (long long)p.num_pages));
+                most_rows = (int)r;
+                most_take = (int)t;
+                most_back = (int)min(k, (long long)p.num_pages);
             }
             if (!served) {
                 if (rank == 0) report_error(p.dev_status, GVA_ERR_NO_ROOM, b);
@@ -168,11 +170,19 @@ assign_pages_kernel(AssignParams p) {
                 a[i].rows = -1;                                // stays as it is
             }
         }
+        most_rows = __reduce_max_sync(0xffffffffu, most_rows);
+        most_take = __reduce_max_sync(0xffffffffu, most_take);
+        most_back = __reduce_max_sync(0xffffffffu, most_back);
+        if ((tid & 31) == 0) {
+            atomicMax(&s_served[0], most_rows);
+            atomicMax(&s_served[1], most_take);
+            atomicMax(&s_served[2], most_back);
+        }
     }
     __syncthreads();
     const int n_rows = s_served[0], n_take = s_served[1], n_back = s_served[2];
 #pragma unroll
-    for (int i = 0; i < kAssignItems; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         const int b = tid * per + i;
         if (i >= per || b >= p.B) continue;
         s_row[b] = min(s_row[b], n_rows);
@@ -180,18 +190,25 @@ assign_pages_kernel(AssignParams p) {
         s_give[b] = (int)min((long long)s_give[b] + min(s_to[b], n_back), (long long)p.num_pages);
         s_to[b] = a[i].to;
     }
-    int want[kAssignItems];
+    int want[ITEMS];
 #pragma unroll
-    for (int i = 0; i < kAssignItems; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         const int b = tid * per + i;
         if (i < per && b < p.B) want[i] = p.want[b];
     }
     const int n_give = (int)min(give_all + n_back, (long long)p.num_pages + 1);
     // every block of the cluster has read its inputs (and this block's offsets are whole) before anything is written
     cluster.sync();
+    const int me = rank * nt + tid, all = wide * nt;
+    // an entry of the ring: num_pages is below 2^26 (slots are below 2^31), and what is added to `first` below twice that
+    auto entry = [&](int at) {
+        at += first;
+        if (at >= p.num_pages) at -= p.num_pages;
+        return at >= p.num_pages ? at - p.num_pages : at;
+    };
     if (rank == 0) {
 #pragma unroll
-        for (int i = 0; i < kAssignItems; ++i) {
+        for (int i = 0; i < ITEMS; ++i) {
             const int b = tid * per + i;
             if (i >= per || b >= p.B) continue;
             p.pages_out[b] = a[i].to;
@@ -203,33 +220,32 @@ assign_pages_kernel(AssignParams p) {
             // a ring that would overflow held pages twice: it takes no more than fit
             const int room = p.num_pages - count;
             if (sound && n_give > room) report_error(p.dev_status, GVA_ERR_BAD_PAGE, 0);
-            p.free_out[0] = sound ? (int)(((long long)first + n_take) % p.num_pages) : first;
+            p.free_out[0] = sound ? entry(n_take) : first;
             p.free_out[1] = sound ? count - n_take + min(n_give, room) : count;
         }
     }
-    const int me = rank * nt + tid, all = wide * nt;
     for (int i = me; i < n_take; i += all) {                     // (none of these without a sound ring)
         const int b = owner_of(s_take, p.B, i);
-        p.block_table[(size_t)b * p.max_pages + s_pages[b] + (i - s_take[b])] = p.ring[((long long)first + i) % p.num_pages];
+        p.block_table[(size_t)b * p.max_pages + s_pages[b] + (i - s_take[b])] = p.ring[entry(i)];
     }
     for (int i = me; i < n_give && i < p.num_pages - count; i += all) {
         const int b = owner_of(s_give, p.B, i);
         const int page = p.block_table[(size_t)b * p.max_pages + s_to[b] + (i - s_give[b])];
         if (page < 0 || page >= p.num_pages) report_error(p.dev_status, GVA_ERR_BAD_PAGE, b);
-        p.ring[((long long)first + count + i) % p.num_pages] = page;
+        p.ring[entry(count + i)] = page;
     }
     for (int i = p.rows_here ? me : n_rows; i < n_rows; i += all) {
         const int b = owner_of(s_row, p.B, i);
         const int t = s_used[b] + (i - s_row[b]), j = t / p.P;
         const int page = j < s_pages[b] ? p.block_table[(size_t)b * p.max_pages + j]
-                                        : p.ring[((long long)first + s_take[b] + (j - s_pages[b])) % p.num_pages];
+                                        : p.ring[entry(s_take[b] + (j - s_pages[b]))];
         p.positions[i] = t;
         p.slots[i] = page < 0 || page >= p.num_pages ? -1 : page * p.P + t % p.P;
     }
 }
 
-// Positions and slots of many rows, from what assign_pages_kernel has left: 0.2 M rows of 48 prompts in all of the GPU's blocks take 6 us,
-// in the one cluster 29.  A block has 1024 rows in a row, of as few sequences as these lie in.
+// Positions and slots of many rows, from what assign_pages_kernel has left (0.2 M rows of 48 prompts: 9.3 us with that kernel, 33 in its one
+// cluster).  A block has 1024 rows in a row, of as few sequences as these lie in.
 constexpr int kAssignRows = 1024, kAssignRowThreads = 256;
 __global__ void __launch_bounds__(kAssignRowThreads)
 assign_rows_kernel(AssignParams p) {

@@ -28,7 +28,7 @@ struct TreeParams {
     int4 *entries;               // workspace [B][strips]: a strip's first record, its records, first node, nodes -- for the merge
     float *rec_o, *rec_ml;       // workspace records [..][G][128][d_v], [..][G][128][2]
     int B, H, G, P, num_pages, max_pages, words;
-    int max_q_len, max_seq_len;
+    int n_q, max_q_len, max_seq_len;
     int tile;                    // tokens of a tile
     int strips;                  // of a sequence at most
     int ranges;                  // balanced form: ranges of the flat list; uniform form: blocks (of a group) that share the pieces
@@ -46,7 +46,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams &p, int b, bool say
     s.n = p.cu_q[b + 1] - s.r0;
     s.ctx = p.ctx_lens[b];
     const long long total = (long long)s.ctx + s.n;
-    const bool fine = s.n >= 0 && s.n <= p.max_q_len && s.ctx >= 0 && total <= p.max_seq_len && total <= (long long)p.max_pages * p.P;
+    const bool fine = s.n >= 0 && s.n <= p.max_q_len && s.r0 >= 0 && s.r0 <= p.n_q - s.n && s.ctx >= 0 && total <= p.max_seq_len && total <= (long long)p.max_pages * p.P;
     if (!fine && say) report_error(p.dev_status, GVA_ERR_SEQ_LEN, b);
     if (!fine) s.n = 0;
     s.total = (int)total;
@@ -152,12 +152,12 @@ __device__ __forceinline__ size_t record_row(const TreeParams &p, int rec, int g
 __device__ __forceinline__ float tree_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
 __device__ __forceinline__ float tree_lse(float m, float l) { return (m + log2f(l)) * kLn2; }
 
-// What the merge has to know of every strip, written by threads [0, nt) of one block of the attention kernel, so that a block of the
+// What the merge has to know of every strip, shared out among nt threads of each block of the attention kernel, so that a block of the
 // merge finds its work in one trip to memory: it is a chain of trips and little else.
 __device__ __forceinline__ void tree_publish(const TreeParams &p, const int *s_off, int tid, int nt) {
     if (p.num_splits == 1) return;
     const int total = s_off[p.B], n = p.num_splits > 0 ? 0 : partitions_in_use(total, p.ranges);
-    for (int e = tid; e < p.B * p.strips; e += nt) {
+    for (int e = blockIdx.x * nt + tid; e < p.B * p.strips; e += gridDim.x * nt) {
         const int b = e / p.strips, strip = e - b * p.strips;
         const TreeSeq s = tree_seq(p, b, false);
         int4 x = make_int4(0, 0, 0, 0);
@@ -196,7 +196,7 @@ tree_fma_kernel(TreeParams p, int d_r) {
     grid_dependency_wait();
     tree_offsets(p, s_off);
     const int tid = threadIdx.x, c = blockIdx.x / p.G, g = blockIdx.x % p.G;
-    if (blockIdx.x == 0) tree_publish(p, s_off, tid, kTreeFmaThreads);
+    tree_publish(p, s_off, tid, kTreeFmaThreads);
     const CT *v_pool = static_cast<const CT *>(p.v_pool), *kr_pool = static_cast<const CT *>(p.kr_pool);
     const QT *q = static_cast<const QT *>(p.q);
     QT *out = static_cast<QT *>(p.out);
@@ -298,7 +298,7 @@ tree_fma_kernel(TreeParams p, int d_r) {
 // DV / 4 threads read a piece's row.  In both the pieces' weights are made first, one by each lane or thread.
 template <typename OT, int DV, bool WIDE>
 __global__ void __launch_bounds__(256)
-tree_merge_kernel(TreeParams p, int rows) {
+tree_merge_kernel(TreeParams p) {
     grid_dependency_launch();
     constexpr int kMost = 256;                                            // pieces whose weights are held at a time (WIDE)
     __shared__ float s_w[WIDE ? kMost : 1], s_part[WIDE ? 8 : 1], s_o[WIDE ? 256 / (DV / 4) : 1][WIDE ? DV : 1];
@@ -306,7 +306,7 @@ tree_merge_kernel(TreeParams p, int rows) {
     const int4 e = p.entries[blockIdx.x];
     const int h = blockIdx.y, g = h / kHeadsPerGroup, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, count = e.y;
     const int tok = WIDE ? blockIdx.z : blockIdx.z * 8 + warp;
-    if (count == 0 || tok >= e.w || e.z + tok >= rows) return;
+    if (count == 0 || tok >= e.w) return;
     const size_t step = (size_t)p.G * kStripRows, r0 = record_row(p, e.x, g, tok * kHeadsPerGroup + h % kHeadsPerGroup);   // from a piece's row to the next one's
     const size_t row = (size_t)(e.z + tok) * p.H + h;
     OT *out = static_cast<OT *>(p.out) + row * DV;

@@ -270,7 +270,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             if constexpr (T::HALF == 64) tmem_st32u_nowait(addr, x);
             else tmem_st16_nowait(addr, x);
         };
-        if (blockIdx.x == 0 && w == NWG - 1) tree_publish(p, s_off, r, kStripRows);     // (its first tile comes last)
+        if (w == NWG - 1) tree_publish(p, s_off, r, kStripRows);     // (its first tile comes last)
         bool have = next_piece(pc);
         uint32_t t_base = 0;                            // running number of the piece's first tile
         if (have && w == 0) ok = stage_query(pc, 0, 0, false);

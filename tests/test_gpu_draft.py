@@ -128,6 +128,16 @@ def test_bad_lengths_pages_and_rings():
         assert got["slots"][-3:] == [-1] * 3
 
 
+def test_no_sequences_and_no_rows():
+    with Handle(wl.SHAPE_A) as h:
+        ring, free, cu, free_out, status = ints([3, 1, 2]), ints([1, 2]), zeros(1) - 3, zeros(2) - 3, zeros(1)
+        gb.gva_assign_pages(h.h, None, None, None, None, None, 4, 3, ring, free, free_out, None, cu, None, None, 0, 0, status)
+        assert cu.tolist() == [0] and free_out.tolist() == [1, 2]
+        s = Pages(5, 64, 4, seed=1, held=[0] * 5, ahead=0)
+        for rows in (0, 20_000):
+            check_assign(h, s, [0] * 5, rows)
+
+
 def test_a_captured_step_goes_on_in_place():
     with Handle(wl.SHAPE_A) as h:
         s = Pages(50, 64, 30, seed=9, spare=400)
@@ -504,6 +514,20 @@ def test_bad_lengths_and_pages_stay_with_their_sequence():
             assert (np.abs(out[5:14] - o) <= 2.0 ** -7 * size + 1e-6).all() and np.abs(lse[5:14] - l).max() <= 1e-4
 
 
+def test_rows_beyond_what_the_call_allows_for_are_not_written():
+    shape, ctx, sizes = wl.SHAPE_A, [30, 40, 500], [4, 5, 6]
+    for kind in ("bf16", "f32"):
+        with Handle(shape, dtype=DTYPE[kind]) as h:
+            c, q, see = tree_case(shape, ctx, sizes, kind=kind, seed=9)
+            clean, clean_lse, _ = tree(h, c, q, see, ctx, sizes, num_splits=2)
+            mask = dev(np.concatenate([ref.mask_words(x, 1) for x in see]).view(np.int32))
+            out, lse, status = torch.full((15, 16, 64), 7.0, dtype=q.dtype, device="cuda"), torch.full((15, 16), 7.0, device="cuda"), zeros(1)
+            ws = torch.empty(gb.gva_decode_tree_workspace_bytes(h.h, 3, 14, 6, 506, 2), dtype=torch.uint8, device="cuda")
+            gb.gva_decode_tree(h.h, c.c, q, mask, 1, ints([0, 4, 9, 15]), ints(ctx), out, lse, ws, 3, 14, 6, 506, 2, status)
+            assert code(status) == (gb.GVA_ERR_SEQ_LEN, 2) and (out[9:] == 7).all() and (lse[9:] == 7).all()
+            assert np.array_equal(out[:9].float().cpu().numpy(), clean[:9]) and np.array_equal(lse[:9].cpu().numpy(), clean_lse[:9])
+
+
 def test_large_scores_and_moving_maxima():
     """Queries 30 times as long, and values that grow along the sequence: the softmax's reference moves again and again."""
     shape, ctx, sizes = wl.SHAPE_A, [900], [20]
@@ -701,7 +725,7 @@ def test_refusals():
         for k in ("B", "n", "most", "max_len", "splits"):
             assert refused(h, "gva_decode_tree", a, **{k: -1}) == I
         assert refused(h, "gva_decode_tree", a, most=257, words=9) == U and refused(h, "gva_decode_tree", a, B=8193) == U and refused(h, "gva_decode_tree", a, splits=65) == U
-        assert refused(h, "gva_decode_tree", a, B=8192, most=256, words=8, max_len=2 ** 31 - 1) == U
+        assert refused(h, "gva_decode_tree", a, B=8192, most=256, words=8, max_len=2 ** 31 - 1) == U and refused(h, "gva_decode_tree", a, max_len=2 ** 30 + 1) == U
         assert gb.gva_decode_tree_workspace_bytes(h.h, 8193, 1, 1, 1) == 0 and gb.gva_decode_tree_workspace_bytes(h.h, 1, 1, 257, 1) == 0
         a = dict(cache=c.c, parents=t, tokens=t, chosen=t, cu=t, ctx=t, path=t, lens=t, last=t, B=2, most=8)
         for k in ("parents", "tokens", "chosen", "cu", "ctx", "path", "lens", "last"):

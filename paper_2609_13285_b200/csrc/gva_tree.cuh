@@ -100,20 +100,22 @@ struct TreePieces {
             step = p.ranges;
         } else {
             const int n = partitions_in_use(total, p.ranges);
-            x = c < n ? range_begin(c, total, n) : 0;
-            end = c < n ? range_begin(c + 1, total, n) : 0;
+            // range_begin() in 32 bits: floor(c total / n) = c floor(total / n) + floor(c (total mod n) / n)
+            const int whole = n > 0 ? total / n : 0, rest = total - whole * n;
+            x = c < n ? c * whole + c * rest / n : 0;
+            end = c < n ? (c + 1) * whole + (c + 1) * rest / n : 0;
             step = c;
         }
     }
-    __device__ __noinline__ bool next(const TreeParams &p, const int *s_off, TreePiece &t) {      // (rare, and large: 64-bit divisions)
+    __device__ __noinline__ bool next(const TreeParams &p, const int *s_off, TreePiece &t) {      // (rare, and large)
         if (x >= end) return false;
         if (p.num_splits > 0) {
             const int strip = x / p.num_splits, k = x - strip * p.num_splits;
             t.b = seq_of_tile(s_off, p.B, strip);
             t.s = tree_seq(p, t.b, false);
             t.strip = strip - s_off[t.b];
-            t.lo = (int)((long long)k * t.s.tiles / p.num_splits);
-            t.hi = (int)((long long)(k + 1) * t.s.tiles / p.num_splits);
+            t.lo = k * t.s.tiles / p.num_splits;                          // (2^24 tiles and 64 splits at most)
+            t.hi = (k + 1) * t.s.tiles / p.num_splits;
             t.rec = p.num_splits == 1 ? -1 : (t.b * p.strips + t.strip) * p.num_splits + k;
             x += step;
         } else {

@@ -486,7 +486,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
     } else {
         int t = 0;                                      // running number of a tile
         if (warp >= 4 * NWG + 2) {
-            // ========================== loaders: of even and of odd tiles; all lanes look pages up, one issues ==========================
+            // ========================== loaders: of even and of odd tiles; a lane per box ==========================
             const int rows = p.P % 64 == 0 ? 64 : 32, boxes = T::TILE / rows;      // a box of that many rows lies in one page
             const uint64_t stream = l2_policy_evict_first();
             const uint32_t box_bytes = (uint32_t)rows * (T::BOXES * 128 + T::KR_ROW);
@@ -516,13 +516,12 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                             if (good == 0) mbar_arrive(full);
                             else mbar_expect_tx(full, __popc(good) * box_bytes);
                         }
-                        for (int k = 0; k < boxes; ++k) {
-                            const int va = __shfl_sync(kAll, v0, i * boxes + k), ka = __shfl_sync(kAll, k0, i * boxes + k);
-                            if (va >= 0 && elect_one()) {
+                        __syncwarp();                   // (what is expected is known before any of it comes)
+                        const int k = lane - i * boxes; // a lane fetches the box that it has looked up
+                        if (k >= 0 && k < boxes && v0 >= 0) {
 #pragma unroll
-                                for (int bx = 0; bx < T::BOXES; ++bx) tma_load_2d_stream(dst + bx * T::VBOX_BYTES + k * rows * 128, &tm_v, bx * 64, va, full, stream);
-                                if constexpr (DR > 0) tma_load_2d(dst + T::V_BYTES + k * rows * T::KR_ROW, &tm_k, 0, ka, full);
-                            }
+                            for (int bx = 0; bx < T::BOXES; ++bx) tma_load_2d_stream(dst + bx * T::VBOX_BYTES + k * rows * 128, &tm_v, bx * 64, v0, full, stream);
+                            if constexpr (DR > 0) tma_load_2d(dst + T::V_BYTES + k * rows * T::KR_ROW, &tm_k, 0, k0, full);
                         }
                         __syncwarp();
                     }

@@ -2,7 +2,8 @@
 // sequence it belongs to.  A slot below 0 is a padded row: nothing of it is cached.
 //
 // Both kernels are bound by memory: f32 rows in, cache rows (and rotated queries) out, each byte once.  A thread moves pieces
-// of eight elements (two 16-byte loads; one 16-byte store into a bf16 page) and has the loads of four pieces in flight.
+// of eight elements (two 16-byte loads; one 16-byte store into a bf16 page) and has the loads of four pieces in flight.  65536 rows of
+// 32 + 16 heads of 128 into bf16 pages, half of each head rotated: 438 - 453 us, 6.5 - 6.75 TB/s, the rate of a copy; one row 4.0 us, a launch.
 #pragma once
 
 #include "gva_rope.cuh"

@@ -7,9 +7,10 @@
 //   S[t % NWG] = Q K^T (Q from tensor memory)  ->  weights as bf16 pairs in P[t % NWG]  ->  O += P V
 // What bounds it is neither bytes nor a pipe but every role's chain of steps per tile: a wait that is complete already takes 150
 // cycles, an MMA 40 to 60 to issue, a tile in all some 600 for each issuer and 1500 and more for the softmax.  Hence large tiles for
-// narrow heads (of 64 tokens with four groups: 180 us for 1 M tokens, 16 nodes), and several of them side by side.  They share one O, so they share the
-// rows' softmax references too: those go from tile to tile through shared memory in the tiles' order (`turn`), which is a short step as
-// long as no maximum moves one.  Sums stay with each group, relative to the reference they were made with.
+// narrow heads (1 M tokens, 16 nodes, the same pools every pass: tiles of 128 and two groups 147 us = 0.60 of the bytes' time, of 64 and four
+// groups 179; wide heads, 16 x 32768, 8 nodes: tiles of 64 and three groups 239 us = 0.71, of 128 and two 267), and several tiles side by side.  They
+// share one O, so they share the rows' softmax references too: those go from tile to tile through shared memory in the tiles' order
+// (`turn`), which is a short step as long as no maximum moves one.  Sums stay with each group, relative to the reference they were made with.
 // Few nodes leave rows of the MMA unused, and its time is the same: up to 16 nodes are laid out twice, and each copy weighs its half
 // of every tile's tokens and has zeros for the others -- a sequence of its own, joined with the other at the end.
 // The running number of a tile over the block's pieces decides its stage, its group and every barrier's phase; loader and query run
@@ -74,7 +75,7 @@ struct TreeTraits {
     static constexpr int PART = 32, JOIN_LD = 36;                // columns of O at a time in the join of copies; f32 of a row there, padded
     static constexpr int OFF_JOIN = NSTAGE * STAGE_BYTES;
     static constexpr int OFF_REF = OFF_JOIN + NWG * (kStripRows / 2) * JOIN_LD * 4;
-    static constexpr int OFF_SUM = OFF_REF + 2 * kStripRows * 4, OFF_BAR = OFF_SUM + 2 * SOFTMAX * 4;
+    static constexpr int OFF_SUM = OFF_REF + 3 * kStripRows * 4, OFF_BAR = OFF_SUM + 2 * SOFTMAX * 4;
     static constexpr int N_BARS = 2 * NSTAGE + 8 * NWG + 6;
     static constexpr int OFF_WORDS = OFF_BAR + N_BARS * 8;       // tensor-memory address, abort flag, a flag per stage, bad rows of a group's tile
     static constexpr int OFF_SEQ = OFF_WORDS + (2 + NSTAGE + 8 * NWG) * 4;
@@ -143,6 +144,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
     TreePieces pieces(p, s_off, c);
     TreePiece pc = {};
     uint32_t n_pc = 0;                                  // running number of a piece
+    int refs_at = 0;                                    // its references: n_pc % 3 * kStripRows
     int st = 0;                                         // stage of a tile, and the parity of its round through the ring
     uint32_t ph = 0;
     auto advance = [&](int by) {
@@ -187,8 +189,10 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             }
             return false;
         };
-        // The query's rows into tensor memory, once the score products before are done, and fresh references.
-        auto stage_query = [&](const TreePiece &x, uint32_t number, uint32_t last_tile, bool any) {
+        // The query's rows into tensor memory, once the score products before are done, and fresh references.  (Three sets of those: while
+        // this group is at piece k and prepares k + 1, others may still read those of k - 1, but not of k - 2, since all have met at k - 1's end.)
+        auto next_refs = [&]() { return refs_at == 2 * kStripRows ? 0 : refs_at + kStripRows; };
+        auto stage_query = [&](const TreePiece &x, int refs_of, uint32_t last_tile, bool any) {
             const int tok = node_of(x);
             const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) +
                                                                (((size_t)x.s.r0 + x.n0 + min(tok, x.nv - 1)) * p.H + h) * (DV + DR));
@@ -213,7 +217,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                     tmem_st4_nowait(lane_base + T::COL_Q + at * 4, words);
                 }
             }
-            s_ref[(number & 1) * kStripRows + r] = -INFINITY;
+            s_ref[refs_of + r] = -INFINITY;
             tmem_st_wait();
             tc_fence_before();
             arrive(q_ready);
@@ -287,7 +291,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             sum_ref = -INFINITY;
             poison = false;
             const uint32_t t_end = t_base + (uint32_t)(pc.hi - pc.lo);
-            const int first = pc.lo, ctx = pc.s.ctx, halves = 2 / copies, half0 = copy;                              // of a tile: those whose tokens this copy weighs
+            const int first = pc.lo, ctx = pc.s.ctx, halves = 2 / copies, half0 = copy;   // (halves of a tile that this copy weighs)
             for (; n_tiles * NWG + w < t_end; ++n_tiles) {
                 const int t = (int)(n_tiles * NWG) + w, t0 = (first + (int)(t - t_base)) * T::TILE;
                 if (!wait(s_full(w), n_tiles)) { ok = false; break; }
@@ -349,7 +353,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                 const uint32_t turn1 = w == 0 ? n_tiles - 1 : n_tiles;
                 if (t > 0 && !(n_tiles == 0 ? wait(turn(w1, quarter), turn1)
                                             : warp_wait(turn(w1, quarter), turn1 & 1u, kv_empty(st_own), ph_own, s_abort))) { ok = false; break; }
-                float ref = s_ref[(n_pc & 1) * kStripRows + r];
+                float ref = s_ref[refs_at + r];
                 const bool move = m_tile > ref + kRescaleLog2;
                 if (__any_sync(kAll, move)) {
                     if ((uint32_t)t != t_base) {
@@ -369,7 +373,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                         tmem_st_wait();
                         tc_fence_before();
                     }
-                    if (move) s_ref[(n_pc & 1) * kStripRows + r] = ref = m_tile;
+                    if (move) s_ref[refs_at + r] = ref = m_tile;
                 }
                 arrive(turn(w, quarter));
                 tc_fence_after();
@@ -410,12 +414,11 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             }
             TreePiece nx;
             const bool more = next_piece(nx);
-            if (ok && more && w == 0) ok = stage_query(nx, n_pc + 1, t_end - 1, true);
+            if (ok && more && w == 0) ok = stage_query(nx, next_refs(), t_end - 1, true);
             ok = ok && wait(o_full, n_pc);
             if (!__all_sync(kAll, ok)) { ok = false; break; }
             // All value products are done, so all references are final: sums relative to them from every group, then the copies' shares.
-            const uint32_t set = n_pc & 1;
-            volatile float *refs = s_ref + set * kStripRows, *sums = s_sum + set * T::SOFTMAX;
+            volatile float *refs = s_ref + refs_at, *sums = s_sum + (n_pc & 1) * T::SOFTMAX;
             const float own_ref = refs[r];
             sums[tid] = poison ? __int_as_float(0x7fc00000) : sum == 0.f ? 0.f : sum * fast_exp2(sum_ref - own_ref);
             arrive(met_all);
@@ -480,6 +483,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
             arrive(o_free);
             t_base = t_end;
             ++n_pc;
+            refs_at = next_refs();
             pc = nx;
             have = more;
         }

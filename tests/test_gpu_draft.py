@@ -831,6 +831,74 @@ def test_steps_with_trees_end_where_single_tokens_do(shape, kind):
         assert f[1] == pages and sorted(ring.cpu().tolist()) == list(range(pages)) and int(status.item()) == 0
 
 
+def test_a_whole_step_captured_and_replayed():
+    """Pages, masks, rows, attention and commit in one graph, in place, against the same calls made one by one on a copy of the state."""
+    shape, B, n, P, most = wl.SHAPE_A, 5, 7, 64, 8
+    with Handle(shape, page=P) as h:
+        def state():
+            c = Cache(shape, [most * P] * B, page=P, kind="bf16", seed=3, paged=False, spare=0)
+            x = {"v": c.d[0], "kr": c.d[1], "table": zeros(B, most) - 1, "ring": ints(np.random.default_rng(1).permutation(c.num_pages)), "free": ints([2, c.num_pages])}
+            x.update({k: zeros(*v) for k, v in {"used": [B], "held": [B], "want": [B], "cu": [B + 1], "pos": [B * n], "slots": [B * n], "mask": [B * n, 1], "at": [B * n], "ctx": [B],
+                                                "path": [B * n], "last": [B], "status": [1]}.items()})
+            x["out"], x["lse"] = torch.zeros(B * n, 16, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(B * n, 16, device="cuda")
+            x["ws"] = torch.zeros(gb.gva_decode_tree_workspace_bytes(h.h, B, B * n, n, most * P), dtype=torch.uint8, device="cuda")
+            x["cache"] = gb.make_cache(x["v"], x["kr"], x["table"], c.num_pages, most)
+            x["pages"] = c.num_pages
+            return x
+
+        rng = np.random.default_rng(4)
+        inputs = {"parents": zeros(B * n), "tokens": zeros(B * n), "chosen": zeros(B * n), "v_new": torch.zeros(B * n, 4, 64, device="cuda"), "kr_new": torch.zeros(B * n, 16, device="cuda"),
+                  "q": torch.zeros(B * n, 16, 80, dtype=torch.bfloat16, device="cuda")}
+
+        def step(x):
+            i = inputs
+            x["ctx"].copy_(x["used"])
+            torch.add(x["used"], n, out=x["want"])
+            gb.gva_assign_pages(h.h, x["used"], x["want"], x["held"], x["held"], x["table"], most, x["pages"], x["ring"], x["free"], x["free"], x["used"], x["cu"], x["pos"], x["slots"], B * n, B,
+                                x["status"])
+            gb.gva_tree_masks(h.h, i["parents"], x["cu"], x["ctx"], x["mask"], 1, x["at"], B, n, x["status"])
+            gb.gva_append_rows(h.h, x["cache"], i["v_new"], i["kr_new"], x["at"], x["slots"], B * n, x["status"])
+            gb.gva_decode_tree(h.h, x["cache"], i["q"], x["mask"], 1, x["cu"], x["ctx"], x["out"], x["lse"], x["ws"], B, B * n, n, most * P, 0, x["status"])
+            gb.gva_tree_commit(h.h, x["cache"], i["parents"], i["tokens"], i["chosen"], x["cu"], x["ctx"], x["path"], x["used"], x["last"], B, n, x["status"])
+
+        one, two = state(), state()
+        torch.cuda.synchronize()
+        g, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(g, stream=stream):
+            step(one)
+        for k in range(25):
+            trees = [random_parents(n, 100 * k + b, chain=0.5) for b in range(B)]
+            tokens, chosen = rng.integers(0, 3, (B, n)), rng.integers(0, 3, (B, n))
+            for name, x in (("parents", ints(sum(trees, []))), ("tokens", ints(tokens.ravel())), ("chosen", ints(chosen.ravel())), ("v_new", torch.randn(B * n, 4, 64, device="cuda")),
+                            ("kr_new", torch.randn(B * n, 16, device="cuda")), ("q", torch.randn(B * n, 16, 80, device="cuda").bfloat16())):
+                inputs[name].copy_(x)
+            torch.cuda.synchronize()
+            g.replay()
+            step(two)
+            torch.cuda.synchronize()
+            assert int(one["status"]) == int(two["status"]) == 0
+            for name in ("v", "kr", "table", "ring", "free", "used", "held", "cu", "pos", "slots", "mask", "at", "path", "last", "out", "lse"):
+                a, b = one[name], two[name]
+                assert torch.equal(a.view(torch.int16) if a.dtype == torch.bfloat16 else a, b.view(torch.int16) if b.dtype == torch.bfloat16 else b), (k, name)
+            paths = [ref.commit(t, a, b)[0] for t, a, b in zip(trees, tokens, chosen)]
+            assert (one["used"] - one["ctx"]).tolist() == [len(x) for x in paths] and torch.isfinite(one["lse"]).all()
+        del g
+
+
+def test_commit_over_contiguous_pages():
+    shape = wl.SHAPE_A
+    with Handle(shape) as h:
+        c = Cache(shape, [70, 70], kind="bf16", seed=5, paged=False)
+        path, lens, last = zeros(8), zeros(2), zeros(2)
+        gb.gva_tree_commit(h.h, c.c, ints([-1, 0, 0, 2] * 2), ints([1, 2, 3, 4] * 2), ints([3, 9, 4, 7] * 2), ints([0, 4, 8]), ints([62, 63]), path, lens, last, 2, 4)
+        assert path.tolist() == [0, 2, 3, -1] * 2 and lens.tolist() == [65, 66] and last.tolist() == [7, 7]
+        for w, g in zip(c.pools, c.download()):
+            for b, ctx in ((0, 62), (1, 63)):
+                for i, node in enumerate([0, 2, 3]):
+                    d, s = ctx + i, ctx + node
+                    assert np.array_equal(g[c.ids[b, d // 64], ..., d % 64, :], w[c.ids[b, s // 64], ..., s % 64, :])
+
+
 def test_queries_and_keys_by_slot_map_feed_gqa_decode():
     H, G, d, P, lens = 16, 4, 64, 64, [130, 1, 64]
     rng = np.random.default_rng(3)

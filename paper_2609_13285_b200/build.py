@@ -14,7 +14,7 @@ _SHARED = ["gva_common.cuh", "gva_rope.cuh", "gva_decode_mma.cuh", "gva_handle.c
 SOURCES = {   # source -> the headers it is compiled from
     "gva_api.cu": _SHARED + ["gva_small_kernels.cuh", "gva_decode_fma.cuh", "gva_decode_fp8.cuh", "gva_prefill.cuh", "gva_project.cuh"],
     "gva_compact.cu": _SHARED + ["gva_q4.cuh", "gva_q4_decode.cuh", "gva_weights.cuh", "gva_evict.cuh"],
-    "gva_draft.cu": _SHARED + ["gva_decode_fp8.cuh", "gva_prefill.cuh", "gva_pages.cuh", "gva_rows.cuh", "gva_tree.cuh", "gva_tree_mma.cuh"],
+    "gva_draft.cu": _SHARED + ["gva_decode_fp8.cuh", "gva_prefill.cuh", "gva_pages.cuh", "gva_rows.cuh", "gva_tree.cuh", "gva_waits.cuh", "gva_tree_mma.cuh"],
 }
 
 

@@ -20,6 +20,7 @@
 #pragma once
 
 #include "gva_tree.cuh"
+#include "gva_waits.cuh"
 
 namespace gva {
 
@@ -31,22 +32,6 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
                  : "r"(addr)
                  : "memory");
     tmem_ld_wait();
-}
-// Bounded wait of a whole warp, straight-line where the phase is complete already, as it mostly is (with one lane waiting and the others
-// behind a shuffle it took 100 cycles more).
-constexpr uint32_t kWarpPolls = 1u << 24;       // 100 cycles each: about a second
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
-    for (uint32_t it = 0; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity));)
-        if ((++it & 1023u) == 0 && (it >= kWarpPolls || __any_sync(0xffffffffu, *abort_flag))) return false;
-    return true;
-}
-// Both of two phases: what they cost when complete overlaps.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t bar2, uint32_t parity2, volatile int *abort_flag) {
-    for (uint32_t it = 0;;) {
-        const bool one = mbar_try_wait(bar, parity), two = mbar_try_wait(bar2, parity2);
-        if (__all_sync(0xffffffffu, one && two)) return true;
-        if ((++it & 1023u) == 0 && (it >= kWarpPolls || __any_sync(0xffffffffu, *abort_flag))) return false;
-    }
 }
 __device__ __forceinline__ bool elect_one() {
     uint32_t yes;
@@ -532,9 +517,10 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                 }
             }
             // copies in flight must land before the block's shared memory is released
-            if (!ok || *s_abort)
-                for (int k = 0; k < min(t, NS); ++k)    // (the last tile of every stage, the other loader's too: bounded waits)
-                    for (int it = 0; it < kDrainPolls && !mbar_try_wait(kv_full(k), ((t - 1 - k) / NS) & 1); ++it) {}
+            if (!ok || __any_sync(kAll, *s_abort)) {
+                bool landed = true;                     // (the last tile of every stage, the other loader's too, which may never have been asked for)
+                for (int k = 0; k < min(t, NS) && landed; ++k) landed = warp_wait(kv_full(k), ((t - 1 - k) / NS) & 1, nullptr);
+            }
         } else if (warp < 4 * NWG + 2) {
             // ================================= MMA issuers: a warp per product, one elected lane issues =================================
             constexpr uint32_t hi128 = (1024u >> 4) | (1u << 14) | ((uint32_t)kSwz128 << 29);    // (descriptors as in the prefill kernel)
@@ -598,7 +584,7 @@ tree_mma_kernel(TreeParams p, const __grid_constant__ CUtensorMap tm_v, const __
                 const uint32_t dr = warp == 4 * NWG + 1 ? drain_s : drain_o;
                 if (elect_one()) umma_commit(dr);
                 __syncwarp();
-                for (int it = 0; it < kDrainPolls * 16 && !mbar_try_wait(dr, 0); ++it) {}
+                warp_wait(dr, 0, nullptr);
             }
         }
     }

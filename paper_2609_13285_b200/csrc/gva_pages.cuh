@@ -67,6 +67,40 @@ __device__ __forceinline__ int warp_owner_of(const int32_t *off, int B, int x) {
     }
     return lo;
 }
+// An entry of the ring, `at` behind the first free page: num_pages is below 2^26 (slots are below 2^31), and `at` at most num_pages.
+__device__ __forceinline__ int ring_entry(const AssignParams &p, int first, int at) {
+    at += first;
+    if (at >= p.num_pages) at -= p.num_pages;
+    return at >= p.num_pages ? at - p.num_pages : at;
+}
+// Returned page i of the call, and whose it was.
+__device__ __forceinline__ int returned_page(const AssignParams &p, const int *s_give, const int *s_to, int i, int &b) {
+    b = owner_of(s_give, p.B, i);
+    return p.block_table[(size_t)b * p.max_pages + s_to[b] + (i - s_give[b])];
+}
+// The ring's end where some of the n returned pages are bad: the good ones in their order, as many as there is room for, by one
+// block, a page a thread at a time.  How many are good.  (Only an unsound block table leads here.)
+__device__ __forceinline__ int return_good_pages(const AssignParams &p, const int *s_give, const int *s_to, int n, int first, int count, int *s_warp) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    int before = 0;
+    for (int base = 0; base < n; base += blockDim.x) {
+        const int i = base + threadIdx.x;
+        int page = -1, b;
+        if (i < n) page = returned_page(p, s_give, s_to, i, b);
+        const bool good = page >= 0 && page < p.num_pages;
+        const unsigned those = __ballot_sync(0xffffffffu, good);
+        __syncthreads();
+        if (lane == 0) s_warp[warp] = __popc(those);
+        __syncthreads();
+        int at = before + __popc(those & ((1u << lane) - 1));
+        for (int w = 0; w < warps; ++w) {
+            if (w < warp) at += s_warp[w];
+            before += s_warp[w];
+        }
+        if (good && at < p.num_pages - count) p.ring[ring_entry(p, first, count + at)] = page;
+    }
+    return before;
+}
 // Inclusive sums over the block's threads of four values, in place; s_part holds 4 x 32 words.  The last value's total is returned.
 struct Sums {
     long long v[4];
@@ -116,11 +150,13 @@ assign_pages_kernel(AssignParams p) {
     int *s_row = s_mem, *s_take = s_row + p.B, *s_give = s_take + p.B, *s_used = s_give + p.B, *s_pages = s_used + p.B, *s_to = s_pages + p.B;
     __shared__ long long s_part[4][32];
     __shared__ int s_served[3];      // rows, pages taken, pages returned by growing sequences: of those served
+    __shared__ int s_bad, s_warp[32];        // (of the first block:) whether any block has met a bad page; scratch of a scan
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, nt = blockDim.x, rank = (int)cluster.block_rank(), wide = (int)cluster.num_blocks();
     const int per = (p.B + nt - 1) / nt;
     if (tid < 3) s_served[tid] = 0;
+    if (tid == 3) s_bad = 0;
     grid_dependency_wait();
     const int first = p.free_in[0], count = p.free_in[1];
     const bool sound = first >= 0 && first < p.num_pages && count >= 0 && count <= p.num_pages;    // else all stays as it is
@@ -200,13 +236,8 @@ assign_pages_kernel(AssignParams p) {
     const int n_give = (int)min(give_all + n_back, (long long)p.num_pages + 1);
     // every block of the cluster has read its inputs (and this block's offsets are whole) before anything is written
     cluster.sync();
-    const int me = rank * nt + tid, all = wide * nt;
-    // an entry of the ring: num_pages is below 2^26 (slots are below 2^31), and what is added to `first` below twice that
-    auto entry = [&](int at) {
-        at += first;
-        if (at >= p.num_pages) at -= p.num_pages;
-        return at >= p.num_pages ? at - p.num_pages : at;
-    };
+    const int me = rank * nt + tid, all = wide * nt, room = p.num_pages - count;
+    auto entry = [&](int at) { return ring_entry(p, first, at); };
     if (rank == 0) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
@@ -218,9 +249,6 @@ assign_pages_kernel(AssignParams p) {
         }
         if (tid == 0) {
             p.cu_q[p.B] = n_rows;
-            // a ring that would overflow held pages twice: it takes no more than fit
-            const int room = p.num_pages - count;
-            if (sound && n_give > room) report_error(p.dev_status, GVA_ERR_BAD_PAGE, 0);
             p.free_out[0] = sound ? entry(n_take) : first;
             p.free_out[1] = sound ? count - n_take + min(n_give, room) : count;
         }
@@ -229,11 +257,16 @@ assign_pages_kernel(AssignParams p) {
         const int b = owner_of(s_take, p.B, i);
         p.block_table[(size_t)b * p.max_pages + s_pages[b] + (i - s_take[b])] = p.ring[entry(i)];
     }
-    for (int i = me; i < n_give && i < p.num_pages - count; i += all) {
-        const int b = owner_of(s_give, p.B, i);
-        const int page = p.block_table[(size_t)b * p.max_pages + s_to[b] + (i - s_give[b])];
-        if (page < 0 || page >= p.num_pages) report_error(p.dev_status, GVA_ERR_BAD_PAGE, b);
-        p.ring[entry(count + i)] = page;
+    bool bad = false;
+    for (int i = me; i < n_give && i < room; i += all) {
+        int b;
+        const int page = returned_page(p, s_give, s_to, i, b);
+        if (page >= 0 && page < p.num_pages) {
+            p.ring[entry(count + i)] = page;
+        } else {
+            bad = true;
+            report_error(p.dev_status, GVA_ERR_BAD_PAGE, b);
+        }
     }
     for (int i = p.rows_here ? me : n_rows; i < n_rows; i += all) {
         const int b = owner_of(s_row, p.B, i);
@@ -242,6 +275,21 @@ assign_pages_kernel(AssignParams p) {
                                         : p.ring[entry(s_take[b] + (j - s_pages[b]))];
         p.positions[i] = t;
         p.slots[i] = page < 0 || page >= p.num_pages ? -1 : page * p.P + t % p.P;
+    }
+    if (n_give == 0) return;                                     // (the same for the whole cluster)
+    // a returned page that is outside the pool goes to nobody: where any block has met one, the first lays the ring's end out anew
+    bad = __syncthreads_or(bad);
+    if (wide > 1) {
+        if (bad && tid == 0) *cluster.map_shared_rank(&s_bad, 0) = 1;
+        cluster.sync();
+        bad = s_bad != 0;
+    }
+    if (rank > 0) return;
+    const int n_kept = bad ? return_good_pages(p, s_give, s_to, min(n_give, p.num_pages), first, count, s_warp) : n_give;
+    if (tid == 0) {
+        if (bad) p.free_out[1] = count - n_take + min(n_kept, room);
+        // a ring that would overflow held pages twice: it takes no more than fit
+        if (n_kept > room || n_give > p.num_pages) report_error(p.dev_status, GVA_ERR_BAD_PAGE, 0);
     }
 }
 

@@ -1,0 +1,113 @@
+"""GPU tests of what gva_assign_pages says of bad sequences, pages and rings, and of what becomes of bad pages.  All whole numbers: exact."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_13285_b200 import binding as gb
+from paper_2609_13285_b200 import workloads as wl
+from tests import draft_ref as ref
+from tests.test_gpu_compact import Handle, ints
+from tests.test_gpu_draft import Pages, code, zeros
+
+pytestmark = pytest.mark.gpu
+ROWS = [500, 9000]             # rows allowed for: by the kernel of the plan itself, by one of their own
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from tests import gpu_util
+    gpu_util.ensure_built()
+
+
+def plan(handle, s, want, max_rows):
+    """The call in place on a state of tests.test_gpu_draft.Pages, which it moves on: rows, (error, index)."""
+    used, pages, table, ring, free = ints(s.used), ints(s.pages), ints(s.table), ints(s.ring), ints(s.free)
+    cu, pos, slots, status = zeros(s.B + 1), zeros(max_rows), zeros(max_rows), zeros(1)
+    gb.gva_assign_pages(handle.h, used, ints(want), pages, pages, table, s.most, s.N, ring, free, free, used, cu, pos, slots, max_rows, s.B, status)
+    n = int(cu[-1])
+    s.used, s.pages, s.free = used.tolist(), pages.tolist(), tuple(free.tolist())
+    s.table, s.ring = table.cpu().numpy().astype(np.int64), ring.cpu().numpy().astype(np.int64)
+    return {"cu": cu.tolist(), "pos": pos[:n].tolist(), "slots": slots[:n].tolist()}, code(status)
+
+
+def expected(s, want, max_rows):
+    """What the call is to leave where pages that come back may be bad: the reference's, but for those, which are dropped.  (What ring
+    entries hold beside the free pages is nobody's business.)"""
+    r = ref.assign_pages(s.used, want, s.pages, s.table, s.P, s.N, s.ring, s.free, max_rows)
+    first, count = s.free
+    back = [(b, int(s.table[b, j])) for b in range(s.B) for j in range(r["pages"][b], s.pages[b])]
+    taken = sum(max(0, r["pages"][b] - s.pages[b]) for b in range(s.B))
+    good = [p for _, p in back if 0 <= p < s.N]
+    ring = s.ring.copy()
+    for i, p in enumerate(good[: s.N - count]):
+        ring[(first + count + i) % s.N] = p
+    r["ring"], r["free"] = ring, ((first + taken) % s.N, count - taken + min(len(good), s.N - count))
+    return r, sorted({b for b, p in back if not 0 <= p < s.N})
+
+
+def check(handle, s, want, max_rows, errors=()):
+    """errors: the (error, index) pairs of which the call has to say one; none: all is well."""
+    r, dropped = expected(s, want, max_rows)
+    got, said = plan(handle, s, want, max_rows)
+    errors = set(errors) | {(gb.GVA_ERR_BAD_PAGE, b) for b in dropped}
+    assert said in errors if errors else said == (0, 0), (said, errors)
+    for k in ("cu", "pos", "slots"):
+        assert got[k] == [int(x) for x in r[k]], k
+    assert s.used == [int(x) for x in r["lens"]] and s.pages == [int(x) for x in r["pages"]] and s.free == tuple(r["free"])
+    assert np.array_equal(s.table, r["table"]) and np.array_equal(free_pages(s, s.ring), free_pages(s, r["ring"]))
+    return r
+
+
+def free_pages(s, ring):
+    return ring[(s.free[0] + np.arange(s.free[1])) % s.N]
+
+
+@pytest.mark.parametrize("rows", ROWS)
+def test_a_bad_page_that_comes_back_goes_to_nobody(rows):
+    with Handle(wl.SHAPE_A) as h:
+        s = Pages(3, 64, 8, seed=1, held=[300, 100, 64], ahead=0, spare=2)
+        s.table[0, 2], s.table[0, 4] = s.N, -3
+        check(h, s, [0, 101, 64], rows)                             # sequence 0 is done: five pages, two of them bad
+        assert s.free[1] == 5 and len(set(s.ring[(s.free[0] + np.arange(5)) % s.N])) == 5
+        check(h, s, [8 * 64, 101, 64], rows, [(gb.GVA_ERR_NO_ROOM, 0)])
+        r = check(h, s, [5 * 64, 101, 64], rows)                    # what is left of the ring serves: every row has a slot
+        assert min(r["slots"]) >= 0 and s.free[1] == 0
+
+
+@pytest.mark.parametrize("B,most", [(40, 9), (1025, 6), (3000, 5), (8192, 3), (2, 3000)])
+@pytest.mark.parametrize("rows", ROWS)
+def test_bad_pages_among_many_that_come_back(B, most, rows):
+    """Scattered, first and last, all of a sequence's; of sequences that shrink, end, and grow within pages they hold too many of."""
+    with Handle(wl.SHAPE_A) as h:
+        for share in (0.001, 0.1, 1.0):
+            s = Pages(B, 64, most, seed=B, spare=7 * B // 2, ahead=0.5)
+            rng = np.random.default_rng(B)
+            room = rows
+            want = []
+            for b, u in enumerate(s.used):
+                x = rng.random()
+                new = int(rng.integers(1, 6)) if x < 0.3 and room > 6 else 0
+                want.append(min(u + new, most * 64) if new else 0 if x < 0.6 else int(rng.integers(0, u + 1)))
+                room -= max(0, want[-1] - u)
+            keep = [-(-w // 64) for w in want]
+            for b in range(B):
+                for j in range(keep[b], s.pages[b]):
+                    if rng.random() < share:
+                        s.table[b, j] = rng.choice([-1, s.N, s.N + 5, 2 ** 31 - 1, -2 ** 31])
+            for b in (0, B - 1):
+                if s.pages[b] > keep[b]:
+                    s.table[b, keep[b]] = s.N
+            check(h, s, want, rows)
+            for step in range(2):                                   # ... and the ring that is left serves the next steps
+                check(h, s, [min(most * 64, u + 1 + b % 2) if b < rows // 2 else u for b, u in enumerate(s.used)], rows)
+
+
+def test_more_bad_pages_than_a_full_ring_has_room_for():
+    with Handle(wl.SHAPE_A) as h:
+        s = Pages(4, 64, 8, seed=3, held=[300, 300, 300, 300], ahead=0, spare=2)
+        s.free = (s.free[0], s.N - 3)                               # a ring that says it holds nearly all
+        s.table[1, 1] = -1
+        r, _ = expected(s, [300, 0, 300, 0], 10)
+        got, said = plan(h, s, [300, 0, 300, 0], 10)
+        assert said in {(gb.GVA_ERR_BAD_PAGE, 0), (gb.GVA_ERR_BAD_PAGE, 1)}
+        assert s.free == tuple(r["free"]) and np.array_equal(free_pages(s, s.ring), free_pages(s, r["ring"])) and s.free[1] == s.N

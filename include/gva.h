@@ -483,7 +483,7 @@ int gva_q4_evict(gva_handle *h, const gva_q4_cache *cache, const float *weights_
  *   new_lens [B]       want[b], or used[b] where the sequence was not served
  *   cu_q     [B + 1]   rows cu_q[b] .. cu_q[b+1] - 1 are the new tokens of b, max(want - used, 0) of them
  *   positions, slots [max_rows]   of every row: its position used[b] + i, and its place page * page_size + position % page_size
- *                      (-1 if the block table holds a bad page there).  Rows at or beyond cu_q[B] are left as they were
+ *                      (-1 if that page is none of the pool: GVA_ERR_BAD_PAGE, the row will not be cached).  Rows at or beyond cu_q[B] are left as they were
  * pages_out may be pages_in, new_lens may be used, free_out may be free_in; nothing else overlaps.
  * Sequences that grow are served in order as long as free pages and rows suffice: the first that does not fit, and all growing
  * ones after it, stay as they are (GVA_ERR_NO_ROOM with the index of one of them).  Pages returned by a call are there for the next one.

@@ -44,6 +44,12 @@ __device__ __forceinline__ Asks sequence_asks(const AssignParams &p, int b, bool
     a.give = max(a.pages - a.to, 0);
     return a;
 }
+// The slot of a row of sequence b, `at` tokens into its page.  A row on a bad page has none: appends take it for a padded row, so it is said here.
+__device__ __forceinline__ int slot_of(const AssignParams &p, int b, int page, int at) {
+    if (page >= 0 && page < p.num_pages) return page * p.P + at;
+    report_error(p.dev_status, GVA_ERR_BAD_PAGE, b);
+    return -1;
+}
 // Largest b in [0, B) with off[b] <= x, for off non-decreasing, off[0] <= x.
 __device__ __forceinline__ int owner_of(const int *off, int B, int x) {
     int lo = 0, hi = B - 1;
@@ -274,7 +280,7 @@ assign_pages_kernel(AssignParams p) {
         const int page = j < s_pages[b] ? p.block_table[(size_t)b * p.max_pages + j]
                                         : p.ring[entry(s_take[b] + (j - s_pages[b]))];
         p.positions[i] = t;
-        p.slots[i] = page < 0 || page >= p.num_pages ? -1 : page * p.P + t % p.P;
+        p.slots[i] = slot_of(p, b, page, t % p.P);
     }
     if (n_give == 0) return;                                     // (the same for the whole cluster)
     // a returned page that is outside the pool goes to nobody: where any block has met one, the first lays the ring's end out anew
@@ -317,7 +323,7 @@ assign_rows_kernel(AssignParams p) {
         const int b = b0 + owner_of(p.cu_q + b0, n, i), t = p.new_lens[b] - (p.cu_q[b + 1] - i), j = t / p.P;
         const int page = p.block_table[(size_t)b * p.max_pages + j];
         p.positions[i] = t;
-        p.slots[i] = page < 0 || page >= p.num_pages ? -1 : page * p.P + (t - j * p.P);
+        p.slots[i] = slot_of(p, b, page, t - j * p.P);
     }
 }
 

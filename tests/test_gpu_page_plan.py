@@ -111,3 +111,20 @@ def test_more_bad_pages_than_a_full_ring_has_room_for():
         got, said = plan(h, s, [300, 0, 300, 0], 10)
         assert said in {(gb.GVA_ERR_BAD_PAGE, 0), (gb.GVA_ERR_BAD_PAGE, 1)}
         assert s.free == tuple(r["free"]) and np.array_equal(free_pages(s, s.ring), free_pages(s, r["ring"])) and s.free[1] == s.N
+
+
+@pytest.mark.parametrize("rows", ROWS)
+def test_new_rows_on_a_bad_page_are_reported(rows):
+    bad = lambda b: {(gb.GVA_ERR_BAD_PAGE, b)}  # noqa: E731
+    with Handle(wl.SHAPE_A) as h:
+        s = Pages(8, 64, 8, seed=8, held=[10, 100, 64, 65, 0, 0, 200, 300], ahead=0)
+        s.table[7, 300 // 64] = s.N                                 # under the sequence's next rows
+        r = check(h, s, [u + 3 for u in s.used], rows, bad(7))
+        assert r["slots"][-3:] == [-1] * 3 and min(r["slots"][:-3]) >= 0
+        s.table[7, 0] = -1                                          # under rows that it has had: nothing is asked of it
+        check(h, s, [u + 3 for u in s.used[:7]] + [s.used[7]], rows)
+        for value in (s.N, -1, 2 ** 31 - 1, -2 ** 31):              # among the free pages: with who takes it
+            s = Pages(5, 64, 8, seed=9, held=[64, 64, 10, 64, 128], ahead=0, spare=6)
+            s.ring[(s.free[0] + 1) % s.N] = value
+            r = check(h, s, [65, 64, 20, 70, 129], rows, bad(3))
+            assert [x < 0 for x in r["slots"]] == [False] * 11 + [True] * 6 + [False]

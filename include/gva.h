@@ -542,7 +542,7 @@ int gqa_set_rope(gva_handle *h, const gva_rope *rope);
  * The angle is reduced to a fraction of a turn in fp64, sine and cosine are f32, and so are the two products and the sum of an element;
  * keys and values are rounded once to the cache dtype (nearest even; e4m3 saturates).  All pointers are 16-byte aligned
  * (pos and slots 4).  A slot beyond the pool -> GVA_ERR_BAD_PAGE, pos < 0 with a slot -> GVA_ERR_SEQ_LEN, each with the row's
- * number in the place of a sequence's: that row is not cached.  Two rows with the same slot leave either's elements.  cache->block_table
+ * number (2^23 - 1 from there on) in the place of a sequence's: that row is not cached.  Two rows with the same slot leave either's elements.  cache->block_table
  * and max_pages_per_seq are not used. */
 int gqa_append(gva_handle *h, const gqa_cache *cache, const float *q, int64_t q_stride, const float *k_new, int64_t k_stride,
                const float *v_new, int64_t v_stride, const int32_t *pos, const int32_t *slots, float *q_out, int n,

@@ -50,16 +50,18 @@ struct AppendRowsParams {
     int vec;                         // v_new is 16-byte aligned
 };
 
+// Reports row r as it does a sequence; a status word has 23 bits for the number, the last of which stands for all rows behind it too.
+__device__ __forceinline__ void report_row(int32_t *dev_status, int code, int r) { report_error(dev_status, code, min(r, (1 << 23) - 1)); }
 // The slot of a row: < 0 where nothing is to be written.
 __device__ __forceinline__ int row_slot(const int32_t *slots, const int32_t *pos, int r, int P, int num_pages, int32_t *dev_status, bool say) {
     const int s = slots[r];
     if (s < 0) return -1;
     if (s / P >= num_pages) {
-        if (say) report_error(dev_status, GVA_ERR_BAD_PAGE, r);
+        if (say) report_row(dev_status, GVA_ERR_BAD_PAGE, r);
         return -1;
     }
     if (pos[r] < 0) {
-        if (say) report_error(dev_status, GVA_ERR_SEQ_LEN, r);
+        if (say) report_row(dev_status, GVA_ERR_SEQ_LEN, r);
         return -1;
     }
     return s;

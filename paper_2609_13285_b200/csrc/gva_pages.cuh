@@ -309,7 +309,7 @@ assign_rows_kernel(AssignParams p) {
     grid_dependency_wait();
     const int r0 = blockIdx.x * kAssignRows, total = p.cu_q[p.B];
     if (r0 >= total) return;
-    const int end = min(r0 + kAssignRows, total), warp = threadIdx.x >> 5;
+    const int end = r0 + min(kAssignRows, total - r0), warp = threadIdx.x >> 5;         // (rows are numbers of 32 bits: up to 2^31 - 32 of them)
     if (warp < 2) {
         const int b = warp_owner_of(p.cu_q, p.B, warp == 0 ? r0 : end - 1);
         if ((threadIdx.x & 31) == 0) s_b[warp] = b;

@@ -128,3 +128,24 @@ def test_new_rows_on_a_bad_page_are_reported(rows):
             s.ring[(s.free[0] + 1) % s.N] = value
             r = check(h, s, [65, 64, 20, 70, 129], rows, bad(3))
             assert [x < 0 for x in r["slots"]] == [False] * 11 + [True] * 6 + [False]
+
+
+@pytest.mark.parametrize("P,pages", [(32, 2 ** 26 - 1), (2 ** 20, 2 ** 11 - 1)])
+def test_as_many_rows_as_slots_have_numbers(P, pages):
+    """One prompt over the whole pool (17 GB of positions and slots), and one of nearly nothing behind it."""
+    n = pages * P
+    with Handle(wl.SHAPE_A, page=P) as h:
+        ring = torch.randperm(pages, dtype=torch.int32, device="cuda")
+        table, held, lens, cu, status = torch.full((2, pages), -1, dtype=torch.int32, device="cuda"), zeros(2), zeros(2), zeros(3), zeros(1)
+        pos, slots = (torch.full((n,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+        free = ints([pages // 3, pages])
+        order = torch.roll(ring, -(pages // 3))
+        gb.gva_assign_pages(h.h, zeros(2), ints([n - P, 1]), held, held, table, pages, pages, ring, free, free, lens, cu, pos, slots, n, 2, status)
+        assert int(status) == 0 and cu.tolist() == [0, n - P, n - P + 1] and lens.tolist() == [n - P, 1] and free.tolist()[1] == 0
+        assert torch.equal(table[0, :-1], order[:-1]) and int(table[1, 0]) == int(order[-1])
+        step = P * max(1, 2 ** 26 // P)
+        for at in range(0, n - P, step):
+            t = torch.arange(at, min(at + step, n - P), device="cuda")
+            assert torch.equal(pos[at:at + len(t)], t.int())
+            assert torch.equal(slots[at:at + len(t)].long(), order[t // P].long() * P + t % P)
+        assert pos[n - P:].tolist()[:2] == [0, -7] and int(slots[n - P]) == int(order[-1]) * P and (slots[n - P + 1:] == -7).all()

@@ -149,3 +149,32 @@ def test_as_many_rows_as_slots_have_numbers(P, pages):
             assert torch.equal(pos[at:at + len(t)], t.int())
             assert torch.equal(slots[at:at + len(t)].long(), order[t // P].long() * P + t % P)
         assert pos[n - P:].tolist()[:2] == [0, -7] and int(slots[n - P]) == int(order[-1]) * P and (slots[n - P + 1:] == -7).all()
+
+
+@pytest.mark.parametrize("rows", ROWS)
+def test_every_error_names_its_sequence(rows):
+    L, N, F = gb.GVA_ERR_SEQ_LEN, gb.GVA_ERR_NO_ROOM, gb.GVA_ERR_BAD_PAGE
+    held = [10, 100, 64, 65, 0, 0, 200, 300]
+    with Handle(wl.SHAPE_A) as h:
+        for b, change in enumerate([{"used": -1}, {"want": -1}, {"pages": 0}, {"pages": 9}, {"pages": -1}, {"want": 8 * 64 + 1}, {"want": 2 ** 31 - 1}, {"used": 2 ** 31 - 1}]):
+            s = Pages(8, 64, 8, seed=5, held=held, ahead=0)
+            want = [u + 50 for u in s.used]
+            if "want" in change:
+                want[b] = change["want"]
+            for k in ("used", "pages"):
+                if k in change:
+                    getattr(s, k)[b] = change[k]
+            check(h, s, want, rows, {(L, b)})
+        for first, count in ((-1, 5), (None, -1), (10 ** 6, 3), (None, 10 ** 6)):
+            s = Pages(8, 64, 8, seed=6, held=held)
+            s.free = (s.free[0] if first is None else first, count)
+            before = (list(s.used), list(s.pages), s.free)
+            got, said = plan(h, s, [u + 70 if i % 2 else 0 for i, u in enumerate(s.used)], rows)
+            assert said == (F, 0) and got["cu"] == [0] * 9 and (s.used, s.pages, s.free) == before
+        s = Pages(8, 64, 8, seed=7, held=held, ahead=0, spare=3)     # pages for the first three that need one
+        check(h, s, [u + 64 for u in held], rows, {(N, b) for b in range(3, 8)})
+        s = Pages(8, 64, 8, seed=7, held=held, ahead=0, spare=40)    # rows for the first three
+        check(h, s, [u + 150 for u in held], 3 * 150 + 5 if rows < 8192 else rows, {(N, b) for b in range(3, 8)} if rows < 8192 else ())
+        s = Pages(8, 64, 8, seed=7, held=held, ahead=0)              # a ring that is full, and pages that come back
+        s.free = (3, s.N)
+        check(h, s, [0] * 8, rows, {(F, 0)})

@@ -68,7 +68,8 @@ typedef enum {
  * gva_absorb_query, gva_append_cache, gva_append_chunk, gva_decode, gva_decode_step, gva_decode_step_host,
  * gva_decode_static, gqa_decode (keys and values as e4m3 codes), the projections, gva_layer_step and (with a positional
  * slice, d_r > 0) gva_decode_tokens / gva_decode_tokens_ragged serve it, and so do gva_prefill and gva_decode_multi (the
- * byte tiles are widened to f16 in shared memory; queries and weights are then f16 instead of bf16). */
+ * byte tiles are widened to f16 in shared memory; queries and weights are then f16 instead of bf16), gva_append_cache_at, gva_append_rows,
+ * gqa_append, gva_attention_weights, gva_evict and gva_tree_commit; gva_decode_tree serves it on CUDA cores. */
 typedef enum { GVA_F32 = 0, GVA_BF16 = 1, GVA_E4M3 = 2 } gva_dtype;
 
 /* Which decode kernel gva_decode launches.  AUTO = tensor-core kernel when the cache is bf16 or e4m3,
@@ -466,8 +467,10 @@ int gva_q4_evict(gva_handle *h, const gva_q4_cache *cache, const float *weights_
 /* ---- A step with drafted tokens: pages and slots, rows by slot map, attention of a tree, commit -----------------------
  * (Not in the paper, whose steps add one token: this library's calls for serving programs that draft several continuations of
  * every sequence as a tree, look at all of them in one step and keep the path the model agrees with.)  One step in order:
- *   gva_assign_pages -> gva_tree_masks -> gva_absorb_query(q_pos = positions) -> gva_append_rows -> gva_decode_tree -> the rest of the
- *   model -> gva_tree_commit;
+ *   gva_assign_pages -> gva_tree_masks -> gva_absorb_query(q_pos = positions) -> (its queries to bf16) -> gva_append_rows -> gva_decode_tree ->
+ *   (its output to f32) -> gva_project_out and the rest of the model -> gva_tree_commit;
+ * the two conversions are the caller's, and over an f32 cache there are none: gva_decode_tree takes and gives 16-bit numbers where its
+ * neighbours take and give f32 (what that costs is said there);
  * the first and gqa_append serve single tokens and prompts as well.  All of them want the handle's device to be the current
  * one (GVA_ERR_INVALID_ARG otherwise), use no state of the handle on the device, and may be captured into CUDA graphs and
  * replayed; calls on different streams may overlap as long as they share no workspace, no output and no page that one of them
@@ -565,12 +568,18 @@ int gva_append_rows(gva_handle *h, const gva_cache *cache, const float *v_new, c
  *   num_splits               0: all sequences' tiles in a row are cut into equal ranges; n: every 32 nodes' tiles into n ranges (64 at most)
  * Over a bf16 cache the products are taken of the bf16 numbers as they are, accumulated in f32; softmax weights enter the value product
  * rounded to bf16 (2^-8 at most, as the output; their sum is taken before), everything else is f32: over a thousand tokens and more the output is
- * as far off as its own rounding makes it (1.7e-3 of its size), over a hundred 1.1 times.  Over e4m3 and f32 caches all is f32 but the output's type.  Bitwise reproducible for fixed arguments.  What is cached for a node does not reach rows that do
- * not see it, not even infinities and NaN; a row that sees a node with an infinity or NaN among a group's values has NaN in the heads of that
- * group, in those elements or in all.
+ * as far off as its own rounding makes it (1.7e-3 of its size), over a hundred 1.1 times.  Over e4m3 and f32 caches all is f32 but the type of
+ * queries and output; these caches are served on CUDA cores (1 M tokens of 80, 16 nodes: 12.3 ms, over bf16 0.16 ms).
+ * That is the error for the queries as they are given.  Rounding f32 queries to bf16 is one of its own, 2^-8 sum |q k| scale of a score at
+ * most: with queries of 1, 5 and 30 times the unit scale outputs were 2.5e-3, 4.4e-3 and 1.0e-2 of their size (3e-3, 4e-2 and 2.4e-1 of a
+ * unit at most) from those of f32 queries.  The calls that take f32 queries (gva_decode_tokens and gva_decode_multi for
+ * chains, this one over an f32 cache) stay within 2e-2 of a unit at any scale.
+ * Bitwise reproducible for fixed arguments.  What is cached for a node does not reach rows that do not see it, not even infinities and NaN;
+ * a row that sees a node with an infinity or NaN among a group's values has NaN in the heads of that group, in those elements or in all.
  * n_b < 0 or > max_q_len, rows outside [0, n_q), ctx_lens[b] < 0, or ctx_lens[b] + n_b beyond max_seq_len or the block table -> GVA_ERR_SEQ_LEN, the
  * sequence's rows are left as they were; tokens of a page outside the pool count as absent (GVA_ERR_BAD_PAGE).  Rows at or beyond cu_q[B] are left as they were.
- * Workspace: at least gva_decode_tree_workspace_bytes(...) bytes, 256-byte aligned. */
+ * Workspace: at least gva_decode_tree_workspace_bytes(...) bytes, 256-byte aligned: a record of 128 rows x G for every 32 nodes of every
+ * sequence and some more (32 sequences of 16 narrow nodes 9 MB; 256 of 64 wide ones 282 MB). */
 size_t gva_decode_tree_workspace_bytes(const gva_handle *h, int B, int n_q, int max_q_len, int max_seq_len, int num_splits);
 int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const uint32_t *mask, int mask_words, const int32_t *cu_q,
                     const int32_t *ctx_lens, void *out, float *lse, void *workspace, size_t workspace_bytes, int B, int n_q, int max_q_len,

@@ -57,7 +57,11 @@ TreePlan tree_plan(const gva_handle *h, int B, int max_q_len, int max_seq_len, i
     t.strips = (int)std::max<long long>(1, ceil_div(max_q_len, kStripNodes));
     t.tile = c.cache_dtype == GVA_BF16 ? tree_mma_tile(c.d_v) : kTreeFmaTile;
     const long long tiles = std::max<long long>(1, ceil_div(max_seq_len, t.tile)), all = (long long)std::max(B, 1) * t.strips;
-    // Short sequences: one piece per strip, which writes its result itself -- there is nothing to merge.
+    // Short sequences: one piece per strip, which writes its result itself -- there is nothing to merge.  us, in one piece / in ranges, 8 nodes:
+    //   narrow heads, 500 tokens (4 tiles)  1 sequence 10.5 / 12.0   8: 10.8 / 13.7   64: 18.9 / 26.9;   800 tokens (7)   12.6 / 13.3   13.0 / 17.8   23.6 / 32.3
+    //   wide heads, 200 tokens (4 tiles)    1 sequence 13.0 / 16.3   8: 13.7 / 18.7   64: 43.3 / 53.7;   800 tokens (13)  16.3 / 16.3   17.1 / 26.5   58.5 / 66.6
+    // Four tiles stay clear of the border, which one long sequence among short ones moves down.  The bound decides, not the lengths: a call
+    // captured with a larger one takes ranges.
     t.num_splits = num_splits > 0 ? num_splits : tiles <= 4 ? 1 : 0;
     num_splits = t.num_splits;
     const bool mma = c.cache_dtype == GVA_BF16;
@@ -180,7 +184,9 @@ int gva_assign_pages(gva_handle *h, const int32_t *used, const int32_t *want, co
     // Up to 8192 rows the kernel's threads have one row each, in a cluster of up to eight blocks; more rows get a kernel of their own
     // (in the cluster and apart, us: 5000 rows of 256 trees 6.8 and 12.3, 0.2 M rows of 48 prompts 33 and 9.3).
     p.rows_here = max_rows <= 8192 ? 1 : 0;
-    const int work = (int)std::max<long long>(B, p.rows_here ? max_rows : std::max<long long>(1024, ceil_div(max_rows, p.P)));   // (as many pages taken, at least)
+    // As many threads as rows, or as pages taken (at least), up to the cluster's.  How many pages come back is not known here: 8769 of them
+    // from 111 of 1000 sequences take 14.1 us in the one block of a call for 1000 rows, 8.2 in the eight of one for 8000.
+    const int work = (int)std::max<long long>(B, p.rows_here ? max_rows : std::max<long long>(1024, ceil_div(max_rows, p.P)));
     const int threads = work <= 128 ? 128 : work <= 256 ? 256 : work <= 512 ? 512 : 1024;
     const int blocks = work <= 1024 ? 1 : work <= 2048 ? 2 : work <= 4096 ? 4 : 8;
     const size_t smem = (size_t)6 * B * 4;
@@ -268,7 +274,11 @@ int gva_decode_tree(gva_handle *h, const gva_cache *cache, const void *q, const 
         rc = launched(launch_pdl(fn, grid, dim3(kTreeFmaThreads), plan.smem, s, p, c.d_r));
     }
     if (rc != GVA_OK || plan.num_splits == 1) return rc;
-    // many pieces a strip: a block per node with the pieces side by side; few: a warp per node
+    // Many pieces a strip: a block per node with the pieces side by side; few: a warp per node.  us, side by side / by warps, 4000 tokens:
+    //   narrow heads (37 ranges), 8 nodes   1 sequence 13.8 / 17.5   2: 14.1 / 15.3   4: 15.7 / 15.6   5: 20.5 / 20.6   8: 23.3 / 21.6
+    //                             32 nodes  1 sequence 16.7 / 20.4   2: 18.1 / 18.8   4: 21.8 / 19.5   5: 29.7 / 26.7   8: 35.0 / 28.8
+    //   wide heads (18 ranges), 8 nodes     1 sequence 19.3 / 22.3   2: 21.0 / 23.0   3: 22.2 / 23.5   8: 37.7 / 35.5
+    //   narrow, 4 (16) sequences in splits  4 splits 16.4 / 16.1 (30.6 / 26.2)   8: 15.4 / 15.2 (39.7 / 36.7)   16: 19.2 / 20.3 (51.6 / 50.5)
     const bool wide = plan.ranges >= 8 * plan.strips * B || plan.num_splits >= 8;
     const int nodes = std::min(max_q_len, kStripNodes);
     const dim3 merge_grid((unsigned)(B * plan.strips), c.H, wide ? nodes : (nodes + 7) / 8);

@@ -2,8 +2,8 @@
 // drafted tokens of a tree see of one another, and the tokens of a tree that become part of their sequence.
 //
 // All three move a few kilobytes: what they cost is a launch and their chains of dependent steps, so each is one launch whose
-// chains are short (a scan of all sequences in every block rather than a pass for the scan and one for its use).  Measured, us a call: pages of 4
-// sequences 4.1, of 256 with 5000 rows 6.8, masks of 256 trees 3.6 - 4.8, commit of 2 and of 256 trees 5.8.
+// chains are short (a scan of all sequences in every block rather than a pass for the scan and one for its use).  Measured, us a call among others: pages
+// of 4 sequences 4.5, of 256 with 5000 rows 6.8, masks of 256 trees 3.6 - 4.8, commit of 2 and of 256 trees 5.8 - 6.1.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -299,7 +299,7 @@ assign_pages_kernel(AssignParams p) {
     }
 }
 
-// Positions and slots of many rows, from what assign_pages_kernel has left (0.2 M rows of 48 prompts: 9.3 us with that kernel, 33 in its one
+// Positions and slots of many rows, from what assign_pages_kernel has left (0.2 M rows of 48 prompts: 8.4 - 9.3 us with that kernel, 33 in its one
 // cluster).  A block has 1024 rows in a row, of as few sequences as these lie in.
 constexpr int kAssignRows = 1024, kAssignRowThreads = 256;
 __global__ void __launch_bounds__(kAssignRowThreads)

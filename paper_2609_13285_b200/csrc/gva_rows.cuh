@@ -3,7 +3,9 @@
 //
 // Both kernels are bound by memory: f32 rows in, cache rows (and rotated queries) out, each byte once.  A thread moves pieces
 // of eight elements (two 16-byte loads; one 16-byte store into a bf16 page) and has the loads of four pieces in flight.  65536 rows of
-// 32 + 16 heads of 128 into bf16 pages, half of each head rotated: 438 - 453 us, 6.5 - 6.75 TB/s, the rate of a copy; one row 4.0 us, a launch.
+// 32 + 16 heads of 128 into bf16 pages, half of each head rotated: 438 - 456 us, 6.5 - 6.75 TB/s, the rate of a copy; one row 4.0 us, a launch.
+// GVA rows (their rotation in fp64), us, and TB/s: 65536 of 8 x 128 + 32 into bf16, e4m3, f32 pages 76, 71, 100 (5.5, 4.9, 5.5); of 4 x 64 + 16 37, 37, 39 (2.9, 2.4,
+// 3.6: the fp64 chains of 8 pairs a row); 8192 of them 7.6, 7.5, 7.8; 500 4.1 - 4.3.
 #pragma once
 
 #include "gva_rope.cuh"

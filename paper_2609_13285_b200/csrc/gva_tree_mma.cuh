@@ -7,12 +7,16 @@
 //   S[t % NWG] = Q K^T (Q from tensor memory)  ->  weights as bf16 pairs in P[t % NWG]  ->  O += P V
 // What bounds it is neither bytes nor a pipe but every role's chain of steps per tile: a wait that is complete already takes 150
 // cycles, an MMA 40 to 60 to issue, a tile in all some 600 for each issuer and 1500 and more for the softmax.  Hence large tiles for
-// narrow heads (1 M tokens, 16 nodes, the same pools every pass: tiles of 128 and two groups 147 us = 0.60 of the bytes' time, of 64 and four
-// groups 179; wide heads, 16 x 32768, 8 nodes: tiles of 64 and three groups 239 us = 0.71, of 128 and two 267), and several tiles side by side.  They
+// narrow heads (1 M tokens, 16 nodes, the same pools every pass: tiles of 128 and two groups 147 - 154 us = 0.57 - 0.60 of the bytes' time, of 64 and
+// four groups 179; wide heads, 16 x 32768, 8 nodes: tiles of 64 and three groups 239 - 243 us = 0.70, of 128 and two 267), and several tiles side by side.  They
 // share one O, so they share the rows' softmax references too: those go from tile to tile through shared memory in the tiles' order
 // (`turn`), which is a short step as long as no maximum moves one.  Sums stay with each group, relative to the reference they were made with.
 // Few nodes leave rows of the MMA unused, and its time is the same: up to 16 nodes are laid out twice, and each copy weighs its half
-// of every tile's tokens and has zeros for the others -- a sequence of its own, joined with the other at the end.
+// of every tile's tokens and has zeros for the others -- a sequence of its own, joined with the other at the end.  What is issued is
+// the same for 1 to 32 nodes: 155 GFLOP for 1 M narrow tokens, 95 us at the measured rate, more than the 87 us of their bytes.
+// The weights are rounded to bf16 because the value product's operands have one type and the values are bf16; in two parts they would cost
+// a second product.  It adds half as much error to the output as its own rounding does where a hundred tokens share the weight, and less the
+// more there are.  Their sums are of what is rounded, before it is, in f32.
 // The running number of a tile over the block's pieces decides its stage, its group and every barrier's phase; loader and query run
 // ahead over pieces.
 // Rules as in the prefill kernel: tcgen05.ld / .st never sit in a per-lane branch; no barrier is waited on by parity two phases

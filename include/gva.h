@@ -492,7 +492,8 @@ int gva_q4_evict(gva_handle *h, const gva_q4_cache *cache, const float *weights_
  * ones after it, stay as they are (GVA_ERR_NO_ROOM with the index of one of them).  Pages returned by a call are there for the next one.
  * used < 0, want < 0, pages_in outside [0, max_pages_per_seq], used beyond those pages or want beyond the block table -> GVA_ERR_SEQ_LEN,
  * the sequence stays as it is.  A ring state outside its range -> GVA_ERR_BAD_PAGE, everything stays as it is; more pages returned
- * than the ring has room for -> GVA_ERR_BAD_PAGE, those beyond it are lost; a returned page that is none of the pool -> GVA_ERR_BAD_PAGE, it is lost too.  Pages must belong to one sequence only. */
+ * than the ring has room for -> GVA_ERR_BAD_PAGE, those beyond it are lost; a returned page that is none of the pool -> GVA_ERR_BAD_PAGE, it
+ * is lost too.  Pages must belong to one sequence only. */
 int gva_assign_pages(gva_handle *h, const int32_t *used, const int32_t *want, const int32_t *pages_in, int32_t *pages_out, int32_t *block_table,
                      int max_pages_per_seq, int num_pages, int32_t *free_ring, const int32_t *free_in, int32_t *free_out, int32_t *new_lens,
                      int32_t *cu_q, int32_t *positions, int32_t *slots, int max_rows, int B, int32_t *dev_status, void *stream);

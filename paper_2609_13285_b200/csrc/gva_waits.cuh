@@ -7,7 +7,7 @@ namespace gva {
 
 // Bounded wait of a whole warp, straight-line where the phase is complete already, as it mostly is (with one lane waiting and the others
 // behind a shuffle it took 100 cycles more).  Bounded like mbar_wait_bounded: kWaitLimitNs of wall time -- how long a poll takes that
-// finds nothing is the hardware's choice, so a number of polls bounds nothing -- or until another warp of the block has given up.
+// finds nothing is the hardware's choice (4 us measured), so a number of polls bounds nothing -- or until another warp of the block has given up.
 __device__ __forceinline__ bool warp_gives_up(unsigned long long &t0, const volatile int *abort_flag) {
     const unsigned long long now = __shfl_sync(0xffffffffu, global_timer_ns(), 0);       // (one reading, so that all lanes leave together)
     if (t0 == 0) t0 = now;
